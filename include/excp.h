@@ -370,6 +370,96 @@ excp_status excp_selftest_wait_timeout(excp_handle h, unsigned long long nanosec
  * EXCP_ERR_INVALID_ARG.  Applies to the handle's later calls. */
 excp_status excp_set_kmeans_margin(excp_handle h, int margin);
 
+/* ---- Scoring a restored checkpoint -------------------------------------------------------------
+ * (The paper judges a restored checkpoint by evaluation suites, which score texts by the log probabilities
+ * of their tokens, and leaves the code to them.)  Restored matrices are held in microscaled 4-bit floating
+ * point, multiplied with activations, and the logits are turned into log probabilities.
+ *
+ * These calls only enqueue work: nothing is copied to the host and nothing synchronises (the first call on a
+ * handle that needs its little workspace allocates it), so they can be captured in a graph after one ordinary
+ * call.  Calls on one handle must be ordered on the device (one stream, or events between streams): they share
+ * the workspace.  A matrix in ordinary layout is `rows` rows of `cols` values, `row_stride` values apart
+ * (>= cols), aligned to its element; its type is an excp_dtype. */
+typedef enum {
+    EXCP_F32 = 0,
+    EXCP_F16 = 1,
+    EXCP_BF16 = 2
+} excp_dtype;
+
+/* Microscaled 4-bit floating point.  A value is the nearest of 0, .5, 1, 1.5, 2, 3, 4, 6 (ties to the even
+ * code, at most 6) with a sign, times the scale of its block of consecutive columns:
+ *   EXCP_MX4_E8M0_32  blocks of 32, scale 2^e, e = max(floor(log2 A) - 2, -127) with A the block's largest
+ *                     magnitude; byte e + 127.
+ *   EXCP_MX4_E4M3_16  blocks of 16, scale s * g: g the matrix's fp32 tensor scale (positive, device memory;
+ *                     NULL = 1), s = A / (6 g) rounded to the nearest float of 4 exponent and 3 mantissa bits
+ *                     (at most 448).  Where s = 0 every code is 0.  A value is divided by fl(s g) and the quotient
+ *                     rounded to fp32 before it is rounded to 4 bits; it stands for fl(fl(code s) g).
+ * A block that holds a NaN or an infinity has the scale NaN (0xff / 0x7f) and codes 0: all its values are NaN.
+ *
+ * Packed layout (rows R, columns C, CT = ceil(C / 256)): row tiles of 128 rows; the last one holds its rows
+ * rounded up to 8 (h rows, else h = 128); column tiles of 256.  Tiles lie one after another, the column tiles of a
+ * row tile first.  One tile is
+ *     h * 128 bytes of codes, two per byte, the lower column in the low bits; a row's 128 bytes are eight
+ *             chunks of 16, chunk c at place c ^ (row % 8);
+ *     scales: one 512-byte piece per 4 blocks of columns (2 pieces, or 4 for blocks of 16); row 32 c + l,
+ *             block k of the four at byte 16 l + 4 c + k.  Always 128 rows; 0 where there is no row or block.
+ * Codes of missing rows and columns are 0.  excp_mx4_bytes gives the size (0 for an unknown format). */
+typedef enum {
+    EXCP_MX4_E8M0_32 = 1,
+    EXCP_MX4_E4M3_16 = 2
+} excp_mx4_format;
+
+size_t excp_mx4_bytes(size_t rows, size_t cols, int format);
+
+/* Tensor scale of a matrix: its largest finite magnitude / (6 * 448), rounded up to 8 significant bits (the
+ * products with the block scales are then exact); 1 for a matrix of zeros.  scale_out: device, one float. */
+excp_status excp_mx4_tensor_scale(excp_handle h, const void* x, int dtype, size_t rows, size_t cols, size_t row_stride,
+                                  float* scale_out, void* cuda_stream);
+
+/* x -> packed_out (device, excp_mx4_bytes, 16-byte aligned), and back. */
+excp_status excp_mx4_quantize(excp_handle h, const void* x, int dtype, size_t rows, size_t cols, size_t row_stride,
+                              int format, const float* tensor_scale, void* packed_out, void* cuda_stream);
+excp_status excp_mx4_dequantize(excp_handle h, const void* packed, size_t rows, size_t cols, int format,
+                                const float* tensor_scale, void* out, int dtype, size_t row_stride, void* cuda_stream);
+
+/* y[i, j] = sum over k of a[i, k] b[j, k] + bias[j], rounded once to y's type.  a and b are packed matrices of the
+ * same format and number of columns; the products of codes and block scales are summed in fp32, then multiplied
+ * with both tensor scales.  bias: device fp32 [b_rows] or NULL.
+ *   excp_mx4_linear quantises x first (x_scale: its tensor scale, from calibration; x_packed: device,
+ *   excp_mx4_bytes(rows, cols, format), receives the packed x). */
+excp_status excp_mx4_matmul(excp_handle h, const void* a, size_t a_rows, const float* a_scale, const void* b, size_t b_rows,
+                            const float* b_scale, size_t cols, int format, const float* bias, void* y, int y_dtype,
+                            size_t y_row_stride, void* cuda_stream);
+excp_status excp_mx4_linear(excp_handle h, const void* x, int x_dtype, size_t rows, size_t x_row_stride, const float* x_scale,
+                            const void* w, size_t w_rows, const float* w_scale, size_t cols, int format, const float* bias,
+                            void* y, int y_dtype, size_t y_row_stride, void* x_packed, void* cuda_stream);
+
+/* Log probabilities of given tokens.  With z = scale * logits[i, :] (scale positive and finite: an inverse temperature),
+ * m its maximum and S = sum exp(z - m):
+ *   logprob_out[i]   log probability of tokens[i]; 0 where the token is negative (ignored), NaN where it is >= vocab
+ *   entropy_out[i]   - sum p log p (may be NULL)
+ *   top_*_out        [rows, top], top <= 64 and <= vocab: the largest logits' log probabilities and indices,
+ *                    in descending order; equal logits (-0 and 0 are equal) by ascending index
+ *   row_stats_out    [rows, 4], 16-byte aligned, for the gradient (may be NULL): m, S, entropy, 0
+ * A logit of -infinity has probability 0 and adds nothing to the entropy.  A row of nothing else has log
+ * probabilities -infinity, entropy 0 and gradient 0.  A row with a NaN or +infinity gives NaN; a NaN counts as the largest
+ * logit.  tokens: device int64 [rows]. */
+excp_status excp_token_logprobs(excp_handle h, const void* logits, int dtype, size_t rows, size_t vocab, size_t row_stride,
+                                const long long* tokens, float scale, int top, float* logprob_out, float* entropy_out,
+                                float* row_stats_out, float* top_logprob_out, long long* top_index_out, void* cuda_stream);
+
+/* The gradient of sum_i g_logprob[i] logprob[i] + g_entropy[i] entropy[i] with respect to the logits, in their type:
+ *   scale * (g_logprob ([v = token] - p_v) - g_entropy p_v (log p_v + entropy))
+ * g_logprob, g_entropy: device fp32 [rows], NULL = 0; row_stats: what excp_token_logprobs wrote for the same logits,
+ * tokens and scale.  An ignored token's g_logprob counts as 0.  grad_out may be the logits themselves (same stride). */
+excp_status excp_token_logprobs_grad(excp_handle h, const void* logits, int dtype, size_t rows, size_t vocab, size_t row_stride,
+                                     const long long* tokens, float scale, const float* row_stats, const float* g_logprob,
+                                     const float* g_entropy, void* grad_out, size_t grad_row_stride, void* cuda_stream);
+
+/* Synchronises the stream and reports whether a bounded wait of a product since the last report ran out
+ * (excp_set_wait_limit; EXCP_ERR_TIMEOUT: that product's result is unspecified). */
+excp_status excp_score_status(excp_handle h, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,7 +24,9 @@ EXPORTS = ["excp_create", "excp_destroy", "excp_record_bytes", "excp_compress_bo
            "excp_compress_checkpoint_host", "excp_decompress_tensor", "excp_decompress_checkpoint",
            "excp_decompress_tensor_noalloc", "excp_dense_bytes", "excp_record_to_dense", "excp_checkpoint_to_dense",
            "excp_decompress_dense_tensor", "excp_decompress_dense_checkpoint", "excp_profile_enable", "excp_profile_stage_count", "excp_profile_stage_name", "excp_profile_read",
-           "excp_set_kmeans_margin", "excp_set_wait_limit", "excp_selftest_wait_timeout", "excp_set_report_sse"]
+           "excp_set_kmeans_margin", "excp_set_wait_limit", "excp_selftest_wait_timeout", "excp_set_report_sse",
+           "excp_mx4_bytes", "excp_mx4_tensor_scale", "excp_mx4_quantize", "excp_mx4_dequantize", "excp_mx4_matmul", "excp_mx4_linear",
+           "excp_token_logprobs", "excp_token_logprobs_grad", "excp_score_status"]
 
 
 class ExcpError(RuntimeError):
@@ -116,6 +118,16 @@ def load_library() -> C.CDLL:
     lib.excp_profile_stage_name.argtypes = [C.c_int]
     lib.excp_profile_stage_name.restype = C.c_char_p
     lib.excp_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_ulonglong)]
+    lib.excp_mx4_bytes.argtypes = [sz, sz, C.c_int]
+    lib.excp_mx4_bytes.restype = sz
+    lib.excp_mx4_tensor_scale.argtypes = [vp, vp, C.c_int, sz, sz, sz, vp, vp]
+    lib.excp_mx4_quantize.argtypes = [vp, vp, C.c_int, sz, sz, sz, C.c_int, vp, vp, vp]
+    lib.excp_mx4_dequantize.argtypes = [vp, vp, sz, sz, C.c_int, vp, vp, C.c_int, sz, vp]
+    lib.excp_mx4_matmul.argtypes = [vp, vp, sz, vp, vp, sz, vp, sz, C.c_int, vp, vp, C.c_int, sz, vp]
+    lib.excp_mx4_linear.argtypes = [vp, vp, C.c_int, sz, sz, vp, vp, sz, vp, sz, C.c_int, vp, vp, C.c_int, sz, vp, vp]
+    lib.excp_token_logprobs.argtypes = [vp, vp, C.c_int, sz, sz, sz, vp, C.c_float, C.c_int, vp, vp, vp, vp, vp, vp]
+    lib.excp_token_logprobs_grad.argtypes = [vp, vp, C.c_int, sz, sz, sz, vp, C.c_float, vp, vp, vp, vp, sz, vp]
+    lib.excp_score_status.argtypes = [vp, vp]
     for name in EXPORTS:
         if getattr(lib, name).restype is C.c_int:
             getattr(lib, name).restype = C.c_int
@@ -173,6 +185,38 @@ def decompress_tensor_noalloc(blob: torch.Tensor, blob_bytes: int, w_prev, w_out
                                                        _ptr(w_out), _ptr(ea_out), _ptr(eas_out), _stream())
     if st != 0:
         raise ExcpError(st, "excp_decompress_tensor_noalloc")
+
+
+# ---- scoring a restored checkpoint ---------------------------------------------
+MX4_FORMAT = {"e8m0_32": 1, "e4m3_16": 2}
+_DTYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def mx4_bytes(rows: int, cols: int, fmt: str) -> int:
+    """Size of a packed 4-bit matrix (layout: include/excp.h)."""
+    return load_library().excp_mx4_bytes(rows, cols, MX4_FORMAT[fmt])
+
+
+class Mx4Matrix:
+    """A packed 4-bit matrix: `data` (uint8, mx4_bytes), its shape, its format ("e8m0_32" or "e4m3_16") and, for
+    the latter, the tensor scale (a float32 tensor of one value on the same device; None = 1)."""
+    __slots__ = ("data", "rows", "cols", "fmt", "scale", "code")
+
+    def __init__(self, data: torch.Tensor, rows: int, cols: int, fmt: str, scale: torch.Tensor | None = None):
+        self.data, self.rows, self.cols, self.fmt, self.scale = data, rows, cols, fmt, scale
+        self.code = MX4_FORMAT[fmt]
+        if not (data.is_cuda and data.dtype == torch.uint8 and data.is_contiguous()) or data.numel() < mx4_bytes(rows, cols, fmt):
+            raise TypeError("expected a contiguous uint8 CUDA tensor of mx4_bytes(rows, cols, fmt)")
+
+
+@dataclass
+class TokenLogprobs:
+    logprob: torch.Tensor           # float32 [rows]
+    entropy: torch.Tensor           # float32 [rows]
+    top_logprob: torch.Tensor | None   # float32 [rows, top]
+    top_index: torch.Tensor | None     # int64 [rows, top]
+    row_stats: torch.Tensor         # float32 [rows, 4], for the gradient
+    scale: float
 
 
 class Handle:
@@ -359,3 +403,152 @@ class Handle:
                                                    w_prev.numel(), _ptr(w_out), _ptr(ea_out), _ptr(eas_out), _stream())
         if st != 0:
             raise ExcpError(st, "excp_decompress_dense_tensor")
+
+    # ---- scoring a restored checkpoint -------------------------------------
+    # Only enqueued; outputs are allocated by torch where the caller gives none.
+    def _rows(self, t: torch.Tensor, what: str) -> tuple[int, int, int, int, int]:
+        """(pointer, dtype, rows, cols, row stride) of a 2-D tensor whose last dimension is dense."""
+        if t.dim() != 2 or t.dtype not in _DTYPE or t.device.type != "cuda" or t.device.index != self.device:
+            raise TypeError(f"{what}: expected a 2-D float32, float16 or bfloat16 tensor on cuda:{self.device}")
+        rows, cols = t.shape
+        stride, inner = t.stride()
+        if inner != 1 and cols > 1:
+            raise TypeError(f"{what}: the last dimension must be dense")
+        return t.data_ptr(), _DTYPE[t.dtype], rows, cols, stride if rows > 1 else cols
+
+    def _vector(self, t: torch.Tensor | None, what: str, dtype: torch.dtype, n: int) -> int:
+        if t is None:
+            return 0
+        if t.dtype != dtype or t.numel() != n or t.device.type != "cuda" or t.device.index != self.device or not t.is_contiguous():
+            raise TypeError(f"{what}: expected {n} contiguous {dtype} values on cuda:{self.device}")
+        return t.data_ptr()
+
+    def _raw_stream(self) -> int:
+        return torch._C._cuda_getCurrentRawStream(self.device)
+
+    def _packed(self, m: Mx4Matrix, what: str) -> int:
+        if m.data.device.index != self.device:
+            raise TypeError(f"{what}: expected a packed matrix on cuda:{self.device}")
+        return m.data.data_ptr()
+
+    def mx4_tensor_scale(self, x: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
+        """excp_mx4_tensor_scale: the tensor scale of a matrix, as a float32 tensor of one value."""
+        p, dt, rows, cols, stride = self._rows(x, "x")
+        if out is None:
+            out = torch.empty((), dtype=torch.float32, device=x.device)
+        st = self.lib.excp_mx4_tensor_scale(self._h, p, dt, rows, cols, stride, self._vector(out, "out", torch.float32, 1), self._raw_stream())
+        if st != 0:
+            raise ExcpError(st, "excp_mx4_tensor_scale")
+        return out
+
+    def mx4_quantize(self, x: torch.Tensor, fmt: str, tensor_scale: torch.Tensor | None = None,
+                     out: torch.Tensor | None = None) -> Mx4Matrix:
+        """excp_mx4_quantize: x [rows, cols] as a packed 4-bit matrix (into `out`, uint8, if given)."""
+        p, dt, rows, cols, stride = self._rows(x, "x")
+        if out is None:
+            out = torch.empty(mx4_bytes(rows, cols, fmt), dtype=torch.uint8, device=x.device)
+        m = Mx4Matrix(out, rows, cols, fmt, tensor_scale)
+        st = self.lib.excp_mx4_quantize(self._h, p, dt, rows, cols, stride, m.code, self._vector(tensor_scale, "tensor_scale", torch.float32, 1),
+                                        self._packed(m, "out"), self._raw_stream())
+        if st != 0:
+            raise ExcpError(st, "excp_mx4_quantize")
+        return m
+
+    def mx4_dequantize(self, m: Mx4Matrix, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
+        """excp_mx4_dequantize: the values that the codes stand for."""
+        if out is None:
+            out = torch.empty((m.rows, m.cols), dtype=dtype, device=m.data.device)
+        p, dt, rows, cols, stride = self._rows(out, "out")
+        if (rows, cols) != (m.rows, m.cols):
+            raise TypeError("out: expected the matrix's shape")
+        st = self.lib.excp_mx4_dequantize(self._h, self._packed(m, "m"), rows, cols, m.code, self._vector(m.scale, "scale", torch.float32, 1),
+                                          p, dt, stride, self._raw_stream())
+        if st != 0:
+            raise ExcpError(st, "excp_mx4_dequantize")
+        return out
+
+    def mx4_matmul(self, a: Mx4Matrix, b: Mx4Matrix, bias: torch.Tensor | None = None, dtype: torch.dtype = torch.bfloat16,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+        """excp_mx4_matmul: a b^T (+ bias per row of b) of two packed matrices, [a.rows, b.rows]."""
+        if a.code != b.code or a.cols != b.cols:
+            raise TypeError("a, b: expected the same format and number of columns")
+        if out is None:
+            out = torch.empty((a.rows, b.rows), dtype=dtype, device=b.data.device)
+        y, dt, rows, cols, stride = self._rows(out, "out")
+        if (rows, cols) != (a.rows, b.rows):
+            raise TypeError("out: expected [a.rows, b.rows]")
+        f32 = torch.float32
+        st = self.lib.excp_mx4_matmul(self._h, self._packed(a, "a"), a.rows, self._vector(a.scale, "a.scale", f32, 1), self._packed(b, "b"), b.rows,
+                                      self._vector(b.scale, "b.scale", f32, 1), a.cols, a.code, self._vector(bias, "bias", f32, b.rows), y, dt,
+                                      stride, self._raw_stream())
+        if st != 0:
+            raise ExcpError(st, "excp_mx4_matmul")
+        return out
+
+    def mx4_linear(self, x: torch.Tensor, w: Mx4Matrix, bias: torch.Tensor | None = None, tensor_scale: torch.Tensor | None = None,
+                   out: torch.Tensor | None = None, dtype: torch.dtype | None = None, x_packed: torch.Tensor | None = None) -> torch.Tensor:
+        """excp_mx4_linear: x w^T (+ bias), x [rows, w.cols] quantised to w's format with the tensor scale given; the result
+        has x's type unless `dtype` or `out` says otherwise.  `x_packed` (uint8) is room for the packed x."""
+        p, xdt, rows, cols, xstride = self._rows(x, "x")
+        if cols != w.cols:
+            raise TypeError(f"x: expected {w.cols} columns")
+        if out is None:
+            out = torch.empty((rows, w.rows), dtype=dtype or x.dtype, device=x.device)
+        y, dt, yrows, ycols, stride = self._rows(out, "out")
+        if (yrows, ycols) != (rows, w.rows):
+            raise TypeError("out: expected [x rows, w.rows]")
+        need = self.lib.excp_mx4_bytes(rows, cols, w.code)
+        if x_packed is None:
+            x_packed = torch.empty(need, dtype=torch.uint8, device=x.device)
+        elif x_packed.dtype != torch.uint8 or x_packed.numel() < need or not x_packed.is_contiguous() or x_packed.device != x.device:
+            raise TypeError("x_packed: expected a contiguous uint8 tensor of mx4_bytes(rows, cols, fmt) on x's device")
+        f32 = torch.float32
+        st = self.lib.excp_mx4_linear(self._h, p, xdt, rows, xstride, self._vector(tensor_scale, "tensor_scale", f32, 1), self._packed(w, "w"), w.rows,
+                                      self._vector(w.scale, "w.scale", f32, 1), cols, w.code, self._vector(bias, "bias", f32, w.rows), y, dt, stride,
+                                      x_packed.data_ptr(), self._raw_stream())
+        if st != 0:
+            raise ExcpError(st, "excp_mx4_linear")
+        return out
+
+    def token_logprobs(self, logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, scale: float = 1.0) -> TokenLogprobs:
+        """excp_token_logprobs: log probability of each row's token, entropy, and the `top` likeliest alternatives."""
+        p, dt, rows, vocab, stride = self._rows(logits, "logits")
+        f32 = torch.float32
+        stats = torch.empty((rows, 4), dtype=f32, device=logits.device)
+        both = torch.empty((2, rows), dtype=f32, device=logits.device)
+        tl = ti = None
+        if top > 0:
+            tl = torch.empty((rows, top), dtype=f32, device=logits.device)
+            ti = torch.empty((rows, top), dtype=torch.int64, device=logits.device)
+        r = TokenLogprobs(both[0], both[1], tl, ti, stats, scale)
+        b = both.data_ptr()
+        st = self.lib.excp_token_logprobs(self._h, p, dt, rows, vocab, stride, self._vector(tokens, "tokens", torch.int64, rows), scale, top, b,
+                                          b + 4 * rows, stats.data_ptr(), tl.data_ptr() if top > 0 else 0, ti.data_ptr() if top > 0 else 0,
+                                          self._raw_stream())
+        if st != 0:
+            raise ExcpError(st, "excp_token_logprobs")
+        return r
+
+    def token_logprobs_grad(self, logits: torch.Tensor, tokens: torch.Tensor, r: TokenLogprobs, g_logprob: torch.Tensor | None,
+                            g_entropy: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+        """excp_token_logprobs_grad: the gradient with respect to the logits, from what token_logprobs returned for them.
+        `out` may be `logits`."""
+        p, dt, rows, vocab, stride = self._rows(logits, "logits")
+        if out is None:
+            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+        q, odt, orows, ocols, ostride = self._rows(out, "out")
+        if (odt, orows, ocols) != (dt, rows, vocab):
+            raise TypeError("out: expected the logits' shape and type")
+        f32 = torch.float32
+        st = self.lib.excp_token_logprobs_grad(self._h, p, dt, rows, vocab, stride, self._vector(tokens, "tokens", torch.int64, rows), r.scale,
+                                               self._vector(r.row_stats, "row_stats", f32, rows * 4), self._vector(g_logprob, "g_logprob", f32, rows),
+                                               self._vector(g_entropy, "g_entropy", f32, rows), q, ostride, self._raw_stream())
+        if st != 0:
+            raise ExcpError(st, "excp_token_logprobs_grad")
+        return out
+
+    def score_status(self) -> None:
+        """excp_score_status: synchronises; raises if a product's bounded wait ran out since the last report."""
+        st = self.lib.excp_score_status(self._h, self._raw_stream())
+        if st != 0:
+            raise ExcpError(st, "excp_score_status")
