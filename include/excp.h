@@ -434,7 +434,7 @@ excp_status excp_mx4_linear(excp_handle h, const void* x, int x_dtype, size_t ro
                             const void* w, size_t w_rows, const float* w_scale, size_t cols, int format, const float* bias,
                             void* y, int y_dtype, size_t y_row_stride, void* x_packed, void* cuda_stream);
 
-/* Log probabilities of given tokens.  With z = scale * logits[i, :] (scale positive and finite: an inverse temperature),
+/* Log probabilities of given tokens.  With z = scale * logits[i, :] (an inverse temperature: positive, at most 1e30),
  * m its maximum and S = sum exp(z - m):
  *   logprob_out[i]   log probability of tokens[i]; 0 where the token is negative (ignored), NaN where it is >= vocab
  *   entropy_out[i]   - sum p log p (may be NULL)

@@ -153,7 +153,7 @@ excp_status excp_mx4_linear(excp_handle h, const void* x, int x_dtype, size_t ro
 excp_status excp_token_logprobs(excp_handle h, const void* logits, int dtype, size_t rows, size_t vocab, size_t row_stride,
                                 const long long* tokens, float scale, int top, float* logprob_out, float* entropy_out,
                                 float* row_stats_out, float* top_logprob_out, long long* top_index_out, void* cuda_stream) {
-    if (!h || !rows_ok(logits, dtype, rows, vocab, row_stride) || !(scale > 0.f) || std::isinf(scale)) return EXCP_ERR_INVALID_ARG;
+    if (!h || !rows_ok(logits, dtype, rows, vocab, row_stride) || !(scale > 0.f) || scale > 1e30f) return EXCP_ERR_INVALID_ARG;
     if (top < 0 || top > SCORE_TOP_MAX || (size_t)top > vocab) return EXCP_ERR_INVALID_ARG;
     if (rows == 0) return EXCP_OK;
     if (!tokens || !logprob_out || (reinterpret_cast<uintptr_t>(tokens) & 7u) || !on_float(logprob_out) || !on_float(entropy_out) ||
@@ -172,7 +172,7 @@ excp_status excp_token_logprobs_grad(excp_handle h, const void* logits, int dtyp
                                      const long long* tokens, float scale, const float* row_stats, const float* g_logprob,
                                      const float* g_entropy, void* grad_out, size_t grad_row_stride, void* cuda_stream) {
     if (!h || !rows_ok(logits, dtype, rows, vocab, row_stride) || !rows_ok(grad_out, dtype, rows, vocab, grad_row_stride) ||
-        !(scale > 0.f) || std::isinf(scale))
+        !(scale > 0.f) || scale > 1e30f)
         return EXCP_ERR_INVALID_ARG;
     if (rows == 0 || vocab == 0) return EXCP_OK;
     if (!tokens || !row_stats || (reinterpret_cast<uintptr_t>(tokens) & 7u) || !aligned16(row_stats) || !on_float(g_logprob) || !on_float(g_entropy))
