@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libexcp.so")
 SOURCES = ["stats.cu", "mask_compact.cu", "kmeans.cu", "pack.cu", "decode.cu", "excp_api.cu", "excp_noalloc.cu", "selftest.cu",
-           "mx4.cu", "mx4_matmul.cu", "token_logprobs.cu", "score_api.cu"]
+           "mx4.cu", "mx4_matmul.cu", "mx4_matmul_wide.cu", "token_logprobs.cu", "score_api.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-fmad=false", "-Xcompiler", "-fPIC", "-cudart", "static"]
 

@@ -194,8 +194,9 @@ bool launch_as(cudaStream_t s, const MatmulArgs& g) {
 
 }  // namespace
 
-bool launch_mx4_matmul(int, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
+bool launch_mx4_matmul(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
                        const Mx4Result& r, u64 wait_ns, u32* flag) {
+    if (cols && a.rows > MX4_ROWS && b.rows > MX4_ROWS) return launch_mx4_matmul_wide(sms, s, a, b, cols, fmt, r, wait_ns, flag);
     MatmulArgs g{};
     // few rows of a: they go to the N side, whose width the tensor core takes in steps of 8
     const bool swap = a.rows <= MX4_ROWS;

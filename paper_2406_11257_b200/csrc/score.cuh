@@ -71,6 +71,9 @@ struct Mx4Result {
 bool launch_mx4_matmul(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
                        const Mx4Result& r, u64 wait_ns, u32* flag);
 
+bool launch_mx4_matmul_wide(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
+                            const Mx4Result& r, u64 wait_ns, u32* flag);
+
 struct LogprobsOut {
     float* logprob;
     float* entropy;
