@@ -6,8 +6,8 @@
 // which takes a third off the traffic.
 //
 // Persistent pairs: pair p computes tiles p, p + pairs, ...  Roles in each CTA: warps 0..7 write the result, warp 8
-// fetches (contiguous bulk copies, the packed layout is the tensor core's), warp 9 issues the matrix instructions in the
-// even CTA and reports finished copies to it in the odd one.  The accumulator (256 columns of tensor memory) is read
+// fetches (contiguous bulk copies, the packed layout is the tensor core's), warp 9 of the even CTA issues the matrix
+// instructions, warps 10..13 bring the block scales to tensor memory.  The accumulator (256 columns of tensor memory) is read
 // into registers in one go and handed back before it is converted and written, so that the next tile waits for a
 // few hundred cycles only.
 // Every wait is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and leaves (the
@@ -19,7 +19,8 @@ namespace excp {
 namespace {
 
 constexpr int STORE_WARPS = 8;
-constexpr int THREADS = (STORE_WARPS + 2) * 32;
+constexpr int SCALE_WARPS = 4;
+constexpr int THREADS = (STORE_WARPS + 2 + SCALE_WARPS) * 32;
 constexpr u32 CODES = MX4_ROWS * 128;              // codes of one operand tile
 constexpr u32 SPAN = 2 * MX4_ROWS;                 // rows of a and of b per pair
 constexpr u32 GROUP = 8;                           // tiles of a that are visited before the next tile of b
@@ -42,7 +43,7 @@ struct WideArgs {
 template <int FMT>
 struct Shared {
     unsigned long long full[stages<FMT>()];        // own copies have landed
-    unsigned long long peer[stages<FMT>()];        // even CTA: the partner's have
+    unsigned long long ready[stages<FMT>()];       // even CTA: both CTAs' have, and the scales are in tensor memory
     unsigned long long empty[stages<FMT>()];       // the stage has been multiplied
     unsigned long long acc_full, acc_empty;
     u32 tmem;
@@ -53,10 +54,10 @@ template <typename S>
 __device__ __forceinline__ bool wait_one(S* sh, unsigned long long* bar, u32 parity, const WideArgs& g) {
     if (g.wait_ns) {
         for (int i = 0; i < 64; ++i)
-            if (mbar_try_wait_cluster(bar, parity)) return true;
+            if (mbar_try_wait(bar, parity)) return true;
         const u64 t0 = global_ns();
         while (!sh->abort) {
-            if (mbar_try_wait_cluster(bar, parity)) return true;
+            if (mbar_try_wait(bar, parity)) return true;
             if (global_ns() - t0 > g.wait_ns) break;
         }
     }
@@ -69,7 +70,7 @@ __device__ __forceinline__ bool wait_one(S* sh, unsigned long long* bar, u32 par
 }
 __device__ __forceinline__ void drain_one(unsigned long long* bar, u32 parity) {
     const u64 t0 = global_ns();
-    while (!mbar_try_wait_cluster(bar, parity) && global_ns() - t0 < DRAIN_NS) {}
+    while (!mbar_try_wait(bar, parity) && global_ns() - t0 < DRAIN_NS) {}
 }
 
 // Tile `t` of the pairs' common order: GROUP tiles of m for one tile of n, then the next tile of n.
@@ -90,6 +91,30 @@ __device__ __forceinline__ void store32(void* p, const u32 v[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
+// The first `cols` of a row's results, packed in WORDS words.
+template <typename T, u32 WORDS>
+__device__ __forceinline__ void put_row(T* y, const u32 (&w)[WORDS], u32 cols, u32 wide_store) {
+    constexpr u32 PER = 4 / sizeof(T);
+#pragma unroll
+    for (u32 i = 0; i < WORDS; i += 8) {
+        if (wide_store && (i + 8) * PER <= cols) {
+            const u32 v[8] = {w[i], w[i + 1], w[i + 2], w[i + 3], w[i + 4], w[i + 5], w[i + 6], w[i + 7]};
+            store32(y + i * PER, v);
+        } else {
+#pragma unroll
+            for (u32 e = 0; e < 8; ++e) {
+                if constexpr (PER == 2) {
+                    unsigned short* h = reinterpret_cast<unsigned short*>(y) + (i + e) * 2;
+                    if ((i + e) * 2 < cols) h[0] = (unsigned short)(w[i + e] & 0xffffu);
+                    if ((i + e) * 2 + 1 < cols) h[1] = (unsigned short)(w[i + e] >> 16);
+                } else {
+                    if (i + e < cols) reinterpret_cast<u32*>(y)[i + e] = w[i + e];
+                }
+            }
+        }
+    }
+}
+
 template <int FMT, int DT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_kernel(const __grid_constant__ WideArgs g) {
     typedef typename ElemOf<DT>::type T;
@@ -108,7 +133,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
     const u32 tiles = g.m_tiles * g.n_tiles;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.peer[s], 1); mbar_init(&sh.empty[s], 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.ready[s], 2 * SCALE_WARPS); mbar_init(&sh.empty[s], 1); }
         mbar_init(&sh.acc_full, 1);
         mbar_init(&sh.acc_empty, 2 * STORE_WARPS);
         sh.abort = 0;
@@ -169,17 +194,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
                 tm_fence_after();
                 for (u32 k = 0; k < g.col_tiles; ++k, ++step) {
                     const u32 s = step % STAGES, parity = (step / STAGES) & 1;
-                    if (!wait_one(&sh, &sh.full[s], parity, g) || !wait_one(&sh, &sh.peer[s], parity, g)) { ok = false; break; }
+                    if (!wait_one(&sh, &sh.ready[s], parity, g)) { ok = false; break; }
                     tm_fence_after();
-                    const u32 st = base + s * STAGE, scales = st + 2 * CODES;
-                    // each stage has scale columns of its own, free again when the stage is
+                    const u32 st = base + s * STAGE;
                     const u32 sa = tmem + SPAN + s * SF_COLS, sb = sa + PIECES * 4;
-#pragma unroll
-                    for (u32 j = 0; j < PIECES; ++j) {
-                        tm2_copy_scales(sa + j * 4, desc_scales(scales + j * MX4_PIECE));
-                        tm2_copy_scales(sb + j * 8, desc_scales(scales + SB + j * MX4_PIECE));
-                        tm2_copy_scales(sb + j * 8 + 4, desc_scales(scales + 2 * SB + j * MX4_PIECE));
-                    }
                     const u64 da = desc_swizzled(st), db = desc_swizzled(st + CODES);
 #pragma unroll
                     for (u32 i = 0; i < 4; ++i) {  // 64 columns = 32 bytes of codes each
@@ -198,13 +216,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
                 tm2_commit(&sh.acc_full);
                 drain_one(&sh.acc_full, turn_acc & 1);
             }
-        } else {
-            for (u32 t = pair; ok && t < tiles; t += pairs) {
-                for (u32 k = 0; k < g.col_tiles; ++k, ++step) {
-                    const u32 s = step % STAGES;
-                    if (!wait_one(&sh, &sh.full[s], (step / STAGES) & 1, g)) { ok = false; break; }
-                    mbar_arrive_cluster(cluster_address(&sh.peer[s], 0));
+        }
+    } else if (warp >= STORE_WARPS + 2) {
+        // Scales from shared memory to the tensor-memory lanes of the warp's place: row 32 c + l of a piece is four bytes of
+        // lane l, column c.  (The tensor core's own copy instruction queues up with the products, 65 cycles for 512 bytes.)
+        const u32 quarter = warp & 3;
+        u32 step = 0;
+        bool ok = true;
+        for (u32 t = pair; ok && t < tiles; t += pairs) {
+            for (u32 k = 0; k < g.col_tiles; ++k, ++step) {
+                const u32 s = step % STAGES;
+                const bool landed = lane == 0 ? wait_one(&sh, &sh.full[s], (step / STAGES) & 1, g) : true;
+                if (!__all_sync(0xffffffffu, landed)) { ok = false; break; }
+                const uint4* from = reinterpret_cast<const uint4*>(smem + s * STAGE + 2 * CODES) + lane;
+                // each stage has scale columns of its own, free again when the stage is
+                const u32 sa = tmem + ((quarter * 32) << 16) + SPAN + s * SF_COLS, sb = sa + PIECES * 4;
+                uint4 a[PIECES], b[PIECES * 2];
+#pragma unroll
+                for (u32 j = 0; j < PIECES; ++j) {
+                    a[j] = from[j * 32];
+                    b[2 * j] = from[(PIECES + j) * 32];
+                    b[2 * j + 1] = from[(2 * PIECES + j) * 32];
                 }
+                if (FMT == MX4_E4M3_16) {
+                    tm_store16(sa, reinterpret_cast<const u32*>(a));
+                    tm_store32(sb, reinterpret_cast<const u32*>(b));
+                } else {
+                    tm_store8(sa, reinterpret_cast<const u32*>(a));
+                    tm_store16(sb, reinterpret_cast<const u32*>(b));
+                }
+                tm_wait_store();
+                tm_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(cluster_address(&sh.ready[s], 0));
             }
         }
     } else if (warp < STORE_WARPS) {
@@ -218,43 +262,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             const bool ready = lane == 0 ? wait_one(&sh, &sh.acc_full, turn & 1, g) : true;
             if (!__all_sync(0xffffffffu, ready)) break;
             tm_fence_after();
-            u32 v[128];
-#pragma unroll
-            for (u32 i = 0; i < 4; ++i) tm_load32(tmem + ((quarter * 32) << 16) + c0 + i * 32, v + i * 32);
-            tm_wait_load();
-            tm_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(cluster_address(&sh.acc_empty, 0));
-
             const u64 m = (u64)(2 * mt + rank) * MX4_ROWS + quarter * 32 + lane;
             const u64 n0 = (u64)nt * SPAN + c0;
-            if (m >= g.m.rows || n0 >= g.n.rows) continue;
+            const u32 cols = n0 < g.n.rows ? (u32)min((u64)128, g.n.rows - n0) : 0u;
             T* y = static_cast<T*>(g.y) + m * g.stride + n0;
-            const u32 cols = (u32)min((u64)128, g.n.rows - n0);
-            constexpr u32 PER = 32 / sizeof(T);    // results in 32 bytes
+            // 16-bit results wait in registers until the accumulator has been handed back; fp32 ones, twice as many, leave in
+            // four parts, the last one after that
+            constexpr u32 PER = 4 / sizeof(T), HELD = sizeof(T) == 2 ? 64 : 32;      // results in a word; words in registers
+            u32 w[HELD];
 #pragma unroll
-            for (u32 c = 0; c < 128; c += PER) {
-                float f[PER];
-#pragma unroll
-                for (u32 i = 0; i < PER; ++i) {
-                    f[i] = __uint_as_float(v[c + i]) * alpha;
-                    if (g.bias && c + i < cols) f[i] += __ldg(g.bias + n0 + c + i);
+            for (u32 c = 0; c < 128; c += 32) {
+                u32 v[32];
+                tm_load32(tmem + ((quarter * 32) << 16) + c0 + c, v);
+                tm_wait_load();
+                if (c == 96) {                     // all columns are in registers
+                    tm_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(cluster_address(&sh.acc_empty, 0));
                 }
-                if (g.wide_store && c + PER <= cols) {
-                    u32 w[8];
-                    if constexpr (DT == DT_F32) {
 #pragma unroll
-                        for (u32 i = 0; i < 8; ++i) w[i] = __float_as_uint(f[i]);
-                    } else {
+                for (u32 i = 0; i < 32; i += PER) {
+                    float f[PER];
 #pragma unroll
-                        for (u32 i = 0; i < 8; ++i) w[i] = two<DT>(f[2 * i], f[2 * i + 1]);
+                    for (u32 e = 0; e < PER; ++e) {
+                        f[e] = __uint_as_float(v[i + e]) * alpha;
+                        if (g.bias && c + i + e < cols) f[e] += __ldg(g.bias + n0 + c + i + e);
                     }
-                    store32(y + c, w);
-                } else {
-#pragma unroll
-                    for (u32 i = 0; i < PER; ++i) if (c + i < cols) wput(y, c + i, f[i]);
+                    if constexpr (PER == 2) w[(c + i) / 2] = two<DT>(f[0], f[1]);
+                    else w[i] = __float_as_uint(f[0]);
                 }
+                if (PER == 1 && m < g.m.rows) put_row<T, HELD>(y + c, w, cols > c ? cols - c : 0, g.wide_store);
             }
+            if (PER == 2 && m < g.m.rows) put_row<T, HELD>(y, w, cols, g.wide_store);
         }
     }
     __syncwarp();
