@@ -5,9 +5,9 @@
 // therefore works on one 256 x 256 tile (tcgen05 cta_group::2): each holds 128 rows of a and half the rows of b,
 // which takes a third off the traffic.
 //
-// Persistent pairs: pair p computes tiles p, p + pairs, ...  Roles in each CTA: warps 0..7 write the result, warp 8
-// fetches (contiguous bulk copies, the packed layout is the tensor core's), warp 9 of the even CTA issues the matrix
-// instructions, warps 10..13 bring the block scales to tensor memory.  The accumulator (256 columns of tensor memory) is read
+// Persistent pairs: pair p computes tiles p, p + pairs, ...  Roles in each CTA: warps 0..7 write the result, warps 8..11
+// bring the block scales to tensor memory, warps 12..14 fetch (contiguous bulk copies, the packed layout is the tensor
+// core's), warp 15 of the even CTA issues the matrix instructions.  The accumulator (256 columns of tensor memory) is read
 // into registers in one go and handed back before it is converted and written, so that the next tile waits for a
 // few hundred cycles only.
 // Every wait is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and leaves (the
@@ -20,13 +20,16 @@ namespace {
 
 constexpr int STORE_WARPS = 8;
 constexpr int SCALE_WARPS = 4;
-constexpr int THREADS = (STORE_WARPS + 2 + SCALE_WARPS) * 32;
+constexpr int FETCH_WARPS = 3;
+constexpr u32 SCALE_WARP = STORE_WARPS, FETCH_WARP = SCALE_WARP + SCALE_WARPS, PRODUCT_WARP = FETCH_WARP + FETCH_WARPS;
+constexpr int THREADS = (PRODUCT_WARP + 1) * 32;
 constexpr u32 CODES = MX4_ROWS * 128;              // codes of one operand tile
 constexpr u32 SPAN = 2 * MX4_ROWS;                 // rows of a and of b per pair
 constexpr u32 GROUP = 8;                           // tiles of a that are visited before the next tile of b
 constexpr u64 DRAIN_NS = 100000000ull;
 
 template <int FMT> __host__ __device__ constexpr int stages() { return FMT == MX4_E4M3_16 ? 5 : 6; }
+// A stage: tile of m (codes, scales), own tile of n (codes, scales), scales of the partner's tile of n.
 template <int FMT> __host__ __device__ constexpr u32 stage_bytes() { return 2 * CODES + 3 * mx4_scale_bytes(FMT); }
 
 struct WideArgs {
@@ -50,28 +53,44 @@ struct Shared {
     volatile u32 abort;
 };
 
+// A whole warp waits for phase `parity` of `bar`; false when the limit has passed or another role gave up.
 template <typename S>
-__device__ __forceinline__ bool wait_one(S* sh, unsigned long long* bar, u32 parity, const WideArgs& g) {
-    if (g.wait_ns) {
-        for (int i = 0; i < 64; ++i)
-            if (mbar_try_wait(bar, parity)) return true;
+__device__ __noinline__ bool wait_long(S* sh, unsigned long long* bar, u32 parity, u64 limit_ns, u32* flag) {
+    if (limit_ns) {
         const u64 t0 = global_ns();
-        while (!sh->abort) {
-            if (mbar_try_wait(bar, parity)) return true;
-            if (global_ns() - t0 > g.wait_ns) break;
+        while (!__any_sync(0xffffffffu, sh->abort)) {
+            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+            if (__any_sync(0xffffffffu, global_ns() - t0 > limit_ns)) break;
         }
     }
-    if (!sh->abort) {
+    if (!__any_sync(0xffffffffu, sh->abort)) {
         sh->abort = 1;
-        *reinterpret_cast<volatile u32*>(g.flag) = 1;
+        *reinterpret_cast<volatile u32*>(flag) = 1;
         __threadfence_system();
     }
     return false;
 }
-__device__ __forceinline__ void drain_one(unsigned long long* bar, u32 parity) {
-    const u64 t0 = global_ns();
-    while (!mbar_try_wait(bar, parity) && global_ns() - t0 < DRAIN_NS) {}
+template <typename S>
+__device__ __forceinline__ bool wait_warp(S* sh, unsigned long long* bar, u32 parity, const WideArgs& g) {
+    if (g.wait_ns)
+        for (int i = 0; i < 32; ++i)
+            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return wait_long(sh, bar, parity, g.wait_ns, g.flag);
 }
+// The same without raising anything: for letting one's own work land before leaving.
+__device__ __forceinline__ void drain_warp(unsigned long long* bar, u32 parity) {
+    const u64 t0 = global_ns();
+    while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)) && !__any_sync(0xffffffffu, global_ns() - t0 > DRAIN_NS)) {}
+}
+
+// The place in the ring of stages, and the parity of its current turn.
+template <int STAGES>
+struct Ring {
+    u32 s = 0, parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++s == STAGES) { s = 0; parity ^= 1; }
+    }
+};
 
 // Tile `t` of the pairs' common order: GROUP tiles of m for one tile of n, then the next tile of n.
 __device__ __forceinline__ void place(const WideArgs& g, u32 t, u32& mt, u32& nt) {
@@ -128,115 +147,127 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
     // the swizzle goes by address: stages start on 1024 bytes (the same offset in both CTAs)
     unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const u32 base = smem_u32(smem);
-    const u32 warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const u32 warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const u32 rank = cluster_rank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const u32 tiles = g.m_tiles * g.n_tiles;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.ready[s], 2 * SCALE_WARPS); mbar_init(&sh.empty[s], 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], FETCH_WARPS); mbar_init(&sh.ready[s], 2 * SCALE_WARPS); mbar_init(&sh.empty[s], 1); }
         mbar_init(&sh.acc_full, 1);
         mbar_init(&sh.acc_empty, 2 * STORE_WARPS);
         sh.abort = 0;
         mbar_fence_init();
     }
-    if (warp == STORE_WARPS + 1) tm2_alloc(&sh.tmem, TMEM_COLS);
+    if (warp == PRODUCT_WARP) tm2_alloc(&sh.tmem, TMEM_COLS);
     tm_fence_before();
     __syncthreads();
     cluster_barrier();                             // the partner's barriers are ready
     tm_fence_after();
     const u32 tmem = sh.tmem;
 
-    if (warp == STORE_WARPS && lane == 0) {
-        u32 step = 0;                              // stages filled so far
+    if (warp >= FETCH_WARP && warp < PRODUCT_WARP) {
+        // Three warps fetch: the tile of m, the own tile of n, and of the partner's tile of n the scales (each CTA's tensor memory
+        // holds those of all of n's rows).  Issuing a copy takes one or two hundred cycles, more than a stage has for three.
+        const u32 item = warp - FETCH_WARP;
+        Ring<STAGES> ring;
+        u32 filled = 0;
         bool ok = true;
         for (u32 t = pair; ok && t < tiles; t += pairs) {
             u32 mt, nt;
             place(g, t, mt, nt);
-            const u32 rm = 2 * mt + rank, rn = 2 * nt;
+            const u64 rows = item == 0 ? g.m.rows : g.n.rows;
+            const u32 rt = item == 0 ? 2 * mt + rank : 2 * nt + (item == 1 ? rank : 1 - rank);
             // row tiles past the end are not fetched: their rows' results are not written
-            const bool has_m = (u64)rm * MX4_ROWS < g.m.rows, has_n1 = (u64)(rn + 1) * MX4_ROWS < g.n.rows, has_own = rank == 0 || has_n1;
-            const u32 hm = has_m ? mx4_tile_height(g.m.rows, rm) : 0;
-            const u32 h0 = mx4_tile_height(g.n.rows, rn), h1 = has_n1 ? mx4_tile_height(g.n.rows, rn + 1) : 0;
-            const u32 own = rank == 0 ? h0 : h1;
-            const unsigned char* pm = has_m ? g.m.p + mx4_tile_offset(g.m.rows, g.col_tiles, FMT, rm, 0) : nullptr;
-            const unsigned char* p0 = g.n.p + mx4_tile_offset(g.n.rows, g.col_tiles, FMT, rn, 0);
-            const unsigned char* p1 = has_n1 ? g.n.p + mx4_tile_offset(g.n.rows, g.col_tiles, FMT, rn + 1, 0) : nullptr;
-            const u32 bytes = hm * 128 + (has_m ? SB : 0) + own * 128 + SB + (has_n1 ? SB : 0);
-            for (u32 k = 0; k < g.col_tiles; ++k, ++step) {
-                const u32 s = step % STAGES, turn = step / STAGES;
-                if (turn && !wait_one(&sh, &sh.empty[s], (turn - 1) & 1, g)) { ok = false; break; }
-                unsigned char* st = smem + s * STAGE;
-                unsigned long long* bar = &sh.full[s];
-                mbar_arrive_expect_tx(bar, bytes);
-                if (has_m) {
-                    bulk_g2s(st, pm, hm * 128, bar);
-                    bulk_g2s(st + 2 * CODES, pm + hm * 128, SB, bar);
-                    pm += hm * 128 + SB;
+            const bool there = (u64)rt * MX4_ROWS < rows;
+            const u32 height = there ? mx4_tile_height(rows, rt) : 0, advance = height * 128 + SB;
+            const unsigned char* from = (item == 0 ? g.m.p : g.n.p) + (there ? mx4_tile_offset(rows, g.col_tiles, FMT, rt, 0) : 0);
+            const u32 at = item == 0 ? 0 : item == 1 ? CODES + SB : 2 * (CODES + SB);
+            // codes at their place and the scales, which follow them in the packed tile, behind 128 rows: a full tile is one copy
+            const bool full = there && height == MX4_ROWS && item != 2;
+            for (u32 k = 0; k < g.col_tiles; ++k) {
+                if (filled >= STAGES && !wait_warp(&sh, &sh.empty[ring.s], ring.parity ^ 1, g)) { ok = false; break; }
+                unsigned char* to = smem + ring.s * STAGE + at;
+                unsigned long long* bar = &sh.full[ring.s];
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(bar, !there ? 0 : item == 2 ? SB : advance);
+                    if (full) {
+                        bulk_g2s(to, from, CODES + SB, bar);
+                    } else if (there) {
+                        if (item != 2) bulk_g2s(to, from, height * 128, bar);
+                        bulk_g2s(item == 2 ? to : to + CODES, from + height * 128, SB, bar);
+                    }
                 }
-                if (has_own) bulk_g2s(st + CODES, rank == 0 ? p0 : p1, own * 128, bar);
-                bulk_g2s(st + 2 * CODES + SB, p0 + h0 * 128, SB, bar);      // the scales of all of n's rows go to both CTAs
-                p0 += h0 * 128 + SB;
-                if (has_n1) {
-                    bulk_g2s(st + 2 * CODES + 2 * SB, p1 + h1 * 128, SB, bar);
-                    p1 += h1 * 128 + SB;
-                }
+                __syncwarp();
+                from += advance;
+                ++filled;
+                ring.next();
             }
         }
-        // no copy may be in flight when the CTA leaves
-        for (u32 k = step > STAGES ? step - STAGES : 0; k < step; ++k) drain_one(&sh.full[k % STAGES], (k / STAGES) & 1);
-    } else if (warp == STORE_WARPS + 1 && lane == 0) {
-        u32 step = 0, turn_acc = 0;
-        bool ok = true;
+        // no copy may be in flight when the CTA leaves: the last turn of every stage that was filled
+        for (u32 i = 0; i < STAGES && i < filled; ++i) {
+            if (ring.s == 0) { ring.s = STAGES; ring.parity ^= 1; }
+            --ring.s;
+            drain_warp(&sh.full[ring.s], ring.parity);
+        }
+    } else if (warp == PRODUCT_WARP) {
         if (rank == 0) {
             constexpr u32 IDESC = (1u << 7) | (1u << 10) | ((SPAN >> 3) << 17) | (FMT == MX4_E8M0_32 ? 1u << 23 : 0u) | ((SPAN >> 4) << 24);
-            for (u32 t = pair; ok && t < tiles; t += pairs, ++turn_acc) {
-                if (turn_acc && !wait_one(&sh, &sh.acc_empty, (turn_acc - 1) & 1, g)) { ok = false; break; }
-                tm_fence_after();
-                for (u32 k = 0; k < g.col_tiles; ++k, ++step) {
-                    const u32 s = step % STAGES, parity = (step / STAGES) & 1;
-                    if (!wait_one(&sh, &sh.ready[s], parity, g)) { ok = false; break; }
+            Ring<STAGES> ring;
+            u32 turn = 0;
+            bool ok = true;
+            for (u32 t = pair; ok && t < tiles; t += pairs, ++turn) {
+                if (turn && !wait_warp(&sh, &sh.acc_empty, (turn - 1) & 1, g)) { ok = false; break; }
+                for (u32 k = 0; k < g.col_tiles; ++k) {
+                    if (!wait_warp(&sh, &sh.ready[ring.s], ring.parity, g)) { ok = false; break; }
                     tm_fence_after();
-                    const u32 st = base + s * STAGE;
-                    const u32 sa = tmem + SPAN + s * SF_COLS, sb = sa + PIECES * 4;
-                    const u64 da = desc_swizzled(st), db = desc_swizzled(st + CODES);
+                    const u32 st = base + ring.s * STAGE;
+                    const u32 sa = tmem + SPAN + ring.s * SF_COLS, sb = sa + PIECES * 4;
+                    const u64 da = desc_swizzled(st), db = desc_swizzled(st + CODES + SB);
+                    if (elect_one()) {
 #pragma unroll
-                    for (u32 i = 0; i < 4; ++i) {  // 64 columns = 32 bytes of codes each
-                        if (FMT == MX4_E4M3_16) {
-                            tm2_mma_block16(tmem, da + 2 * i, db + 2 * i, IDESC, sa + i * 4, sb + i * 8, k || i);
-                        } else {
-                            const u32 half = (i & 1) * 2, j = i >> 1;      // a piece serves two instructions
-                            tm2_mma_block32(tmem, da + 2 * i, db + 2 * i, IDESC | (half << 4) | (half << 29), sa + j * 4, sb + j * 8, k || i);
+                        for (u32 i = 0; i < 4; ++i) {  // 64 columns = 32 bytes of codes each
+                            if (FMT == MX4_E4M3_16) {
+                                tm2_mma_block16(tmem, da + 2 * i, db + 2 * i, IDESC, sa + i * 4, sb + i * 8, k || i);
+                            } else {
+                                const u32 half = (i & 1) * 2, j = i >> 1;      // a piece serves two instructions
+                                tm2_mma_block32(tmem, da + 2 * i, db + 2 * i, IDESC | (half << 4) | (half << 29), sa + j * 4, sb + j * 8, k || i);
+                            }
                         }
+                        tm2_commit(&sh.empty[ring.s]);
+                        if (k + 1 == g.col_tiles) tm2_commit(&sh.acc_full);
                     }
-                    tm2_commit(&sh.empty[s]);
+                    __syncwarp();
+                    ring.next();
                 }
-                if (ok) tm2_commit(&sh.acc_full);
             }
             if (!ok) {                             // what has been issued is done before tensor memory goes
-                tm2_commit(&sh.acc_full);
-                drain_one(&sh.acc_full, turn_acc & 1);
+                if (elect_one()) tm2_commit(&sh.acc_full);
+                __syncwarp();
+                drain_warp(&sh.acc_full, turn & 1);
             }
         }
-    } else if (warp >= STORE_WARPS + 2) {
+    } else if (warp >= SCALE_WARP) {
         // Scales from shared memory to the tensor-memory lanes of the warp's place: row 32 c + l of a piece is four bytes of
         // lane l, column c.  (The tensor core's own copy instruction queues up with the products, 65 cycles for 512 bytes.)
         const u32 quarter = warp & 3;
-        u32 step = 0;
+        Ring<STAGES> ring;
         bool ok = true;
         for (u32 t = pair; ok && t < tiles; t += pairs) {
-            for (u32 k = 0; k < g.col_tiles; ++k, ++step) {
-                const u32 s = step % STAGES;
-                const bool landed = lane == 0 ? wait_one(&sh, &sh.full[s], (step / STAGES) & 1, g) : true;
-                if (!__all_sync(0xffffffffu, landed)) { ok = false; break; }
-                const uint4* from = reinterpret_cast<const uint4*>(smem + s * STAGE + 2 * CODES) + lane;
+            for (u32 k = 0; k < g.col_tiles; ++k) {
+                if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g)) { ok = false; break; }
+                const uint4* from = reinterpret_cast<const uint4*>(smem + ring.s * STAGE + CODES) + lane;
+                const uint4* own = from + (CODES + SB) / 16;
+                const uint4* other = own + SB / 16;
+                const uint4* n0 = rank == 0 ? own : other;
+                const uint4* n1 = rank == 0 ? other : own;
                 // each stage has scale columns of its own, free again when the stage is
-                const u32 sa = tmem + ((quarter * 32) << 16) + SPAN + s * SF_COLS, sb = sa + PIECES * 4;
+                const u32 sa = tmem + ((quarter * 32) << 16) + SPAN + ring.s * SF_COLS, sb = sa + PIECES * 4;
                 uint4 a[PIECES], b[PIECES * 2];
 #pragma unroll
                 for (u32 j = 0; j < PIECES; ++j) {
                     a[j] = from[j * 32];
-                    b[2 * j] = from[(PIECES + j) * 32];
-                    b[2 * j + 1] = from[(2 * PIECES + j) * 32];
+                    b[2 * j] = n0[j * 32];
+                    b[2 * j + 1] = n1[j * 32];
                 }
                 if (FMT == MX4_E4M3_16) {
                     tm_store16(sa, reinterpret_cast<const u32*>(a));
@@ -248,7 +279,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
                 tm_wait_store();
                 tm_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(cluster_address(&sh.ready[s], 0));
+                if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.ready[ring.s], 0));
+                ring.next();
             }
         }
     } else if (warp < STORE_WARPS) {
@@ -259,8 +291,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             u32 mt, nt;
             place(g, t, mt, nt);
             __syncwarp();
-            const bool ready = lane == 0 ? wait_one(&sh, &sh.acc_full, turn & 1, g) : true;
-            if (!__all_sync(0xffffffffu, ready)) break;
+            if (!wait_warp(&sh, &sh.acc_full, turn & 1, g)) break;
             tm_fence_after();
             const u64 m = (u64)(2 * mt + rank) * MX4_ROWS + quarter * 32 + lane;
             const u64 n0 = (u64)nt * SPAN + c0;
@@ -300,7 +331,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
     tm_fence_before();
     __syncthreads();
     cluster_barrier();                             // neither CTA's memory is needed any more
-    if (warp == STORE_WARPS + 1) tm2_dealloc(tmem, TMEM_COLS);
+    if (warp == PRODUCT_WARP) tm2_dealloc(tmem, TMEM_COLS);
 }
 
 template <int FMT, int DT>

@@ -7,6 +7,14 @@
 
 namespace excp {
 
+// One lane of a converged warp.  Roles run their loops as whole warps and elect the lane that issues, so that addresses
+// and descriptors stay in uniform registers, where these instructions take them.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 // Whole warp: `cols` (a power of two, 32..512) columns of tensor memory; the address lands in shared memory.
 __device__ __forceinline__ void tm_alloc(uint32_t* dst_smem, uint32_t cols) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst_smem)), "r"(cols) : "memory");
