@@ -298,31 +298,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             const u32 cols = n0 < g.n.rows ? (u32)min((u64)128, g.n.rows - n0) : 0u;
             T* y = static_cast<T*>(g.y) + m * g.stride + n0;
             // 16-bit results wait in registers until the accumulator has been handed back; fp32 ones, twice as many, leave in
-            // four parts, the last one after that
-            constexpr u32 PER = 4 / sizeof(T), HELD = sizeof(T) == 2 ? 64 : 32;      // results in a word; words in registers
-            u32 w[HELD];
+            // parts of 16, the last one after that
+            constexpr u32 PART = 16, PER = 4 / sizeof(T), HELD = sizeof(T) == 2 ? 64 : PART;   // columns; results in a word; words held
+            const u32 from = tmem + ((quarter * 32) << 16) + c0;
+            u32 w[HELD], v[2][PART];
+            tm_load16(from, v[0]);
 #pragma unroll
-            for (u32 c = 0; c < 128; c += 32) {
-                u32 v[32];
-                tm_load32(tmem + ((quarter * 32) << 16) + c0 + c, v);
+            for (u32 p = 0; p < 128 / PART; ++p) {
                 tm_wait_load();
-                if (c == 96) {                     // all columns are in registers
+                if (p + 1 < 128 / PART) {
+                    tm_load16(from + (p + 1) * PART, v[(p + 1) & 1]);
+                } else {                           // all columns are in registers
                     tm_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(cluster_address(&sh.acc_empty, 0));
+                    if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.acc_empty, 0));
+                }
+                float f[PART];
+#pragma unroll
+                for (u32 i = 0; i < PART; ++i) f[i] = __uint_as_float(v[p & 1][i]) * alpha;
+                if (g.bias) {
+#pragma unroll
+                    for (u32 i = 0; i < PART; ++i) f[i] += p * PART + i < cols ? __ldg(g.bias + n0 + p * PART + i) : 0.f;
                 }
 #pragma unroll
-                for (u32 i = 0; i < 32; i += PER) {
-                    float f[PER];
-#pragma unroll
-                    for (u32 e = 0; e < PER; ++e) {
-                        f[e] = __uint_as_float(v[i + e]) * alpha;
-                        if (g.bias && c + i + e < cols) f[e] += __ldg(g.bias + n0 + c + i + e);
-                    }
-                    if constexpr (PER == 2) w[(c + i) / 2] = two<DT>(f[0], f[1]);
-                    else w[i] = __float_as_uint(f[0]);
+                for (u32 i = 0; i < PART; i += PER) {
+                    if constexpr (PER == 2) w[(p * PART + i) / 2] = two<DT>(f[i], f[i + 1]);
+                    else w[i] = __float_as_uint(f[i]);
                 }
-                if (PER == 1 && m < g.m.rows) put_row<T, HELD>(y + c, w, cols > c ? cols - c : 0, g.wide_store);
+                if (PER == 1 && m < g.m.rows) put_row<T, HELD>(y + p * PART, w, cols > p * PART ? cols - p * PART : 0, g.wide_store);
             }
             if (PER == 2 && m < g.m.rows) put_row<T, HELD>(y, w, cols, g.wide_store);
         }
