@@ -23,6 +23,7 @@ constexpr int SCALE_WARPS = 4;
 constexpr int FETCH_WARPS = 3;
 constexpr u32 SCALE_WARP = STORE_WARPS, FETCH_WARP = SCALE_WARP + SCALE_WARPS, PRODUCT_WARP = FETCH_WARP + FETCH_WARPS;
 constexpr int THREADS = (PRODUCT_WARP + 1) * 32;
+constexpr int UP = 168, DOWN = 88;                 // registers per thread of the store warps and of the others
 constexpr u32 CODES = MX4_ROWS * 128;              // codes of one operand tile
 constexpr u32 SPAN = 2 * MX4_ROWS;                 // rows of a and of b per pair
 constexpr u32 GROUP = 8;                           // tiles of a that are visited before the next tile of b
@@ -55,7 +56,7 @@ struct Shared {
 
 // A whole warp waits for phase `parity` of `bar`; false when the limit has passed or another role gave up.
 template <typename S>
-__device__ __noinline__ bool wait_long(S* sh, unsigned long long* bar, u32 parity, u64 limit_ns, u32* flag) {
+__device__ __forceinline__ bool wait_long(S* sh, unsigned long long* bar, u32 parity, u64 limit_ns, u32* flag) {
     if (limit_ns) {
         const u64 t0 = global_ns();
         while (!__any_sync(0xffffffffu, sh->abort)) {
@@ -165,52 +166,56 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
     tm_fence_after();
     const u32 tmem = sh.tmem;
 
-    if (warp >= FETCH_WARP && warp < PRODUCT_WARP) {
-        // Three warps fetch: the tile of m, the own tile of n, and of the partner's tile of n the scales (each CTA's tensor memory
-        // holds those of all of n's rows).  Issuing a copy takes one or two hundred cycles, more than a stage has for three.
-        const u32 item = warp - FETCH_WARP;
-        Ring<STAGES> ring;
-        u32 filled = 0;
-        bool ok = true;
-        for (u32 t = pair; ok && t < tiles; t += pairs) {
-            u32 mt, nt;
-            place(g, t, mt, nt);
-            const u64 rows = item == 0 ? g.m.rows : g.n.rows;
-            const u32 rt = item == 0 ? 2 * mt + rank : 2 * nt + (item == 1 ? rank : 1 - rank);
-            // row tiles past the end are not fetched: their rows' results are not written
-            const bool there = (u64)rt * MX4_ROWS < rows;
-            const u32 height = there ? mx4_tile_height(rows, rt) : 0, advance = height * 128 + SB;
-            const unsigned char* from = (item == 0 ? g.m.p : g.n.p) + (there ? mx4_tile_offset(rows, g.col_tiles, FMT, rt, 0) : 0);
-            const u32 at = item == 0 ? 0 : item == 1 ? CODES + SB : 2 * (CODES + SB);
-            // codes at their place and the scales, which follow them in the packed tile, behind 128 rows: a full tile is one copy
-            const bool full = there && height == MX4_ROWS && item != 2;
-            for (u32 k = 0; k < g.col_tiles; ++k) {
-                if (filled >= STAGES && !wait_warp(&sh, &sh.empty[ring.s], ring.parity ^ 1, g)) { ok = false; break; }
-                unsigned char* to = smem + ring.s * STAGE + at;
-                unsigned long long* bar = &sh.full[ring.s];
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(bar, !there ? 0 : item == 2 ? SB : advance);
-                    if (full) {
-                        bulk_g2s(to, from, CODES + SB, bar);
-                    } else if (there) {
-                        if (item != 2) bulk_g2s(to, from, height * 128, bar);
-                        bulk_g2s(item == 2 ? to : to + CODES, from + height * 128, SB, bar);
+    // The store warps hold 128 accumulator columns at a time: they take the registers that the others do without.
+    static_assert(THREADS == 512 && STORE_WARPS == 8 && 256 * UP + 256 * DOWN <= 512 * 128, "registers: launched with 128 a thread");
+
+    if (warp >= FETCH_WARP) {
+        registers_down<DOWN>();
+        if (warp < PRODUCT_WARP) {
+            // Three warps fetch: the tile of m, the own tile of n, and of the partner's tile of n the scales (each CTA's tensor memory
+            // holds those of all of n's rows).  Issuing a copy takes one or two hundred cycles, more than a stage has for three.
+            const u32 item = warp - FETCH_WARP;
+            Ring<STAGES> ring;
+            u32 filled = 0;
+            bool ok = true;
+            for (u32 t = pair; ok && t < tiles; t += pairs) {
+                u32 mt, nt;
+                place(g, t, mt, nt);
+                const u64 rows = item == 0 ? g.m.rows : g.n.rows;
+                const u32 rt = item == 0 ? 2 * mt + rank : 2 * nt + (item == 1 ? rank : 1 - rank);
+                // row tiles past the end are not fetched: their rows' results are not written
+                const bool there = (u64)rt * MX4_ROWS < rows;
+                const u32 height = there ? mx4_tile_height(rows, rt) : 0, advance = height * 128 + SB;
+                const unsigned char* from = (item == 0 ? g.m.p : g.n.p) + (there ? mx4_tile_offset(rows, g.col_tiles, FMT, rt, 0) : 0);
+                const u32 at = item == 0 ? 0 : item == 1 ? CODES + SB : 2 * (CODES + SB);
+                // codes at their place and the scales, which follow them in the packed tile, behind 128 rows: a full tile is one copy
+                const bool full = there && height == MX4_ROWS && item != 2;
+                for (u32 k = 0; k < g.col_tiles; ++k) {
+                    if (filled >= STAGES && !wait_warp(&sh, &sh.empty[ring.s], ring.parity ^ 1, g)) { ok = false; break; }
+                    unsigned char* to = smem + ring.s * STAGE + at;
+                    unsigned long long* bar = &sh.full[ring.s];
+                    if (elect_one()) {
+                        mbar_arrive_expect_tx(bar, !there ? 0 : item == 2 ? SB : advance);
+                        if (full) {
+                            bulk_g2s(to, from, CODES + SB, bar);
+                        } else if (there) {
+                            if (item != 2) bulk_g2s(to, from, height * 128, bar);
+                            bulk_g2s(item == 2 ? to : to + CODES, from + height * 128, SB, bar);
+                        }
                     }
+                    __syncwarp();
+                    from += advance;
+                    ++filled;
+                    ring.next();
                 }
-                __syncwarp();
-                from += advance;
-                ++filled;
-                ring.next();
             }
-        }
-        // no copy may be in flight when the CTA leaves: the last turn of every stage that was filled
-        for (u32 i = 0; i < STAGES && i < filled; ++i) {
-            if (ring.s == 0) { ring.s = STAGES; ring.parity ^= 1; }
-            --ring.s;
-            drain_warp(&sh.full[ring.s], ring.parity);
-        }
-    } else if (warp == PRODUCT_WARP) {
-        if (rank == 0) {
+            // no copy may be in flight when the CTA leaves: the last turn of every stage that was filled
+            for (u32 i = 0; i < STAGES && i < filled; ++i) {
+                if (ring.s == 0) { ring.s = STAGES; ring.parity ^= 1; }
+                --ring.s;
+                drain_warp(&sh.full[ring.s], ring.parity);
+            }
+        } else if (rank == 0) {
             constexpr u32 IDESC = (1u << 7) | (1u << 10) | ((SPAN >> 3) << 17) | (FMT == MX4_E8M0_32 ? 1u << 23 : 0u) | ((SPAN >> 4) << 24);
             Ring<STAGES> ring;
             u32 turn = 0;
@@ -247,6 +252,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             }
         }
     } else if (warp >= SCALE_WARP) {
+        registers_down<DOWN>();
         // Scales from shared memory to the tensor-memory lanes of the warp's place: row 32 c + l of a piece is four bytes of
         // lane l, column c.  (The tensor core's own copy instruction queues up with the products, 65 cycles for 512 bytes.)
         const u32 quarter = warp & 3;
@@ -283,7 +289,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
                 ring.next();
             }
         }
-    } else if (warp < STORE_WARPS) {
+    } else {
+        registers_up<UP>();
         const float alpha = (g.m.scale ? __ldg(g.m.scale) : 1.f) * (g.n.scale ? __ldg(g.n.scale) : 1.f);
         const u32 quarter = warp & 3, c0 = (warp >> 2) * 128;              // a warp reads the tensor-memory lanes of its place
         u32 turn = 0;
@@ -297,37 +304,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             const u64 n0 = (u64)nt * SPAN + c0;
             const u32 cols = n0 < g.n.rows ? (u32)min((u64)128, g.n.rows - n0) : 0u;
             T* y = static_cast<T*>(g.y) + m * g.stride + n0;
-            // 16-bit results wait in registers until the accumulator has been handed back; fp32 ones, twice as many, leave in
-            // parts of 16, the last one after that
-            constexpr u32 PART = 16, PER = 4 / sizeof(T), HELD = sizeof(T) == 2 ? 64 : PART;   // columns; results in a word; words held
             const u32 from = tmem + ((quarter * 32) << 16) + c0;
-            u32 w[HELD], v[2][PART];
-            tm_load16(from, v[0]);
+            u32 v[128];
 #pragma unroll
-            for (u32 p = 0; p < 128 / PART; ++p) {
-                tm_wait_load();
-                if (p + 1 < 128 / PART) {
-                    tm_load16(from + (p + 1) * PART, v[(p + 1) & 1]);
-                } else {                           // all columns are in registers
-                    tm_fence_before();
-                    __syncwarp();
-                    if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.acc_empty, 0));
-                }
+            for (u32 i = 0; i < 4; ++i) tm_load32(from + i * 32, v + i * 32);
+            tm_wait_load();
+            tm_fence_before();
+            __syncwarp();
+            if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.acc_empty, 0));
+
+            constexpr u32 PART = 32, PER = 4 / sizeof(T);                  // columns at a time; results in a word
+#pragma unroll
+            for (u32 p = 0; p < 128; p += PART) {
                 float f[PART];
 #pragma unroll
-                for (u32 i = 0; i < PART; ++i) f[i] = __uint_as_float(v[p & 1][i]) * alpha;
+                for (u32 i = 0; i < PART; ++i) f[i] = __uint_as_float(v[p + i]) * alpha;
                 if (g.bias) {
 #pragma unroll
-                    for (u32 i = 0; i < PART; ++i) f[i] += p * PART + i < cols ? __ldg(g.bias + n0 + p * PART + i) : 0.f;
+                    for (u32 i = 0; i < PART; ++i) f[i] += p + i < cols ? __ldg(g.bias + n0 + p + i) : 0.f;
                 }
+                u32 w[PART / PER];
 #pragma unroll
                 for (u32 i = 0; i < PART; i += PER) {
-                    if constexpr (PER == 2) w[(p * PART + i) / 2] = two<DT>(f[i], f[i + 1]);
+                    if constexpr (PER == 2) w[i / 2] = two<DT>(f[i], f[i + 1]);
                     else w[i] = __float_as_uint(f[i]);
                 }
-                if (PER == 1 && m < g.m.rows) put_row<T, HELD>(y + p * PART, w, cols > p * PART ? cols - p * PART : 0, g.wide_store);
+                if (m < g.m.rows) put_row<T, PART / PER>(y + p, w, cols > p ? cols - p : 0, g.wide_store);
             }
-            if (PER == 2 && m < g.m.rows) put_row<T, HELD>(y, w, cols, g.wide_store);
         }
     }
     __syncwarp();
