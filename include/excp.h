@@ -425,8 +425,10 @@ excp_status excp_mx4_dequantize(excp_handle h, const void* packed, size_t rows, 
 /* y[i, j] = sum over k of a[i, k] b[j, k] + bias[j], rounded once to y's type.  a and b are packed matrices of the
  * same format and number of columns; the products of codes and block scales are summed in fp32, then multiplied
  * with both tensor scales.  bias: device fp32 [b_rows] or NULL.
- *   excp_mx4_linear quantises x first (x_scale: its tensor scale, from calibration; x_packed: device,
- *   excp_mx4_bytes(rows, cols, format), receives the packed x). */
+ *   excp_mx4_linear quantises x first (x_scale: its tensor scale, from calibration).  x_packed: device scratch of
+ *   excp_mx4_linear_scratch bytes, 16-byte aligned; that is excp_mx4_bytes(rows, cols, format), or 0 (x_packed may be NULL)
+ *   for the few rows that are quantised within the product.  Its contents afterwards are unspecified. */
+size_t excp_mx4_linear_scratch(excp_handle h, size_t rows, size_t w_rows, size_t cols, int format);
 excp_status excp_mx4_matmul(excp_handle h, const void* a, size_t a_rows, const float* a_scale, const void* b, size_t b_rows,
                             const float* b_scale, size_t cols, int format, const float* bias, void* y, int y_dtype,
                             size_t y_row_stride, void* cuda_stream);

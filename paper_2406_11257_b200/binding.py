@@ -25,7 +25,7 @@ EXPORTS = ["excp_create", "excp_destroy", "excp_record_bytes", "excp_compress_bo
            "excp_decompress_tensor_noalloc", "excp_dense_bytes", "excp_record_to_dense", "excp_checkpoint_to_dense",
            "excp_decompress_dense_tensor", "excp_decompress_dense_checkpoint", "excp_profile_enable", "excp_profile_stage_count", "excp_profile_stage_name", "excp_profile_read",
            "excp_set_kmeans_margin", "excp_set_wait_limit", "excp_selftest_wait_timeout", "excp_set_report_sse",
-           "excp_mx4_bytes", "excp_mx4_tensor_scale", "excp_mx4_quantize", "excp_mx4_dequantize", "excp_mx4_matmul", "excp_mx4_linear",
+           "excp_mx4_bytes", "excp_mx4_tensor_scale", "excp_mx4_quantize", "excp_mx4_dequantize", "excp_mx4_matmul", "excp_mx4_linear", "excp_mx4_linear_scratch",
            "excp_token_logprobs", "excp_token_logprobs_grad", "excp_score_status"]
 
 
@@ -124,6 +124,8 @@ def load_library() -> C.CDLL:
     lib.excp_mx4_quantize.argtypes = [vp, vp, C.c_int, sz, sz, sz, C.c_int, vp, vp, vp]
     lib.excp_mx4_dequantize.argtypes = [vp, vp, sz, sz, C.c_int, vp, vp, C.c_int, sz, vp]
     lib.excp_mx4_matmul.argtypes = [vp, vp, sz, vp, vp, sz, vp, sz, C.c_int, vp, vp, C.c_int, sz, vp]
+    lib.excp_mx4_linear_scratch.argtypes = [vp, sz, sz, sz, C.c_int]
+    lib.excp_mx4_linear_scratch.restype = sz
     lib.excp_mx4_linear.argtypes = [vp, vp, C.c_int, sz, sz, vp, vp, sz, vp, sz, C.c_int, vp, vp, C.c_int, sz, vp, vp]
     lib.excp_token_logprobs.argtypes = [vp, vp, C.c_int, sz, sz, sz, vp, C.c_float, C.c_int, vp, vp, vp, vp, vp, vp]
     lib.excp_token_logprobs_grad.argtypes = [vp, vp, C.c_int, sz, sz, sz, vp, C.c_float, vp, vp, vp, vp, sz, vp]
@@ -488,7 +490,7 @@ class Handle:
     def mx4_linear(self, x: torch.Tensor, w: Mx4Matrix, bias: torch.Tensor | None = None, tensor_scale: torch.Tensor | None = None,
                    out: torch.Tensor | None = None, dtype: torch.dtype | None = None, x_packed: torch.Tensor | None = None) -> torch.Tensor:
         """excp_mx4_linear: x w^T (+ bias), x [rows, w.cols] quantised to w's format with the tensor scale given; the result
-        has x's type unless `dtype` or `out` says otherwise.  `x_packed` (uint8) is room for the packed x."""
+        has x's type unless `dtype` or `out` says otherwise.  `x_packed` (uint8, excp_mx4_linear_scratch bytes) is room for the packed x."""
         p, xdt, rows, cols, xstride = self._rows(x, "x")
         if cols != w.cols:
             raise TypeError(f"x: expected {w.cols} columns")
@@ -497,15 +499,16 @@ class Handle:
         y, dt, yrows, ycols, stride = self._rows(out, "out")
         if (yrows, ycols) != (rows, w.rows):
             raise TypeError("out: expected [x rows, w.rows]")
-        need = self.lib.excp_mx4_bytes(rows, cols, w.code)
+        need = self.lib.excp_mx4_linear_scratch(self._h, rows, w.rows, cols, w.code)
         if x_packed is None:
-            x_packed = torch.empty(need, dtype=torch.uint8, device=x.device)
+            if need:
+                x_packed = torch.empty(need, dtype=torch.uint8, device=x.device)
         elif x_packed.dtype != torch.uint8 or x_packed.numel() < need or not x_packed.is_contiguous() or x_packed.device != x.device:
-            raise TypeError("x_packed: expected a contiguous uint8 tensor of mx4_bytes(rows, cols, fmt) on x's device")
+            raise TypeError("x_packed: expected a contiguous uint8 tensor of excp_mx4_linear_scratch bytes on x's device")
         f32 = torch.float32
         st = self.lib.excp_mx4_linear(self._h, p, xdt, rows, xstride, self._vector(tensor_scale, "tensor_scale", f32, 1), self._packed(w, "w"), w.rows,
                                       self._vector(w.scale, "w.scale", f32, 1), cols, w.code, self._vector(bias, "bias", f32, w.rows), y, dt, stride,
-                                      x_packed.data_ptr(), self._raw_stream())
+                                      0 if x_packed is None else x_packed.data_ptr(), self._raw_stream())
         if st != 0:
             raise ExcpError(st, "excp_mx4_linear")
         return out

@@ -9,15 +9,13 @@
 //   - a block's largest magnitude is two shuffles (B = 32) or one (B = 16) away,
 //   - a row's codes leave as 128 consecutive bytes, and the four rows' scales of a block of columns as whole
 //     16-byte groups of the layout the tensor core reads (row 32 c + l of piece j at byte 16 l + 4 c).
-#include <cuda_fp8.h>
-
-#include "score.cuh"
+#include "mx4_codes.cuh"
+#include "mx4_pipe.cuh"
 
 namespace excp {
 namespace {
 
 constexpr int WARPS = 8;
-constexpr u32 NONFINITE_BITS = 0x7f800000u;       // magnitudes at or above: infinity and NaN
 
 // ---- tensor scale: max |x| / 2688, rounded up to 8 significant bits -----------------
 template <typename T>
@@ -60,53 +58,11 @@ __global__ void __launch_bounds__(256) tensor_scale_kernel(const T* __restrict__
     scale_out[0] = q > 0.f ? __uint_as_float((__float_as_uint(q) + 0xffffu) & 0xffff0000u) : 1.f;
 }
 
-// ---- codes -----------------------------------------------------------------------------
-// Eight values as eight 4-bit floats (nearest, ties to even, at most 6), the first in the low bits.
-__device__ __forceinline__ u32 e2m1x8(const float t[8]) {
-    u32 w;
-    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
-        "mov.b32 %0, {a, b, c, d};\n\t}"
-        : "=r"(w)
-        : "f"(t[0]), "f"(t[1]), "f"(t[2]), "f"(t[3]), "f"(t[4]), "f"(t[5]), "f"(t[6]), "f"(t[7]));
-    return w;
-}
-
-// The block's scale byte, and its values divided by the scale (in place).  `m`: pattern of the block's
-// largest magnitude.
-__device__ __forceinline__ u32 scale_e8m0(float v[8], u32 m) {
-    if (m >= NONFINITE_BITS) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = 0.f;
-        return 0xffu;
-    }
-    const int lg = (m >> 23) ? (int)(m >> 23) - 127 : (m ? -118 - __clz(m) : -1000);   // floor(log2): bit b of a subnormal is 2^(b - 149)
-    const int e = max(lg - 2, -127);
-    const float inv = __uint_as_float((u32)(127 - e) << 23);                            // 2^-e: exact, -e in [-125, 127]
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= inv;
-    return (u32)(e + 127);
-}
-__device__ __forceinline__ u32 scale_e4m3(float v[8], u32 m, float g, float six_g) {
-    u32 byte = 0x7fu;
-    float sg = 0.f;
-    if (m < NONFINITE_BITS) {
-        const __nv_fp8_storage_t s = __nv_cvt_float_to_fp8(m ? __fdiv_rn(__uint_as_float(m), six_g) : 0.f, __NV_SATFINITE, __NV_E4M3);
-        byte = s;
-        sg = __half2float(__half(__nv_cvt_fp8_to_halfraw(s, __NV_E4M3))) * g;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = sg > 0.f ? __fdiv_rn(v[k], sg) : 0.f;
-    return byte;
-}
-
 template <typename T, int FMT>
 __global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const T* __restrict__ x, u64 rows, u64 cols, u64 stride, bool vec,
                                                               u32 col_tiles, u64 tasks, const float* __restrict__ tensor_scale,
                                                               unsigned char* __restrict__ out) {
+    let_next_start();                              // a product of this matrix may set itself up and fetch the other one
     const u64 task = (u64)blockIdx.x * WARPS + (threadIdx.x >> 5);
     if (task >= tasks) return;
     const u32 lane = threadIdx.x & 31;
@@ -153,9 +109,7 @@ __global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const T* __restric
     u32 word = 0;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-        u32 w = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w |= __shfl_sync(0xffffffffu, bytes[c], src + k * PER) << (8 * k);
+        const u32 w = scale_word<FMT>(bytes[c], src);
         if ((lane & 3) == (u32)c) word = w;
     }
     if (piece < (u32)mx4_pieces(FMT))

@@ -1,224 +1,433 @@
 // Product of two microscaled 4-bit matrices: y[a row, b row] = scales * sum over columns (+ bias), fp32 sums.
+// This file: few rows on one side (the tokens of a decoding step); mx4_matmul_wide.cu: many rows on both.
 //
-// Tensor cores: tcgen05.mma on packed 4-bit floats with their block scales (64 columns per instruction), fp32
-// accumulators in tensor memory.  The packed layout is the one the tensor core reads, tile by tile: a stage of
-// the pipeline is a handful of contiguous bulk copies (codes of the M rows, codes of the N rows, scales of
-// both), no address pattern, no tensor map.
+// Bound: the bytes of the larger matrix.  Its rows go on the M side of the tensor core (128 per tile), the few rows on the N
+// side, which takes them in steps of 8.  Several CTAs share an SM, and the columns of a tile are split over a cluster so
+// that every SM streams; the parts are added through distributed shared memory in a fixed order.
 //
-// Roles: warps 0..3 write the result, warp 4 fetches, warp 5 issues the matrix instructions.
-// Every wait is bounded; where one runs out the block raises the handle's flag, lets its copies land and leaves.
-#include "score.cuh"
-#include "tcgen05.cuh"
+// Roles: warp 4 fetches (contiguous bulk copies: the packed layout is the tensor core's), warp 5 issues the matrix
+// instructions; warps 0..3 bring the block scales to tensor memory and write the result.  Where the few rows come as plain
+// values (linear), warps 0..3 first quantise them into shared memory, each CTA the columns it needs, while the first tiles
+// are on their way: a launch less.
+// Every wait is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and leaves.
+#include <cooperative_groups.h>
+
+#include "mx4_codes.cuh"
+#include "mx4_pipe.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace excp {
 namespace {
 
-constexpr int THREADS = 192;
-constexpr int STAGES = 4;
-constexpr u32 A_CODES = MX4_ROWS * 128;
-constexpr u64 DRAIN_NS = 100000000ull;             // a copy in flight lands within microseconds
+constexpr int WORK_WARPS = 4;                      // scales, quantisation, result
+constexpr u32 FETCH_WARP = WORK_WARPS, PRODUCT_WARP = WORK_WARPS + 1;
+constexpr int THREADS = (WORK_WARPS + 2) * 32;
+constexpr int STAGES = 3;
+constexpr u32 CODES = MX4_ROWS * 128;
+constexpr u32 MAX_SPLIT = 8;
+constexpr u32 RAW_TASKS = 24;                      // plain rows x column tiles that a CTA quantises itself
+constexpr u32 RAW_MAX = 96 * 1024;                 // shared memory for plain rows that are quantised in the product
+constexpr u32 RAW_ROWS = 16;                       // and at most so many (at most 32: one column of tensor memory holds their scales)
 
-struct MatmulArgs {
-    Mx4Operand m, n;             // the operands on the M side (128 rows per tile) and on the N side
-    u32 col_tiles;
-    u32 nt;                      // rows of n per block: a multiple of 8, at most 256
+struct NarrowArgs {
+    Mx4Operand m;                                  // M side
+    Mx4Operand n;                                  // N side, packed (not RAW)
+    const void* x;                                 // N side as plain values (RAW)
+    u64 x_stride, cols;
+    u32 x_vec;                                     // its rows start on 16 bytes
+    u32 col_tiles, nt, n_tiles;                    // rows of n per CTA: a multiple of 8, at most 128
+    u32 x_codes, x_scales;                         // where the quantised rows lie in shared memory (RAW)
     void* y;
-    u64 sm, sn;                  // strides of y along the rows of m and of n
+    u64 sm, sn;                                    // strides of y along the rows of m and of n
     const float* bias;
     u32 bias_on_m;
+    u32 wait_m;                                    // m is what the launch before packs
     u32 stage_bytes, tmem_cols;
     u64 wait_ns;
     u32* flag;
 };
 
 struct Shared {
-    unsigned long long full[STAGES], empty[STAGES], done;
+    unsigned long long full[STAGES];               // copies have landed
+    unsigned long long ready[STAGES];              // and the scales are in tensor memory (and plain rows quantised)
+    unsigned long long empty[STAGES];              // the stage has been multiplied
+    unsigned long long done;
     u32 tmem;
     volatile u32 abort;
 };
 
-// One thread waits for phase `parity` of `bar`; false when the limit has passed or another role gave up.
-__device__ __forceinline__ bool wait_one(Shared* sh, unsigned long long* bar, u32 parity, u64 limit_ns, u32* flag) {
-    if (limit_ns) {
-        for (int i = 0; i < 64; ++i)
-            if (mbar_try_wait(bar, parity)) return true;
-        const u64 t0 = global_ns();
-        while (!sh->abort) {
-            if (mbar_try_wait(bar, parity)) return true;
-            if (global_ns() - t0 > limit_ns) break;
-        }
+__device__ __forceinline__ void work_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+// Columns 8 lane .. 8 lane + 7 of column tile `ct` of a plain row, 0 past the end.
+template <typename T>
+__device__ __forceinline__ void load_part(const NarrowArgs& g, u64 row, u32 ct, u32 lane, float v[8]) {
+    const u64 c0 = (u64)ct * MX4_COLS + lane * 8;
+    const T* p = static_cast<const T*>(g.x) + row * g.x_stride + c0;
+    if (row < g.n.rows && g.x_vec && c0 + 8 <= g.cols) {
+        load8(p, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = row < g.n.rows && c0 + k < g.cols ? wget(p, k) : 0.f;
     }
-    if (!sh->abort) {
-        sh->abort = 1;
-        *reinterpret_cast<volatile u32*>(flag) = 1;
-        __threadfence_system();
-    }
-    return false;
-}
-// The same without raising anything: for letting one's own work land before leaving.
-__device__ __forceinline__ void drain_one(unsigned long long* bar, u32 parity) {
-    const u64 t0 = global_ns();
-    while (!mbar_try_wait(bar, parity) && global_ns() - t0 < DRAIN_NS) {}
 }
 
-template <int DT>
-__device__ __forceinline__ void put(void* y, u64 at, float v) {
-    wput(static_cast<typename ElemOf<DT>::type*>(y), at, v);
+// One plain row of a column tile -> its codes, and its scales as one word per piece, `rows` words apart.
+template <int FMT>
+__device__ __forceinline__ void quantize_row(float v[8], u32 r, u32 lane, float gx, unsigned char* codes, u32* scales, u32 rows) {
+    u32 top = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    if (FMT == MX4_E8M0_32) top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const u32 byte = FMT == MX4_E8M0_32 ? scale_e8m0(v, top) : scale_e4m3(v, top, gx, 6.f * gx);
+    *reinterpret_cast<u32*>(codes + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + ((lane & 3) << 2)) = e2m1x8(v);
+    constexpr u32 PER = mx4_block(FMT) / 8, PIECES = mx4_pieces(FMT);
+    const u32 piece = min(lane, PIECES - 1);
+    const u32 word = scale_word<FMT>(byte, piece * 4 * PER);
+    if (lane < PIECES) scales[piece * rows + r] = word;
 }
 
-template <int FMT, int DT>
-__global__ void __launch_bounds__(THREADS, 1) matmul_kernel(const __grid_constant__ MatmulArgs g) {
+template <int FMT, int DT, int XT>                 // XT: type of the plain rows, -1 = both sides packed
+__global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constant__ NarrowArgs g) {
+    constexpr bool RAW = XT >= 0;
+    constexpr u32 PIECES = mx4_pieces(FMT), SB = mx4_scale_bytes(FMT), SF_COLS = PIECES * 8;
+    typedef typename ElemOf<RAW ? XT : DT_F32>::type X;
+    typedef typename ElemOf<DT>::type T;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Shared sh;
-    // the swizzle goes by address: stages start on 1024 bytes
+    cg::cluster_group cluster = cg::this_cluster();
+    const u32 part = cluster.block_rank(), parts = cluster.num_blocks();
+    // the swizzle goes by address: stages start on 1024 bytes (the same offset in every CTA)
     unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    constexpr u32 PIECES = mx4_pieces(FMT), SB = mx4_scale_bytes(FMT);
-    const u32 warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const u32 n_tiles = (u32)((g.n.rows + g.nt - 1) / g.nt);
-    const u32 mt = blockIdx.x / n_tiles, n0 = (blockIdx.x - mt * n_tiles) * g.nt;
-    // the N side spans one or two row tiles of its matrix
-    const u32 nt0 = n0 / MX4_ROWS;
-    const u32 parts = g.nt > MX4_ROWS && (u64)(nt0 + 1) * MX4_ROWS < g.n.rows ? 2 : 1;
-
-    const u32 base = smem_u32(smem);
-    const u32 b_codes = A_CODES, scales = A_CODES + g.nt * 128;
+    const u32 warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const u32 tile = blockIdx.x / parts, mt = tile / g.n_tiles, ntile = tile - mt * g.n_tiles;
+    const u32 k0 = (u32)((u64)g.col_tiles * part / parts), k1 = (u32)((u64)g.col_tiles * (part + 1) / parts);
+    // a stage: tile of m (codes, scales), packed rows of n (codes), their scales
+    const u32 n_codes = CODES + SB, n_scales = n_codes + g.nt * 128;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.ready[s], WORK_WARPS); mbar_init(&sh.empty[s], 1); }
         mbar_init(&sh.done, 1);
         sh.abort = 0;
         mbar_fence_init();
     }
-    if (warp == 5) tm_alloc(&sh.tmem, g.tmem_cols);
+    if (warp == PRODUCT_WARP) tm_alloc(&sh.tmem, g.tmem_cols);
     tm_fence_before();
     __syncthreads();
     tm_fence_after();
     const u32 tmem = sh.tmem;
+    bool ok = true;                                // this warp's waits were all met
 
-    if (warp == 4 && lane == 0) {
-        const u32 hm = mx4_tile_height(g.m.rows, mt);
-        const u32 h0 = mx4_tile_height(g.n.rows, nt0), h1 = parts == 2 ? mx4_tile_height(g.n.rows, nt0 + 1) : 0;
-        const u32 bytes = (hm + h0 + h1) * 128 + (1 + parts) * SB;
-        const unsigned char* pm = g.m.p + mx4_tile_offset(g.m.rows, g.col_tiles, FMT, mt, 0);
-        const unsigned char* p0 = g.n.p + mx4_tile_offset(g.n.rows, g.col_tiles, FMT, nt0, 0);
-        const unsigned char* p1 = parts == 2 ? g.n.p + mx4_tile_offset(g.n.rows, g.col_tiles, FMT, nt0 + 1, 0) : nullptr;
-        u32 issued = 0;
-        for (u32 k = 0; k < g.col_tiles; ++k) {
-            const u32 s = k % STAGES, turn = k / STAGES;
-            if (turn && !wait_one(&sh, &sh.empty[s], (turn - 1) & 1, g.wait_ns, g.flag)) break;
+    if (warp == FETCH_WARP) {
+        const u32 hm = mx4_tile_height(g.m.rows, mt), hn = RAW ? 0 : mx4_tile_height(g.n.rows, ntile);
+        const unsigned char* pm = g.m.p + mx4_tile_offset(g.m.rows, g.col_tiles, FMT, mt, k0);
+        const unsigned char* pn = RAW ? nullptr : g.n.p + mx4_tile_offset(g.n.rows, g.col_tiles, FMT, ntile, k0);
+        const u32 bytes = hm * 128 + SB + (RAW ? 0 : hn * 128 + SB);
+        Ring<STAGES> ring;
+        u32 filled = 0;
+        auto fetch_m = [&](u32 s) {                // announces the whole stage
             unsigned char* st = smem + s * g.stage_bytes;
-            mbar_arrive_expect_tx(&sh.full[s], bytes);
-            bulk_g2s(st, pm, hm * 128, &sh.full[s]);
-            bulk_g2s(st + scales, pm + hm * 128, SB, &sh.full[s]);
-            bulk_g2s(st + b_codes, p0, h0 * 128, &sh.full[s]);
-            bulk_g2s(st + scales + SB, p0 + h0 * 128, SB, &sh.full[s]);
-            pm += hm * 128 + SB;
-            p0 += h0 * 128 + SB;
-            if (parts == 2) {
-                bulk_g2s(st + b_codes + A_CODES, p1, h1 * 128, &sh.full[s]);
-                bulk_g2s(st + scales + 2 * SB, p1 + h1 * 128, SB, &sh.full[s]);
-                p1 += h1 * 128 + SB;
-            }
-            ++issued;
-        }
-        // no copy may be in flight when the block leaves (a matrix instruction need not have waited for it)
-        for (u32 k = issued > STAGES ? issued - STAGES : 0; k < issued; ++k) drain_one(&sh.full[k % STAGES], (k / STAGES) & 1);
-    } else if (warp == 5 && lane == 0) {
-        const u32 idesc0 = (1u << 7) | (1u << 10) | ((g.nt >> 3) << 17) | (FMT == MX4_E8M0_32 ? 1u << 23 : 0u) | (8u << 24);
-        const u32 b_groups = (g.nt + MX4_ROWS - 1) / MX4_ROWS;
-        const u32 sf_cols = PIECES * 4 * (1 + b_groups);
-        bool ok = true;
-        for (u32 k = 0; k < g.col_tiles; ++k) {
-            const u32 s = k % STAGES;
-            if (!wait_one(&sh, &sh.full[s], (k / STAGES) & 1, g.wait_ns, g.flag)) { ok = false; break; }
-            tm_fence_after();
-            const u32 st = base + s * g.stage_bytes;
-            // each stage has scale columns of its own, free again when the stage is
-            const u32 sa = tmem + g.nt + s * sf_cols, sb = sa + PIECES * 4;
-            for (u32 j = 0; j < PIECES; ++j) {
-                tm_copy_scales(sa + j * 4, desc_scales(st + scales + j * MX4_PIECE));
-                for (u32 q = 0; q < parts; ++q)
-                    tm_copy_scales(sb + j * 4 * b_groups + q * 4, desc_scales(st + scales + (1 + q) * SB + j * MX4_PIECE));
-            }
-            const u64 da = desc_swizzled(st), db = desc_swizzled(st + b_codes);
-#pragma unroll
-            for (u32 i = 0; i < 4; ++i) {             // 64 columns = 32 bytes of codes each
-                if (FMT == MX4_E4M3_16) {
-                    tm_mma_block16(tmem, da + 2 * i, db + 2 * i, idesc0, sa + i * 4, sb + i * 4 * b_groups, k || i);
+            if (elect_one()) {
+                mbar_arrive_expect_tx(&sh.full[s], bytes);
+                if (hm == MX4_ROWS) {
+                    bulk_g2s(st, pm, CODES + SB, &sh.full[s]);
                 } else {
-                    const u32 half = (i & 1) * 2;     // a piece serves two instructions: its bytes 0, 1, then 2, 3
-                    const u32 j = i >> 1;
-                    tm_mma_block32(tmem, da + 2 * i, db + 2 * i, idesc0 | (half << 4) | (half << 29), sa + j * 4, sb + j * 4 * b_groups, k || i);
+                    bulk_g2s(st, pm, hm * 128, &sh.full[s]);
+                    bulk_g2s(st + CODES, pm + hm * 128, SB, &sh.full[s]);
                 }
             }
-            tm_commit(&sh.empty[s]);
+            __syncwarp();
+            pm += hm * 128 + SB;
+        };
+        auto fetch_n = [&](u32 s) {
+            unsigned char* st = smem + s * g.stage_bytes;
+            if (elect_one()) {
+                bulk_g2s(st + n_codes, pn, hn * 128, &sh.full[s]);
+                bulk_g2s(st + n_scales, pn + hn * 128, SB, &sh.full[s]);
+            }
+            __syncwarp();
+            pn += hn * 128 + SB;
+        };
+        // the first stages' tiles of m, before the launch that may just be packing n has ended
+        const u32 first = min((u32)STAGES, k1 - k0);
+        if (g.wait_m) wait_for_previous();
+        for (u32 s = 0; s < first; ++s) fetch_m(s);
+        if (!RAW) {
+            wait_for_previous();
+            for (u32 s = 0; s < first; ++s) fetch_n(s);
         }
-        tm_commit(&sh.done);
-        if (!ok) drain_one(&sh.done, 0);
-    } else if (warp < 4) {
-        const bool ok = g.col_tiles == 0 || __all_sync(0xffffffffu, wait_one(&sh, &sh.done, 0, g.wait_ns, g.flag));
-        tm_fence_after();
-        if (ok) {
-            const float alpha = (g.m.scale ? __ldg(g.m.scale) : 1.f) * (g.n.scale ? __ldg(g.n.scale) : 1.f);
-            const u64 m = (u64)mt * MX4_ROWS + warp * 32 + lane;
-            const float bias_m = g.bias && g.bias_on_m && m < g.m.rows ? __ldg(g.bias + m) : 0.f;
-            for (u32 c = 0; c < g.nt; c += 8) {
-                u32 v[8];
-                tm_load8(tmem + ((warp * 32) << 16) + c, v);
-                tm_wait_load();
+        for (u32 s = 0; s < first; ++s, ++filled) ring.next();
+        for (u32 k = k0 + first; k < k1; ++k) {
+            if (!(ok = wait_warp(&sh, &sh.empty[ring.s], ring.parity ^ 1, g.wait_ns, g.flag))) break;
+            fetch_m(ring.s);
+            if (!RAW) fetch_n(ring.s);
+            ++filled;
+            ring.next();
+        }
+        // no copy may be in flight when the CTA leaves: the last turn of every stage that was filled
+        for (u32 i = 0; i < STAGES && i < filled; ++i) {
+            if (ring.s == 0) { ring.s = STAGES; ring.parity ^= 1; }
+            --ring.s;
+            drain_warp(&sh.full[ring.s], ring.parity);
+        }
+    } else if (warp == PRODUCT_WARP) {
+        const u32 idesc = (1u << 7) | (1u << 10) | ((g.nt >> 3) << 17) | (FMT == MX4_E8M0_32 ? 1u << 23 : 0u) | (8u << 24);
+        Ring<STAGES> ring;
+        for (u32 k = k0; k < k1; ++k) {
+            if (!(ok = wait_warp(&sh, &sh.ready[ring.s], ring.parity, g.wait_ns, g.flag))) break;
+            tm_fence_after();
+            const u32 st = smem_u32(smem) + ring.s * g.stage_bytes;
+            const u32 sa = tmem + g.nt + ring.s * SF_COLS, sb = sa + PIECES * 4;
+            const u64 da = desc_swizzled(st), db = desc_swizzled(RAW ? smem_u32(smem) + g.x_codes + (k - k0) * g.nt * 128 : st + n_codes);
+            if (elect_one()) {
 #pragma unroll
-                for (u32 i = 0; i < 8; ++i) {
-                    const u64 n = (u64)n0 + c + i;
-                    if (n >= g.n.rows || m >= g.m.rows) continue;
-                    float f = g.col_tiles ? __uint_as_float(v[i]) * alpha : 0.f;
-                    if (g.bias) f += g.bias_on_m ? bias_m : __ldg(g.bias + n);
-                    put<DT>(g.y, m * g.sm + n * g.sn, f);
+                for (u32 i = 0; i < 4; ++i) {      // 64 columns = 32 bytes of codes each
+                    if (FMT == MX4_E4M3_16) {
+                        tm_mma_block16(tmem, da + 2 * i, db + 2 * i, idesc, sa + i * 4, sb + i * 4, k > k0 || i);
+                    } else {
+                        const u32 half = (i & 1) * 2, j = i >> 1;          // a piece serves two instructions: its bytes 0, 1, then 2, 3
+                        tm_mma_block32(tmem, da + 2 * i, db + 2 * i, idesc | (half << 4) | (half << 29), sa + j * 4, sb + j * 4, k > k0 || i);
+                    }
+                }
+                tm_commit(&sh.empty[ring.s]);
+            }
+            __syncwarp();
+            ring.next();
+        }
+        if (elect_one()) tm_commit(&sh.done);
+        __syncwarp();
+        drain_warp(&sh.done, 0);                   // what has been issued is done before tensor memory goes
+    } else {
+        if (RAW) {
+            // Row r of column tile k0 + t is task t * rows + r; the rows past the end stay as they are (only their own
+            // results, which are not written, would see them).
+            const float gx = g.n.scale ? __ldg(g.n.scale) : 1.f;
+            const u32 rows = (u32)g.n.rows, tasks = (k1 - k0) * rows;
+            constexpr u32 AHEAD = 2;
+            float v[AHEAD][8];
+            auto fetch = [&](u32 i, float (&to)[8]) {
+                if (i < tasks) load_part<X>(g, i % rows, k0 + i / rows, lane, to);
+            };
+#pragma unroll
+            for (u32 a = 0; a < AHEAD; ++a) fetch(warp + a * WORK_WARPS, v[a]);
+            for (u32 i = warp; i < tasks; i += AHEAD * WORK_WARPS) {
+#pragma unroll
+                for (u32 a = 0; a < AHEAD; ++a) {
+                    const u32 at = i + a * WORK_WARPS;
+                    if (at >= tasks) break;
+                    const u32 t = at / rows, r = at - t * rows;
+                    quantize_row<FMT>(v[a], r, lane, gx, smem + g.x_codes + t * g.nt * 128,
+                                      reinterpret_cast<u32*>(smem + g.x_scales) + t * PIECES * g.nt, g.nt);
+                    fetch(at + AHEAD * WORK_WARPS, v[a]);
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // the tensor core reads what was just written
+            work_barrier();
+        }
+        Ring<STAGES> ring;
+        for (u32 k = k0; k < k1; ++k) {
+            if (!(ok = wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag))) break;
+            const unsigned char* st = smem + ring.s * g.stage_bytes;
+            const uint4* from = reinterpret_cast<const uint4*>(st + CODES) + lane;
+            // each stage has scale columns of its own, free again when the stage is
+            const u32 sa = tmem + ((warp * 32) << 16) + g.nt + ring.s * SF_COLS;
+            uint4 a[2 * PIECES];
+#pragma unroll
+            for (u32 j = 0; j < PIECES; ++j) a[j] = from[j * 32];
+            if (RAW) {                             // at most 32 rows: the first of the four columns
+                const u32* words = reinterpret_cast<const u32*>(smem + g.x_scales) + (k - k0) * PIECES * g.nt;
+#pragma unroll
+                for (u32 j = 0; j < PIECES; ++j) a[PIECES + j] = make_uint4(lane < g.nt ? words[j * g.nt + lane] : 0u, 0u, 0u, 0u);
+            } else {
+                const uint4* from_n = reinterpret_cast<const uint4*>(st + n_scales) + lane;
+#pragma unroll
+                for (u32 j = 0; j < PIECES; ++j) a[PIECES + j] = from_n[j * 32];
+            }
+            if (FMT == MX4_E4M3_16) tm_store32(sa, reinterpret_cast<const u32*>(a));
+            else tm_store16(sa, reinterpret_cast<const u32*>(a));
+            tm_wait_store();
+            tm_fence_before();
+            __syncwarp();
+            if (elect_one()) mbar_arrive_own(&sh.ready[ring.s]);
+            ring.next();
+        }
+        if (ok) ok = wait_warp(&sh, &sh.done, 0, g.wait_ns, g.flag);
+        tm_fence_after();
+    }
+
+    const float alpha = (g.m.scale ? __ldg(g.m.scale) : 1.f) * (g.n.scale ? __ldg(g.n.scale) : 1.f);
+    const u64 n0 = (u64)ntile * MX4_ROWS;
+    const u32 cols = (u32)min((u64)g.nt, g.n.rows - n0);       // of the result
+    float* const sums = reinterpret_cast<float*>(smem);        // [nt][128], where the stages were
+    T* const y = static_cast<T*>(g.y) + n0 * g.sn;
+    if (warp < WORK_WARPS) {
+        // thread t of the work warps has row t of m's tile
+        const u64 m = (u64)mt * MX4_ROWS + threadIdx.x;
+        const float bias_m = g.bias && g.bias_on_m && m < g.m.rows ? __ldg(g.bias + m) : 0.f;
+        for (u32 c = 0; c < cols; c += 16) {
+            u32 v[16];
+            tm_load8(tmem + ((warp * 32) << 16) + c, v);
+            if (c + 8 < g.nt) tm_load8(tmem + ((warp * 32) << 16) + c + 8, v + 8);
+            tm_wait_load();
+#pragma unroll
+            for (u32 i = 0; i < 16; ++i) {
+                if (c + i >= cols) break;
+                const float f = k0 < k1 ? __uint_as_float(v[i]) : 0.f;
+                if (parts > 1) {
+                    sums[(c + i) * MX4_ROWS + threadIdx.x] = f;
+                } else if (m < g.m.rows) {
+                    float r = f * alpha;
+                    if (g.bias) r += g.bias_on_m ? bias_m : __ldg(g.bias + n0 + c + i);
+                    wput(y, m * g.sm + (c + i) * g.sn, r);
                 }
             }
         }
         tm_fence_before();
     }
+    if (parts > 1) {
+        cluster.sync();
+        // columns dealt to the CTAs and their warps; a lane adds four rows' parts, in ascending order
+        const u64 m = (u64)mt * MX4_ROWS + lane * 4;
+        float bias_m[4];
+#pragma unroll
+        for (u32 i = 0; i < 4; ++i) bias_m[i] = g.bias && g.bias_on_m && m + i < g.m.rows ? __ldg(g.bias + m + i) : 0.f;
+        const u32 step = parts * (THREADS / 32);
+        for (u32 c = part + parts * warp; c < cols; c += 2 * step) {           // two columns' parts on their way at a time
+            float4 f[2][MAX_SPLIT];
+#pragma unroll
+            for (u32 p = 0; p < MAX_SPLIT; ++p) {
+                if (p >= parts) continue;
+                const float4* of = reinterpret_cast<const float4*>(cluster.map_shared_rank(sums, p));
+                f[0][p] = of[c * (MX4_ROWS / 4) + lane];
+                if (c + step < cols) f[1][p] = of[(c + step) * (MX4_ROWS / 4) + lane];
+            }
+#pragma unroll
+            for (u32 h = 0; h < 2; ++h) {
+                const u32 col = c + h * step;
+                if (col >= cols) break;
+                float4 sum = f[h][0];
+#pragma unroll
+                for (u32 p = 1; p < MAX_SPLIT; ++p) {
+                    if (p >= parts) continue;
+                    sum.x += f[h][p].x; sum.y += f[h][p].y; sum.z += f[h][p].z; sum.w += f[h][p].w;
+                }
+                const float r[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+                for (u32 i = 0; i < 4; ++i) {
+                    float v = r[i] * alpha;
+                    if (g.bias) v += g.bias_on_m ? bias_m[i] : __ldg(g.bias + n0 + col);
+                    if (m + i < g.m.rows) wput(y, (m + i) * g.sm + col * g.sn, v);
+                }
+            }
+        }
+        cluster.sync();                            // the others have read this CTA's sums
+    }
     __syncwarp();
     __syncthreads();
-    if (warp == 5) tm_dealloc(tmem, g.tmem_cols);
+    tm_fence_after();
+    if (warp == PRODUCT_WARP) tm_dealloc(tmem, g.tmem_cols);
 }
 
-template <int FMT, int DT>
-bool launch_as(cudaStream_t s, const MatmulArgs& g) {
-    const u32 smem = g.stage_bytes * STAGES + 1024;
-    if (cudaFuncSetAttribute(matmul_kernel<FMT, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
-    const u32 grid = (u32)((g.n.rows + g.nt - 1) / g.nt) * mx4_row_tiles(g.m.rows);
-    matmul_kernel<FMT, DT><<<grid, THREADS, smem, s>>>(g);
-    return true;
+template <int FMT, int DT, int XT>
+bool launch_as(cudaStream_t s, const NarrowArgs& g, u32 parts, u32 smem, bool behind) {
+    if (cudaFuncSetAttribute(narrow_kernel<FMT, DT, XT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(mx4_row_tiles(g.m.rows) * g.n_tiles * parts);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = parts;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = behind ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, narrow_kernel<FMT, DT, XT>, g) == cudaSuccess;
+}
+
+template <int XT>
+bool launch_typed(cudaStream_t s, const NarrowArgs& g, u32 parts, u32 smem, int fmt, int dtype, bool behind) {
+#define EXCP_MM(DT) (fmt == MX4_E4M3_16 ? launch_as<MX4_E4M3_16, DT, XT>(s, g, parts, smem, behind) : launch_as<MX4_E8M0_32, DT, XT>(s, g, parts, smem, behind))
+    return dtype == DT_F32 ? EXCP_MM(DT_F32) : dtype == DT_F16 ? EXCP_MM(DT_F16) : EXCP_MM(DT_BF16);
+#undef EXCP_MM
+}
+
+u32 split(int sms, u64 m_tiles, u64 n_tiles, u32 nt, u32 col_tiles) {
+    // two CTAs per SM as long as there are columns to split, and no more sums to exchange than a block of 128 x 128
+    u64 parts = (u64)sms * 2 / (m_tiles * n_tiles);
+    if (parts > MAX_SPLIT) parts = MAX_SPLIT;
+    if (parts > col_tiles) parts = col_tiles;
+    if (parts > MX4_ROWS / nt) parts = MX4_ROWS / nt;
+    return parts < 1 ? 1u : (u32)parts;
+}
+// Shared memory of the quantised rows of a CTA.
+u32 raw_bytes(u32 nt, u32 col_tiles, u32 parts, int fmt) {
+    return (col_tiles + parts - 1) / parts * nt * (128 + (u32)mx4_pieces(fmt) * 4);
+}
+
+// `x`: the few rows as plain values instead of a.p (may be null).
+bool launch_narrow(int sms, cudaStream_t s, const Mx4Operand& a, const RowsIn* x, const Mx4Operand& b, u64 cols, int fmt,
+                   const Mx4Result& r, u64 wait_ns, u32* flag, bool behind) {
+    NarrowArgs g{};
+    // b on the M side, so that neighbouring lanes write neighbouring results, unless b has the few rows
+    const bool turned = a.rows <= MX4_ROWS || b.rows > MX4_ROWS;
+    g.m = turned ? b : a;
+    g.n = turned ? a : b;
+    g.cols = cols;
+    g.col_tiles = mx4_col_tiles(cols);
+    g.nt = g.n.rows > MX4_ROWS ? MX4_ROWS : (u32)((g.n.rows + 7) & ~7ull);
+    g.n_tiles = mx4_row_tiles(g.n.rows);
+    g.y = r.y;
+    g.sm = turned ? 1 : r.stride;
+    g.sn = turned ? r.stride : 1;
+    g.bias = r.bias;
+    g.bias_on_m = turned;
+    g.wait_m = !turned;
+    const u32 sb = (u32)mx4_scale_bytes(fmt), parts = split(sms, mx4_row_tiles(g.m.rows), g.n_tiles, g.nt, g.col_tiles);
+    g.stage_bytes = CODES + sb + (x ? 0 : g.nt * 128 + sb);
+    u32 smem = g.stage_bytes * STAGES + 1024;
+    const u32 need = g.nt + STAGES * (u32)mx4_pieces(fmt) * 8;
+    g.tmem_cols = 32;
+    while (g.tmem_cols < need) g.tmem_cols *= 2;
+    g.wait_ns = wait_ns;
+    g.flag = flag;
+    if (!x) return launch_typed<-1>(s, g, parts, smem, fmt, r.dtype, behind);
+    g.x = x->p;
+    g.x_stride = x->stride;
+    const u64 size = x->dtype == DT_F32 ? 4 : 2;
+    g.x_vec = (reinterpret_cast<uintptr_t>(x->p) & 15) == 0 && (x->rows == 1 || ((x->stride * size) & 15) == 0);
+    g.x_codes = g.stage_bytes * STAGES;
+    g.x_scales = g.x_codes + (g.col_tiles + parts - 1) / parts * g.nt * 128;
+    smem += raw_bytes(g.nt, g.col_tiles, parts, fmt);
+    return x->dtype == DT_F32 ? launch_typed<DT_F32>(s, g, parts, smem, fmt, r.dtype, false)
+         : x->dtype == DT_F16 ? launch_typed<DT_F16>(s, g, parts, smem, fmt, r.dtype, false)
+                              : launch_typed<DT_BF16>(s, g, parts, smem, fmt, r.dtype, false);
 }
 
 }  // namespace
 
 bool launch_mx4_matmul(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
+                       const Mx4Result& r, u64 wait_ns, u32* flag, bool behind) {
+    // 256 x 256 tiles only where they are enough for half the pairs of SMs
+    const u64 wide_tiles = ((a.rows + 255) / 256) * ((b.rows + 255) / 256);
+    if (cols && a.rows > MX4_ROWS && b.rows > MX4_ROWS && wide_tiles * 4 >= (u64)sms)
+        return launch_mx4_matmul_wide(sms, s, a, b, cols, fmt, r, wait_ns, flag, behind);
+    return launch_narrow(sms, s, a, nullptr, b, cols, fmt, r, wait_ns, flag, behind);
+}
+
+bool mx4_linear_in_one(int sms, u64 rows, u64 w_rows, u64 cols, int fmt) {
+    if (rows > RAW_ROWS) return false;
+    const u32 nt = (u32)((rows + 7) & ~7ull), ct = mx4_col_tiles(cols), parts = split(sms, mx4_row_tiles(w_rows), 1, nt, ct);
+    return rows * ((ct + parts - 1) / parts) <= RAW_TASKS && raw_bytes(nt, ct, parts, fmt) <= RAW_MAX;
+}
+
+bool launch_mx4_linear(int sms, cudaStream_t s, const RowsIn& x, const float* x_scale, const Mx4Operand& w, int fmt,
                        const Mx4Result& r, u64 wait_ns, u32* flag) {
-    if (cols && a.rows > MX4_ROWS && b.rows > MX4_ROWS) return launch_mx4_matmul_wide(sms, s, a, b, cols, fmt, r, wait_ns, flag);
-    MatmulArgs g{};
-    // few rows of a: they go to the N side, whose width the tensor core takes in steps of 8
-    const bool swap = a.rows <= MX4_ROWS;
-    g.m = swap ? b : a;
-    g.n = swap ? a : b;
-    g.col_tiles = mx4_col_tiles(cols);
-    g.nt = g.n.rows > 2 * MX4_ROWS ? 2 * MX4_ROWS : (u32)((g.n.rows + 7) & ~7ull);
-    g.y = r.y;
-    g.sm = swap ? 1 : r.stride;
-    g.sn = swap ? r.stride : 1;
-    g.bias = r.bias;
-    g.bias_on_m = swap;
-    const u32 groups = (g.nt + MX4_ROWS - 1) / MX4_ROWS;
-    g.stage_bytes = A_CODES + g.nt * 128 + (1 + groups) * (u32)mx4_scale_bytes(fmt);
-    const u32 need = g.nt + STAGES * (u32)mx4_pieces(fmt) * 4 * (1 + groups);
-    g.tmem_cols = 32;
-    while (g.tmem_cols < need) g.tmem_cols *= 2;
-    g.wait_ns = wait_ns;
-    g.flag = flag;
-#define EXCP_MM(DT) (fmt == MX4_E4M3_16 ? launch_as<MX4_E4M3_16, DT>(s, g) : launch_as<MX4_E8M0_32, DT>(s, g))
-    return r.dtype == DT_F32 ? EXCP_MM(DT_F32) : r.dtype == DT_F16 ? EXCP_MM(DT_F16) : EXCP_MM(DT_BF16);
-#undef EXCP_MM
+    const Mx4Operand a{nullptr, x.rows, x_scale};
+    return launch_narrow(sms, s, a, &x, w, x.cols, fmt, r, wait_ns, flag, false);
 }
 
 }  // namespace excp

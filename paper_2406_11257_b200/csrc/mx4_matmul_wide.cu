@@ -12,8 +12,7 @@
 // few hundred cycles only.
 // Every wait is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and leaves (the
 // partner's waits run out in turn).
-#include "score.cuh"
-#include "tcgen05.cuh"
+#include "mx4_pipe.cuh"
 
 namespace excp {
 namespace {
@@ -27,7 +26,6 @@ constexpr int UP = 168, DOWN = 88;                 // registers per thread of th
 constexpr u32 CODES = MX4_ROWS * 128;              // codes of one operand tile
 constexpr u32 SPAN = 2 * MX4_ROWS;                 // rows of a and of b per pair
 constexpr u32 GROUP = 8;                           // tiles of a that are visited before the next tile of b
-constexpr u64 DRAIN_NS = 100000000ull;
 
 template <int FMT> __host__ __device__ constexpr int stages() { return FMT == MX4_E4M3_16 ? 5 : 6; }
 // A stage: tile of m (codes, scales), own tile of n (codes, scales), scales of the partner's tile of n.
@@ -52,45 +50,6 @@ struct Shared {
     unsigned long long acc_full, acc_empty;
     u32 tmem;
     volatile u32 abort;
-};
-
-// A whole warp waits for phase `parity` of `bar`; false when the limit has passed or another role gave up.
-template <typename S>
-__device__ __forceinline__ bool wait_long(S* sh, unsigned long long* bar, u32 parity, u64 limit_ns, u32* flag) {
-    if (limit_ns) {
-        const u64 t0 = global_ns();
-        while (!__any_sync(0xffffffffu, sh->abort)) {
-            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-            if (__any_sync(0xffffffffu, global_ns() - t0 > limit_ns)) break;
-        }
-    }
-    if (!__any_sync(0xffffffffu, sh->abort)) {
-        sh->abort = 1;
-        *reinterpret_cast<volatile u32*>(flag) = 1;
-        __threadfence_system();
-    }
-    return false;
-}
-template <typename S>
-__device__ __forceinline__ bool wait_warp(S* sh, unsigned long long* bar, u32 parity, const WideArgs& g) {
-    if (g.wait_ns)
-        for (int i = 0; i < 32; ++i)
-            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    return wait_long(sh, bar, parity, g.wait_ns, g.flag);
-}
-// The same without raising anything: for letting one's own work land before leaving.
-__device__ __forceinline__ void drain_warp(unsigned long long* bar, u32 parity) {
-    const u64 t0 = global_ns();
-    while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)) && !__any_sync(0xffffffffu, global_ns() - t0 > DRAIN_NS)) {}
-}
-
-// The place in the ring of stages, and the parity of its current turn.
-template <int STAGES>
-struct Ring {
-    u32 s = 0, parity = 0;
-    __device__ __forceinline__ void next() {
-        if (++s == STAGES) { s = 0; parity ^= 1; }
-    }
 };
 
 // Tile `t` of the pairs' common order: GROUP tiles of m for one tile of n, then the next tile of n.
@@ -178,6 +137,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             Ring<STAGES> ring;
             u32 filled = 0;
             bool ok = true;
+            if (item == 0) wait_for_previous();    // m may have been packed by the launch before this one
             for (u32 t = pair; ok && t < tiles; t += pairs) {
                 u32 mt, nt;
                 place(g, t, mt, nt);
@@ -191,7 +151,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
                 // codes at their place and the scales, which follow them in the packed tile, behind 128 rows: a full tile is one copy
                 const bool full = there && height == MX4_ROWS && item != 2;
                 for (u32 k = 0; k < g.col_tiles; ++k) {
-                    if (filled >= STAGES && !wait_warp(&sh, &sh.empty[ring.s], ring.parity ^ 1, g)) { ok = false; break; }
+                    if (filled >= STAGES && !wait_warp(&sh, &sh.empty[ring.s], ring.parity ^ 1, g.wait_ns, g.flag)) { ok = false; break; }
                     unsigned char* to = smem + ring.s * STAGE + at;
                     unsigned long long* bar = &sh.full[ring.s];
                     if (elect_one()) {
@@ -221,9 +181,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             u32 turn = 0;
             bool ok = true;
             for (u32 t = pair; ok && t < tiles; t += pairs, ++turn) {
-                if (turn && !wait_warp(&sh, &sh.acc_empty, (turn - 1) & 1, g)) { ok = false; break; }
+                if (turn && !wait_warp(&sh, &sh.acc_empty, (turn - 1) & 1, g.wait_ns, g.flag)) { ok = false; break; }
                 for (u32 k = 0; k < g.col_tiles; ++k) {
-                    if (!wait_warp(&sh, &sh.ready[ring.s], ring.parity, g)) { ok = false; break; }
+                    if (!wait_warp(&sh, &sh.ready[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
                     tm_fence_after();
                     const u32 st = base + ring.s * STAGE;
                     const u32 sa = tmem + SPAN + ring.s * SF_COLS, sb = sa + PIECES * 4;
@@ -260,7 +220,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
         bool ok = true;
         for (u32 t = pair; ok && t < tiles; t += pairs) {
             for (u32 k = 0; k < g.col_tiles; ++k) {
-                if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g)) { ok = false; break; }
+                if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
                 const uint4* from = reinterpret_cast<const uint4*>(smem + ring.s * STAGE + CODES) + lane;
                 const uint4* own = from + (CODES + SB) / 16;
                 const uint4* other = own + SB / 16;
@@ -298,7 +258,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             u32 mt, nt;
             place(g, t, mt, nt);
             __syncwarp();
-            if (!wait_warp(&sh, &sh.acc_full, turn & 1, g)) break;
+            if (!wait_warp(&sh, &sh.acc_full, turn & 1, g.wait_ns, g.flag)) break;
             tm_fence_after();
             const u64 m = (u64)(2 * mt + rank) * MX4_ROWS + quarter * 32 + lane;
             const u64 n0 = (u64)nt * SPAN + c0;
@@ -341,19 +301,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
 }
 
 template <int FMT, int DT>
-bool launch_as(int sms, cudaStream_t s, const WideArgs& g) {
+bool launch_as(int sms, cudaStream_t s, const WideArgs& g, bool behind) {
     const u32 smem = stage_bytes<FMT>() * stages<FMT>() + 1024;
     if (cudaFuncSetAttribute(wide_kernel<FMT, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
     const u64 tiles = (u64)g.m_tiles * g.n_tiles;
     const u32 pairs = (u32)(tiles < (u64)(sms / 2) ? tiles : (u64)(sms / 2));
-    wide_kernel<FMT, DT><<<pairs * 2, THREADS, smem, s>>>(g);
-    return true;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(pairs * 2);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = behind ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, wide_kernel<FMT, DT>, g) == cudaSuccess;
 }
 
 }  // namespace
 
 bool launch_mx4_matmul_wide(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
-                            const Mx4Result& r, u64 wait_ns, u32* flag) {
+                            const Mx4Result& r, u64 wait_ns, u32* flag, bool behind) {
     WideArgs g{};
     g.m = a;
     g.n = b;
@@ -367,7 +336,7 @@ bool launch_mx4_matmul_wide(int sms, cudaStream_t s, const Mx4Operand& a, const 
     g.wide_store = ((reinterpret_cast<uintptr_t>(r.y) | (r.stride * size)) & 31) == 0;
     g.wait_ns = wait_ns;
     g.flag = flag;
-#define EXCP_MM(DT) (fmt == MX4_E4M3_16 ? launch_as<MX4_E4M3_16, DT>(sms, s, g) : launch_as<MX4_E8M0_32, DT>(sms, s, g))
+#define EXCP_MM(DT) (fmt == MX4_E4M3_16 ? launch_as<MX4_E4M3_16, DT>(sms, s, g, behind) : launch_as<MX4_E8M0_32, DT>(sms, s, g, behind))
     return r.dtype == DT_F32 ? EXCP_MM(DT_F32) : r.dtype == DT_F16 ? EXCP_MM(DT_F16) : EXCP_MM(DT_BF16);
 #undef EXCP_MM
 }

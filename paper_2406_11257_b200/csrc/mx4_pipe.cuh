@@ -1,0 +1,54 @@
+// What the two kernels of the 4-bit product share: bounded waits of whole warps, the ring of stages.
+#pragma once
+#include "score.cuh"
+#include "tcgen05.cuh"
+
+namespace excp {
+
+constexpr u64 DRAIN_NS = 100000000ull;             // a copy in flight lands within microseconds
+
+// Programmatic dependent launch: a kernel launched behind another one may start when the first says so, and waits for its
+// end (and for its results) where it says so itself.  Both do nothing in a launch of the ordinary kind.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// A whole warp waits for phase `parity` of `bar`; false when the limit has passed or another role gave up.
+template <typename S>
+__device__ __forceinline__ bool wait_long(S* sh, unsigned long long* bar, u32 parity, u64 limit_ns, u32* flag) {
+    if (limit_ns) {
+        const u64 t0 = global_ns();
+        while (!__any_sync(0xffffffffu, sh->abort)) {
+            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+            if (__any_sync(0xffffffffu, global_ns() - t0 > limit_ns)) break;
+        }
+    }
+    if (!__any_sync(0xffffffffu, sh->abort)) {
+        sh->abort = 1;
+        *reinterpret_cast<volatile u32*>(flag) = 1;
+        __threadfence_system();
+    }
+    return false;
+}
+template <typename S>
+__device__ __forceinline__ bool wait_warp(S* sh, unsigned long long* bar, u32 parity, u64 limit_ns, u32* flag) {
+    if (limit_ns)
+        for (int i = 0; i < 32; ++i)
+            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return wait_long(sh, bar, parity, limit_ns, flag);
+}
+// The same without raising anything: for letting one's own work land before leaving.
+__device__ __forceinline__ void drain_warp(unsigned long long* bar, u32 parity) {
+    const u64 t0 = global_ns();
+    while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)) && !__any_sync(0xffffffffu, global_ns() - t0 > DRAIN_NS)) {}
+}
+
+// The place in the ring of stages, and the parity of its current turn.
+template <int STAGES>
+struct Ring {
+    u32 s = 0, parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++s == STAGES) { s = 0; parity ^= 1; }
+    }
+};
+
+}  // namespace excp

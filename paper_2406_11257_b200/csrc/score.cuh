@@ -67,12 +67,17 @@ struct Mx4Result {
     u64 stride;
     const float* bias;               // one per row of b, device; null = none
 };
-// False if the device refused the kernel's shared memory (cudaGetLastError then says why).
+// `behind`: the launch before packs a, and nothing but a depends on it.  False if the launch was refused (cudaGetLastError
+// then says why).
 bool launch_mx4_matmul(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
-                       const Mx4Result& r, u64 wait_ns, u32* flag);
+                       const Mx4Result& r, u64 wait_ns, u32* flag, bool behind);
 
+// x quantised within the product: where mx4_linear_in_one says so (few rows, and their columns fit shared memory).
+bool mx4_linear_in_one(int sms, u64 rows, u64 w_rows, u64 cols, int fmt);
+bool launch_mx4_linear(int sms, cudaStream_t s, const RowsIn& x, const float* x_scale, const Mx4Operand& w, int fmt,
+                       const Mx4Result& r, u64 wait_ns, u32* flag);
 bool launch_mx4_matmul_wide(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
-                            const Mx4Result& r, u64 wait_ns, u32* flag);
+                            const Mx4Result& r, u64 wait_ns, u32* flag, bool behind);
 
 struct LogprobsOut {
     float* logprob;

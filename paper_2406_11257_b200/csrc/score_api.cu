@@ -61,11 +61,11 @@ excp_status finish(excp_handle h) {
 
 excp_status matmul_impl(excp_handle h, const void* a, size_t a_rows, const float* a_scale, const void* b, size_t b_rows,
                         const float* b_scale, size_t cols, int format, const float* bias, void* y, int y_dtype,
-                        size_t y_stride, cudaStream_t stream) {
+                        size_t y_stride, cudaStream_t stream, bool behind) {
     const Mx4Operand ma{static_cast<const unsigned char*>(a), a_rows, format == MX4_E4M3_16 ? a_scale : nullptr};
     const Mx4Operand mb{static_cast<const unsigned char*>(b), b_rows, format == MX4_E4M3_16 ? b_scale : nullptr};
     const Mx4Result r{y, y_dtype, y_stride, bias};
-    if (!launch_mx4_matmul(h->sms, stream, ma, mb, cols, format, r, h->wait_limit_ns, h->score.d_flag)) {
+    if (!launch_mx4_matmul(h->sms, stream, ma, mb, cols, format, r, h->wait_limit_ns, h->score.d_flag, behind)) {
         check(h, cudaGetLastError());
         return EXCP_ERR_CUDA;
     }
@@ -132,22 +132,38 @@ excp_status excp_mx4_matmul(excp_handle h, const void* a, size_t a_rows, const f
     DeviceGuard guard(h->device);
     if (!guard.ok || !ensure_score(h)) return EXCP_ERR_CUDA;
     return matmul_impl(h, a, a_rows, a_scale, b, b_rows, b_scale, cols, format, bias, y, y_dtype, y_row_stride,
-                       static_cast<cudaStream_t>(cuda_stream));
+                       static_cast<cudaStream_t>(cuda_stream), false);
+}
+
+size_t excp_mx4_linear_scratch(excp_handle h, size_t rows, size_t w_rows, size_t cols, int format) {
+    if (!h || !rows || !w_rows || mx4_linear_in_one(h->sms, rows, w_rows, cols, format)) return 0;
+    return excp_mx4_bytes(rows, cols, format);
 }
 
 excp_status excp_mx4_linear(excp_handle h, const void* x, int x_dtype, size_t rows, size_t x_row_stride, const float* x_scale,
                             const void* w, size_t w_rows, const float* w_scale, size_t cols, int format, const float* bias,
                             void* y, int y_dtype, size_t y_row_stride, void* x_packed, void* cuda_stream) {
-    if (!h || !rows_ok(x, x_dtype, rows, cols, x_row_stride) || !packed_ok(x_packed, rows, cols, format) ||
+    if (!h || !rows_ok(x, x_dtype, rows, cols, x_row_stride) ||
         !packed_ok(w, w_rows, cols, format) || !product_ok(rows, w_rows, x_scale, w_scale, bias, y, y_dtype, y_row_stride))
         return EXCP_ERR_INVALID_ARG;
     if (rows == 0 || w_rows == 0) return EXCP_OK;
+    const bool direct = mx4_linear_in_one(h->sms, rows, w_rows, cols, format);     // no packed x: x_packed is not looked at
+    if (!direct && !packed_ok(x_packed, rows, cols, format)) return EXCP_ERR_INVALID_ARG;
     DeviceGuard guard(h->device);
     if (!guard.ok || !ensure_score(h)) return EXCP_ERR_CUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (direct) {
+        const Mx4Operand mw{static_cast<const unsigned char*>(w), w_rows, format == MX4_E4M3_16 ? w_scale : nullptr};
+        if (!launch_mx4_linear(h->sms, stream, RowsIn{x, x_dtype, rows, cols, x_row_stride}, format == MX4_E4M3_16 ? x_scale : nullptr, mw, format,
+                               Mx4Result{y, y_dtype, y_row_stride, bias}, h->wait_limit_ns, h->score.d_flag)) {
+            check(h, cudaGetLastError());
+            return EXCP_ERR_CUDA;
+        }
+        return finish(h);
+    }
     if (cols)
         launch_mx4_quantize(h->sms, stream, RowsIn{x, x_dtype, rows, cols, x_row_stride}, format, x_scale, static_cast<unsigned char*>(x_packed));
-    return matmul_impl(h, x_packed, rows, x_scale, w, w_rows, w_scale, cols, format, bias, y, y_dtype, y_row_stride, stream);
+    return matmul_impl(h, x_packed, rows, x_scale, w, w_rows, w_scale, cols, format, bias, y, y_dtype, y_row_stride, stream, cols != 0);
 }
 
 excp_status excp_token_logprobs(excp_handle h, const void* logits, int dtype, size_t rows, size_t vocab, size_t row_stride,

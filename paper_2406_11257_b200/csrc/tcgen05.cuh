@@ -103,6 +103,9 @@ __device__ __forceinline__ uint32_t cluster_address(const void* p, uint32_t rank
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t address) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
 }
+__device__ __forceinline__ void mbar_arrive_own(unsigned long long* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));

@@ -452,7 +452,7 @@ def test_refusals_of_the_c_abi(h):
     assert lib.excp_mx4_matmul(H, qp, 4, 0, qp, 4, 0, 64, 1, 0, 0, 0, 4, 0) == bad
     assert lib.excp_mx4_matmul(H, qp, 4, 0, qp, 4, 0, 64, 1, 0, p, 0, 3, 0) == bad
     assert lib.excp_mx4_matmul(H, qp, 4, fp + 1, qp, 4, 0, 64, 2, 0, p, 0, 4, 0) == bad
-    assert lib.excp_mx4_linear(H, p, 0, 4, 64, 0, qp, 4, 0, 64, 1, 0, p, 0, 4, 0, 0) == bad   # no room for the packed x
+    assert lib.excp_mx4_linear(H, p, 0, 17, 64, 0, qp, 4, 0, 64, 1, 0, p, 0, 4, 0, 0) == bad  # no room for the packed x
     assert lib.excp_token_logprobs(H, p, 0, 4, 64, 64, 0, 1.0, 0, fp, fp, 0, 0, 0, 0) == bad
     assert lib.excp_token_logprobs(H, p, 0, 4, 64, 64, tp, 1.0, 0, 0, fp, 0, 0, 0, 0) == bad
     assert lib.excp_token_logprobs(H, p, 0, 4, 64, 64, tp, 1.0, 2, fp, fp, 0, 0, 0, 0) == bad
