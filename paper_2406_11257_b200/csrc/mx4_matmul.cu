@@ -12,6 +12,8 @@
 // Every wait is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and leaves.
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "mx4_codes.cuh"
 #include "mx4_pipe.cuh"
 
@@ -265,24 +267,47 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
         // thread t of the work warps has row t of m's tile
         const u64 m = (u64)mt * MX4_ROWS + threadIdx.x;
         const float bias_m = g.bias && g.bias_on_m && m < g.m.rows ? __ldg(g.bias + m) : 0.f;
-        for (u32 c = 0; c < cols; c += 16) {
-            u32 v[16];
-            tm_load8(tmem + ((warp * 32) << 16) + c, v);
-            if (c + 8 < g.nt) tm_load8(tmem + ((warp * 32) << 16) + c + 8, v + 8);
-            tm_wait_load();
+        auto take = [&](auto width, u32 c) {       // that many columns from c on
+            constexpr u32 W = decltype(width)::value;
+            u32 v[W];
 #pragma unroll
-            for (u32 i = 0; i < 16; ++i) {
-                if (c + i >= cols) break;
-                const float f = k0 < k1 ? __uint_as_float(v[i]) : 0.f;
-                if (parts > 1) {
-                    sums[(c + i) * MX4_ROWS + threadIdx.x] = f;
-                } else if (m < g.m.rows) {
-                    float r = f * alpha;
-                    if (g.bias) r += g.bias_on_m ? bias_m : __ldg(g.bias + n0 + c + i);
-                    wput(y, m * g.sm + (c + i) * g.sn, r);
+            for (u32 i = 0; i < W; i += 32) {
+                if constexpr (W >= 32) tm_load32(tmem + ((warp * 32) << 16) + c + i, v + i);
+                else tm_load8(tmem + ((warp * 32) << 16) + c + i, v + i);
+            }
+            tm_wait_load();
+            if (k0 == k1) {
+#pragma unroll
+                for (u32 i = 0; i < W; ++i) v[i] = 0u;
+            }
+            if (parts > 1) {
+#pragma unroll
+                for (u32 i = 0; i < W; ++i) sums[(c + i) * MX4_ROWS + threadIdx.x] = __uint_as_float(v[i]);
+            } else if (m < g.m.rows) {
+                // a warp per scheduler: no branches between the columns, so that they overlap
+                float r[W];
+#pragma unroll
+                for (u32 i = 0; i < W; ++i) r[i] = __uint_as_float(v[i]) * alpha;
+                if (g.bias && g.bias_on_m) {
+#pragma unroll
+                    for (u32 i = 0; i < W; ++i) r[i] += bias_m;
+                } else if (g.bias) {
+#pragma unroll
+                    for (u32 i = 0; i < W; ++i) r[i] += c + i < cols ? __ldg(g.bias + n0 + c + i) : 0.f;
+                }
+                T* const p = y + m * g.sm + c * g.sn;
+                if (c + W <= cols) {
+#pragma unroll
+                    for (u32 i = 0; i < W; ++i) wput(p + i * g.sn, 0, r[i]);
+                } else {
+#pragma unroll
+                    for (u32 i = 0; i < W; ++i) if (c + i < cols) wput(p + i * g.sn, 0, r[i]);
                 }
             }
-        }
+        };
+        u32 c = 0;
+        for (; c + 64 <= g.nt; c += 64) take(std::integral_constant<u32, 64>(), c);
+        for (; c < g.nt; c += 8) take(std::integral_constant<u32, 8>(), c);
         tm_fence_before();
     }
     if (parts > 1) {
