@@ -3,21 +3,18 @@
 //
 // Bound: the bytes of the larger matrix.  Its rows go on the M side of the tensor core (128 per tile), the few rows on the N
 // side, which takes them in steps of 8.  Several CTAs share an SM, and the columns of a tile are split over a cluster so
-// that every SM streams; the parts are added through distributed shared memory in a fixed order.
+// that every SM streams; each CTA sends its part of a column of the result to the CTA that owns the column (distributed shared
+// memory), which adds them in a fixed order.
 //
 // Roles: warp 4 fetches (contiguous bulk copies: the packed layout is the tensor core's), warp 5 issues the matrix
 // instructions; warps 0..3 bring the block scales to tensor memory and write the result.  Where the few rows come as plain
 // values (linear), warps 0..3 first quantise them into shared memory, each CTA the columns it needs, while the first tiles
 // are on their way: a launch less.
 // Every wait is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and leaves.
-#include <cooperative_groups.h>
-
 #include <type_traits>
 
 #include "mx4_codes.cuh"
 #include "mx4_pipe.cuh"
-
-namespace cg = cooperative_groups;
 
 namespace excp {
 namespace {
@@ -41,10 +38,9 @@ struct NarrowArgs {
     u32 col_tiles, nt, n_tiles;                    // rows of n per CTA: a multiple of 8, at most 128
     u32 x_codes, x_scales;                         // where the quantised rows lie in shared memory (RAW)
     void* y;
-    u64 sm, sn;                                    // strides of y along the rows of m and of n
-    const float* bias;
-    u32 bias_on_m;
-    u32 wait_m;                                    // m is what the launch before packs
+    u64 stride;                                    // y[row of n, row of m]
+    const float* bias;                             // per row of m
+    u32 sums;                                      // where the parts of the CTA's columns lie in shared memory
     u32 stage_bytes, tmem_cols;
     u64 wait_ns;
     u32* flag;
@@ -98,13 +94,13 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
     typedef typename ElemOf<DT>::type T;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Shared sh;
-    cg::cluster_group cluster = cg::this_cluster();
-    const u32 part = cluster.block_rank(), parts = cluster.num_blocks();
+    const u32 part = cluster_rank(), parts = cluster_size();
     // the swizzle goes by address: stages start on 1024 bytes (the same offset in every CTA)
     unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const u32 warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const u32 tile = blockIdx.x / parts, mt = tile / g.n_tiles, ntile = tile - mt * g.n_tiles;
     const u32 k0 = (u32)((u64)g.col_tiles * part / parts), k1 = (u32)((u64)g.col_tiles * (part + 1) / parts);
+    const u32 per_owner = (g.nt + parts - 1) / parts;          // columns of the result per CTA of the cluster
     // a stage: tile of m (codes, scales), packed rows of n (codes), their scales
     const u32 n_codes = CODES + SB, n_scales = n_codes + g.nt * 128;
 
@@ -117,6 +113,7 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
     if (warp == PRODUCT_WARP) tm_alloc(&sh.tmem, g.tmem_cols);
     tm_fence_before();
     __syncthreads();
+    if (parts > 1) cluster_arrive();
     tm_fence_after();
     const u32 tmem = sh.tmem;
     bool ok = true;                                // this warp's waits were all met
@@ -153,7 +150,6 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
         };
         // the first stages' tiles of m, before the launch that may just be packing n has ended
         const u32 first = min((u32)STAGES, k1 - k0);
-        if (g.wait_m) wait_for_previous();
         for (u32 s = 0; s < first; ++s) fetch_m(s);
         if (!RAW) {
             wait_for_previous();
@@ -261,92 +257,84 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
     const float alpha = (g.m.scale ? __ldg(g.m.scale) : 1.f) * (g.n.scale ? __ldg(g.n.scale) : 1.f);
     const u64 n0 = (u64)ntile * MX4_ROWS;
     const u32 cols = (u32)min((u64)g.nt, g.n.rows - n0);       // of the result
-    float* const sums = reinterpret_cast<float*>(smem);        // [nt][128], where the stages were
-    T* const y = static_cast<T*>(g.y) + n0 * g.sn;
+    // thread t of the work warps has row t of m's tile
+    const u32 t = threadIdx.x;
+    const u64 m = (u64)mt * MX4_ROWS + t;
+    T* const y = static_cast<T*>(g.y) + n0 * g.stride + m;
+    const float bias = g.bias && warp < WORK_WARPS && m < g.m.rows ? __ldg(g.bias + m) : 0.f;
+    // A warp per scheduler: no branches between the columns, so that they overlap.
+    auto put = [&](auto width, const float (&sum)[decltype(width)::value], u32 c, u32 step) {    // columns c, c + step, ...
+        constexpr u32 W = decltype(width)::value;
+        if (m >= g.m.rows) return;
+        float r[W];
+#pragma unroll
+        for (u32 i = 0; i < W; ++i) r[i] = sum[i] * alpha;
+        if (g.bias) {
+#pragma unroll
+            for (u32 i = 0; i < W; ++i) r[i] += bias;
+        }
+        T* const p = y + c * g.stride;
+        const u64 jump = step * g.stride;
+        if (c + (W - 1) * step < cols) {
+#pragma unroll
+            for (u32 i = 0; i < W; ++i) wput(p + i * jump, 0, r[i]);
+        } else {
+#pragma unroll
+            for (u32 i = 0; i < W; ++i) if (c + i * step < cols) wput(p + i * jump, 0, r[i]);
+        }
+    };
+    auto take = [&](auto width, u32 c) {           // that many columns of the accumulator
+        constexpr u32 W = decltype(width)::value;
+        u32 v[W];
+#pragma unroll
+        for (u32 i = 0; i < W; i += 32) {
+            if constexpr (W >= 32) tm_load32(tmem + ((warp * 32) << 16) + c + i, v + i);
+            else tm_load8(tmem + ((warp * 32) << 16) + c + i, v + i);
+        }
+        tm_wait_load();
+        float f[W];
+#pragma unroll
+        for (u32 i = 0; i < W; ++i) f[i] = k0 < k1 ? __uint_as_float(v[i]) : 0.f;
+        if (parts == 1) {
+            put(width, f, c, 1);
+        } else {
+            // column c belongs to CTA c % parts, which has a place for this CTA's part of it
+            u32 owner = c % parts, at = ((part * per_owner + c / parts) * MX4_ROWS + t) * 4;
+#pragma unroll
+            for (u32 i = 0; i < W; ++i) {
+                if (c + i < cols) st_cluster(cluster_address(smem + g.sums, owner) + at, f[i]);
+                if (++owner == parts) { owner = 0; at += MX4_ROWS * 4; }
+            }
+        }
+    };
+    if (parts > 1) cluster_wait();                 // every CTA of the cluster has started
     if (warp < WORK_WARPS) {
-        // thread t of the work warps has row t of m's tile
-        const u64 m = (u64)mt * MX4_ROWS + threadIdx.x;
-        const float bias_m = g.bias && g.bias_on_m && m < g.m.rows ? __ldg(g.bias + m) : 0.f;
-        auto take = [&](auto width, u32 c) {       // that many columns from c on
-            constexpr u32 W = decltype(width)::value;
-            u32 v[W];
-#pragma unroll
-            for (u32 i = 0; i < W; i += 32) {
-                if constexpr (W >= 32) tm_load32(tmem + ((warp * 32) << 16) + c + i, v + i);
-                else tm_load8(tmem + ((warp * 32) << 16) + c + i, v + i);
-            }
-            tm_wait_load();
-            if (k0 == k1) {
-#pragma unroll
-                for (u32 i = 0; i < W; ++i) v[i] = 0u;
-            }
-            if (parts > 1) {
-#pragma unroll
-                for (u32 i = 0; i < W; ++i) sums[(c + i) * MX4_ROWS + threadIdx.x] = __uint_as_float(v[i]);
-            } else if (m < g.m.rows) {
-                // a warp per scheduler: no branches between the columns, so that they overlap
-                float r[W];
-#pragma unroll
-                for (u32 i = 0; i < W; ++i) r[i] = __uint_as_float(v[i]) * alpha;
-                if (g.bias && g.bias_on_m) {
-#pragma unroll
-                    for (u32 i = 0; i < W; ++i) r[i] += bias_m;
-                } else if (g.bias) {
-#pragma unroll
-                    for (u32 i = 0; i < W; ++i) r[i] += c + i < cols ? __ldg(g.bias + n0 + c + i) : 0.f;
-                }
-                T* const p = y + m * g.sm + c * g.sn;
-                if (c + W <= cols) {
-#pragma unroll
-                    for (u32 i = 0; i < W; ++i) wput(p + i * g.sn, 0, r[i]);
-                } else {
-#pragma unroll
-                    for (u32 i = 0; i < W; ++i) if (c + i < cols) wput(p + i * g.sn, 0, r[i]);
-                }
-            }
-        };
         u32 c = 0;
         for (; c + 64 <= g.nt; c += 64) take(std::integral_constant<u32, 64>(), c);
         for (; c < g.nt; c += 8) take(std::integral_constant<u32, 8>(), c);
         tm_fence_before();
     }
+    __syncwarp();
     if (parts > 1) {
-        cluster.sync();
-        // columns dealt to the CTAs and their warps; a lane adds four rows' parts, in ascending order
-        const u64 m = (u64)mt * MX4_ROWS + lane * 4;
-        float bias_m[4];
+        cluster_arrive_release();
+        cluster_wait();
+        if (warp < WORK_WARPS) {
+            const float* own = reinterpret_cast<const float*>(smem + g.sums) + t;
+            auto join = [&](auto width, u32 j) {   // own columns j ..: their parts in ascending order
+                constexpr u32 W = decltype(width)::value;
+                float f[W];
 #pragma unroll
-        for (u32 i = 0; i < 4; ++i) bias_m[i] = g.bias && g.bias_on_m && m + i < g.m.rows ? __ldg(g.bias + m + i) : 0.f;
-        const u32 step = parts * (THREADS / 32);
-        for (u32 c = part + parts * warp; c < cols; c += 2 * step) {           // two columns' parts on their way at a time
-            float4 f[2][MAX_SPLIT];
+                for (u32 i = 0; i < W; ++i) f[i] = own[min(j + i, per_owner - 1) * MX4_ROWS];
+                for (u32 p = 1; p < parts; ++p) {
 #pragma unroll
-            for (u32 p = 0; p < MAX_SPLIT; ++p) {
-                if (p >= parts) continue;
-                const float4* of = reinterpret_cast<const float4*>(cluster.map_shared_rank(sums, p));
-                f[0][p] = of[c * (MX4_ROWS / 4) + lane];
-                if (c + step < cols) f[1][p] = of[(c + step) * (MX4_ROWS / 4) + lane];
-            }
-#pragma unroll
-            for (u32 h = 0; h < 2; ++h) {
-                const u32 col = c + h * step;
-                if (col >= cols) break;
-                float4 sum = f[h][0];
-#pragma unroll
-                for (u32 p = 1; p < MAX_SPLIT; ++p) {
-                    if (p >= parts) continue;
-                    sum.x += f[h][p].x; sum.y += f[h][p].y; sum.z += f[h][p].z; sum.w += f[h][p].w;
+                    for (u32 i = 0; i < W; ++i) f[i] += own[(p * per_owner + min(j + i, per_owner - 1)) * MX4_ROWS];
                 }
-                const float r[4] = {sum.x, sum.y, sum.z, sum.w};
-#pragma unroll
-                for (u32 i = 0; i < 4; ++i) {
-                    float v = r[i] * alpha;
-                    if (g.bias) v += g.bias_on_m ? bias_m[i] : __ldg(g.bias + n0 + col);
-                    if (m + i < g.m.rows) wput(y, (m + i) * g.sm + col * g.sn, v);
-                }
-            }
+                put(width, f, part + j * parts, parts);
+            };
+            u32 j = 0;
+            for (; j + 8 <= per_owner; j += 8) join(std::integral_constant<u32, 8>(), j);
+            for (; j < per_owner; j += 2) join(std::integral_constant<u32, 2>(), j);
         }
-        cluster.sync();                            // the others have read this CTA's sums
     }
     __syncwarp();
     __syncthreads();
@@ -381,11 +369,12 @@ bool launch_typed(cudaStream_t s, const NarrowArgs& g, u32 parts, u32 smem, int 
 }
 
 u32 split(int sms, u64 m_tiles, u64 n_tiles, u32 nt, u32 col_tiles) {
-    // two CTAs per SM as long as there are columns to split, and no more sums to exchange than a block of 128 x 128
+    // Two CTAs per SM as long as there are columns to split, and few sums to exchange: 64 rows in two parts 4096 -> 11008 take
+    // 18.7 us, whole 11.4; 8 rows whole 8.3, in three parts 7.6.
     u64 parts = (u64)sms * 2 / (m_tiles * n_tiles);
     if (parts > MAX_SPLIT) parts = MAX_SPLIT;
     if (parts > col_tiles) parts = col_tiles;
-    if (parts > MX4_ROWS / nt) parts = MX4_ROWS / nt;
+    if (parts > 64 / nt) parts = 64 / nt;
     return parts < 1 ? 1u : (u32)parts;
 }
 // Shared memory of the quantised rows of a CTA.
@@ -397,23 +386,21 @@ u32 raw_bytes(u32 nt, u32 col_tiles, u32 parts, int fmt) {
 bool launch_narrow(int sms, cudaStream_t s, const Mx4Operand& a, const RowsIn* x, const Mx4Operand& b, u64 cols, int fmt,
                    const Mx4Result& r, u64 wait_ns, u32* flag, bool behind) {
     NarrowArgs g{};
-    // b on the M side, so that neighbouring lanes write neighbouring results, unless b has the few rows
-    const bool turned = a.rows <= MX4_ROWS || b.rows > MX4_ROWS;
-    g.m = turned ? b : a;
-    g.n = turned ? a : b;
+    // b on the M side: neighbouring lanes write neighbouring results
+    g.m = b;
+    g.n = a;
     g.cols = cols;
     g.col_tiles = mx4_col_tiles(cols);
     g.nt = g.n.rows > MX4_ROWS ? MX4_ROWS : (u32)((g.n.rows + 7) & ~7ull);
     g.n_tiles = mx4_row_tiles(g.n.rows);
     g.y = r.y;
-    g.sm = turned ? 1 : r.stride;
-    g.sn = turned ? r.stride : 1;
+    g.stride = r.stride;
     g.bias = r.bias;
-    g.bias_on_m = turned;
-    g.wait_m = !turned;
     const u32 sb = (u32)mx4_scale_bytes(fmt), parts = split(sms, mx4_row_tiles(g.m.rows), g.n_tiles, g.nt, g.col_tiles);
     g.stage_bytes = CODES + sb + (x ? 0 : g.nt * 128 + sb);
     u32 smem = g.stage_bytes * STAGES + 1024;
+    g.sums = g.stage_bytes * STAGES;
+    if (parts > 1) smem += ((g.nt + parts - 1) / parts * parts * MX4_ROWS * 4 + 1023) & ~1023u;      // what follows starts on 1024 bytes
     const u32 need = g.nt + STAGES * (u32)mx4_pieces(fmt) * 8;
     g.tmem_cols = 32;
     while (g.tmem_cols < need) g.tmem_cols *= 2;
@@ -424,7 +411,7 @@ bool launch_narrow(int sms, cudaStream_t s, const Mx4Operand& a, const RowsIn* x
     g.x_stride = x->stride;
     const u64 size = x->dtype == DT_F32 ? 4 : 2;
     g.x_vec = (reinterpret_cast<uintptr_t>(x->p) & 15) == 0 && (x->rows == 1 || ((x->stride * size) & 15) == 0);
-    g.x_codes = g.stage_bytes * STAGES;
+    g.x_codes = smem - 1024;
     g.x_scales = g.x_codes + (g.col_tiles + parts - 1) / parts * g.nt * 128;
     smem += raw_bytes(g.nt, g.col_tiles, parts, fmt);
     return x->dtype == DT_F32 ? launch_typed<DT_F32>(s, g, parts, smem, fmt, r.dtype, false)
