@@ -65,12 +65,16 @@ class Params:
                        self.flags)
 
 
+# what the native half of the binding calls (csrc/score_binding.cpp, in the order of its table)
+_SCORE_CALLS = ["excp_mx4_bytes", "excp_mx4_tensor_scale", "excp_mx4_quantize", "excp_mx4_dequantize", "excp_mx4_matmul",
+                "excp_mx4_linear_scratch", "excp_mx4_linear", "excp_token_logprobs", "excp_token_logprobs_grad"]
 _lib = None
+_score = None
 
 
 def load_library() -> C.CDLL:
     """Loads (building first if the sources are newer) libexcp.so and declares the prototypes."""
-    global _lib
+    global _lib, _score
     if _lib is not None:
         return _lib
     path = _build.build()
@@ -133,6 +137,10 @@ def load_library() -> C.CDLL:
     for name in EXPORTS:
         if getattr(lib, name).restype is C.c_int:
             getattr(lib, name).restype = C.c_int
+    _build.build_binding()
+    from . import _score as native
+    native.bind(*[C.cast(getattr(lib, name), vp).value for name in _SCORE_CALLS], ExcpError)
+    _score = native
     _lib = lib
     return lib
 
@@ -207,18 +215,16 @@ class Mx4Matrix:
     def __init__(self, data: torch.Tensor, rows: int, cols: int, fmt: str, scale: torch.Tensor | None = None):
         self.data, self.rows, self.cols, self.fmt, self.scale = data, rows, cols, fmt, scale
         self.code = MX4_FORMAT[fmt]
-        if not (data.is_cuda and data.dtype == torch.uint8 and data.is_contiguous()) or data.numel() < mx4_bytes(rows, cols, fmt):
-            raise TypeError("expected a contiguous uint8 CUDA tensor of mx4_bytes(rows, cols, fmt)")
 
 
-@dataclass
 class TokenLogprobs:
-    logprob: torch.Tensor           # float32 [rows]
-    entropy: torch.Tensor           # float32 [rows]
-    top_logprob: torch.Tensor | None   # float32 [rows, top]
-    top_index: torch.Tensor | None     # int64 [rows, top]
-    row_stats: torch.Tensor         # float32 [rows, 4], for the gradient
-    scale: float
+    """What token_logprobs returns: logprob and entropy (float32 [rows]), top_logprob (float32) and top_index (int64,
+    [rows, top]; None without alternatives), row_stats (float32 [rows, 4]) and scale for the gradient."""
+    __slots__ = ("logprob", "entropy", "top_logprob", "top_index", "row_stats", "scale")
+
+    def __init__(self, logprob, entropy, top_logprob, top_index, row_stats, scale):
+        self.logprob, self.entropy, self.top_logprob, self.top_index = logprob, entropy, top_logprob, top_index
+        self.row_stats, self.scale = row_stats, scale
 
 
 class Handle:
@@ -407,151 +413,51 @@ class Handle:
             raise ExcpError(st, "excp_decompress_dense_tensor")
 
     # ---- scoring a restored checkpoint -------------------------------------
-    # Only enqueued; outputs are allocated by torch where the caller gives none.
-    def _rows(self, t: torch.Tensor, what: str) -> tuple[int, int, int, int, int]:
-        """(pointer, dtype, rows, cols, row stride) of a 2-D tensor whose last dimension is dense."""
-        if t.dim() != 2 or t.dtype not in _DTYPE or t.device.type != "cuda" or t.device.index != self.device:
-            raise TypeError(f"{what}: expected a 2-D float32, float16 or bfloat16 tensor on cuda:{self.device}")
-        rows, cols = t.shape
-        stride, inner = t.stride()
-        if inner != 1 and cols > 1:
-            raise TypeError(f"{what}: the last dimension must be dense")
-        return t.data_ptr(), _DTYPE[t.dtype], rows, cols, stride if rows > 1 else cols
-
-    def _vector(self, t: torch.Tensor | None, what: str, dtype: torch.dtype, n: int) -> int:
-        if t is None:
-            return 0
-        if t.dtype != dtype or t.numel() != n or t.device.type != "cuda" or t.device.index != self.device or not t.is_contiguous():
-            raise TypeError(f"{what}: expected {n} contiguous {dtype} values on cuda:{self.device}")
-        return t.data_ptr()
-
-    def _raw_stream(self) -> int:
-        return torch._C._cuda_getCurrentRawStream(self.device)
-
-    def _packed(self, m: Mx4Matrix, what: str) -> int:
-        if m.data.device.index != self.device:
-            raise TypeError(f"{what}: expected a packed matrix on cuda:{self.device}")
-        return m.data.data_ptr()
-
+    # Only enqueued on the current stream; results are allocated by torch where the caller gives no `out`.  The arguments
+    # are marshalled by csrc/score_binding.cpp: TypeError for tensors of the wrong kind, ExcpError for a status.
     def mx4_tensor_scale(self, x: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
         """excp_mx4_tensor_scale: the tensor scale of a matrix, as a float32 tensor of one value."""
-        p, dt, rows, cols, stride = self._rows(x, "x")
-        if out is None:
-            out = torch.empty((), dtype=torch.float32, device=x.device)
-        st = self.lib.excp_mx4_tensor_scale(self._h, p, dt, rows, cols, stride, self._vector(out, "out", torch.float32, 1), self._raw_stream())
-        if st != 0:
-            raise ExcpError(st, "excp_mx4_tensor_scale")
-        return out
+        return _score.mx4_tensor_scale(self._h.value, self.device, x, out)
 
     def mx4_quantize(self, x: torch.Tensor, fmt: str, tensor_scale: torch.Tensor | None = None,
                      out: torch.Tensor | None = None) -> Mx4Matrix:
         """excp_mx4_quantize: x [rows, cols] as a packed 4-bit matrix (into `out`, uint8, if given)."""
-        p, dt, rows, cols, stride = self._rows(x, "x")
-        if out is None:
-            out = torch.empty(mx4_bytes(rows, cols, fmt), dtype=torch.uint8, device=x.device)
-        m = Mx4Matrix(out, rows, cols, fmt, tensor_scale)
-        st = self.lib.excp_mx4_quantize(self._h, p, dt, rows, cols, stride, m.code, self._vector(tensor_scale, "tensor_scale", torch.float32, 1),
-                                        self._packed(m, "out"), self._raw_stream())
-        if st != 0:
-            raise ExcpError(st, "excp_mx4_quantize")
-        return m
+        data = _score.mx4_quantize(self._h.value, self.device, x, MX4_FORMAT[fmt], tensor_scale, out)
+        rows, cols = x.shape
+        return Mx4Matrix(data, rows, cols, fmt, tensor_scale)
 
     def mx4_dequantize(self, m: Mx4Matrix, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
         """excp_mx4_dequantize: the values that the codes stand for."""
-        if out is None:
-            out = torch.empty((m.rows, m.cols), dtype=dtype, device=m.data.device)
-        p, dt, rows, cols, stride = self._rows(out, "out")
-        if (rows, cols) != (m.rows, m.cols):
-            raise TypeError("out: expected the matrix's shape")
-        st = self.lib.excp_mx4_dequantize(self._h, self._packed(m, "m"), rows, cols, m.code, self._vector(m.scale, "scale", torch.float32, 1),
-                                          p, dt, stride, self._raw_stream())
-        if st != 0:
-            raise ExcpError(st, "excp_mx4_dequantize")
-        return out
+        return _score.mx4_dequantize(self._h.value, self.device, m.data, m.rows, m.cols, m.code, m.scale, dtype, out)
 
     def mx4_matmul(self, a: Mx4Matrix, b: Mx4Matrix, bias: torch.Tensor | None = None, dtype: torch.dtype = torch.bfloat16,
                    out: torch.Tensor | None = None) -> torch.Tensor:
         """excp_mx4_matmul: a b^T (+ bias per row of b) of two packed matrices, [a.rows, b.rows]."""
         if a.code != b.code or a.cols != b.cols:
             raise TypeError("a, b: expected the same format and number of columns")
-        if out is None:
-            out = torch.empty((a.rows, b.rows), dtype=dtype, device=b.data.device)
-        y, dt, rows, cols, stride = self._rows(out, "out")
-        if (rows, cols) != (a.rows, b.rows):
-            raise TypeError("out: expected [a.rows, b.rows]")
-        f32 = torch.float32
-        st = self.lib.excp_mx4_matmul(self._h, self._packed(a, "a"), a.rows, self._vector(a.scale, "a.scale", f32, 1), self._packed(b, "b"), b.rows,
-                                      self._vector(b.scale, "b.scale", f32, 1), a.cols, a.code, self._vector(bias, "bias", f32, b.rows), y, dt,
-                                      stride, self._raw_stream())
-        if st != 0:
-            raise ExcpError(st, "excp_mx4_matmul")
-        return out
+        return _score.mx4_matmul(self._h.value, self.device, a.data, a.rows, a.scale, b.data, b.rows, b.scale, a.cols, a.code, bias,
+                                 dtype, out)
 
     def mx4_linear(self, x: torch.Tensor, w: Mx4Matrix, bias: torch.Tensor | None = None, tensor_scale: torch.Tensor | None = None,
                    out: torch.Tensor | None = None, dtype: torch.dtype | None = None, x_packed: torch.Tensor | None = None) -> torch.Tensor:
         """excp_mx4_linear: x w^T (+ bias), x [rows, w.cols] quantised to w's format with the tensor scale given; the result
-        has x's type unless `dtype` or `out` says otherwise.  `x_packed` (uint8, excp_mx4_linear_scratch bytes) is room for the packed x."""
-        p, xdt, rows, cols, xstride = self._rows(x, "x")
-        if cols != w.cols:
-            raise TypeError(f"x: expected {w.cols} columns")
-        if out is None:
-            out = torch.empty((rows, w.rows), dtype=dtype or x.dtype, device=x.device)
-        y, dt, yrows, ycols, stride = self._rows(out, "out")
-        if (yrows, ycols) != (rows, w.rows):
-            raise TypeError("out: expected [x rows, w.rows]")
-        need = self.lib.excp_mx4_linear_scratch(self._h, rows, w.rows, cols, w.code)
-        if x_packed is None:
-            if need:
-                x_packed = torch.empty(need, dtype=torch.uint8, device=x.device)
-        elif x_packed.dtype != torch.uint8 or x_packed.numel() < need or not x_packed.is_contiguous() or x_packed.device != x.device:
-            raise TypeError("x_packed: expected a contiguous uint8 tensor of excp_mx4_linear_scratch bytes on x's device")
-        f32 = torch.float32
-        st = self.lib.excp_mx4_linear(self._h, p, xdt, rows, xstride, self._vector(tensor_scale, "tensor_scale", f32, 1), self._packed(w, "w"), w.rows,
-                                      self._vector(w.scale, "w.scale", f32, 1), cols, w.code, self._vector(bias, "bias", f32, w.rows), y, dt, stride,
-                                      0 if x_packed is None else x_packed.data_ptr(), self._raw_stream())
-        if st != 0:
-            raise ExcpError(st, "excp_mx4_linear")
-        return out
+        has x's type unless `dtype` or `out` says otherwise.  `x_packed` (uint8, excp_mx4_linear_scratch bytes) is room for
+        the packed x."""
+        return _score.mx4_linear(self._h.value, self.device, x, tensor_scale, w.data, w.rows, w.scale, w.cols, w.code, bias, dtype, out,
+                                 x_packed)
 
     def token_logprobs(self, logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, scale: float = 1.0) -> TokenLogprobs:
         """excp_token_logprobs: log probability of each row's token, entropy, and the `top` likeliest alternatives."""
-        p, dt, rows, vocab, stride = self._rows(logits, "logits")
-        f32 = torch.float32
-        stats = torch.empty((rows, 4), dtype=f32, device=logits.device)
-        both = torch.empty((2, rows), dtype=f32, device=logits.device)
-        tl = ti = None
-        if top > 0:
-            tl = torch.empty((rows, top), dtype=f32, device=logits.device)
-            ti = torch.empty((rows, top), dtype=torch.int64, device=logits.device)
-        r = TokenLogprobs(both[0], both[1], tl, ti, stats, scale)
-        b = both.data_ptr()
-        st = self.lib.excp_token_logprobs(self._h, p, dt, rows, vocab, stride, self._vector(tokens, "tokens", torch.int64, rows), scale, top, b,
-                                          b + 4 * rows, stats.data_ptr(), tl.data_ptr() if top > 0 else 0, ti.data_ptr() if top > 0 else 0,
-                                          self._raw_stream())
-        if st != 0:
-            raise ExcpError(st, "excp_token_logprobs")
-        return r
+        return TokenLogprobs(*_score.token_logprobs(self._h.value, self.device, logits, tokens, top, scale), scale)
 
     def token_logprobs_grad(self, logits: torch.Tensor, tokens: torch.Tensor, r: TokenLogprobs, g_logprob: torch.Tensor | None,
                             g_entropy: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
         """excp_token_logprobs_grad: the gradient with respect to the logits, from what token_logprobs returned for them.
         `out` may be `logits`."""
-        p, dt, rows, vocab, stride = self._rows(logits, "logits")
-        if out is None:
-            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-        q, odt, orows, ocols, ostride = self._rows(out, "out")
-        if (odt, orows, ocols) != (dt, rows, vocab):
-            raise TypeError("out: expected the logits' shape and type")
-        f32 = torch.float32
-        st = self.lib.excp_token_logprobs_grad(self._h, p, dt, rows, vocab, stride, self._vector(tokens, "tokens", torch.int64, rows), r.scale,
-                                               self._vector(r.row_stats, "row_stats", f32, rows * 4), self._vector(g_logprob, "g_logprob", f32, rows),
-                                               self._vector(g_entropy, "g_entropy", f32, rows), q, ostride, self._raw_stream())
-        if st != 0:
-            raise ExcpError(st, "excp_token_logprobs_grad")
-        return out
+        return _score.token_logprobs_grad(self._h.value, self.device, logits, tokens, r.row_stats, r.scale, g_logprob, g_entropy, out)
 
     def score_status(self) -> None:
         """excp_score_status: synchronises; raises if a product's bounded wait ran out since the last report."""
-        st = self.lib.excp_score_status(self._h, self._raw_stream())
+        st = self.lib.excp_score_status(self._h, torch.cuda.current_stream(self.device).cuda_stream)
         if st != 0:
             raise ExcpError(st, "excp_score_status")

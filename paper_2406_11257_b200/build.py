@@ -1,10 +1,13 @@
-"""Builds the CUDA library in-tree: csrc/*.cu -> libexcp.so (sm_100a only)."""
+"""Builds the CUDA library in-tree: csrc/*.cu -> libexcp.so (sm_100a only), and the native half of the Python
+binding: csrc/score_binding.cpp -> _score.so (against the installed torch)."""
 from __future__ import annotations
 
 import hashlib
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -39,6 +42,25 @@ def _stale(lib: str) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_binding(force: bool = False) -> str:
+    """Compiles _score.so if it is missing or older than its sources; returns its path."""
+    import torch
+    out = os.path.join(HERE, "_score.so")
+    deps = [os.path.join(CSRC, "score_binding.cpp"), os.path.join(os.path.dirname(HERE), "include", "excp.h")]
+    if not force and os.path.exists(out) and all(os.path.getmtime(d) <= os.path.getmtime(out) for d in deps):
+        return out
+    at = os.path.dirname(torch.__file__)
+    nvcc = os.environ.get("NVCC", "nvcc")
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which(nvcc) or "/usr/local/cuda/bin/nvcc")))
+    include = [os.path.join(at, "include"), sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    part = out + f".{os.getpid()}"
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *["-I" + i for i in include], deps[0], "-o", part,
+                           "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+    os.replace(part, out)      # whole or not at all: another process may be loading it
+    return out
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compiles the library if it is missing or older than its sources; returns its path."""
     lib = lib_path()
@@ -69,3 +91,4 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_binding(force="--force" in sys.argv))
