@@ -3,12 +3,17 @@
 // A block of B consecutive values of a row shares a scale; a value is held as the nearest of
 // 0, .5, 1, 1.5, 2, 3, 4, 6 (and sign) to value / scale.  Definitions, byte for byte: include/excp.h.
 //
-// Work split: a warp takes 256 columns (one tile) of the four rows l, l + 32, l + 64, l + 96 of a row tile;
-// lane i holds the eight consecutive values 8 i .. 8 i + 7 of each, so that
-//   - a load of the warp is 512 (16-bit) or 1024 (fp32) consecutive bytes of a row, four rows in flight,
-//   - a block's largest magnitude is two shuffles (B = 32) or one (B = 16) away,
-//   - a row's codes leave as 128 consecutive bytes, and the four rows' scales of a block of columns as whole
-//     16-byte groups of the layout the tensor core reads (row 32 c + l of piece j at byte 16 l + 4 c).
+// Work split: a warp takes 256 columns (one tile) of the four rows l, l + 32, l + 64, l + 96 of a row tile, two rows at a
+// time: a half-warp has a row, a lane 16 consecutive values of it, so that
+//   - a lane's values are one or two 32-byte loads, all four rows in flight,
+//   - a block's largest magnitude is in the lane (blocks of 16) or one shuffle away, and its scale is worked out once or twice,
+//   - a row's codes leave as 128 consecutive bytes, and its scales as words of the layout the tensor core reads
+//     (row 32 c + l of piece j at byte 16 l + 4 c).
+// Rows that do not start on 32 bytes go through shared memory: loaded and stored value by value, neighbouring lanes
+// neighbouring values.
+// Bound: the values' bytes at fp32; at 16 bits instruction issue comes close (about ten instructions per value).
+#include <type_traits>
+
 #include "mx4_codes.cuh"
 #include "mx4_pipe.cuh"
 
@@ -17,33 +22,104 @@ namespace {
 
 constexpr int WARPS = 8;
 
-// ---- tensor scale: max |x| / 2688, rounded up to 8 significant bits -----------------
+// How a matrix in ordinary layout is reached: its rows all start on 32 bytes, on 16, or anywhere.
+enum Reach { REACH_32, REACH_16, REACH_ANY };
+
+// Values c0 .. c0 + 15 of a row of `cols`, 0 past the end; p: the first one.
+__device__ __forceinline__ void load32(const void* p, uint4& a, uint4& b) {
+    asm volatile("ld.global.nc.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p));
+}
+__device__ __forceinline__ void store32(void* p, const uint4& a, const uint4& b) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
+template <typename T> struct Sixteen { uint4 w[sizeof(T)]; };          // 16 values as words
+template <typename T, int REACH>
+__device__ __forceinline__ void load_words(const T* p, u64 left, Sixteen<T>& v) {      // left: values of the row from p on
+    if (left >= 16) {
+        const uint4* q = reinterpret_cast<const uint4*>(p);
+#pragma unroll
+        for (u32 i = 0; i < sizeof(T); i += 2) {
+            if (REACH == REACH_32) load32(q + i, v.w[i], v.w[i + 1]);
+            else { v.w[i] = __ldg(q + i); v.w[i + 1] = __ldg(q + i + 1); }
+        }
+        return;
+    }
+    T* h = reinterpret_cast<T*>(&v);
+#pragma unroll
+    for (u32 k = 0; k < 16; ++k) wput(h, k, k < left ? wget(p, k) : 0.f);
+}
+template <typename T, int REACH>
+__device__ __forceinline__ void store_words(T* p, u64 left, const Sixteen<T>& v) {
+    if (left >= 16) {
+        uint4* q = reinterpret_cast<uint4*>(p);
+#pragma unroll
+        for (u32 i = 0; i < sizeof(T); i += 2) {
+            if (REACH == REACH_32) store32(q + i, v.w[i], v.w[i + 1]);
+            else { q[i] = v.w[i]; q[i + 1] = v.w[i + 1]; }
+        }
+        return;
+    }
+    const T* h = reinterpret_cast<const T*>(&v);
+#pragma unroll
+    for (u32 k = 0; k < 16; ++k) if (k < left) p[k] = h[k];
+}
+
+// Pattern of the largest magnitude of 16 values (at or above NONFINITE_BITS where there is an infinity or a NaN).
+__device__ __forceinline__ u32 largest_bits(const Sixteen<float>& v) {
+    const u32* b = reinterpret_cast<const u32*>(&v);
+    u32 m = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) m = max(m, b[k] & 0x7fffffffu);
+    return m;
+}
 template <typename T>
-__global__ void __launch_bounds__(256) tensor_scale_kernel(const T* __restrict__ x, u64 rows, u64 cols, u64 stride, bool vec,
+__device__ __forceinline__ u32 largest_bits(const Sixteen<T>& v) {
+    typedef typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type T2;
+    const T2* h = reinterpret_cast<const T2*>(&v);
+    T2 m = __habs2(h[0]);
+#pragma unroll
+    for (int k = 1; k < 8; ++k) m = __hmax2_nan(m, __habs2(h[k]));
+    const T* e = reinterpret_cast<const T*>(&m);
+    return max(__float_as_uint(wget(e, 0)) & 0x7fffffffu, __float_as_uint(wget(e, 1)) & 0x7fffffffu);
+}
+
+// ---- tensor scale: max |x| / 2688, rounded up to 8 significant bits -----------------
+// A warp takes 512 values of a row at a time.
+template <typename T, int REACH>
+__global__ void __launch_bounds__(256) tensor_scale_kernel(const T* __restrict__ x, u64 rows, u64 cols, u64 stride, u32 chunks,
                                                            u32* words, float* scale_out) {
     u32 best = 0;
-    auto take = [&](float v) {
-        const u32 m = __float_as_uint(v) & 0x7fffffffu;
+    auto take = [&](u32 m) {
         if (m < NONFINITE_BITS && m > best) best = m;
     };
-    const u64 groups = (cols + 7) / 8;
-    const u64 total = rows * groups;
-    for (u64 i = (u64)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (u64)gridDim.x * blockDim.x) {
-        const u64 r = i / groups, c = (i - r * groups) * 8;
-        const T* p = x + r * stride + c;
-        float v[8];
-        if (vec && c + 8 <= cols) {
-            load8(p, v);
+    const u32 lane = threadIdx.x & 31;
+    const u64 total = rows * chunks, step = (u64)gridDim.x * 8;
+    for (u64 i = (u64)blockIdx.x * 8 + (threadIdx.x >> 5); i < total; i += step) {
+        const u64 r = i / chunks, c0 = (i - r * chunks) * 512;
+        const T* p = x + r * stride + c0;
+        const u64 left = cols - c0;
+        if (REACH == REACH_ANY || left < 512) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) take(v[k]);
+            for (u32 k = 0; k < 16; ++k) if (lane + 32 * k < left) take(__float_as_uint(wget(p, lane + 32 * k)) & 0x7fffffffu);
         } else {
-            for (int k = 0; k < 8 && c + k < cols; ++k) take(wget(p, k));
+            Sixteen<T> v;
+            load_words<T, REACH>(p + lane * 16, 16, v);
+            const u32 m = largest_bits(v);
+            if (m < NONFINITE_BITS) {
+                take(m);
+            } else {                               // the finite ones one by one
+                const T* h = reinterpret_cast<const T*>(&v);
+#pragma unroll
+                for (u32 k = 0; k < 16; ++k) take(__float_as_uint(wget(h, k)) & 0x7fffffffu);
+            }
         }
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
     __shared__ u32 part[8];
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = best;
+    if (lane == 0) part[threadIdx.x >> 5] = best;
     __syncthreads();
     if (threadIdx.x) return;
     for (int w = 1; w < 8; ++w) best = max(best, part[w]);
@@ -58,175 +134,237 @@ __global__ void __launch_bounds__(256) tensor_scale_kernel(const T* __restrict__
     scale_out[0] = q > 0.f ? __uint_as_float((__float_as_uint(q) + 0xffffu) & 0xffff0000u) : 1.f;
 }
 
-template <typename T, int FMT>
-__global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const T* __restrict__ x, u64 rows, u64 cols, u64 stride, bool vec,
-                                                              u32 col_tiles, u64 tasks, const float* __restrict__ tensor_scale,
-                                                              unsigned char* __restrict__ out) {
-    let_next_start();                              // a product of this matrix may set itself up and fetch the other one
-    const u64 task = (u64)blockIdx.x * WARPS + (threadIdx.x >> 5);
-    if (task >= tasks) return;
-    const u32 lane = threadIdx.x & 31;
-    const u32 l = (u32)(task & 31);
-    const u64 tile = task >> 5;
-    const u32 rt = (u32)(tile / col_tiles), ct = (u32)(tile - (u64)rt * col_tiles);
-    const u32 height = mx4_tile_height(rows, rt);
-    unsigned char* const dst = out + mx4_tile_offset(rows, col_tiles, FMT, rt, ct);
-    const u64 row0 = (u64)rt * MX4_ROWS + l, c0 = (u64)ct * MX4_COLS + lane * 8;
+// Where a warp works: tile (rt, ct), rows l + 32 c.
+struct Place {
+    u32 rt, ct, l, height;
+    u64 offset, row0;
+    __device__ __forceinline__ Place(u64 task, u64 rows, u32 col_tiles, int fmt) {
+        l = (u32)(task & 31);
+        const u64 tile = task >> 5;
+        rt = (u32)(tile / col_tiles);
+        ct = (u32)(tile - (u64)rt * col_tiles);
+        height = mx4_tile_height(rows, rt);
+        offset = mx4_tile_offset(rows, col_tiles, fmt, rt, ct);
+        row0 = (u64)rt * MX4_ROWS + l;
+    }
+};
 
+template <typename T, int FMT, int REACH>
+__global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const T* __restrict__ x, u64 rows, u64 cols, u64 stride, u32 col_tiles,
+                                                              u64 tasks, const float* __restrict__ tensor_scale, unsigned char* __restrict__ out) {
+    let_next_start();                              // a product of this matrix may set itself up and fetch the other one
+    __shared__ __align__(16) T buffer[REACH == REACH_ANY ? WARPS : 1][REACH == REACH_ANY ? 4 : 1][MX4_COLS];
+    const u32 warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, part = lane & 15;
+    const u64 task = (u64)blockIdx.x * WARPS + warp;
+    if (task >= tasks) return;
+    const Place at(task, rows, col_tiles, FMT);
+    unsigned char* const dst = out + at.offset;
+    const u64 first = (u64)at.ct * MX4_COLS, c0 = first + part * 16;
+
+    Sixteen<T> v[2];
+    if (REACH == REACH_ANY) {
+#pragma unroll
+        for (u32 c = 0; c < 4; ++c) {
+            const u64 row = at.row0 + 32 * c;
+            const T* p = x + row * stride + first;
+#pragma unroll
+            for (u32 k = 0; k < MX4_COLS / 32; ++k)
+                wput(buffer[warp][c], lane + 32 * k, row < rows && first + lane + 32 * k < cols ? wget(p, lane + 32 * k) : 0.f);
+        }
+        __syncwarp();
+#pragma unroll
+        for (u32 i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const Sixteen<T>*>(&buffer[warp][2 * i + half][part * 16]);
+    } else {
+#pragma unroll
+        for (u32 i = 0; i < 2; ++i) {
+            const u64 row = at.row0 + 32 * (2 * i + half);
+            load_words<T, REACH>(x + row * stride + c0, row < rows && c0 < cols ? cols - c0 : 0, v[i]);
+        }
+    }
     float g = 1.f;
     if (FMT == MX4_E4M3_16 && tensor_scale) g = __ldg(tensor_scale);
     const float six_g = 6.f * g;
-
-    float v[4][8];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const T* p = x + (row0 + 32 * c) * stride + c0;
-        if (row0 + 32 * c < rows && vec && c0 + 8 <= cols) {
-            load8(p, v[c]);
-        } else {
+    for (u32 i = 0; i < 2; ++i) {
+        const u32 c = 2 * i + half, r = at.l + 32 * c;
+        u32 m = largest_bits(v[i]);
+        if (FMT == MX4_E8M0_32) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        float f[16];
+        const T* h = reinterpret_cast<const T*>(&v[i]);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[c][k] = row0 + 32 * c < rows && c0 + k < cols ? wget(p, k) : 0.f;
-        }
-    }
-    u32 bytes[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        u32 m = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(v[c][k]) & 0x7fffffffu);
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        if (FMT == MX4_E8M0_32) m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        bytes[c] = FMT == MX4_E8M0_32 ? scale_e8m0(v[c], m) : scale_e4m3(v[c], m, g, six_g);
+        for (u32 k = 0; k < 16; ++k) f[k] = wget(h, k);
+        u32 byte = FMT == MX4_E8M0_32 ? scale_e8m0(f, m) : scale_e4m3(f, m, g, six_g);
         // no row here, or no such block in the row: scale byte 0
-        constexpr u32 B = (u32)mx4_block(FMT);
-        if (row0 + 32 * c >= rows || c0 / B * B >= cols) bytes[c] = 0;
-        const u32 r = l + 32 * c;
-        if (r < height) *reinterpret_cast<u32*>(dst + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + ((lane & 3) << 2)) = e2m1x8(v[c]);
+        constexpr u64 B = (u64)mx4_block(FMT);
+        if (at.row0 + 32 * c >= rows || c0 / B * B >= cols) byte = 0;
+        // lane `part` has half a chunk of 16 bytes
+        if (r < at.height)
+            *reinterpret_cast<uint2*>(dst + r * 128 + (((part >> 1) ^ (r & 7)) << 4) + ((part & 1) << 3)) = make_uint2(e2m1x8(f), e2m1x8(f + 8));
+        // the bytes of four blocks as a word
+        constexpr u32 STEP = (u32)mx4_block(FMT) / 16;          // lanes to a block
+        u32 word = byte | __shfl_xor_sync(0xffffffffu, byte, STEP) << 8;
+        word |= __shfl_xor_sync(0xffffffffu, word, 2 * STEP) << 16;
+        if (part % (4 * STEP) == 0)
+            *reinterpret_cast<u32*>(dst + at.height * 128 + part / (4 * STEP) * MX4_PIECE + at.l * 16 + c * 4) = word;
     }
-    // scale word of row c, piece j: the bytes of blocks 4 j .. 4 j + 3, held by lanes PER apart
-    constexpr int PER = mx4_block(FMT) / 8;
-    const u32 piece = lane >> 2, src = min(piece, (u32)mx4_pieces(FMT) - 1) * 4 * PER;
-    u32 word = 0;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const u32 w = scale_word<FMT>(bytes[c], src);
-        if ((lane & 3) == (u32)c) word = w;
-    }
-    if (piece < (u32)mx4_pieces(FMT))
-        *reinterpret_cast<u32*>(dst + height * 128 + piece * MX4_PIECE + l * 16 + (lane & 3) * 4) = word;
 }
 
 // ---- and back ------------------------------------------------------------------------------
-__device__ __forceinline__ float e2m1_value(u32 code) {
-    // as fp16 bits the exponent and mantissa of a 4-bit float read 2^-14 times too small, its subnormal included
-    return __half2float(__ushort_as_half((unsigned short)(((code & 7u) << 9) | ((code & 8u) << 12)))) * 16384.f;
-}
-template <int FMT>
-__device__ __forceinline__ float scale_value(u32 byte) {
-    if (FMT == MX4_E4M3_16) return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3)));
-    if (byte == 0xffu) return __uint_as_float(0x7fffffffu);
-    return __uint_as_float(byte ? byte << 23 : 0x00400000u);           // 2^(byte - 127), subnormal at 0
+// Eight codes as fp16 values, two to a word.
+__device__ __forceinline__ void values_of(u32 codes, __half2 (&v)[4]) {
+    u32 w[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(codes));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const __half2*>(&w[i]);
 }
 
-template <typename T, int FMT>
+template <typename T, int FMT, int REACH>
 __global__ void __launch_bounds__(WARPS * 32) dequantize_kernel(const unsigned char* __restrict__ packed, u64 rows, u64 cols,
                                                                 u32 col_tiles, u64 tasks, const float* __restrict__ tensor_scale,
-                                                                T* __restrict__ out, u64 stride, bool vec) {
-    const u64 task = (u64)blockIdx.x * WARPS + (threadIdx.x >> 5);
+                                                                T* __restrict__ out, u64 stride) {
+    __shared__ __align__(16) T buffer[REACH == REACH_ANY ? WARPS : 1][REACH == REACH_ANY ? 4 : 1][MX4_COLS];
+    const u32 warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, part = lane & 15;
+    const u64 task = (u64)blockIdx.x * WARPS + warp;
     if (task >= tasks) return;
-    const u32 lane = threadIdx.x & 31;
-    const u32 l = (u32)(task & 31);
-    const u64 tile = task >> 5;
-    const u32 rt = (u32)(tile / col_tiles), ct = (u32)(tile - (u64)rt * col_tiles);
-    const u32 height = mx4_tile_height(rows, rt);
-    const unsigned char* const src = packed + mx4_tile_offset(rows, col_tiles, FMT, rt, ct);
-    const u64 row0 = (u64)rt * MX4_ROWS + l, c0 = (u64)ct * MX4_COLS + lane * 8;
+    const Place at(task, rows, col_tiles, FMT);
+    if (at.row0 >= rows) return;                   // the whole warp
+    const unsigned char* const src = packed + at.offset;
+    const u64 first = (u64)at.ct * MX4_COLS, c0 = first + part * 16;
+    constexpr u32 STEP = (u32)mx4_block(FMT) / 16;
+    const u32 block = part / STEP;
+    uint2 codes[2];
+    u32 byte[2];
+#pragma unroll
+    for (u32 i = 0; i < 2; ++i) {
+        const u32 c = 2 * i + half, r = at.l + 32 * c;
+        const bool there = at.row0 + 32 * c < rows;
+        codes[i] = there ? __ldg(reinterpret_cast<const uint2*>(src + r * 128 + (((part >> 1) ^ (r & 7)) << 4) + ((part & 1) << 3))) : make_uint2(0u, 0u);
+        byte[i] = there ? __ldg(src + at.height * 128 + (block >> 2) * MX4_PIECE + at.l * 16 + c * 4 + (block & 3)) : 0u;
+    }
     float g = 1.f;
     if (FMT == MX4_E4M3_16 && tensor_scale) g = __ldg(tensor_scale);
-    constexpr int PER = mx4_block(FMT) / 8;
-    const u32 block = lane / PER;
-    u32 word[4], byte[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const u32 r = l + 32 * c;
-        const bool there = row0 + 32 * c < rows;
-        word[c] = there ? *reinterpret_cast<const u32*>(src + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + ((lane & 3) << 2)) : 0u;
-        byte[c] = there ? src[height * 128 + (block >> 2) * MX4_PIECE + l * 16 + c * 4 + (block & 3)] : 0u;
-    }
+    for (u32 i = 0; i < 2; ++i) {
+        const u64 row = at.row0 + 32 * (2 * i + half);
+        __half2 q[8];
+        values_of(codes[i].x, reinterpret_cast<__half2 (&)[4]>(q[0]));
+        values_of(codes[i].y, reinterpret_cast<__half2 (&)[4]>(q[4]));
+        float by;                                  // what the fp16 products below are multiplied with
+        if (FMT == MX4_E4M3_16) {                  // code times scale has six significant bits and fits fp16
+            const __half s = __half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte[i], __NV_E4M3));
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        if (row0 + 32 * c >= rows) break;
-        const float s = scale_value<FMT>(byte[c]);
-        float v[8];
+            for (int k = 0; k < 8; ++k) q[k] = __hmul2(q[k], __half2half2(s));
+            by = g;
+        } else {
+            by = byte[i] == 0xffu ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte[i] ? byte[i] << 23 : 0x00400000u);   // 2^(byte - 127), subnormal at 0
+        }
+        Sixteen<T> v;
+        T* h = reinterpret_cast<T*>(&v);
+        const u64 by2 = f2_pack(by, by);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            v[k] = e2m1_value(word[c] >> (4 * k) & 15u) * s;
-            if (FMT == MX4_E4M3_16) v[k] *= g;
+            const float2 f = __half22float2(q[k]);
+            float a, b;
+            f2_unpack(f2_mul(f2_pack(f.x, f.y), by2), a, b);
+            wput(h, 2 * k, a);
+            wput(h, 2 * k + 1, b);
         }
-        T* p = out + (row0 + 32 * c) * stride + c0;
-        if (vec && c0 + 8 <= cols) {
-            store8(p, v);
-        } else {
+        if (REACH == REACH_ANY) *reinterpret_cast<Sixteen<T>*>(&buffer[warp][2 * i + half][part * 16]) = v;
+        else if (row < rows && c0 < cols) store_words<T, REACH>(out + row * stride + c0, cols - c0, v);
+    }
+    if (REACH == REACH_ANY) {
+        __syncwarp();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) if (c0 + k < cols) wput(p, k, v[k]);
+        for (u32 c = 0; c < 4; ++c) {
+            const u64 row = at.row0 + 32 * c;
+            T* p = out + row * stride + first;
+#pragma unroll
+            for (u32 k = 0; k < MX4_COLS / 32; ++k)
+                if (row < rows && first + lane + 32 * k < cols) p[lane + 32 * k] = buffer[warp][c][lane + 32 * k];
         }
     }
 }
 
-// Rows that all start on 16 bytes.
 template <typename T>
-bool rows_aligned(const void* p, u64 rows, u64 stride) {
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || (stride * sizeof(T)) % 16 == 0);
+int reach(const void* p, u64 rows, u64 stride) {
+    const u64 bits = reinterpret_cast<uintptr_t>(p) | (rows <= 1 ? 0 : stride * sizeof(T));
+    return (bits & 31) == 0 ? REACH_32 : (bits & 15) == 0 ? REACH_16 : REACH_ANY;
 }
+#define EXCP_REACH(r, CALL) ((r) == REACH_32 ? CALL(REACH_32) : (r) == REACH_16 ? CALL(REACH_16) : CALL(REACH_ANY))
 
-template <typename T>
+template <typename T, int REACH>
 void tensor_scale_as(int sms, cudaStream_t s, const RowsIn& x, u32* words, float* out) {
-    const u64 groups = x.rows * ((x.cols + 7) / 8);
-    const u64 want = (groups + 255) / 256;
+    const u32 chunks = (u32)((x.cols + 511) / 512);
+    const u64 want = (x.rows * chunks + 7) / 8;
     const u32 grid = (u32)(want < 1 ? 1 : (want > (u64)sms * 8 ? (u64)sms * 8 : want));
-    tensor_scale_kernel<T><<<grid, 256, 0, s>>>(static_cast<const T*>(x.p), x.rows, x.cols, x.stride,
-                                                rows_aligned<T>(x.p, x.rows, x.stride), words, out);
+    tensor_scale_kernel<T, REACH><<<grid, 256, 0, s>>>(static_cast<const T*>(x.p), x.rows, x.cols, x.stride, chunks, words, out);
 }
-
-template <typename T, int FMT>
+template <typename T, int FMT, int REACH>
 void quantize_as(cudaStream_t s, const RowsIn& x, const float* tensor_scale, unsigned char* out) {
     const u32 ct = mx4_col_tiles(x.cols);
     const u64 tasks = (u64)mx4_row_tiles(x.rows) * ct * 32;
-    quantize_kernel<T, FMT><<<(u32)((tasks + WARPS - 1) / WARPS), WARPS * 32, 0, s>>>(
-        static_cast<const T*>(x.p), x.rows, x.cols, x.stride, rows_aligned<T>(x.p, x.rows, x.stride), ct, tasks, tensor_scale, out);
+    quantize_kernel<T, FMT, REACH><<<(u32)((tasks + WARPS - 1) / WARPS), WARPS * 32, 0, s>>>(static_cast<const T*>(x.p), x.rows, x.cols, x.stride,
+                                                                                            ct, tasks, tensor_scale, out);
 }
-template <typename T, int FMT>
+template <typename T, int FMT, int REACH>
 void dequantize_as(cudaStream_t s, const unsigned char* packed, u64 rows, u64 cols, const float* tensor_scale, void* out, u64 stride) {
     const u32 ct = mx4_col_tiles(cols);
     const u64 tasks = (u64)mx4_row_tiles(rows) * ct * 32;
-    dequantize_kernel<T, FMT><<<(u32)((tasks + WARPS - 1) / WARPS), WARPS * 32, 0, s>>>(
-        packed, rows, cols, ct, tasks, tensor_scale, static_cast<T*>(out), stride, rows_aligned<T>(out, rows, stride));
+    dequantize_kernel<T, FMT, REACH><<<(u32)((tasks + WARPS - 1) / WARPS), WARPS * 32, 0, s>>>(packed, rows, cols, ct, tasks, tensor_scale,
+                                                                                              static_cast<T*>(out), stride);
 }
 
 }  // namespace
 
 void launch_mx4_tensor_scale(int sms, cudaStream_t s, const RowsIn& x, u32* words, float* scale_out) {
-    if (x.dtype == DT_F32) tensor_scale_as<float>(sms, s, x, words, scale_out);
-    else if (x.dtype == DT_F16) tensor_scale_as<__half>(sms, s, x, words, scale_out);
-    else tensor_scale_as<__nv_bfloat16>(sms, s, x, words, scale_out);
+#define EXCP_S(R) tensor_scale_as<T, R>(sms, s, x, words, scale_out)
+    auto run = [&](auto zero) {
+        typedef decltype(zero) T;
+        EXCP_REACH(reach<T>(x.p, x.rows, x.stride), EXCP_S);
+    };
+    if (x.dtype == DT_F32) run(float());
+    else if (x.dtype == DT_F16) run(__half());
+    else run(__nv_bfloat16());
+#undef EXCP_S
 }
 
 void launch_mx4_quantize(int, cudaStream_t s, const RowsIn& x, int fmt, const float* tensor_scale, unsigned char* out) {
-#define EXCP_Q(T) (fmt == MX4_E4M3_16 ? quantize_as<T, MX4_E4M3_16>(s, x, tensor_scale, out) : quantize_as<T, MX4_E8M0_32>(s, x, tensor_scale, out))
-    if (x.dtype == DT_F32) EXCP_Q(float);
-    else if (x.dtype == DT_F16) EXCP_Q(__half);
-    else EXCP_Q(__nv_bfloat16);
-#undef EXCP_Q
+#define EXCP_Q4(R) quantize_as<T, MX4_E4M3_16, R>(s, x, tensor_scale, out)
+#define EXCP_Q8(R) quantize_as<T, MX4_E8M0_32, R>(s, x, tensor_scale, out)
+    auto run = [&](auto zero) {
+        typedef decltype(zero) T;
+        const int r = reach<T>(x.p, x.rows, x.stride);
+        if (fmt == MX4_E4M3_16) EXCP_REACH(r, EXCP_Q4);
+        else EXCP_REACH(r, EXCP_Q8);
+    };
+    if (x.dtype == DT_F32) run(float());
+    else if (x.dtype == DT_F16) run(__half());
+    else run(__nv_bfloat16());
+#undef EXCP_Q4
+#undef EXCP_Q8
 }
 
 void launch_mx4_dequantize(int, cudaStream_t s, const unsigned char* packed, u64 rows, u64 cols, int fmt,
                            const float* tensor_scale, void* out, int dtype, u64 stride) {
-#define EXCP_D(T) (fmt == MX4_E4M3_16 ? dequantize_as<T, MX4_E4M3_16>(s, packed, rows, cols, tensor_scale, out, stride) \
-                                      : dequantize_as<T, MX4_E8M0_32>(s, packed, rows, cols, tensor_scale, out, stride))
-    if (dtype == DT_F32) EXCP_D(float);
-    else if (dtype == DT_F16) EXCP_D(__half);
-    else EXCP_D(__nv_bfloat16);
-#undef EXCP_D
+#define EXCP_D4(R) dequantize_as<T, MX4_E4M3_16, R>(s, packed, rows, cols, tensor_scale, out, stride)
+#define EXCP_D8(R) dequantize_as<T, MX4_E8M0_32, R>(s, packed, rows, cols, tensor_scale, out, stride)
+    auto run = [&](auto zero) {
+        typedef decltype(zero) T;
+        const int r = reach<T>(out, rows, stride);
+        if (fmt == MX4_E4M3_16) EXCP_REACH(r, EXCP_D4);
+        else EXCP_REACH(r, EXCP_D8);
+    };
+    if (dtype == DT_F32) run(float());
+    else if (dtype == DT_F16) run(__half());
+    else run(__nv_bfloat16());
+#undef EXCP_D4
+#undef EXCP_D8
 }
 
 }  // namespace excp

@@ -9,7 +9,7 @@ namespace excp {
 constexpr u32 NONFINITE_BITS = 0x7f800000u;        // magnitudes at or above: infinity and NaN
 
 // Eight values as eight 4-bit floats (nearest, ties to even, at most 6), the first in the low bits.
-__device__ __forceinline__ u32 e2m1x8(const float t[8]) {
+__device__ __forceinline__ u32 e2m1x8(const float* t) {
     u32 w;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
@@ -22,22 +22,31 @@ __device__ __forceinline__ u32 e2m1x8(const float t[8]) {
     return w;
 }
 
-// The block's scale byte, and its values divided by the scale (in place).  `m`: pattern of the block's
-// largest magnitude.
-__device__ __forceinline__ u32 scale_e8m0(float v[8], u32 m) {
+// Two fp32 lanes per instruction.
+__device__ __forceinline__ u64 f2_pack(float a, float b) { u64 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void f2_unpack(u64 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ u64 f2_mul(u64 a, u64 b) { u64 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ u64 f2_fma(u64 a, u64 b, u64 c) { u64 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// The block's scale byte, and N of its values divided by the scale (in place).  `m`: pattern of the block's largest
+// magnitude.
+template <int N>
+__device__ __forceinline__ u32 scale_e8m0(float (&v)[N], u32 m) {
     if (m >= NONFINITE_BITS) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = 0.f;
+        for (int k = 0; k < N; ++k) v[k] = 0.f;
         return 0xffu;
     }
     const int lg = (m >> 23) ? (int)(m >> 23) - 127 : (m ? -118 - __clz(m) : -1000);   // floor(log2): bit b of a subnormal is 2^(b - 149)
     const int e = max(lg - 2, -127);
     const float inv = __uint_as_float((u32)(127 - e) << 23);                            // 2^-e: exact, -e in [-125, 127]
+    const u64 inv2 = f2_pack(inv, inv);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= inv;
+    for (int k = 0; k < N; k += 2) f2_unpack(f2_mul(f2_pack(v[k], v[k + 1]), inv2), v[k], v[k + 1]);
     return (u32)(e + 127);
 }
-__device__ __forceinline__ u32 scale_e4m3(float v[8], u32 m, float g, float six_g) {
+template <int N>
+__device__ __forceinline__ u32 scale_e4m3(float (&v)[N], u32 m, float g, float six_g) {
     u32 byte = 0x7fu;
     float sg = 0.f;
     if (m < NONFINITE_BITS) {
@@ -46,17 +55,18 @@ __device__ __forceinline__ u32 scale_e4m3(float v[8], u32 m, float g, float six_
         sg = __half2float(__half(__nv_cvt_fp8_to_halfraw(s, __NV_E4M3))) * g;
     }
     if (sg >= 0x1p-80f && sg <= 0x1p80f && __uint_as_float(m) < 0x1p20f * sg) {
-        // The rounded quotient from the rounded reciprocal: one step with the exact remainder (Markstein 1990), three
-        // instructions.  Without it a value halfway between two codes could fall to the wrong side.
+        // The rounded quotient from the rounded reciprocal: one step with the exact remainder (Markstein 1990).  Without it a
+        // value halfway between two codes could fall to the wrong side.
         const float r = __frcp_rn(sg);
+        const u64 r2 = f2_pack(r, r), d2 = f2_pack(-sg, -sg);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float q = v[k] * r;
-            v[k] = fmaf(fmaf(-q, sg, v[k]), r, q);
+        for (int k = 0; k < N; k += 2) {
+            const u64 x = f2_pack(v[k], v[k + 1]), q = f2_mul(x, r2);
+            f2_unpack(f2_fma(f2_fma(q, d2, x), r2, q), v[k], v[k + 1]);
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = sg > 0.f ? __fdiv_rn(v[k], sg) : 0.f;
+        for (int k = 0; k < N; ++k) v[k] = sg > 0.f ? __fdiv_rn(v[k], sg) : 0.f;
     }
     return byte;
 }

@@ -72,7 +72,7 @@ __device__ __forceinline__ void load_part(const NarrowArgs& g, u64 row, u32 ct, 
 
 // One plain row of a column tile -> its codes, and its scales as one word per piece, `rows` words apart.
 template <int FMT>
-__device__ __forceinline__ void quantize_row(float v[8], u32 r, u32 lane, float gx, unsigned char* codes, u32* scales, u32 rows) {
+__device__ __forceinline__ void quantize_row(float (&v)[8], u32 r, u32 lane, float gx, unsigned char* codes, u32* scales, u32 rows) {
     u32 top = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
