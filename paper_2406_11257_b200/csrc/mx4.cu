@@ -163,14 +163,27 @@ __global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const T* __restric
 
     Sixteen<T> v[2];
     if (REACH == REACH_ANY) {
+        constexpr u32 PER = MX4_COLS / 32;
+        T t[4][PER];                               // everything on its way before anything is stored
 #pragma unroll
         for (u32 c = 0; c < 4; ++c) {
             const u64 row = at.row0 + 32 * c;
-            const T* p = x + row * stride + first;
+            const T* p = x + row * stride + first + lane;
+            const u32 n = row < rows ? (u32)min(cols - first, (u64)MX4_COLS) : 0u;
 #pragma unroll
-            for (u32 k = 0; k < MX4_COLS / 32; ++k)
-                wput(buffer[warp][c], lane + 32 * k, row < rows && first + lane + 32 * k < cols ? wget(p, lane + 32 * k) : 0.f);
+            for (u32 k = 0; k < PER; ++k) t[c][k] = T(0.f);
+            if (n == MX4_COLS) {
+#pragma unroll
+                for (u32 k = 0; k < PER; ++k) t[c][k] = __ldg(p + 32 * k);
+            } else {
+#pragma unroll
+                for (u32 k = 0; k < PER; ++k) if (lane + 32 * k < n) t[c][k] = p[32 * k];
+            }
         }
+#pragma unroll
+        for (u32 c = 0; c < 4; ++c)
+#pragma unroll
+            for (u32 k = 0; k < PER; ++k) buffer[warp][c][lane + 32 * k] = t[c][k];
         __syncwarp();
 #pragma unroll
         for (u32 i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const Sixteen<T>*>(&buffer[warp][2 * i + half][part * 16]);
@@ -283,10 +296,10 @@ __global__ void __launch_bounds__(WARPS * 32) dequantize_kernel(const unsigned c
 #pragma unroll
         for (u32 c = 0; c < 4; ++c) {
             const u64 row = at.row0 + 32 * c;
-            T* p = out + row * stride + first;
+            T* p = out + row * stride + first + lane;
+            const u32 n = row < rows ? (u32)min(cols - first, (u64)MX4_COLS) : 0u;
 #pragma unroll
-            for (u32 k = 0; k < MX4_COLS / 32; ++k)
-                if (row < rows && first + lane + 32 * k < cols) p[lane + 32 * k] = buffer[warp][c][lane + 32 * k];
+            for (u32 k = 0; k < MX4_COLS / 32; ++k) if (lane + 32 * k < n) p[32 * k] = buffer[warp][c][lane + 32 * k];
         }
     }
 }

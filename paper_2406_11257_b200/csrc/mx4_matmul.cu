@@ -369,13 +369,16 @@ bool launch_typed(cudaStream_t s, const NarrowArgs& g, u32 parts, u32 smem, int 
 }
 
 u32 split(int sms, u64 m_tiles, u64 n_tiles, u32 nt, u32 col_tiles) {
-    // Two CTAs per SM as long as there are columns to split, and few sums to exchange: 64 rows in two parts 4096 -> 11008 take
-    // 18.7 us, whole 11.4; 8 rows whole 8.3, in three parts 7.6.
-    u64 parts = (u64)sms * 2 / (m_tiles * n_tiles);
-    if (parts > MAX_SPLIT) parts = MAX_SPLIT;
-    if (parts > col_tiles) parts = col_tiles;
-    if (parts > 64 / nt) parts = 64 / nt;
-    return parts < 1 ? 1u : (u32)parts;
+    // Two CTAs per SM as long as there are columns to split, if that pays: a column tile takes a CTA about 0.3 us, exchanging the
+    // parts 1.5 us and 0.06 us per row.  (4096 -> 11008: 8 rows whole 8.3 us, in three parts 7.6; 64 rows whole 9.2, in two
+    // parts 18.7.)
+    u32 best = 1;
+    float least = 0.3f * col_tiles;
+    for (u32 parts = 2; parts <= MAX_SPLIT && parts <= col_tiles && m_tiles * n_tiles * parts <= (u64)sms * 2; ++parts) {
+        const float cost = 0.3f * ((col_tiles + parts - 1) / parts) + 1.5f + 0.06f * nt;
+        if (cost < least) { least = cost; best = parts; }
+    }
+    return best;
 }
 // Shared memory of the quantised rows of a CTA.
 u32 raw_bytes(u32 nt, u32 col_tiles, u32 parts, int fmt) {

@@ -36,8 +36,10 @@ struct WideArgs {
     u32 col_tiles, m_tiles, n_tiles;
     void* y;
     u64 stride;
-    const float* bias;                             // per row of b (the operand on the contiguous side of y)
-    u32 wide_store;                                // rows of y start on 32 bytes
+    const float* bias;                             // per row of b
+    // Usually a is m: a lane has a row of y and writes 32 bytes at a time.  Where rows of y do not start on 32 bytes the operands
+    // change places: a lane has a column, and neighbouring lanes write neighbouring results.
+    u32 turned;
     u64 wait_ns;
     u32* flag;
 };
@@ -72,11 +74,11 @@ __device__ __forceinline__ void store32(void* p, const u32 v[8]) {
 
 // The first `cols` of a row's results, packed in WORDS words.
 template <typename T, u32 WORDS>
-__device__ __forceinline__ void put_row(T* y, const u32 (&w)[WORDS], u32 cols, u32 wide_store) {
+__device__ __forceinline__ void put_row(T* y, const u32 (&w)[WORDS], u32 cols) {
     constexpr u32 PER = 4 / sizeof(T);
 #pragma unroll
     for (u32 i = 0; i < WORDS; i += 8) {
-        if (wide_store && (i + 8) * PER <= cols) {
+        if ((i + 8) * PER <= cols) {
             const u32 v[8] = {w[i], w[i + 1], w[i + 2], w[i + 3], w[i + 4], w[i + 5], w[i + 6], w[i + 7]};
             store32(y + i * PER, v);
         } else {
@@ -137,7 +139,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             Ring<STAGES> ring;
             u32 filled = 0;
             bool ok = true;
-            if (item == 0) wait_for_previous();    // m may have been packed by the launch before this one
+            if ((item == 0) != (g.turned != 0)) wait_for_previous();       // a may have been packed by the launch before this one
             for (u32 t = pair; ok && t < tiles; t += pairs) {
                 u32 mt, nt;
                 place(g, t, mt, nt);
@@ -263,7 +265,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             const u64 m = (u64)(2 * mt + rank) * MX4_ROWS + quarter * 32 + lane;
             const u64 n0 = (u64)nt * SPAN + c0;
             const u32 cols = n0 < g.n.rows ? (u32)min((u64)128, g.n.rows - n0) : 0u;
-            T* y = static_cast<T*>(g.y) + m * g.stride + n0;
             const u32 from = tmem + ((quarter * 32) << 16) + c0;
             u32 v[128];
 #pragma unroll
@@ -274,6 +275,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.acc_empty, 0));
 
             constexpr u32 PART = 32, PER = 4 / sizeof(T);                  // columns at a time; results in a word
+            if (g.turned) {
+                T* const y = static_cast<T*>(g.y) + n0 * g.stride + m;
+                const float bias = g.bias && m < g.m.rows ? __ldg(g.bias + m) : 0.f;
+#pragma unroll
+                for (u32 p = 0; p < 128; p += PART) {
+                    float f[PART];
+#pragma unroll
+                    for (u32 i = 0; i < PART; ++i) f[i] = __uint_as_float(v[p + i]) * alpha;
+                    if (g.bias) {
+#pragma unroll
+                        for (u32 i = 0; i < PART; ++i) f[i] += bias;
+                    }
+                    if (m >= g.m.rows) continue;
+                    if (p + PART <= cols) {
+#pragma unroll
+                        for (u32 i = 0; i < PART; ++i) wput(y + (p + i) * g.stride, 0, f[i]);
+                    } else {
+#pragma unroll
+                        for (u32 i = 0; i < PART; ++i) if (p + i < cols) wput(y + (p + i) * g.stride, 0, f[i]);
+                    }
+                }
+                continue;
+            }
+            T* const y = static_cast<T*>(g.y) + m * g.stride + n0;
 #pragma unroll
             for (u32 p = 0; p < 128; p += PART) {
                 float f[PART];
@@ -289,7 +314,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
                     if constexpr (PER == 2) w[i / 2] = two<DT>(f[i], f[i + 1]);
                     else w[i] = __float_as_uint(f[i]);
                 }
-                if (m < g.m.rows) put_row<T, PART / PER>(y + p, w, cols > p ? cols - p : 0, g.wide_store);
+                if (m < g.m.rows) put_row<T, PART / PER>(y + p, w, cols > p ? cols - p : 0);
             }
         }
     }
@@ -324,16 +349,16 @@ bool launch_as(int sms, cudaStream_t s, const WideArgs& g, bool behind) {
 bool launch_mx4_matmul_wide(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
                             const Mx4Result& r, u64 wait_ns, u32* flag, bool behind) {
     WideArgs g{};
-    g.m = a;
-    g.n = b;
+    const u64 size = r.dtype == DT_F32 ? 4 : 2;
+    g.turned = ((reinterpret_cast<uintptr_t>(r.y) | (r.stride * size)) & 31) != 0;
+    g.m = g.turned ? b : a;
+    g.n = g.turned ? a : b;
     g.col_tiles = mx4_col_tiles(cols);
-    g.m_tiles = (u32)((a.rows + SPAN - 1) / SPAN);
-    g.n_tiles = (u32)((b.rows + SPAN - 1) / SPAN);
+    g.m_tiles = (u32)((g.m.rows + SPAN - 1) / SPAN);
+    g.n_tiles = (u32)((g.n.rows + SPAN - 1) / SPAN);
     g.y = r.y;
     g.stride = r.stride;
     g.bias = r.bias;
-    const u64 size = r.dtype == DT_F32 ? 4 : 2;
-    g.wide_store = ((reinterpret_cast<uintptr_t>(r.y) | (r.stride * size)) & 31) == 0;
     g.wait_ns = wait_ns;
     g.flag = flag;
 #define EXCP_MM(DT) (fmt == MX4_E4M3_16 ? launch_as<MX4_E4M3_16, DT>(sms, s, g, behind) : launch_as<MX4_E8M0_32, DT>(sms, s, g, behind))
