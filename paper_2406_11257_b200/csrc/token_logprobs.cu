@@ -10,11 +10,14 @@
 // itself and is subtracted before anything is multiplied, so that neither a mask of the type's lowest value nor
 // a row of nothing else overflows; a logit of -infinity adds 0.  Sums are fp32.
 //
-// The alternatives need no second pass: of the k largest thread maxima the smallest is a lower bound of the k-th largest
-// logit.  Each thread also notes the maximum of every step, so that only the few steps that reach the bound are read again.
+// The alternatives need no second pass.  With k of them wanted and W warps, each warp finds the ceil(k / W)-th largest of its
+// threads' maxima; the smallest of these is a lower bound of the k-th largest logit.  Each thread also notes the maximum of
+// every step, so that only the few steps that reach the bound are read again, and what reaches it is ranked.
 //
-// Bound: the row's bytes.  A block takes a row; where there are too few rows to fill the card, a cluster of blocks
-// takes one and joins its sums and alternatives through distributed shared memory.
+// Bound: the row's bytes, and close behind them the exponentials (16 per SM and cycle).  A block takes a row; where there
+// are too few rows to fill the card, a cluster of blocks takes one and joins its sums and alternatives through distributed
+// shared memory.  (Persistent blocks with a ring of chunks that bulk copies keep filled were slower, 4096 x 32000 bf16 58 us
+// against 51: what they hide is not what is missing.)
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -29,8 +32,8 @@ namespace {
 constexpr int GRAD_BLOCK = 256;
 constexpr int UNROLL = 4;                          // 16-byte loads in flight per thread
 constexpr int TOP_MAX = 64;
-constexpr int SLOTS = 16, OWNERS = 512;
-constexpr int LIST = 1024;                         // candidates (or 8 blocks' alternatives) that are ranked at once
+constexpr int SLOTS = 16, OWNERS = 512;            // step maxima kept per thread; of them that are read again
+constexpr int LIST = 512;                          // candidates (or 8 blocks' alternatives) that are ranked at once
 constexpr float NEG_INF = -__builtin_huge_valf();
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float FAR = -200.f;                      // 2^FAR is 0 in fp32
@@ -154,60 +157,42 @@ __device__ __forceinline__ Share<T> share_of(const T* x, u32 vocab, u32 part, u3
 
 template <int BLOCK>
 struct Joint {                                     // shared memory of a block
-    float m[BLOCK / 32], s[BLOCK / 32], t[BLOCK / 32];
-    Sums sums;                                     // the block's
-    alignas(16) unsigned short max_key[BLOCK];     // upper half of the keys of the thread maxima
-    unsigned short step_key[SLOTS][BLOCK];         // the same of every slot (one or more steps) of every thread
-    unsigned short owner[OWNERS];                  // slot << 8 | thread of the slots that hold candidates
-    u32 bound, owners, count;
-    u64 list[LIST];
+    alignas(16) u64 list[LIST];
     u64 best[TOP_MAX];                             // the block's alternatives, descending; 0 = none
     u64 warp_best[BLOCK / 32];
+    float m[BLOCK / 32], s[BLOCK / 32], t[BLOCK / 32];
+    u32 warp_bound[BLOCK / 32];
+    Sums sums;                                     // the block's
+    u32 owners[2], count[2];                       // of this row and, being reset, of the next
+    unsigned short step_key[SLOTS][BLOCK];         // upper half of the key of every slot's (one or more steps') maximum
+    unsigned short owner[OWNERS];                  // slot << 8 | thread of the slots that hold candidates
 };
 
-// Warp 0: a lower bound of the k-th largest logit of the share, as the upper 16 bits of its key (one bfloat16 step): the
-// k-th largest of the thread maxima, found bit by bit.  0 where fewer than k threads have a maximum.
+// Rank of `mine` among list[0..n) (distinct keys).
 template <int BLOCK>
-__device__ __forceinline__ u32 find_bound(const Joint<BLOCK>& j, u32 k) {
-    constexpr int PAIRS = BLOCK / 64;
-    u32 pair[PAIRS];
+__device__ __forceinline__ u32 rank_of(const Joint<BLOCK>& j, u64 mine, u32 n) {
+    u32 rank = 0;
+    u32 o = 0;
+    for (; o + 8 <= n; o += 8) {
 #pragma unroll
-    for (int i = 0; i < PAIRS; ++i) pair[i] = reinterpret_cast<const u32*>(j.max_key)[threadIdx.x + 32 * i];
-    u32 low = 0;
-#pragma unroll
-    for (int bit = 15; bit >= 0; --bit) {
-        const u32 test = low | (1u << bit);
-        u32 n = 0;
-#pragma unroll
-        for (int i = 0; i < PAIRS; ++i) n += ((pair[i] & 0xffffu) >= test) + ((pair[i] >> 16) >= test);
-        if (__reduce_add_sync(0xffffffffu, n) >= k) low = test;
+        for (u32 i = 0; i < 8; i += 2) {
+            const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(j.list + o + i);
+            rank += (two.x > mine) + (two.y > mine);
+        }
     }
-    return low;
+    for (; o < n; ++o) rank += j.list[o] > mine;
+    return rank;
 }
 
-// Writes the k largest of list[0..n) (distinct keys) to best[0..k), descending; 0 where there are fewer.
-template <int BLOCK>
-__device__ __forceinline__ void rank_list(Joint<BLOCK>& j, u32 n, u32 k) {
-    for (u32 i = threadIdx.x; i < k; i += BLOCK) j.best[i] = 0;
-    __syncthreads();
-    for (u32 i = threadIdx.x; i < n; i += BLOCK) {
-        const u64 mine = j.list[i];
-        u32 rank = 0;
-        for (u32 o = 0; o < n; ++o) rank += j.list[o] > mine;
-        if (rank < k && mine) j.best[rank] = mine;
-    }
-    __syncthreads();
-}
-
-// The k largest of the share, one after another: where candidates outnumber the list (a row of equal logits), or a NaN
+// The k largest of the share to best[], one after another: where candidates outnumber the list (a row of equal logits), or a NaN
 // keeps the thread maxima from saying anything.
 template <typename T, int BLOCK>
-__device__ void top_by_rounds(Joint<BLOCK>& j, const Share<T>& w, u32 k) {
+__device__ __noinline__ void top_by_rounds(Joint<BLOCK>& j, const T* x, u32 lo, u32 hi, u32 k) {
     u64 last = ~0ull;
     for (u32 r = 0; r < k; ++r) {
         u64 mine = 0;
-        for (u32 i = w.lo + threadIdx.x; i < w.hi; i += BLOCK) {
-            const u64 key = order_key(wget(w.x, i), i);
+        for (u32 i = lo + threadIdx.x; i < hi; i += BLOCK) {
+            const u64 key = order_key(wget(x, i), i);
             if (key < last && key > mine) mine = key;
         }
 #pragma unroll
@@ -225,125 +210,130 @@ __device__ void top_by_rounds(Joint<BLOCK>& j, const Share<T>& w, u32 k) {
     __syncthreads();
 }
 
-template <typename T, int BLOCK, bool CLUSTER>
-__global__ void __launch_bounds__(BLOCK) logprobs_kernel(const T* __restrict__ logits, u32 vocab, u64 stride,
-                                                         const long long* __restrict__ tokens, float scale, LogprobsOut out) {
-    __shared__ Joint<BLOCK> j;
-    constexpr u32 N = per16<T>();
-    const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    u32 part = 0, parts = 1;
-    if constexpr (CLUSTER) { part = cg::this_cluster().block_rank(); parts = cg::this_cluster().num_blocks(); }
-    const u64 row = blockIdx.x / parts;
-    const Share<T> w = share_of(logits + row * stride, vocab, part, parts);
-    const float c = scale * LOG2E;
-    long long token = -1;                          // the last thread writes the row's results
-    float at_token = __uint_as_float(0x7fffffffu);
-    if (part == 0 && tid == BLOCK - 1) {
-        token = tokens[row];
-        if (token >= 0 && token < (long long)vocab) at_token = wget(logits + row * stride, (u64)token);
-    }
-
-    // The body in UNROLL equal stretches; a step of the block takes BLOCK 16-byte words of each.
-    const uint4* const body = reinterpret_cast<const uint4*>(w.x + w.body);
-    const u32 stretch = (w.nvec + UNROLL - 1) / UNROLL;
-    auto fetch = [&](uint4 (&q)[UNROLL][1], u32 p) {
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) if (p < stretch && u * stretch + p < w.nvec) q[u][0] = __ldg(body + u * stretch + p);
-    };
-    uint4 q[UNROLL][1];
-    fetch(q, tid);
-    // what lies before the first 16-byte word and behind the last
-    const u32 tail = w.body + w.nvec * N;
-    const bool has_head = w.lo + tid < w.body, has_tail = tail + tid < w.hi, any = has_head || has_tail || tid < stretch;
-    const float head[1] = {has_head ? wget(w.x, w.lo + tid) : NEG_INF}, behind[1] = {has_tail ? wget(w.x, tail + tid) : NEG_INF};
-    const u32 k = (u32)out.top;
-    const u32 steps = (stretch + BLOCK - 1) / BLOCK, per_slot = (steps + SLOTS - 1) / SLOTS;
-    if (tid == 0) j.owners = j.count = 0;
-
+// What a thread holds of its share while it walks through it: a step of the block is U * BLOCK words, of which word
+// u * BLOCK + thread is the thread's.
+template <typename T, int BLOCK, int U>
+struct Walk {
+    static constexpr u32 N = (u32)per16<T>(), STEP = U * BLOCK;
+    Share<T> w;
     Sums a{NEG_INF, 0.f, 0.f};
-    if (has_head) add_many(a, head, head[0], c);
-    if (has_tail) add_many(a, behind, behind[0], c);
-    u32 slot = 0, left = per_slot;                 // steps that the slot still takes
-    float slot_top = NEG_INF;
-    for (u32 p = tid; p < stretch; p += BLOCK) {
-        uint4 next[UNROLL][1];
-        fetch(next, p + BLOCK);
-        float top;
-        if ((UNROLL - 1) * stretch + p < w.nvec) {
-            float v[UNROLL * N];
+    float head, behind;                            // what lies before the first word and behind the last
+    bool has_head, has_tail;
+    u32 steps, per_slot, slot, left;
+    float slot_top;
+
+    __device__ __forceinline__ void start(const Share<T>& share, float c) {
+        w = share;
+        const u32 tid = threadIdx.x, tail = w.body + w.nvec * N;
+        a = Sums{NEG_INF, 0.f, 0.f};
+        has_head = w.lo + tid < w.body;
+        has_tail = tail + tid < w.hi;
+        head = has_head ? wget(w.x, w.lo + tid) : NEG_INF;
+        behind = has_tail ? wget(w.x, tail + tid) : NEG_INF;
+        steps = (w.nvec + STEP - 1) / STEP;
+        per_slot = (steps + SLOTS - 1) / SLOTS;
+        slot = 0;
+        left = per_slot;
+        slot_top = NEG_INF;
+    }
+    __device__ __forceinline__ u32 words(u32 step) const {       // the thread's words of a step
+        const u32 first = step * STEP + threadIdx.x;
+        return first >= w.nvec ? 0 : min((u32)U, (w.nvec - first + BLOCK - 1) / BLOCK);
+    }
+    __device__ __forceinline__ void take(const uint4 (&q)[U], u32 n, float c, bool keys, Joint<BLOCK>& j) {
+        float top = NEG_INF;
+        if (n == U) {
+            float v[U * N];
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) unpack<T>(q[u][0], v + u * N);
-            top = largest_of(reinterpret_cast<const uint4 (&)[UNROLL]>(q), v, T());
+            for (int u = 0; u < U; ++u) unpack<T>(q[u], v + u * N);
+            top = largest_of(q, v, T());
             add_many(a, v, top, c);
         } else {
-            top = NEG_INF;
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                if (u * stretch + p >= w.nvec) break;
+            for (u32 u = 0; u < U; ++u) {
+                if (u >= n) break;
+                const uint4 one[1] = {q[u]};
                 float v[N];
-                unpack<T>(q[u][0], v);
-                const float t = largest_of(q[u], v, T());
+                unpack<T>(q[u], v);
+                const float t = largest_of(one, v, T());
                 add_many(a, v, t, c);
                 top = fmaxf(top, t);
             }
         }
-        if (k) {
+        if (keys) {
             slot_top = fmaxf(slot_top, top);
-            j.step_key[slot][tid] = (unsigned short)(value_key(slot_top) >> 16);
+            j.step_key[slot][threadIdx.x] = (unsigned short)(value_key(slot_top) >> 16);
             if (--left == 0) { ++slot; left = per_slot; slot_top = NEG_INF; }
         }
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) q[u][0] = next[u][0];
     }
-    if (k) j.max_key[tid] = (unsigned short)(any ? value_key(a.m) >> 16 : 0u);
 
-    // join the threads: the maximum first, then sums relative to it
-    float m = a.m;
+    // Joins the block: a becomes its sums, and with k > 0 its alternatives are either in list[0..count), to be ranked, or (true)
+    // in best[].  `turn`: which of the counters.
+    __device__ __forceinline__ bool join(Joint<BLOCK>& j, u32 k, float c, u32 turn, u32& count) {
+        constexpr u32 WARPS = BLOCK / 32;
+        const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+        if (has_head) { const float v[1] = {head}; add_many(a, v, head, c); }
+        if (has_tail) { const float v[1] = {behind}; add_many(a, v, behind, c); }
+        float m = a.m;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane == 0) j.m[warp] = m;
-    __syncthreads();
+        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (lane == 0) j.m[warp] = m;
+        // warps whose threads all have a word (the first ones)
+        const u32 full = min(w.nvec, (u32)BLOCK) / 32, nth = full ? (k + full - 1) / full : 33;
+        if (k && warp < full) {
+            u32 key = value_key(a.m) >> 16, low = 0;
+            for (u32 r = 0; r < nth && nth <= 32; ++r) {
+                low = __reduce_max_sync(0xffffffffu, key);
+                const u32 holds = __ballot_sync(0xffffffffu, key == low);
+                if (lane == __ffs(holds) - 1) key = 0;
+            }
+            if (lane == 0) j.warp_bound[warp] = low;
+        }
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < BLOCK / 32; ++i) m = fmaxf(m, j.m[i]);
-    if (k && warp == 0) {
-        const u32 low = find_bound(j, k);
-        if (lane == 0) j.bound = low;
-    }
-    if (m != NEG_INF) move_to(a, m, c);
+        for (u32 i = 0; i < WARPS; ++i) m = fmaxf(m, j.m[i]);
+        if (m != NEG_INF) move_to(a, m, c);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
-        a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
-    }
-    if (lane == 0) { j.s[warp] = a.s; j.t[warp] = a.t; }
-    __syncthreads();
-    a.s = a.t = 0.f;
-#pragma unroll
-    for (int i = 0; i < BLOCK / 32; ++i) { a.s += j.s[i]; a.t += j.t[i]; }
-    a.m = m;
-
-    if (k) {
-        // the slots that reach the bound are read again, all their words at once, and their logits that reach it are ranked
-        const u32 bound = j.bound;
+        for (int o = 16; o; o >>= 1) {
+            a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+            a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
+        }
+        if (lane == 0) { j.s[warp] = a.s; j.t[warp] = a.t; }
+        u32 bound = 0;                             // 0: everything is a candidate
         auto push = [&](float v, u32 i) {
             const u64 key = order_key(v, i);
             if ((u32)(key >> 48) < bound) return;
-            const u32 at = atomicAdd(&j.count, 1u);
+            const u32 at = atomicAdd(&j.count[turn], 1u);
             if (at < LIST) j.list[at] = key;
         };
-        for (u32 o = 0; tid + o * per_slot * BLOCK < stretch; ++o) {
-            if (j.step_key[o][tid] < bound) continue;
-            const u32 at = atomicAdd(&j.owners, 1u);
-            if (at < OWNERS) j.owner[at] = (unsigned short)(o << 8 | tid);
+        const u32 tail = w.body + w.nvec * N;
+        if (k) {
+            if (nth <= 32) {
+                bound = 0xffffu;
+                for (u32 i = 0; i < full; ++i) bound = min(bound, j.warp_bound[i]);
+            }
+            if (tid == 0) j.owners[turn ^ 1] = j.count[turn ^ 1] = 0;
+            for (u32 o = 0; (u64)o * per_slot * STEP + tid < w.nvec; ++o) {
+                if (j.step_key[o][tid] < bound) continue;
+                const u32 at = atomicAdd(&j.owners[turn], 1u);
+                if (at < OWNERS) j.owner[at] = (unsigned short)(o << 8 | tid);
+            }
+            if (has_head) push(head, w.lo + tid);
+            if (has_tail) push(behind, tail + tid);
         }
-        if (has_head) push(head[0], w.lo + tid);
-        if (has_tail) push(behind[0], tail + tid);
         __syncthreads();
-        const u32 words = per_slot * UNROLL, total = min(j.owners, (u32)OWNERS) * words;
+        a.s = a.t = 0.f;
+#pragma unroll
+        for (u32 i = 0; i < WARPS; ++i) { a.s += j.s[i]; a.t += j.t[i]; }
+        a.m = m;
+        if (!k) return false;
+        // the slots that reach the bound are read again, all their words at once
+        const uint4* body = reinterpret_cast<const uint4*>(w.x + w.body);
+        const u32 owners = j.owners[turn], per = per_slot * U, total = min(owners, (u32)OWNERS) * per;
         for (u32 it = tid; it < total; it += BLOCK) {
-            const u32 o = it / words, r = it - o * words, who = j.owner[o];
-            const u32 p = (who & 255u) + ((who >> 8) * per_slot + r / UNROLL) * BLOCK, i = r % UNROLL * stretch + p;
-            if (p >= stretch || i >= w.nvec) continue;
+            const u32 o = it / per, r = it - o * per, who = j.owner[o];
+            const u32 i = ((who >> 8) * per_slot * U + r) * BLOCK + (who & 255u);
+            if (i >= w.nvec) continue;
             const uint4 again = __ldg(body + i);
             float v[N];
             unpack<T>(again, v);
@@ -351,11 +341,85 @@ __global__ void __launch_bounds__(BLOCK) logprobs_kernel(const T* __restrict__ l
             for (u32 e = 0; e < N; ++e) push(v[e], w.body + i * N + e);
         }
         __syncthreads();
-        if (a.s != a.s || j.owners > OWNERS || j.count > LIST) top_by_rounds(j, w, k);
-        else rank_list(j, j.count, k);
+        count = j.count[turn];
+        if (a.s == a.s && owners <= OWNERS && count <= LIST) return false;
+        top_by_rounds<T, BLOCK>(j, w.x, w.lo, w.hi, k);
+        return true;
     }
+};
+
+// The results of a row from its sums.
+struct Row {
+    float m, log_s, scale;
+    bool empty;
+    __device__ __forceinline__ Row(const Sums& a, float scale_) : m(a.m), log_s(logf(a.s)), scale(scale_), empty(a.m == NEG_INF && a.s == 0.f) {}
+    __device__ __forceinline__ float log_p(float v) const { return empty && v == v ? NEG_INF : fmaf(v - m, scale, -log_s); }
+    __device__ __forceinline__ void put(const LogprobsOut& out, u64 row, const Sums& a, long long token, float at_token) const {
+        const float h = empty ? 0.f : fmaf(-LN2, a.t / a.s, log_s);
+        out.logprob[row] = token < 0 ? 0.f : log_p(at_token);      // NaN for a token past the vocabulary
+        if (out.entropy) out.entropy[row] = h;
+        if (out.row_stats) reinterpret_cast<float4*>(out.row_stats)[row] = make_float4(a.m, a.s, h, 0.f);
+    }
+    __device__ __forceinline__ void put_top(const LogprobsOut& out, u64 row, u32 place, u64 key) const {
+        out.top_index[row * out.top + place] = 0xffffffffu - (u32)key;
+        out.top_logprob[row * out.top + place] = log_p(key_value((u32)(key >> 32)));
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ float token_logit(const T* x, long long token, u32 vocab) {
+    return token >= 0 && token < (long long)vocab ? wget(x, (u64)token) : __uint_as_float(0x7fffffffu);
+}
+
+template <typename T, int BLOCK, bool CLUSTER>
+__global__ void __launch_bounds__(BLOCK) logprobs_kernel(const T* __restrict__ logits, u32 vocab, u64 stride, const long long* __restrict__ tokens,
+                                                      float scale, LogprobsOut out) {
+    constexpr int U = 4;
+    __shared__ Joint<BLOCK> j;
+    u32 part = 0, parts = 1;
+    if constexpr (CLUSTER) { part = cg::this_cluster().block_rank(); parts = cg::this_cluster().num_blocks(); }
+    const u32 tid = threadIdx.x;
+    const u64 row = blockIdx.x / parts;
+    const float c = scale * LOG2E;
+    const T* x = logits + row * stride;
+    const u32 k = (u32)out.top;
+    long long token = -1;                          // the last thread writes the row's results
+    float at_token = 0.f;
+    if (part == 0 && tid == BLOCK - 1) {
+        token = tokens[row];
+        at_token = token_logit(x, token, vocab);
+    }
+    if (tid == 0) j.owners[0] = j.count[0] = 0;
+    if (tid < k) j.best[tid] = 0;
+    Walk<T, BLOCK, U> walk;
+    walk.start(share_of(x, vocab, part, parts), c);
+    const uint4* const body = reinterpret_cast<const uint4*>(walk.w.x + walk.w.body);
+    uint4 q[U];
+    auto fetch = [&](uint4 (&to)[U], u32 step) {
+#pragma unroll
+        for (u32 u = 0; u < U; ++u) if (step * walk.STEP + u * BLOCK + tid < walk.w.nvec) to[u] = __ldg(body + step * walk.STEP + u * BLOCK + tid);
+    };
+    fetch(q, 0);
+    for (u32 step = 0; step < walk.steps; ++step) {
+        uint4 next[U];
+        fetch(next, step + 1);
+        const u32 n = walk.words(step);
+        if (n) walk.take(q, n, c, k != 0, j);
+#pragma unroll
+        for (int u = 0; u < U; ++u) q[u] = next[u];
+    }
+    u32 count = 0;
+    bool listed = !walk.join(j, k, c, 0, count);
+    Sums a = walk.a;
     if constexpr (CLUSTER) {
         cg::cluster_group cluster = cg::this_cluster();
+        if (k && listed) {                         // the block's own alternatives in order
+            for (u32 i = tid; i < count; i += BLOCK) {
+                const u64 mine = j.list[i];
+                const u32 rank = rank_of(j, mine, count);
+                if (rank < k) j.best[rank] = mine;
+            }
+        }
         if (tid == 0) j.sums = a;
         cluster.sync();
         if (part == 0) {
@@ -368,28 +432,23 @@ __global__ void __launch_bounds__(BLOCK) logprobs_kernel(const T* __restrict__ l
                 all.t += b.t;
             }
             a = all;
-            if (k) {
-                for (u32 i = tid; i < parts * k; i += BLOCK) j.list[i] = cluster.map_shared_rank(&j, i / k)->best[i % k];
-            }
+            for (u32 i = tid; i < parts * k; i += BLOCK) j.list[i] = cluster.map_shared_rank(&j, i / k)->best[i % k];
         }
         cluster.sync();                            // the others' shared memory has been read
         if (part != 0) return;
-        if (k) rank_list(j, parts * k, k);
+        count = parts * k;
+        listed = true;
     }
-
-    const float log_s = logf(a.s);
-    const bool empty = a.m == NEG_INF && a.s == 0.f;
-    auto log_p = [&](float v) { return empty && v == v ? NEG_INF : fmaf(v - a.m, scale, -log_s); };
-    if (tid == BLOCK - 1) {
-        const float h = empty ? 0.f : fmaf(-LN2, a.t / a.s, log_s);
-        out.logprob[row] = token < 0 ? 0.f : log_p(at_token);      // NaN for a token past the vocabulary
-        if (out.entropy) out.entropy[row] = h;
-        if (out.row_stats) reinterpret_cast<float4*>(out.row_stats)[row] = make_float4(a.m, a.s, h, 0.f);
-    }
-    for (u32 i = tid; i < k; i += BLOCK) {
-        const u64 key = j.best[i];
-        out.top_index[row * k + i] = 0xffffffffu - (u32)key;
-        out.top_logprob[row * k + i] = log_p(key_value((u32)(key >> 32)));
+    const Row r(a, scale);
+    if (tid == BLOCK - 1) r.put(out, row, a, token, at_token);
+    if (listed) {
+        for (u32 i = tid; k && i < count; i += BLOCK) {
+            const u64 mine = j.list[i];
+            const u32 rank = rank_of(j, mine, count);
+            if (rank < k && mine) r.put_top(out, row, rank, mine);
+        }
+    } else if (tid < k) {
+        r.put_top(out, row, tid, j.best[tid]);
     }
 }
 

@@ -462,3 +462,13 @@ def test_refusals_of_the_c_abi(h):
     assert lib.excp_token_logprobs_grad(H, p, 0, 4, 32, 64, tp, 1.0, fp, 0, 0, p, 32, 0) == bad  # in place with another stride
     assert lib.excp_score_status(None, 0) == bad
     assert lib.excp_token_logprobs(H, 0, 0, 0, 64, 64, 0, 1.0, 0, 0, 0, 0, 0, 0, 0) == 0         # no rows: nothing to do
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("kind", ["normal", "ties", "equal", "masked", "rising"])
+def test_logprobs_of_many_rows(h, kind, dtype):
+    # more rows than SMs: the persistent blocks, several rows each, short and odd rows among them
+    for rows, vocab, top in ((1300, 37, 5), (700, 1030, 64), (1100, 129, 20)):
+        for slack, offset in ((0, 0), (1, 1)):
+            x = make_logits(rows, vocab, dtype, 77 + vocab, slack, offset, kind)
+            check_logprobs(h, x, np.arange(rows) * 7 % vocab, 0.9, top, grad=False)
