@@ -6,7 +6,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -68,8 +68,9 @@ at::ScalarType wanted(PyObject* o) {
 }
 
 bool on(const at::Tensor& t, int device) { return t.is_cuda() && t.get_device() == device; }
-at::TensorOptions options(at::ScalarType t, int device) {
-    return at::TensorOptions().dtype(t).device(at::Device(at::kCUDA, (c10::DeviceIndex)device));
+// A new tensor straight from torch's allocator for the device.
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType t, int device) {
+    return at::detail::empty_cuda(sizes, t, at::Device(at::kCUDA, (c10::DeviceIndex)device), std::nullopt);
 }
 void* stream(int device) { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 
@@ -100,7 +101,7 @@ void* packed(const at::Tensor& t, int device, size_t need, const char* what) {
 }
 // `out`, or a new [r, c] tensor where it is None.
 at::Tensor result(PyObject* out, int device, at::ScalarType type, int64_t r, int64_t c) {
-    if (out == Py_None) return at::empty({r, c}, options(type, device));
+    if (out == Py_None) return fresh({r, c}, type, device);
     const at::Tensor& t = tensor(out, "out");
     if (t.dim() != 2 || t.size(0) != r || t.size(1) != c)
         throw Refused("out: expected the shape [" + std::to_string(r) + ", " + std::to_string(c) + "]");
@@ -111,7 +112,7 @@ at::Tensor result(PyObject* out, int device, at::ScalarType type, int64_t r, int
 PyObject* tensor_scale(PyObject* const* a) {
     const int device = (int)integer(a[1]);
     const Rows x = rows(tensor(a[2], "x"), device, "x");
-    const at::Tensor out = a[3] == Py_None ? at::empty({}, options(at::kFloat, device)) : tensor(a[3], "out");
+    const at::Tensor out = a[3] == Py_None ? fresh({}, at::kFloat, device) : tensor(a[3], "out");
     if (out.scalar_type() != at::kFloat || out.numel() != 1 || !on(out, device)) throw Refused("out: expected one float32 value on the handle's device");
     check(api.mx4_tensor_scale(handle(a[0]), x.p, x.dtype, x.rows, x.cols, x.stride, static_cast<float*>(out.data_ptr()), stream(device)), "excp_mx4_tensor_scale");
     return wrap(out);
@@ -122,7 +123,7 @@ PyObject* quantize(PyObject* const* a) {
     const int device = (int)integer(a[1]), format = (int)integer(a[3]);
     const Rows x = rows(tensor(a[2], "x"), device, "x");
     const size_t need = api.mx4_bytes(x.rows, x.cols, format);
-    const at::Tensor out = a[5] == Py_None ? at::empty({(int64_t)need}, options(at::kByte, device)) : tensor(a[5], "out");
+    const at::Tensor out = a[5] == Py_None ? fresh({(int64_t)need}, at::kByte, device) : tensor(a[5], "out");
     check(api.mx4_quantize(handle(a[0]), x.p, x.dtype, x.rows, x.cols, x.stride, format,
                            static_cast<float*>(vector(a[4], device, at::kFloat, 1, "tensor_scale")), packed(out, device, need, "out"), stream(device)), "excp_mx4_quantize");
     return wrap(out);
@@ -168,7 +169,7 @@ PyObject* linear(PyObject* const* a) {
     at::Tensor room;                               // torch's allocator hands it out again only behind this call's work
     void* px = nullptr;
     if (a[12] != Py_None) px = packed(tensor(a[12], "x_packed"), device, need, "x_packed");
-    else if (need) px = (room = at::empty({(int64_t)need}, options(at::kByte, device))).data_ptr();
+    else if (need) px = (room = fresh({(int64_t)need}, at::kByte, device)).data_ptr();
     check(api.mx4_linear(h, x.p, x.dtype, x.rows, x.stride, static_cast<float*>(vector(a[3], device, at::kFloat, 1, "tensor_scale")), w, wr,
                          static_cast<float*>(vector(a[6], device, at::kFloat, 1, "w.scale")), c, format,
                          static_cast<float*>(vector(a[9], device, at::kFloat, wr, "bias")), y.p, y.dtype, y.stride, px, stream(device)), "excp_mx4_linear");
@@ -184,12 +185,11 @@ PyObject* logprobs(PyObject* const* a) {
     if (scale == -1.0 && PyErr_Occurred()) throw PythonError{};
     const int64_t r = (int64_t)x.rows;
     const long long* tokens = static_cast<long long*>(vector(a[3], device, at::kLong, r, "tokens"));
-    const at::TensorOptions f32 = options(at::kFloat, device);
-    const at::Tensor lp = at::empty({r}, f32), h = at::empty({r}, f32), stats = at::empty({r, 4}, f32);
+    const at::Tensor lp = fresh({r}, at::kFloat, device), h = fresh({r}, at::kFloat, device), stats = fresh({r, 4}, at::kFloat, device);
     at::Tensor tl, ti;
     if (top > 0 && top <= (1 << 20)) {
-        tl = at::empty({r, top}, f32);
-        ti = at::empty({r, top}, options(at::kLong, device));
+        tl = fresh({r, top}, at::kFloat, device);
+        ti = fresh({r, top}, at::kLong, device);
     }
     check(api.token_logprobs(handle(a[0]), x.p, x.dtype, x.rows, x.cols, x.stride, tokens, (float)scale, (int)top, static_cast<float*>(lp.data_ptr()),
                              static_cast<float*>(h.data_ptr()), static_cast<float*>(stats.data_ptr()), tl.defined() ? static_cast<float*>(tl.data_ptr()) : nullptr,
