@@ -134,15 +134,15 @@ __global__ void __launch_bounds__(256) tensor_scale_kernel(const T* __restrict__
     scale_out[0] = q > 0.f ? __uint_as_float((__float_as_uint(q) + 0xffffu) & 0xffff0000u) : 1.f;
 }
 
-// Where a warp works: tile (rt, ct), rows l + 32 c.
+// Where a warp works: tile (rt, ct), rows l + 32 c.  A tile is four blocks of eight warps.  (Four values of l to a warp, and
+// the addresses worked out once for them, were slower: 11008 x 4096 bf16 30 us against 26, too few warps.)
 struct Place {
-    u32 rt, ct, l, height;
+    u32 ct, l, height;
     u64 offset, row0;
-    __device__ __forceinline__ Place(u64 task, u64 rows, u32 col_tiles, int fmt) {
-        l = (u32)(task & 31);
-        const u64 tile = task >> 5;
-        rt = (u32)(tile / col_tiles);
-        ct = (u32)(tile - (u64)rt * col_tiles);
+    __device__ __forceinline__ Place(u64 rows, u32 col_tiles, int fmt) {
+        const u32 tile = blockIdx.x >> 2, rt = tile / col_tiles;
+        l = (blockIdx.x & 3) * WARPS + (threadIdx.x >> 5);
+        ct = tile - rt * col_tiles;
         height = mx4_tile_height(rows, rt);
         offset = mx4_tile_offset(rows, col_tiles, fmt, rt, ct);
         row0 = (u64)rt * MX4_ROWS + l;
@@ -151,13 +151,11 @@ struct Place {
 
 template <typename T, int FMT, int REACH>
 __global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const T* __restrict__ x, u64 rows, u64 cols, u64 stride, u32 col_tiles,
-                                                              u64 tasks, const float* __restrict__ tensor_scale, unsigned char* __restrict__ out) {
+                                                              const float* __restrict__ tensor_scale, unsigned char* __restrict__ out) {
     let_next_start();                              // a product of this matrix may set itself up and fetch the other one
     __shared__ __align__(16) T buffer[REACH == REACH_ANY ? WARPS : 1][REACH == REACH_ANY ? 4 : 1][MX4_COLS];
     const u32 warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, part = lane & 15;
-    const u64 task = (u64)blockIdx.x * WARPS + warp;
-    if (task >= tasks) return;
-    const Place at(task, rows, col_tiles, FMT);
+    const Place at(rows, col_tiles, FMT);
     unsigned char* const dst = out + at.offset;
     const u64 first = (u64)at.ct * MX4_COLS, c0 = first + part * 16;
 
@@ -239,13 +237,11 @@ __device__ __forceinline__ void values_of(u32 codes, __half2 (&v)[4]) {
 
 template <typename T, int FMT, int REACH>
 __global__ void __launch_bounds__(WARPS * 32) dequantize_kernel(const unsigned char* __restrict__ packed, u64 rows, u64 cols,
-                                                                u32 col_tiles, u64 tasks, const float* __restrict__ tensor_scale,
+                                                                u32 col_tiles, const float* __restrict__ tensor_scale,
                                                                 T* __restrict__ out, u64 stride) {
     __shared__ __align__(16) T buffer[REACH == REACH_ANY ? WARPS : 1][REACH == REACH_ANY ? 4 : 1][MX4_COLS];
     const u32 warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, part = lane & 15;
-    const u64 task = (u64)blockIdx.x * WARPS + warp;
-    if (task >= tasks) return;
-    const Place at(task, rows, col_tiles, FMT);
+    const Place at(rows, col_tiles, FMT);
     if (at.row0 >= rows) return;                   // the whole warp
     const unsigned char* const src = packed + at.offset;
     const u64 first = (u64)at.ct * MX4_COLS, c0 = first + part * 16;
@@ -321,16 +317,13 @@ void tensor_scale_as(int sms, cudaStream_t s, const RowsIn& x, u32* words, float
 template <typename T, int FMT, int REACH>
 void quantize_as(cudaStream_t s, const RowsIn& x, const float* tensor_scale, unsigned char* out) {
     const u32 ct = mx4_col_tiles(x.cols);
-    const u64 tasks = (u64)mx4_row_tiles(x.rows) * ct * 32;
-    quantize_kernel<T, FMT, REACH><<<(u32)((tasks + WARPS - 1) / WARPS), WARPS * 32, 0, s>>>(static_cast<const T*>(x.p), x.rows, x.cols, x.stride,
-                                                                                            ct, tasks, tensor_scale, out);
+    quantize_kernel<T, FMT, REACH><<<mx4_row_tiles(x.rows) * ct * 4, WARPS * 32, 0, s>>>(static_cast<const T*>(x.p), x.rows, x.cols, x.stride, ct,
+                                                                                        tensor_scale, out);
 }
 template <typename T, int FMT, int REACH>
 void dequantize_as(cudaStream_t s, const unsigned char* packed, u64 rows, u64 cols, const float* tensor_scale, void* out, u64 stride) {
     const u32 ct = mx4_col_tiles(cols);
-    const u64 tasks = (u64)mx4_row_tiles(rows) * ct * 32;
-    dequantize_kernel<T, FMT, REACH><<<(u32)((tasks + WARPS - 1) / WARPS), WARPS * 32, 0, s>>>(packed, rows, cols, ct, tasks, tensor_scale,
-                                                                                              static_cast<T*>(out), stride);
+    dequantize_kernel<T, FMT, REACH><<<mx4_row_tiles(rows) * ct * 4, WARPS * 32, 0, s>>>(packed, rows, cols, ct, tensor_scale, static_cast<T*>(out), stride);
 }
 
 }  // namespace
