@@ -15,7 +15,7 @@
 #include <type_traits>
 
 #include "mx4_codes.cuh"
-#include "mx4_pipe.cuh"
+#include "score_launch.cuh"
 
 namespace excp {
 namespace {
@@ -90,6 +90,8 @@ __device__ __forceinline__ u32 largest_bits(const Sixteen<T>& v) {
 template <typename T, int REACH>
 __global__ void __launch_bounds__(256) tensor_scale_kernel(const T* __restrict__ x, u64 rows, u64 cols, u64 stride, u32 chunks,
                                                            u32* words, float* scale_out) {
+    wait_for_previous();
+    let_next_start();
     u32 best = 0;
     auto take = [&](u32 m) {
         if (m < NONFINITE_BITS && m > best) best = m;
@@ -152,6 +154,7 @@ struct Place {
 template <typename T, int FMT, int REACH>
 __global__ void __launch_bounds__(WARPS * 32) quantize_kernel(const T* __restrict__ x, u64 rows, u64 cols, u64 stride, u32 col_tiles,
                                                               const float* __restrict__ tensor_scale, unsigned char* __restrict__ out) {
+    wait_for_previous();
     let_next_start();                              // a product of this matrix may set itself up and fetch the other one
     __shared__ __align__(16) T buffer[REACH == REACH_ANY ? WARPS : 1][REACH == REACH_ANY ? 4 : 1][MX4_COLS];
     const u32 warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, part = lane & 15;
@@ -242,6 +245,8 @@ __global__ void __launch_bounds__(WARPS * 32) dequantize_kernel(const unsigned c
     __shared__ __align__(16) T buffer[REACH == REACH_ANY ? WARPS : 1][REACH == REACH_ANY ? 4 : 1][MX4_COLS];
     const u32 warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, part = lane & 15;
     const Place at(rows, col_tiles, FMT);
+    wait_for_previous();
+    let_next_start();
     if (at.row0 >= rows) return;                   // the whole warp
     const unsigned char* const src = packed + at.offset;
     const u64 first = (u64)at.ct * MX4_COLS, c0 = first + part * 16;
@@ -312,18 +317,19 @@ void tensor_scale_as(int sms, cudaStream_t s, const RowsIn& x, u32* words, float
     const u32 chunks = (u32)((x.cols + 511) / 512);
     const u64 want = (x.rows * chunks + 7) / 8;
     const u32 grid = (u32)(want < 1 ? 1 : (want > (u64)sms * 8 ? (u64)sms * 8 : want));
-    tensor_scale_kernel<T, REACH><<<grid, 256, 0, s>>>(static_cast<const T*>(x.p), x.rows, x.cols, x.stride, chunks, words, out);
+    launch_chained(tensor_scale_kernel<T, REACH>, grid, 256, 0, 0, s, static_cast<const T*>(x.p), x.rows, x.cols, x.stride, chunks, words, out);
 }
 template <typename T, int FMT, int REACH>
 void quantize_as(cudaStream_t s, const RowsIn& x, const float* tensor_scale, unsigned char* out) {
     const u32 ct = mx4_col_tiles(x.cols);
-    quantize_kernel<T, FMT, REACH><<<mx4_row_tiles(x.rows) * ct * 4, WARPS * 32, 0, s>>>(static_cast<const T*>(x.p), x.rows, x.cols, x.stride, ct,
-                                                                                        tensor_scale, out);
+    launch_chained(quantize_kernel<T, FMT, REACH>, mx4_row_tiles(x.rows) * ct * 4, WARPS * 32, 0, 0, s, static_cast<const T*>(x.p), x.rows, x.cols,
+                   x.stride, ct, tensor_scale, out);
 }
 template <typename T, int FMT, int REACH>
 void dequantize_as(cudaStream_t s, const unsigned char* packed, u64 rows, u64 cols, const float* tensor_scale, void* out, u64 stride) {
     const u32 ct = mx4_col_tiles(cols);
-    dequantize_kernel<T, FMT, REACH><<<mx4_row_tiles(rows) * ct * 4, WARPS * 32, 0, s>>>(packed, rows, cols, ct, tensor_scale, static_cast<T*>(out), stride);
+    launch_chained(dequantize_kernel<T, FMT, REACH>, mx4_row_tiles(rows) * ct * 4, WARPS * 32, 0, 0, s, packed, rows, cols, ct, tensor_scale,
+                   static_cast<T*>(out), stride);
 }
 
 }  // namespace

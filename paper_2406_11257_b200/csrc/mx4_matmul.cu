@@ -26,6 +26,7 @@ constexpr int STAGES = 3;
 constexpr u32 CODES = MX4_ROWS * 128;
 constexpr u32 MAX_SPLIT = 8;
 constexpr u32 RAW_TASKS = 24;                      // plain rows x column tiles that a CTA quantises itself
+constexpr u32 SMEM_MAX = 227 * 1024 - 1024;      // dynamic shared memory of a block, beside what the kernel has of its own
 constexpr u32 RAW_MAX = 96 * 1024;                 // shared memory for plain rows that are quantised in the product
 constexpr u32 RAW_ROWS = 16;                       // and at most so many (at most 32: one column of tensor memory holds their scales)
 
@@ -42,6 +43,7 @@ struct NarrowArgs {
     const float* bias;                             // per row of m
     u32 sums;                                      // where the parts of the CTA's columns lie in shared memory
     u32 stage_bytes, tmem_cols;
+    u32 early;                                     // the launch before packs n, and m may be fetched before it ends
     u64 wait_ns;
     u32* flag;
 };
@@ -104,6 +106,8 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
     // a stage: tile of m (codes, scales), packed rows of n (codes), their scales
     const u32 n_codes = CODES + SB, n_scales = n_codes + g.nt * 128;
 
+    if (!g.early) wait_for_previous();
+    let_next_start();
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.ready[s], WORK_WARPS); mbar_init(&sh.empty[s], 1); }
         mbar_init(&sh.done, 1);
@@ -152,7 +156,7 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
         const u32 first = min((u32)STAGES, k1 - k0);
         for (u32 s = 0; s < first; ++s) fetch_m(s);
         if (!RAW) {
-            wait_for_previous();
+            if (g.early) wait_for_previous();
             for (u32 s = 0; s < first; ++s) fetch_n(s);
         }
         for (u32 s = 0; s < first; ++s, ++filled) ring.next();
@@ -343,27 +347,15 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
 }
 
 template <int FMT, int DT, int XT>
-bool launch_as(cudaStream_t s, const NarrowArgs& g, u32 parts, u32 smem, bool behind) {
-    if (cudaFuncSetAttribute(narrow_kernel<FMT, DT, XT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(mx4_row_tiles(g.m.rows) * g.n_tiles * parts);
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = parts;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = behind ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, narrow_kernel<FMT, DT, XT>, g) == cudaSuccess;
+bool launch_as(cudaStream_t s, const NarrowArgs& g, u32 parts, u32 smem) {
+    static std::atomic<u64> allowed{0};
+    if (!allow_smem(narrow_kernel<FMT, DT, XT>, allowed, SMEM_MAX)) return false;
+    return launch_chained(narrow_kernel<FMT, DT, XT>, mx4_row_tiles(g.m.rows) * g.n_tiles * parts, THREADS, smem, parts, s, g);
 }
 
 template <int XT>
-bool launch_typed(cudaStream_t s, const NarrowArgs& g, u32 parts, u32 smem, int fmt, int dtype, bool behind) {
-#define EXCP_MM(DT) (fmt == MX4_E4M3_16 ? launch_as<MX4_E4M3_16, DT, XT>(s, g, parts, smem, behind) : launch_as<MX4_E8M0_32, DT, XT>(s, g, parts, smem, behind))
+bool launch_typed(cudaStream_t s, const NarrowArgs& g, u32 parts, u32 smem, int fmt, int dtype) {
+#define EXCP_MM(DT) (fmt == MX4_E4M3_16 ? launch_as<MX4_E4M3_16, DT, XT>(s, g, parts, smem) : launch_as<MX4_E8M0_32, DT, XT>(s, g, parts, smem))
     return dtype == DT_F32 ? EXCP_MM(DT_F32) : dtype == DT_F16 ? EXCP_MM(DT_F16) : EXCP_MM(DT_BF16);
 #undef EXCP_MM
 }
@@ -407,9 +399,10 @@ bool launch_narrow(int sms, cudaStream_t s, const Mx4Operand& a, const RowsIn* x
     const u32 need = g.nt + STAGES * (u32)mx4_pieces(fmt) * 8;
     g.tmem_cols = 32;
     while (g.tmem_cols < need) g.tmem_cols *= 2;
+    g.early = behind;
     g.wait_ns = wait_ns;
     g.flag = flag;
-    if (!x) return launch_typed<-1>(s, g, parts, smem, fmt, r.dtype, behind);
+    if (!x) return launch_typed<-1>(s, g, parts, smem, fmt, r.dtype);
     g.x = x->p;
     g.x_stride = x->stride;
     const u64 size = x->dtype == DT_F32 ? 4 : 2;
@@ -417,9 +410,9 @@ bool launch_narrow(int sms, cudaStream_t s, const Mx4Operand& a, const RowsIn* x
     g.x_codes = smem - 1024;
     g.x_scales = g.x_codes + (g.col_tiles + parts - 1) / parts * g.nt * 128;
     smem += raw_bytes(g.nt, g.col_tiles, parts, fmt);
-    return x->dtype == DT_F32 ? launch_typed<DT_F32>(s, g, parts, smem, fmt, r.dtype, false)
-         : x->dtype == DT_F16 ? launch_typed<DT_F16>(s, g, parts, smem, fmt, r.dtype, false)
-                              : launch_typed<DT_BF16>(s, g, parts, smem, fmt, r.dtype, false);
+    return x->dtype == DT_F32 ? launch_typed<DT_F32>(s, g, parts, smem, fmt, r.dtype)
+         : x->dtype == DT_F16 ? launch_typed<DT_F16>(s, g, parts, smem, fmt, r.dtype)
+                              : launch_typed<DT_BF16>(s, g, parts, smem, fmt, r.dtype);
 }
 
 }  // namespace

@@ -40,6 +40,7 @@ struct WideArgs {
     // Usually a is m: a lane has a row of y and writes 32 bytes at a time.  Where rows of y do not start on 32 bytes the operands
     // change places: a lane has a column, and neighbouring lanes write neighbouring results.
     u32 turned;
+    u32 early;                                     // the launch before packs a, and b may be fetched before it ends
     u64 wait_ns;
     u32* flag;
 };
@@ -113,6 +114,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
     const u32 rank = cluster_rank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const u32 tiles = g.m_tiles * g.n_tiles;
 
+    if (!g.early) wait_for_previous();
+    let_next_start();
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], FETCH_WARPS); mbar_init(&sh.ready[s], 2 * SCALE_WARPS); mbar_init(&sh.empty[s], 1); }
         mbar_init(&sh.acc_full, 1);
@@ -139,7 +142,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             Ring<STAGES> ring;
             u32 filled = 0;
             bool ok = true;
-            if ((item == 0) != (g.turned != 0)) wait_for_previous();       // a may have been packed by the launch before this one
+            if (g.early && (item == 0) != (g.turned != 0)) wait_for_previous();    // only a depends on the launch before
             for (u32 t = pair; ok && t < tiles; t += pairs) {
                 u32 mt, nt;
                 place(g, t, mt, nt);
@@ -326,22 +329,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
 }
 
 template <int FMT, int DT>
-bool launch_as(int sms, cudaStream_t s, const WideArgs& g, bool behind) {
+bool launch_as(int sms, cudaStream_t s, const WideArgs& g) {
     const u32 smem = stage_bytes<FMT>() * stages<FMT>() + 1024;
-    if (cudaFuncSetAttribute(wide_kernel<FMT, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
+    static std::atomic<u64> allowed{0};
+    if (!allow_smem(wide_kernel<FMT, DT>, allowed, smem)) return false;
     const u64 tiles = (u64)g.m_tiles * g.n_tiles;
     const u32 pairs = (u32)(tiles < (u64)(sms / 2) ? tiles : (u64)(sms / 2));
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(pairs * 2);
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = behind ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, wide_kernel<FMT, DT>, g) == cudaSuccess;
+    return launch_chained(wide_kernel<FMT, DT>, pairs * 2, THREADS, smem, 0, s, g);
 }
 
 }  // namespace
@@ -359,9 +353,10 @@ bool launch_mx4_matmul_wide(int sms, cudaStream_t s, const Mx4Operand& a, const 
     g.y = r.y;
     g.stride = r.stride;
     g.bias = r.bias;
+    g.early = behind;
     g.wait_ns = wait_ns;
     g.flag = flag;
-#define EXCP_MM(DT) (fmt == MX4_E4M3_16 ? launch_as<MX4_E4M3_16, DT>(sms, s, g, behind) : launch_as<MX4_E8M0_32, DT>(sms, s, g, behind))
+#define EXCP_MM(DT) (fmt == MX4_E4M3_16 ? launch_as<MX4_E4M3_16, DT>(sms, s, g) : launch_as<MX4_E8M0_32, DT>(sms, s, g))
     return r.dtype == DT_F32 ? EXCP_MM(DT_F32) : r.dtype == DT_F16 ? EXCP_MM(DT_F16) : EXCP_MM(DT_BF16);
 #undef EXCP_MM
 }

@@ -1,16 +1,11 @@
 // What the two kernels of the 4-bit product share: bounded waits of whole warps, the ring of stages.
 #pragma once
-#include "score.cuh"
+#include "score_launch.cuh"
 #include "tcgen05.cuh"
 
 namespace excp {
 
 constexpr u64 DRAIN_NS = 100000000ull;             // a copy in flight lands within microseconds
-
-// Programmatic dependent launch: a kernel launched behind another one may start when the first says so, and waits for its
-// end (and for its results) where it says so itself.  Both do nothing in a launch of the ordinary kind.
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // A whole warp waits for phase `parity` of `bar`; false when the limit has passed or another role gave up.
 template <typename S>

@@ -22,7 +22,7 @@
 
 #include <type_traits>
 
-#include "score.cuh"
+#include "score_launch.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -376,6 +376,8 @@ __global__ void __launch_bounds__(BLOCK) logprobs_kernel(const T* __restrict__ l
                                                       float scale, LogprobsOut out) {
     constexpr int U = 4;
     __shared__ Joint<BLOCK> j;
+    wait_for_previous();
+    let_next_start();
     u32 part = 0, parts = 1;
     if constexpr (CLUSTER) { part = cg::this_cluster().block_rank(); parts = cg::this_cluster().num_blocks(); }
     const u32 tid = threadIdx.x;
@@ -461,6 +463,8 @@ __global__ void __launch_bounds__(GRAD_BLOCK) grad_kernel(const T* logits, u32 v
                                                      float scale, const float* __restrict__ row_stats, const float* __restrict__ g_logprob,
                                                      const float* __restrict__ g_entropy, T* grad, u64 grad_stride, u32 chunks) {
     constexpr u32 N = per16<T>();
+    wait_for_previous();
+    let_next_start();
     const u64 row = blockIdx.x / chunks;
     const u32 chunk = blockIdx.x - (u32)row * chunks;
     const float4 st = __ldg(reinterpret_cast<const float4*>(row_stats) + row);
@@ -513,17 +517,8 @@ __global__ void __launch_bounds__(GRAD_BLOCK) grad_kernel(const T* logits, u32 v
 
 template <typename T, int BLOCK, bool CLUSTER>
 void logprobs_launch(cudaStream_t s, const RowsIn& x, u32 parts, const long long* tokens, float scale, const LogprobsOut& out) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((u32)x.rows * parts);
-    cfg.blockDim = dim3(BLOCK);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = parts;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = CLUSTER ? 1 : 0;
-    cudaLaunchKernelEx(&cfg, logprobs_kernel<T, BLOCK, CLUSTER>, static_cast<const T*>(x.p), (u32)x.cols, x.stride, tokens, scale, out);
+    launch_chained(logprobs_kernel<T, BLOCK, CLUSTER>, (u32)x.rows * parts, BLOCK, 0, CLUSTER ? parts : 0, s, static_cast<const T*>(x.p), (u32)x.cols,
+                   x.stride, tokens, scale, out);
 }
 
 template <typename T>
@@ -544,8 +539,8 @@ void grad_as(cudaStream_t s, const RowsIn& x, const long long* tokens, float sca
     const bool vec = ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0 &&
                      (x.rows == 1 || (((x.stride - grad_stride) * sizeof(T)) & 15) == 0);
     const u32 grid = (u32)x.rows * chunks;
-    if (vec) grad_kernel<T, true><<<grid, GRAD_BLOCK, 0, s>>>(p, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
-    else grad_kernel<T, false><<<grid, GRAD_BLOCK, 0, s>>>(p, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
+    if (vec) launch_chained(grad_kernel<T, true>, grid, GRAD_BLOCK, 0, 0, s, p, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
+    else launch_chained(grad_kernel<T, false>, grid, GRAD_BLOCK, 0, 0, s, p, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
 }
 
 }  // namespace
