@@ -127,6 +127,9 @@ def check_product(y, codes_a, scales_a, ga, codes_b, scales_b, gb, fmt, bias, dt
 
 PRODUCTS = [(1, 64, 128), (1, 4096, 300), (2, 1, 1), (7, 1000, 513), (8, 256, 128), (16, 2048, 1000), (33, 300, 129), (100, 512, 256),
             (128, 640, 384), (129, 257, 127), (200, 1024, 1000), (256, 256, 256), (300, 4096, 40), (513, 700, 777), (1000, 64, 8), (640, 3000, 512)]
+# 256 x 256 tiles enough for the kernel of many rows: aligned rows of the result and others, ragged on every side, several tiles
+# to a pair of SMs, both halves of a tile missing rows
+PRODUCTS += [(1300, 513, 2048), (1100, 300, 2100), (2100, 260, 2608), (2049, 1500, 2305), (257, 64, 10001), (9000, 100, 260)]
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -153,7 +156,8 @@ def test_matmul(h, rows, k, n, fmt):
 
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
-@pytest.mark.parametrize("rows,k,n,slack", [(1, 4096, 512, 0), (5, 999, 130, 1), (16, 256, 3000, 8), (150, 1000, 260, 3), (300, 512, 520, 0)])
+@pytest.mark.parametrize("rows,k,n,slack", [(1, 4096, 512, 0), (5, 999, 130, 1), (16, 256, 3000, 8), (150, 1000, 260, 3), (300, 512, 520, 0),
+                                             (1100, 600, 2064, 5), (1281, 257, 2047, 0), (17, 11000, 96, 2)])
 def test_linear(h, rows, k, n, slack, dtype, fmt):
     x, w = make(rows, k, dtype, 11, slack), make(n, k, "fp32", 12)
     gx = device_scale(so.tensor_scale(dense(x)) * 1.37) if fmt == "e4m3_16" else None
@@ -171,8 +175,20 @@ def test_linear(h, rows, k, n, slack, dtype, fmt):
     h.score_status()
 
 
+@pytest.mark.parametrize("n", [33000, 32992])
+def test_product_past_32_bit_offsets(h, n):
+    # 2.2e9 results: the last rows lie past element 2^31 and byte 2^32 (rows that start on 32 bytes, and others)
+    rows, k, fmt = 66000, 64, "e8m0_32"
+    x, w = make(rows, k, "bf16", 51), make(n, k, "fp32", 52)
+    y = h.mx4_linear(x, h.mx4_quantize(w, fmt))
+    qw = so.quantize(dense(w), fmt)
+    for part in (slice(0, 2), slice(rows - 3, rows)):
+        check_product(y[part], *so.quantize(dense(x[part]), fmt), None, *qw, None, fmt, None, "bf16")
+    del y
+
+
 @pytest.mark.parametrize("fmt", FMTS)
-@pytest.mark.parametrize("rows", [3, 200])
+@pytest.mark.parametrize("rows", [3, 200, 9000])
 def test_product_of_rows_with_nan_stays_in_its_rows(h, rows, fmt):
     k, n = 320, 300
     x, w = make(rows, k, "fp32", 21), make(n, k, "fp32", 22)
@@ -190,6 +206,8 @@ def test_products_of_nothing(h):
         bias = torch.arange(300, dtype=torch.float32, device=DEV)
         assert torch.equal(h.mx4_matmul(x, w, bias=bias, dtype=torch.float32), bias.expand(5, 300))
         assert not h.mx4_matmul(x, w, dtype=torch.float16).any()
+        assert torch.equal(h.mx4_linear(torch.ones((5, 0), device=DEV), w, bias=bias), bias.expand(5, 300))
+        assert torch.equal(h.mx4_linear(torch.ones((500, 0), device=DEV), w, bias=bias), bias.expand(500, 300))
         w = h.mx4_quantize(torch.ones((30, 64), device=DEV), fmt)
         x = torch.ones((0, 64), device=DEV)
         assert h.mx4_linear(x, w).shape == (0, 30)
@@ -222,19 +240,21 @@ def test_product_on_another_stream_and_in_a_graph(h):
 
 
 def test_a_wait_that_runs_out_is_reported(h):
-    x, w = make(300, 1024, "bf16", 41), make(700, 1024, "bf16", 42)
-    m = h.mx4_quantize(w, "e8m0_32")
-    want = h.mx4_linear(x, m)
-    h.set_wait_limit(0)
-    try:
-        h.mx4_linear(x, m)
-        with pytest.raises(binding.ExcpError) as e:
-            h.score_status()
-        assert e.value.status == -7
-    finally:
-        h.set_wait_limit(2_000_000_000)
-    assert torch.equal(h.mx4_linear(x, m), want)
-    h.score_status()
+    # a token quantised in the product, some packed, split columns, the kernel of many rows
+    for rows, n in ((1, 700), (40, 700), (300, 700), (1100, 2100)):
+        x, w = make(rows, 2048, "bf16", 41), make(n, 2048, "bf16", 42)
+        m = h.mx4_quantize(w, "e8m0_32")
+        want = h.mx4_linear(x, m)
+        h.set_wait_limit(0)
+        try:
+            h.mx4_linear(x, m)
+            with pytest.raises(binding.ExcpError) as e:
+                h.score_status()
+            assert e.value.status == -7
+        finally:
+            h.set_wait_limit(2_000_000_000)
+        assert torch.equal(h.mx4_linear(x, m), want)
+        h.score_status()
 
 
 # ---- log probabilities ---------------------------------------------------------------
