@@ -72,6 +72,13 @@ bool on(const at::Tensor& t, int device) { return t.is_cuda() && t.get_device() 
 at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType t, int device) {
     return at::detail::empty_cuda(sizes, t, at::Device(at::kCUDA, (c10::DeviceIndex)device), std::nullopt);
 }
+// A contiguous tensor within the bytes of another one.
+at::Tensor within(const at::Tensor& base, at::ScalarType t, at::IntArrayRef sizes, int64_t at_byte) {
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(), c10::scalarTypeToTypeMeta(t));
+    impl->set_sizes_contiguous(sizes);
+    impl->set_storage_offset(at_byte / (int64_t)c10::elementSize(t));
+    return at::Tensor(std::move(impl));
+}
 void* stream(int device) { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 
 struct Rows {                                      // a 2-D tensor whose last dimension is dense
@@ -185,12 +192,16 @@ PyObject* logprobs(PyObject* const* a) {
     if (scale == -1.0 && PyErr_Occurred()) throw PythonError{};
     const int64_t r = (int64_t)x.rows;
     const long long* tokens = static_cast<long long*>(vector(a[3], device, at::kLong, r, "tokens"));
-    const at::Tensor lp = fresh({r}, at::kFloat, device), h = fresh({r}, at::kFloat, device), stats = fresh({r, 4}, at::kFloat, device);
+    // one allocation for all results: row statistics first (16 bytes a row), then 8-byte places, then the other floats
+    const int64_t k = top > 0 && top <= (1 << 20) ? top : 0;
+    const at::Tensor all = fresh({r * (24 + 12 * k)}, at::kByte, device);
+    const at::Tensor stats = within(all, at::kFloat, {r, 4}, 0);
     at::Tensor tl, ti;
-    if (top > 0 && top <= (1 << 20)) {
-        tl = fresh({r, top}, at::kFloat, device);
-        ti = fresh({r, top}, at::kLong, device);
+    if (k) {
+        ti = within(all, at::kLong, {r, k}, 16 * r);
+        tl = within(all, at::kFloat, {r, k}, 16 * r + 8 * r * k);
     }
+    const at::Tensor lp = within(all, at::kFloat, {r}, 16 * r + 12 * r * k), h = within(all, at::kFloat, {r}, 20 * r + 12 * r * k);
     check(api.token_logprobs(handle(a[0]), x.p, x.dtype, x.rows, x.cols, x.stride, tokens, (float)scale, (int)top, static_cast<float*>(lp.data_ptr()),
                              static_cast<float*>(h.data_ptr()), static_cast<float*>(stats.data_ptr()), tl.defined() ? static_cast<float*>(tl.data_ptr()) : nullptr,
                              ti.defined() ? static_cast<long long*>(ti.data_ptr()) : nullptr, stream(device)), "excp_token_logprobs");
