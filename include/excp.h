@@ -2,7 +2,8 @@
  * excp.h -- C ABI of the ExCP checkpoint-compression hot path for NVIDIA B200 (sm_100a).
  *
  * What the library computes (arXiv 2406.11257, "ExCP: Extreme LLM Checkpoint
- * Compression via Weight-Momentum Joint Shrinking"):
+ * Compression via Weight-Momentum Joint Shrinking"; at the end of this file, also the operators
+ * that score a restored checkpoint):
  *
  *   compress   Algorithm 1 without its archiver step, per tensor:
  *                dW = W_t - W^_(t-1)                       (Section 3.1, Eq. ckpt_res)

@@ -1,7 +1,9 @@
 // Product of two microscaled 4-bit matrices: y[a row, b row] = scales * sum over columns (+ bias), fp32 sums.
 // This file: few rows on one side (the tokens of a decoding step); mx4_matmul_wide.cu: many rows on both.
 //
-// Bound: the bytes of the larger matrix.  Its rows go on the M side of the tensor core (128 per tile), the few rows on the N
+// Bound: the bytes of the larger matrix; for small ones the chain launch, copy, product, exchange.  (4096 -> 11008, blocks of 16,
+// 25 MB: one token quantised here 7.6 us, 16 packed tokens 8.4 us, 128 tokens 10.9 us; 2048 -> 50304, 55 MB, 16 tokens 12.5 us,
+// 4.4 TB/s; 128 columns alone 3.3 us.)  Its rows go on the M side of the tensor core (128 per tile), the few rows on the N
 // side, which takes them in steps of 8.  Several CTAs share an SM, and the columns of a tile are split over a cluster so
 // that every SM streams; each CTA sends its part of a column of the result to the CTA that owns the column (distributed shared
 // memory), which adds them in a fixed order.
