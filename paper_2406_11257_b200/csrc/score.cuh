@@ -123,6 +123,22 @@ __device__ __forceinline__ void store8(T* p, const float v[8]) {
     for (int k = 0; k < 8; ++k) wput(h, k, v[k]);
     *reinterpret_cast<uint4*>(p) = a;
 }
+
+// 16 bytes from byte `shift` (0 .. 15) of the 32 that a and b hold.
+__device__ __forceinline__ uint4 cut16(uint4 a, uint4 b, u32 shift) {
+    u32 w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (shift & 8) {
+#pragma unroll
+        for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+    }
+    if (shift & 4) {
+#pragma unroll
+        for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
+    }
+    const u32 bits = (shift & 3) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                      __funnelshift_r(w[3], w[4], bits));
+}
 #endif
 
 }  // namespace excp

@@ -457,12 +457,13 @@ __global__ void __launch_bounds__(BLOCK, BLOCK == 96 ? 8 : BLOCK == 128 ? 7 : 1)
 }
 
 // p times a line in the distance: -scale p (g_lp + g_h (log p + entropy)), and scale g_lp at the token.
-// A block takes UNROLL 16-byte words per thread of a row, counted from the row's first 16-byte boundary; the block
-// of a row's first words also takes what lies before it.  VEC: each row of the gradient starts as far from a boundary as
-// the logits' row; else values one by one, all of a thread's on their way at once.  The last rows come first: they are the ones
-// that a preceding forward pass has left in L2; what is written goes past it.
-// Bound: the bytes (2048 x 50304 bf16: 71 us, 5.8 TB/s).
-template <typename T, bool VEC>
+// A block takes UNROLL 16-byte words per thread of a row, counted from the first 16-byte boundary of the gradient's row;
+// the block of a row's first words also takes what lies before it.  SHIFT: the logits' row is not as far from such a
+// boundary as the gradient's, and a word of logits is cut out of the two 16-byte words that hold it; the second is the
+// next thread's first, so it comes from L1 (slack of 3 in 2048 x 50304 bf16: 85 us; value by value it was 162).
+// The last rows come first: they are the ones that a preceding forward pass has left in L2; what is written goes past it.
+// Bound: the bytes (2048 x 50304 bf16: 66 us, 6.2 TB/s).
+template <typename T, bool SHIFT>
 __global__ void __launch_bounds__(GRAD_BLOCK) grad_kernel(const T* logits, u64 rows, u32 vocab, u64 stride, const long long* __restrict__ tokens,
                                                      float scale, const float* __restrict__ row_stats, const float* __restrict__ g_logprob,
                                                      const float* __restrict__ g_entropy, T* grad, u64 grad_stride, u32 chunks) {
@@ -487,41 +488,38 @@ __global__ void __launch_bounds__(GRAD_BLOCK) grad_kernel(const T* logits, u64 r
         if ((long long)i == t) r += at_token;
         return empty ? 0.f : r;
     };
-    if (VEC) {
-        const u32 head = min((u32)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (u32)sizeof(T), vocab);
-        const u32 first = head + chunk * (GRAD_BLOCK * UNROLL * N);
-        if (chunk == 0 && threadIdx.x < head) wput(y, threadIdx.x, value(wget(x, threadIdx.x), threadIdx.x));
-        uint4 q[UNROLL];
+    const u32 head = min((u32)((16 - (reinterpret_cast<uintptr_t>(y) & 15)) & 15) / (u32)sizeof(T), vocab);
+    const u32 first = head + chunk * (GRAD_BLOCK * UNROLL * N);
+    if (chunk == 0 && threadIdx.x < head) wput(y, threadIdx.x, value(wget(x, threadIdx.x), threadIdx.x));
+    // bytes from a 16-byte boundary to the logits that belong to a word of the gradient; the same for the whole row
+    const u32 shift = SHIFT ? (u32)(reinterpret_cast<uintptr_t>(x + head) & 15) : 0u;
+    uint4 q[UNROLL], after[SHIFT ? UNROLL : 1];
+    bool whole[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const u32 i = first + (u * GRAD_BLOCK + threadIdx.x) * N;
-            if (i + N <= vocab) q[u] = __ldcs(reinterpret_cast<const uint4*>(x + i));
+    for (int u = 0; u < UNROLL; ++u) {
+        const u32 i = first + (u * GRAD_BLOCK + threadIdx.x) * N;
+        const char* p = reinterpret_cast<const char*>(x + i) - shift;
+        // every byte that is read belongs to the row
+        whole[u] = i + N <= vocab && (!SHIFT || (p >= reinterpret_cast<const char*>(x) && p + 32 <= reinterpret_cast<const char*>(x + vocab)));
+        if (whole[u]) {
+            q[u] = __ldcs(reinterpret_cast<const uint4*>(p));
+            if (SHIFT) after[u] = __ldg(reinterpret_cast<const uint4*>(p) + 1);
         }
+    }
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const u32 i = first + (u * GRAD_BLOCK + threadIdx.x) * N;
-            if (i + N <= vocab) {
-                float v[N];
-                unpack<T>(q[u], v);
-                uint4 r;
-                T* h = reinterpret_cast<T*>(&r);
+    for (int u = 0; u < UNROLL; ++u) {
+        const u32 i = first + (u * GRAD_BLOCK + threadIdx.x) * N;
+        if (whole[u]) {
+            if (SHIFT) q[u] = cut16(q[u], after[u], shift);
+            float v[N];
+            unpack<T>(q[u], v);
+            uint4 r;
+            T* h = reinterpret_cast<T*>(&r);
 #pragma unroll
-                for (u32 k = 0; k < N; ++k) wput(h, k, value(v[k], i + k));
-                __stcs(reinterpret_cast<uint4*>(y + i), r);
-            } else {
-                for (u32 k = 0; k < N && i + k < vocab; ++k) wput(y, i + k, value(wget(x, i + k), i + k));
-            }
-        }
-    } else {
-        constexpr u32 EACH = UNROLL * N;
-        const u32 first = chunk * (GRAD_BLOCK * EACH) + threadIdx.x;
-        T v[EACH];
-#pragma unroll
-        for (u32 k = 0; k < EACH; ++k) if (first + k * GRAD_BLOCK < vocab) v[k] = x[first + k * GRAD_BLOCK];
-#pragma unroll
-        for (u32 k = 0; k < EACH; ++k) {
-            const u32 i = first + k * GRAD_BLOCK;
-            if (i < vocab) wput(y, i, value(wget(v, k), i));
+            for (u32 k = 0; k < N; ++k) wput(h, k, value(v[k], i + k));
+            __stcs(reinterpret_cast<uint4*>(y + i), r);
+        } else {
+            for (u32 k = 0; k < N && i + k < vocab; ++k) wput(y, i + k, value(wget(x, i + k), i + k));
         }
     }
 }
@@ -549,11 +547,12 @@ void grad_as(cudaStream_t s, const RowsIn& x, const long long* tokens, float sca
              const float* g_entropy, T* grad, u64 grad_stride) {
     const T* p = static_cast<const T*>(x.p);
     const u32 chunk = GRAD_BLOCK * UNROLL * per16<T>(), chunks = (u32)((x.cols + chunk - 1) / chunk);
-    const bool vec = ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0 &&
+    // every row of the logits as far from a 16-byte boundary as the gradient's
+    const bool aligned = ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0 &&
                      (x.rows == 1 || (((x.stride - grad_stride) * sizeof(T)) & 15) == 0);
     const u32 grid = (u32)x.rows * chunks;
-    if (vec) launch_chained(grad_kernel<T, true>, grid, GRAD_BLOCK, 0, 0, s, p, x.rows, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
-    else launch_chained(grad_kernel<T, false>, grid, GRAD_BLOCK, 0, 0, s, p, x.rows, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
+    if (aligned) launch_chained(grad_kernel<T, false>, grid, GRAD_BLOCK, 0, 0, s, p, x.rows, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
+    else launch_chained(grad_kernel<T, true>, grid, GRAD_BLOCK, 0, 0, s, p, x.rows, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
 }
 
 }  // namespace

@@ -492,3 +492,74 @@ def test_logprobs_of_many_rows(h, kind, dtype):
         for slack, offset in ((0, 0), (1, 1)):
             x = make_logits(rows, vocab, dtype, 77 + vocab, slack, offset, kind)
             check_logprobs(h, x, np.arange(rows) * 7 % vocab, 0.9, top, grad=False)
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("vocab", [1, 5, 16, 33, 1001, 20011])
+def test_gradient_of_rows_at_every_offset(h, vocab, dtype):
+    """A value's gradient does not depend on where its row starts: equal bits, and nothing written beside the rows."""
+    rows, gen = 5, torch.Generator(device=DEV).manual_seed(vocab)
+    x = (torch.randn((rows, vocab), device=DEV, generator=gen) * 3).to(DT[dtype])
+    tokens = torch.randint(0, vocab, (rows,), device=DEV, generator=gen)
+    gl, gh = torch.randn(rows, device=DEV, generator=gen), torch.randn(rows, device=DEV, generator=gen)
+    r = h.token_logprobs(x, tokens, scale=0.7)
+    want = h.token_logprobs_grad(x, tokens, r, gl, gh)
+    wg = so.logprobs_grad(dense(x), tokens.cpu().numpy(), 0.7, gl.cpu().numpy(), gh.cpu().numpy())
+    ulp = {torch.float32: 2.0 ** -20, torch.float16: 2.0 ** -10, torch.bfloat16: 2.0 ** -7}[DT[dtype]]
+    size = float((gl.abs() + gh.abs() * (np.log(vocab) + 20)).max())
+    close(dense(want), wg, np.abs(wg) * ulp + size * 2.0 ** -18)
+    per16 = 16 // x.element_size()
+    for start in range(per16):
+        for out_start in (0, 1, per16 - 1):
+            for slack, out_slack in ((0, 0), (1, 0), (3, per16)):
+                xs = torch.full((start + rows * (vocab + slack) + per16,), float("nan"), dtype=x.dtype, device=DEV)
+                ys = torch.full((out_start + rows * (vocab + out_slack) + per16,), 7.0, dtype=x.dtype, device=DEV)
+                xv = xs.as_strided((rows, vocab), (vocab + slack, 1), start)
+                yv = ys.as_strided((rows, vocab), (vocab + out_slack, 1), out_start)
+                xv.copy_(x)
+                h.token_logprobs_grad(xv, tokens, r, gl, gh, out=yv)
+                assert torch.equal(yv, want)
+                yv.fill_(7.0)
+                assert bool((ys == 7).all())
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("cols", [1, 7, 40, 511, 513, 1600])
+def test_tensor_scale_of_rows_at_every_offset(h, cols, dtype):
+    """The largest value is found wherever it lies, and what lies beside the rows is not looked at."""
+    per32 = 32 // torch.empty((), dtype=DT[dtype]).element_size()
+    for start in range(per32):
+        for at in sorted({0, 1 % cols, min(per32 - start, cols - 1), cols // 2, cols - 1}):
+            xs = torch.full((start + 3 * (cols + 1) + per32,), 30000.0, dtype=DT[dtype], device=DEV)
+            x = xs.as_strided((3, cols), (cols + 1, 1), start)
+            x.fill_(0.5)
+            x[2, at] = -21.0
+            assert float(h.mx4_tensor_scale(x)) == so.tensor_scale(dense(x))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("cols", [1, 7, 33, 255, 256, 257, 530])
+def test_quantize_and_back_at_every_offset(h, cols, dtype, fmt):
+    """Codes and values do not depend on where a row starts, and nothing beside the rows is read into them or written."""
+    rows, gen = 37, torch.Generator(device=DEV).manual_seed(cols)
+    x = (torch.randn((rows, cols), device=DEV, generator=gen) * 3).to(DT[dtype])
+    g = h.mx4_tensor_scale(x) if fmt == "e4m3_16" else None
+    m = h.mx4_quantize(x, fmt, tensor_scale=g)
+    codes, scales = so.quantize(dense(x), fmt, None if g is None else float(g))
+    assert np.array_equal(m.data.cpu().numpy(), so.pack(codes, scales, fmt))
+    back = h.mx4_dequantize(m, DT[dtype])
+    want = torch.from_numpy(so.values(codes, scales, fmt, None if g is None else float(g)).astype(np.float32))
+    assert torch.equal(back.cpu(), want.to(DT[dtype]))
+    per16 = 16 // x.element_size()
+    for start in range(per16):
+        for slack in (0, 1, per16 - 1, per16):
+            xs = torch.full((start + rows * (cols + slack) + per16,), float("nan"), dtype=x.dtype, device=DEV)
+            xv = xs.as_strided((rows, cols), (cols + slack, 1), start)
+            xv.copy_(x)
+            assert torch.equal(h.mx4_quantize(xv, fmt, tensor_scale=g).data, m.data)
+            xs.fill_(77.0)
+            h.mx4_dequantize(m, out=xv)
+            assert torch.equal(xv, back)
+            xv.fill_(77.0)
+            assert bool((xs == 77).all())
