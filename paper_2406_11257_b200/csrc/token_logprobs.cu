@@ -31,7 +31,7 @@ namespace cg = cooperative_groups;
 namespace excp {
 namespace {
 
-constexpr int GRAD_BLOCK = 256;
+constexpr int GRAD_BLOCK = 128;                    // (256: 2048 x 50304 bf16 66 us against 64, 5056 x 391 fp32 14 against 8.6)
 constexpr int UNROLL = 4;                          // 16-byte loads in flight per thread
 constexpr int TOP_MAX = 64;
 constexpr int SLOTS = 16, OWNERS = 512;            // step maxima kept per thread; of them that are read again
@@ -374,7 +374,7 @@ __device__ __forceinline__ float token_logit(const T* x, long long token, u32 vo
 }
 
 template <typename T, int BLOCK, bool CLUSTER>
-__global__ void __launch_bounds__(BLOCK, BLOCK == 96 ? 8 : BLOCK == 128 ? 7 : 1) logprobs_kernel(const T* __restrict__ logits, u32 vocab, u64 stride, const long long* __restrict__ tokens,
+__global__ void __launch_bounds__(BLOCK, BLOCK == 128 ? 7 : 768 / BLOCK) logprobs_kernel(const T* __restrict__ logits, u32 vocab, u64 stride, const long long* __restrict__ tokens,
                                                       float scale, LogprobsOut out) {
     constexpr int U = 4;
     __shared__ Joint<BLOCK> j;
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(BLOCK, BLOCK == 96 ? 8 : BLOCK == 128 ? 7 : 1)
         at_token = token_logit(x, token, vocab);
     }
     if (tid == 0) j.owners[0] = j.count[0] = 0;
-    if (tid < k) j.best[tid] = 0;
+    for (u32 i = tid; i < k; i += BLOCK) j.best[i] = 0;
     Walk<T, BLOCK, U> walk;
     walk.start(share_of(x, vocab, part, parts), c);
     const uint4* const body = reinterpret_cast<const uint4*>(walk.w.x + walk.w.body);
@@ -451,8 +451,8 @@ __global__ void __launch_bounds__(BLOCK, BLOCK == 96 ? 8 : BLOCK == 128 ? 7 : 1)
             const u32 rank = rank_of(j, mine, count);
             if (rank < k && mine) r.put_top(out, row, rank, mine);
         }
-    } else if (tid < k) {
-        r.put_top(out, row, tid, j.best[tid]);
+    } else {
+        for (u32 i = tid; i < k; i += BLOCK) r.put_top(out, row, i, j.best[i]);
     }
 }
 
@@ -460,9 +460,9 @@ __global__ void __launch_bounds__(BLOCK, BLOCK == 96 ? 8 : BLOCK == 128 ? 7 : 1)
 // A block takes UNROLL 16-byte words per thread of a row, counted from the first 16-byte boundary of the gradient's row;
 // the block of a row's first words also takes what lies before it.  SHIFT: the logits' row is not as far from such a
 // boundary as the gradient's, and a word of logits is cut out of the two 16-byte words that hold it; the second is the
-// next thread's first, so it comes from L1 (slack of 3 in 2048 x 50304 bf16: 85 us; value by value it was 162).
+// next thread's first, so it comes from L1 (slack of 3 in 2048 x 50304 bf16: 82 us; value by value it was 162).
 // The last rows come first: they are the ones that a preceding forward pass has left in L2; what is written goes past it.
-// Bound: the bytes (2048 x 50304 bf16: 66 us, 6.2 TB/s).
+// Bound: the bytes (2048 x 50304 bf16: 64 us, 6.4 TB/s).
 template <typename T, bool SHIFT>
 __global__ void __launch_bounds__(GRAD_BLOCK) grad_kernel(const T* logits, u64 rows, u32 vocab, u64 stride, const long long* __restrict__ tokens,
                                                      float scale, const float* __restrict__ row_stats, const float* __restrict__ g_logprob,
@@ -532,27 +532,35 @@ void logprobs_launch(cudaStream_t s, const RowsIn& x, u32 parts, const long long
 
 template <typename T>
 void logprobs_as(int sms, cudaStream_t s, const RowsIn& x, const long long* tokens, float scale, const LogprobsOut& out) {
-    // a cluster per row while rows leave SMs idle
+    // Few rows: 256 threads to a row, or a cluster of such blocks while rows leave SMs idle and each row is long enough to pay for
+    // the cluster's two barriers (1 x 16000 bf16: 8 blocks 4.0 us, one 3.8; 1 x 32000: 4.2 and 4.7; 64 x 32000: 2 blocks 5.5,
+    // one 4.8; 64 x 131072: 8.8 and 11.2).
     u32 parts = 1;
     while (parts < 8 && x.rows * parts * 2 <= (u64)sms) parts *= 2;
-    if (parts > 1) logprobs_launch<T, 256, true>(s, x, parts, tokens, scale, out);
-    else if (x.rows <= (u64)sms * 5) logprobs_launch<T, 256, false>(s, x, 1, tokens, scale, out);
+    if (parts > 1 && x.cols * parts >= 160 * 1024) logprobs_launch<T, 256, true>(s, x, parts, tokens, scale, out);
+    else if (x.rows <= (u64)sms * 3 || (sizeof(T) == 2 && x.rows <= (u64)sms * 5 && x.cols > 16384)) logprobs_launch<T, 256, false>(s, x, 1, tokens, scale, out);
     // Many rows: blocks as small as registers last, so that while one joins its row others stream.  (4096 x 32000 bf16, five
-    // alternatives: 96 threads 61 us, 128 65, 64 63, 256 81; 2048 x 50304 fp32: 128 threads 71 us, 96 74.)
+    // alternatives: 96 threads 62 us, 128 65, 64 63, 256 81; 2048 x 50304 fp32: 128 threads 71 us, 96 74.  600 x 50304 bf16: 256
+    // threads 22 us, 96 25; 600 x 4097: 9.3 and 6.5.)  Short ones: a warp to a row (5056 x 391 fp32: 10 us, 128 threads 19;
+    // 4000 x 3000 bf16 15, 96 threads 19; 2000 x 8200 18 and 15); of up to 32 alternatives, each the maximum of a lane.
+    else if (x.rows > (u64)sms * 8 && x.cols <= 4096 && out.top <= 32) logprobs_launch<T, 32, false>(s, x, 1, tokens, scale, out);
     else logprobs_launch<T, sizeof(T) == 2 ? 96 : 128, false>(s, x, 1, tokens, scale, out);
 }
 
+template <typename T, bool SHIFT>
+void grad_launch(cudaStream_t s, const RowsIn& x, const long long* tokens, float scale, const float* row_stats, const float* g_logprob,
+                 const float* g_entropy, T* grad, u64 grad_stride) {
+    const u32 chunk = GRAD_BLOCK * UNROLL * per16<T>(), chunks = (u32)((x.cols + chunk - 1) / chunk);
+    launch_chained(grad_kernel<T, SHIFT>, (u32)x.rows * chunks, GRAD_BLOCK, 0, 0, s, static_cast<const T*>(x.p), x.rows, (u32)x.cols, x.stride, tokens, scale,
+                   row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
+}
 template <typename T>
 void grad_as(cudaStream_t s, const RowsIn& x, const long long* tokens, float scale, const float* row_stats, const float* g_logprob,
              const float* g_entropy, T* grad, u64 grad_stride) {
-    const T* p = static_cast<const T*>(x.p);
-    const u32 chunk = GRAD_BLOCK * UNROLL * per16<T>(), chunks = (u32)((x.cols + chunk - 1) / chunk);
     // every row of the logits as far from a 16-byte boundary as the gradient's
-    const bool aligned = ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0 &&
-                     (x.rows == 1 || (((x.stride - grad_stride) * sizeof(T)) & 15) == 0);
-    const u32 grid = (u32)x.rows * chunks;
-    if (aligned) launch_chained(grad_kernel<T, false>, grid, GRAD_BLOCK, 0, 0, s, p, x.rows, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
-    else launch_chained(grad_kernel<T, true>, grid, GRAD_BLOCK, 0, 0, s, p, x.rows, (u32)x.cols, x.stride, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride, chunks);
+    const bool aligned = ((reinterpret_cast<uintptr_t>(x.p) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0 &&
+                         (x.rows == 1 || (((x.stride - grad_stride) * sizeof(T)) & 15) == 0);
+    (aligned ? grad_launch<T, false> : grad_launch<T, true>)(s, x, tokens, scale, row_stats, g_logprob, g_entropy, grad, grad_stride);
 }
 
 }  // namespace

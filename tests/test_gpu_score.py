@@ -563,3 +563,36 @@ def test_quantize_and_back_at_every_offset(h, cols, dtype, fmt):
             assert torch.equal(xv, back)
             xv.fill_(77.0)
             assert bool((xs == 77).all())
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("kind", ["normal", "ties", "equal", "masked", "lowest", "peaked"])
+def test_logprobs_of_short_rows_by_the_thousand(h, kind, dtype):
+    """A warp to a row: below, at and above its words; as many alternatives as lanes; one more goes another way."""
+    for rows, vocab, top in ((1500, 3, 3), (1500, 39, 5), (1500, 64, 33), (1300, 301, 32)) + (((1200, 4096, 32),) if kind == "ties" else ()):
+        x = make_logits(rows, vocab, dtype, 177 + vocab, vocab % 2, vocab % 3, kind)
+        check_logprobs(h, x, np.arange(rows) * 7 % vocab, 0.9, top, grad=vocab < 40)
+
+
+def test_short_rows_by_the_thousand_that_hold_nothing_or_nan(h):
+    rows, vocab = 1500, 700
+    x = make_logits(rows, vocab, "bf16", 9).clone()
+    x[0] = -float("inf")
+    x[1, 5] = float("nan")
+    x[2, 699] = float("inf")
+    tokens = np.arange(rows) % vocab
+    tokens[3] = -1
+    r = h.token_logprobs(x, torch.from_numpy(tokens).to(DEV), top=9)
+    want = so.logprobs(dense(x)[:8], tokens[:8], 1.0, 9)
+    lp = r.logprob.cpu().numpy()
+    assert lp[0] == -np.inf and np.isnan(lp[1]) and np.isnan(lp[2]) and lp[3] == 0 and np.isfinite(lp[4:]).all()
+    assert np.array_equal(r.top_index.cpu().numpy()[:8], want["top_index"])
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("kind", ["normal", "ties", "equal", "masked", "lowest", "peaked", "rising"])
+def test_logprobs_of_few_long_rows(h, kind, dtype):
+    """Rows that several blocks share."""
+    for rows, vocab, top in ((1, 20480, 64), (3, 33001, 5)) + (((20, 41003, 20), (40, 90001, 4)) if kind == "normal" else ()):
+        x = make_logits(rows, vocab, dtype, 277 + vocab, vocab % 2, vocab % 3, kind)
+        check_logprobs(h, x, np.arange(rows) * 7777 % vocab, 0.9, top, grad=rows < 3)
