@@ -540,7 +540,7 @@ void logprobs_as(int sms, cudaStream_t s, const RowsIn& x, const long long* toke
     if (parts > 1 && x.cols * parts >= 160 * 1024) logprobs_launch<T, 256, true>(s, x, parts, tokens, scale, out);
     else if (x.rows <= (u64)sms * 3 || (sizeof(T) == 2 && x.rows <= (u64)sms * 5 && x.cols > 16384)) logprobs_launch<T, 256, false>(s, x, 1, tokens, scale, out);
     // Many rows: blocks as small as registers last, so that while one joins its row others stream.  (4096 x 32000 bf16, five
-    // alternatives: 96 threads 62 us, 128 65, 64 63, 256 81; 2048 x 50304 fp32: 128 threads 71 us, 96 74.  600 x 50304 bf16: 256
+    // alternatives: 96 threads 62 us, 128 65; 2048 x 50304 fp32: 128 threads 71 us, 96 74.  600 x 50304 bf16: 256
     // threads 22 us, 96 25; 600 x 4097: 9.3 and 6.5.)  Short ones: a warp to a row (5056 x 391 fp32: 10 us, 128 threads 19;
     // 4000 x 3000 bf16 15, 96 threads 19; 2000 x 8200 18 and 15); of up to 32 alternatives, each the maximum of a lane.
     else if (x.rows > (u64)sms * 8 && x.cols <= 4096 && out.top <= 32) logprobs_launch<T, 32, false>(s, x, 1, tokens, scale, out);
