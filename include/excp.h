@@ -376,9 +376,9 @@ excp_status excp_set_kmeans_margin(excp_handle h, int margin);
  * of their tokens, and leaves the code to them.)  Restored matrices are held in microscaled 4-bit floating
  * point, multiplied with activations, and the logits are turned into log probabilities.
  *
- * These calls only enqueue work: nothing is copied to the host and nothing synchronises (the first call on a
- * handle that needs its little workspace allocates it), so they can be captured in a graph after one ordinary
- * call.  Calls on one handle must be ordered on the device (one stream, or events between streams): they share
+ * These calls only enqueue work: nothing is copied to the host and nothing synchronises (but the first call on a
+ * handle that needs its little workspace, which allocates it, clears it on its stream and waits for that), so they
+ * can be captured in a graph after one ordinary call.  Calls on one handle must be ordered on the device (one stream, or events between streams): they share
  * the workspace.  A matrix in ordinary layout is `rows` rows of `cols` values, `row_stride` values apart
  * (>= cols), aligned to its element; its type is an excp_dtype. */
 typedef enum {

@@ -19,16 +19,22 @@ namespace {
 
 constexpr int SCORE_TOP_MAX = 64;
 
-// The workspace, allocated once.
-bool ensure_score(excp_handle h) {
+// The workspace, allocated once and cleared on the stream of the call that needs it first.  That call waits for the clearing, so
+// that calls on other streams, which nothing orders behind this one, find it done.
+bool ensure_score(excp_handle h, cudaStream_t stream) {
     ScoreWorkspace& w = h->score;
     if (w.d_flag) return true;
-    bool ok = true;
     if (!w.words) {
-        ok = check(h, cudaMalloc(reinterpret_cast<void**>(&w.words), 64));
-        ok = ok && check(h, cudaMemset(w.words, 0, 64));
+        u32* words = nullptr;
+        if (!check(h, cudaMalloc(reinterpret_cast<void**>(&words), 64))) return false;
+        if (!check(h, cudaMemsetAsync(words, 0, 64, stream)) || !check(h, cudaStreamSynchronize(stream))) {
+            cudaFree(words);
+            return false;
+        }
+        w.words = words;
     }
-    if (ok && !w.h_flag) {
+    bool ok = true;
+    if (!w.h_flag) {
         ok = check(h, cudaHostAlloc(reinterpret_cast<void**>(&w.h_flag), 64, cudaHostAllocMapped));
         if (ok) *w.h_flag = 0;
     }
@@ -93,8 +99,9 @@ excp_status excp_mx4_tensor_scale(excp_handle h, const void* x, int dtype, size_
                                   float* scale_out, void* cuda_stream) {
     if (!h || !scale_out || !on_float(scale_out) || !rows_ok(x, dtype, rows, cols, row_stride)) return EXCP_ERR_INVALID_ARG;
     DeviceGuard guard(h->device);
-    if (!guard.ok || !ensure_score(h)) return EXCP_ERR_CUDA;
-    launch_mx4_tensor_scale(h->sms, static_cast<cudaStream_t>(cuda_stream), RowsIn{x, dtype, cols ? rows : 0, cols, row_stride}, h->score.words, scale_out);
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!guard.ok || !ensure_score(h, stream)) return EXCP_ERR_CUDA;
+    launch_mx4_tensor_scale(h->sms, stream, RowsIn{x, dtype, cols ? rows : 0, cols, row_stride}, h->score.words, scale_out);
     return finish(h);
 }
 
@@ -130,9 +137,9 @@ excp_status excp_mx4_matmul(excp_handle h, const void* a, size_t a_rows, const f
         return EXCP_ERR_INVALID_ARG;
     if (a_rows == 0 || b_rows == 0) return EXCP_OK;
     DeviceGuard guard(h->device);
-    if (!guard.ok || !ensure_score(h)) return EXCP_ERR_CUDA;
-    return matmul_impl(h, a, a_rows, a_scale, b, b_rows, b_scale, cols, format, bias, y, y_dtype, y_row_stride,
-                       static_cast<cudaStream_t>(cuda_stream), false);
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!guard.ok || !ensure_score(h, stream)) return EXCP_ERR_CUDA;
+    return matmul_impl(h, a, a_rows, a_scale, b, b_rows, b_scale, cols, format, bias, y, y_dtype, y_row_stride, stream, false);
 }
 
 size_t excp_mx4_linear_scratch(excp_handle h, size_t rows, size_t w_rows, size_t cols, int format) {
@@ -150,8 +157,8 @@ excp_status excp_mx4_linear(excp_handle h, const void* x, int x_dtype, size_t ro
     const bool direct = mx4_linear_in_one(h->sms, rows, w_rows, cols, format);     // no packed x: x_packed is not looked at
     if (!direct && !packed_ok(x_packed, rows, cols, format)) return EXCP_ERR_INVALID_ARG;
     DeviceGuard guard(h->device);
-    if (!guard.ok || !ensure_score(h)) return EXCP_ERR_CUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!guard.ok || !ensure_score(h, stream)) return EXCP_ERR_CUDA;
     if (direct) {
         const Mx4Operand mw{static_cast<const unsigned char*>(w), w_rows, format == MX4_E4M3_16 ? w_scale : nullptr};
         if (!launch_mx4_linear(h->sms, stream, RowsIn{x, x_dtype, rows, cols, x_row_stride}, format == MX4_E4M3_16 ? x_scale : nullptr, mw, format,

@@ -1,0 +1,51 @@
+"""Edges of the scoring operators, through the C ABI, against their 64-bit definitions (oracle/score_oracle.py): where a result
+could be wrong at values, sizes or an order of calls that ordinary use seldom meets.
+
+Tolerances (derived, not fitted) are those of test_gpu_score.py unless a test says its own."""
+import pytest
+import torch
+
+from oracle import score_oracle as so
+from paper_2406_11257_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+DT = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def h():
+    handle = binding.Handle(workspace_numel=4096, device=0)
+    yield handle
+    handle.score_status()
+    handle.close()
+
+
+def device_scale(v):
+    return torch.tensor(float(v), dtype=torch.float32, device=DEV)
+
+
+def test_first_call_of_a_handle_on_a_stream_of_its_own():
+    """The workspace is clear before the first kernel uses it, whatever the default stream is busy with."""
+    x = torch.randn((700, 900), device=DEV)
+    want = so.tensor_scale(x.cpu().numpy())
+    big = torch.empty(1 << 28, dtype=torch.float32, device=DEV)
+    side, third = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        handle = binding.Handle(workspace_numel=4096, device=0)
+        for _ in range(40):                        # about 20 ms of work on the default stream
+            big.zero_()
+        with torch.cuda.stream(side):
+            first = handle.mx4_tensor_scale(x)
+        done = side.record_event()
+        with torch.cuda.stream(third):             # the second call on yet another stream, behind the first
+            third.wait_event(done)
+            second = handle.mx4_tensor_scale(x)
+        third.synchronize()
+        with torch.cuda.stream(third):
+            assert float(first) == float(second) == float(want)
+        torch.cuda.synchronize()
+        assert float(handle.mx4_tensor_scale(x)) == float(want)
+        handle.close()
