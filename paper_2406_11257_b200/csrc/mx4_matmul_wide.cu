@@ -55,6 +55,7 @@ struct Shared {
     unsigned long long ready[stages<FMT>()];       // even CTA: both CTAs' have, and the scales are in tensor memory
     unsigned long long empty[stages<FMT>()];       // the stage has been multiplied
     unsigned long long acc_full, acc_empty;
+    unsigned long long last;                       // everything that was issued is done; one turn only
     u32 tmem;
     volatile u32 abort;
 };
@@ -123,6 +124,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], FETCH_WARPS); mbar_init(&sh.ready[s], 2 * SCALE_WARPS); mbar_init(&sh.empty[s], 1); }
         mbar_init(&sh.acc_full, 1);
+        mbar_init(&sh.last, 1);
         mbar_init(&sh.acc_empty, 2 * STORE_WARPS);
         sh.abort = 0;
         mbar_fence_init();
@@ -214,11 +216,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
                     ring.next();
                 }
             }
-            if (!ok) {                             // what has been issued is done before tensor memory goes
-                if (elect_one()) tm2_commit(&sh.acc_full);
-                __syncwarp();
-                drain_warp(&sh.acc_full, turn & 1);
-            }
+            if (elect_one()) tm2_commit(&sh.last);
+            __syncwarp();
         }
     } else if (warp >= SCALE_WARP) {
         registers_down<DOWN>();
@@ -328,6 +327,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
     __syncwarp();
     tm_fence_before();
     __syncthreads();
+    // What has been issued is done before tensor memory and the CTAs go, also where only the warps that wait for it gave up.
+    // (acc_full cannot say so: while a tile is unfinished, a wait for the next one is met by the one before it.)
+    if (warp == PRODUCT_WARP) drain_warp(&sh.last, 0);
     cluster_barrier();                             // neither CTA's memory is needed any more
     if (warp == PRODUCT_WARP) tm2_dealloc(tmem, TMEM_COLS);
 }

@@ -49,3 +49,28 @@ def test_first_call_of_a_handle_on_a_stream_of_its_own():
         torch.cuda.synchronize()
         assert float(handle.mx4_tensor_scale(x)) == float(want)
         handle.close()
+
+
+@pytest.mark.parametrize("fmt", ["e8m0_32", "e4m3_16"])
+@pytest.mark.parametrize("rows,k,n", [(40, 4096, 700), (300, 4096, 700), (1100, 4096, 6000)])
+def test_waits_that_run_out_in_the_middle(h, rows, k, n, fmt):
+    """Limits at which some waits are met and others are not: a result is right or reported, and the calls behind it are right."""
+    x = torch.randn((rows, k), generator=torch.Generator().manual_seed(11)).to(torch.bfloat16).to(DEV)
+    m = h.mx4_quantize(torch.randn((n, k), generator=torch.Generator().manual_seed(12)).to(DEV), fmt)
+    want = h.mx4_linear(x, m)
+    try:
+        for limit in (1, 2000, 10000, 30000, 100000):
+            h.set_wait_limit(limit)
+            y = h.mx4_linear(x, m)
+            reported = False
+            try:
+                h.score_status()
+            except binding.ExcpError as e:
+                assert e.status == -7
+                reported = True
+            assert reported or torch.equal(y, want)
+            h.set_wait_limit(2_000_000_000)
+            assert torch.equal(h.mx4_linear(x, m), want)
+            h.score_status()
+    finally:
+        h.set_wait_limit(2_000_000_000)
