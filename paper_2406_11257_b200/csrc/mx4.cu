@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 2 ? 6 : 4) quantize_k
         if (at.row0 + 32 * c >= rows || c0 / B * B >= cols) byte = 0;
         // lane `part` has half a chunk of 16 bytes
         if (r < at.height)
-            *reinterpret_cast<uint2*>(dst + r * 128 + (((part >> 1) ^ (r & 7)) << 4) + ((part & 1) << 3)) = make_uint2(e2m1x8(f), e2m1x8(f + 8));
+            *reinterpret_cast<uint2*>(dst + r * 128 + (((part >> 1) ^ (r & 7)) << 4) + ((part & 1) << 3)) = make_uint2(codes_of<FMT>(f), codes_of<FMT>(f + 8));
         // the bytes of four blocks as a word
         constexpr u32 STEP = (u32)mx4_block(FMT) / 16;          // lanes to a block
         u32 word = byte | __shfl_xor_sync(0xffffffffu, byte, STEP) << 8;

@@ -45,6 +45,8 @@ __device__ __forceinline__ u32 scale_e8m0(float (&v)[N], u32 m) {
     for (int k = 0; k < N; k += 2) f2_unpack(f2_mul(f2_pack(v[k], v[k + 1]), inv2), v[k], v[k + 1]);
     return (u32)(e + 127);
 }
+// The same for blocks of 16, but the quotients come out with the other sign (codes_of puts it right): one step from a negative
+// reciprocal keeps the sign of a zero, one from a positive reciprocal makes -0 a +0.
 template <int N>
 __device__ __forceinline__ u32 scale_e4m3(float (&v)[N], u32 m, float g, float six_g) {
     u32 byte = 0x7fu;
@@ -57,8 +59,8 @@ __device__ __forceinline__ u32 scale_e4m3(float (&v)[N], u32 m, float g, float s
     if (sg >= 0x1p-80f && sg <= 0x1p80f && __uint_as_float(m) < 0x1p20f * sg) {
         // The rounded quotient from the rounded reciprocal: one step with the exact remainder (Markstein 1990).  Without it a
         // value halfway between two codes could fall to the wrong side.
-        const float r = __frcp_rn(sg);
-        const u64 r2 = f2_pack(r, r), d2 = f2_pack(-sg, -sg);
+        const float r = -__frcp_rn(sg);
+        const u64 r2 = f2_pack(r, r), d2 = f2_pack(sg, sg);
 #pragma unroll
         for (int k = 0; k < N; k += 2) {
             const u64 x = f2_pack(v[k], v[k + 1]), q = f2_mul(x, r2);
@@ -66,9 +68,15 @@ __device__ __forceinline__ u32 scale_e4m3(float (&v)[N], u32 m, float g, float s
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = sg > 0.f ? __fdiv_rn(v[k], sg) : 0.f;
+        for (int k = 0; k < N; ++k) v[k] = sg > 0.f ? __fdiv_rn(v[k], -sg) : -0.f;
     }
     return byte;
+}
+
+// Eight codes of what scale_e8m0 or scale_e4m3 left.
+template <int FMT>
+__device__ __forceinline__ u32 codes_of(const float* t) {
+    return FMT == MX4_E4M3_16 ? e2m1x8(t) ^ 0x88888888u : e2m1x8(t);
 }
 
 // Four scale bytes of a row as one word: block k's byte is held by the lanes around 8-value group src + k * PER.

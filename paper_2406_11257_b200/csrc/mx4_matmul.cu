@@ -83,7 +83,7 @@ __device__ __forceinline__ void quantize_row(float (&v)[8], u32 r, u32 lane, flo
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     if (FMT == MX4_E8M0_32) top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const u32 byte = FMT == MX4_E8M0_32 ? scale_e8m0(v, top) : scale_e4m3(v, top, gx, 6.f * gx);
-    *reinterpret_cast<u32*>(codes + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + ((lane & 3) << 2)) = e2m1x8(v);
+    *reinterpret_cast<u32*>(codes + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + ((lane & 3) << 2)) = codes_of<FMT>(v);
     constexpr u32 PER = mx4_block(FMT) / 8, PIECES = mx4_pieces(FMT);
     const u32 piece = min(lane, PIECES - 1);
     const u32 word = scale_word<FMT>(byte, piece * 4 * PER);

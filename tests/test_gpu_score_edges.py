@@ -2,6 +2,7 @@
 could be wrong at values, sizes or an order of calls that ordinary use seldom meets.
 
 Tolerances (derived, not fitted) are those of test_gpu_score.py unless a test says its own."""
+import numpy as np
 import pytest
 import torch
 
@@ -74,3 +75,19 @@ def test_waits_that_run_out_in_the_middle(h, rows, k, n, fmt):
             h.score_status()
     finally:
         h.set_wait_limit(2_000_000_000)
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("scale", [None, 0.7, 2.0 ** -20, 2.0 ** 90])
+def test_zeros_keep_their_sign_among_other_values(h, scale, dtype):
+    """Code 8 for -0, also where the block's scale is not 0 (a scale of 2^90 takes the division, the others the reciprocal)."""
+    g = torch.Generator().manual_seed(61)
+    x = torch.randn((37, 330), generator=g)
+    if scale == 2.0 ** 90 and dtype != "fp16":
+        x = x * 2.0 ** 90
+    x[:, ::3] = -0.0
+    x[:, 1::7] = 0.0
+    x = x.to(DT[dtype]).to(DEV)
+    m = h.mx4_quantize(x, "e4m3_16", tensor_scale=None if scale is None else device_scale(scale))
+    codes, scales = so.quantize(x.to(torch.float32).cpu().numpy(), "e4m3_16", scale)
+    assert np.array_equal(m.data.cpu().numpy(), so.pack(codes, scales, "e4m3_16"))
