@@ -413,7 +413,8 @@ typedef enum {
 size_t excp_mx4_bytes(size_t rows, size_t cols, int format);
 
 /* Tensor scale of a matrix: its largest finite magnitude / (6 * 448), rounded up to 8 significant bits (the
- * products with the block scales are then exact); 1 for a matrix of zeros.  scale_out: device, one float. */
+ * products with the block scales are then exact, unless they are subnormal); 1 where that is 0, as for a matrix of zeros.
+ * scale_out: device, one float. */
 excp_status excp_mx4_tensor_scale(excp_handle h, const void* x, int dtype, size_t rows, size_t cols, size_t row_stride,
                                   float* scale_out, void* cuda_stream);
 

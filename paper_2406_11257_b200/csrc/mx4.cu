@@ -142,8 +142,10 @@ __global__ void __launch_bounds__(256) tensor_scale_kernel(const T* __restrict__
     best = atomicExch(&words[0], 0u);
     words[1] = 0;
     const float q = __fdiv_rn(__uint_as_float(best), 2688.f);
-    // 8 significant bits = the upper half of the pattern; q > 0 keeps at least one
-    scale_out[0] = q > 0.f ? __uint_as_float((__float_as_uint(q) + 0xffffu) & 0xffff0000u) : 1.f;
+    // 8 significant bits: the upper half of the pattern, or of a subnormal's the 8 from its leading one on; a carry is right as it is
+    const u32 bits = __float_as_uint(q);
+    const u32 low = (1u << (bits >= 0x00800000u ? 16 : max(24 - __clz(bits), 0))) - 1u;
+    scale_out[0] = q > 0.f ? __uint_as_float((bits + low) & ~low) : 1.f;
 }
 
 // Where a warp works: tile (rt, ct), rows l + 32 c.  A tile is four blocks of eight warps.  (Four values of l to a warp, and

@@ -91,3 +91,14 @@ def test_zeros_keep_their_sign_among_other_values(h, scale, dtype):
     m = h.mx4_quantize(x, "e4m3_16", tensor_scale=None if scale is None else device_scale(scale))
     codes, scales = so.quantize(x.to(torch.float32).cpu().numpy(), "e4m3_16", scale)
     assert np.array_equal(m.data.cpu().numpy(), so.pack(codes, scales, "e4m3_16"))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("largest", [1e-34, 2688 * 2.0 ** -126, 3e-35, 1e-36, 777.0 * 2.0 ** -126, 1e-40, 2.0 ** -149 * 2688, 2.0 ** -133])
+def test_tensor_scale_of_tiny_matrices(h, largest, dtype):
+    """The quotient is rounded up to 8 significant bits of its own, subnormal or not; a quotient of 0 gives 1."""
+    x = torch.zeros((5, 300))
+    x[3, 7], x[4, 299] = -largest, largest / 3
+    x = x.to(DT[dtype]).to(DEV)
+    want = so.tensor_scale(x.to(torch.float32).cpu().numpy())
+    assert float(h.mx4_tensor_scale(x)) == float(want)
