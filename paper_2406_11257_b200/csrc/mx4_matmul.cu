@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
         tm_fence_after();
     }
 
-    const float alpha = (g.m.scale ? __ldg(g.m.scale) : 1.f) * (g.n.scale ? __ldg(g.n.scale) : 1.f);
+    const TensorScales by = tensor_scales(g.m.scale, g.n.scale);
     const u64 n0 = (u64)ntile * MX4_ROWS;
     const u32 cols = (u32)min((u64)g.nt, g.n.rows - n0);       // of the result
     // thread t of the work warps has row t of m's tile
@@ -274,7 +274,11 @@ __global__ void __launch_bounds__(THREADS, 3) narrow_kernel(const __grid_constan
         if (m >= g.m.rows) return;
         float r[W];
 #pragma unroll
-        for (u32 i = 0; i < W; ++i) r[i] = sum[i] * alpha;
+        for (u32 i = 0; i < W; ++i) r[i] = sum[i] * by.first;
+        if (by.second != 1.f) {
+#pragma unroll
+            for (u32 i = 0; i < W; ++i) r[i] *= by.second;
+        }
         if (g.bias) {
 #pragma unroll
             for (u32 i = 0; i < W; ++i) r[i] += bias;

@@ -259,7 +259,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
         }
     } else {
         registers_up<UP>();
-        const float alpha = (g.m.scale ? __ldg(g.m.scale) : 1.f) * (g.n.scale ? __ldg(g.n.scale) : 1.f);
+        const TensorScales by = tensor_scales(g.m.scale, g.n.scale);
         const u32 quarter = warp & 3, c0 = (warp >> 2) * 128;              // a warp reads the tensor-memory lanes of its place
         u32 turn = 0;
         for (u32 t = pair; t < tiles; t += pairs, ++turn) {
@@ -288,7 +288,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
                 for (u32 p = 0; p < 128; p += PART) {
                     float f[PART];
 #pragma unroll
-                    for (u32 i = 0; i < PART; ++i) f[i] = __uint_as_float(v[p + i]) * alpha;
+                    for (u32 i = 0; i < PART; ++i) f[i] = __uint_as_float(v[p + i]) * by.first;
+                    if (by.second != 1.f) {
+#pragma unroll
+                        for (u32 i = 0; i < PART; ++i) f[i] *= by.second;
+                    }
                     if (g.bias) {
 #pragma unroll
                         for (u32 i = 0; i < PART; ++i) f[i] += bias;
@@ -309,7 +313,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_ker
             for (u32 p = 0; p < 128; p += PART) {
                 float f[PART];
 #pragma unroll
-                for (u32 i = 0; i < PART; ++i) f[i] = __uint_as_float(v[p + i]) * alpha;
+                for (u32 i = 0; i < PART; ++i) f[i] = __uint_as_float(v[p + i]) * by.first;
+                if (by.second != 1.f) {
+#pragma unroll
+                    for (u32 i = 0; i < PART; ++i) f[i] *= by.second;
+                }
                 if (g.bias) {
 #pragma unroll
                     for (u32 i = 0; i < PART; ++i) f[i] += p + i < cols ? __ldg(g.bias + n0 + p + i) : 0.f;

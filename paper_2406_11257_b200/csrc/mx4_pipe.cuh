@@ -37,6 +37,19 @@ __device__ __forceinline__ void drain_warp(unsigned long long* bar, u32 parity) 
     while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)) && !__any_sync(0xffffffffu, global_ns() - t0 > DRAIN_NS)) {}
 }
 
+// The two tensor scales (null = 1) as factors that a sum is multiplied with, one after the other.  Mostly their product and 1;
+// where the product leaves fp32's normal numbers, what brings the sum back to the middle first goes first, so that
+// neither a result that fits is lost nor 0 times infinity is formed.
+struct TensorScales {
+    float first, second;
+};
+__device__ __forceinline__ TensorScales tensor_scales(const float* a, const float* b) {
+    const float x = a ? __ldg(a) : 1.f, y = b ? __ldg(b) : 1.f, both = x * y;
+    if (both >= 0x1p-126f && both <= 0x1.fffffep127f) return TensorScales{both, 1.f};
+    const float low = fminf(x, y), high = fmaxf(x, y);
+    return both < 1.f ? TensorScales{high, low} : TensorScales{low, high};
+}
+
 // The place in the ring of stages, and the parity of its current turn.
 template <int STAGES>
 struct Ring {

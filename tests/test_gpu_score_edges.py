@@ -102,3 +102,36 @@ def test_tensor_scale_of_tiny_matrices(h, largest, dtype):
     x = x.to(DT[dtype]).to(DEV)
     want = so.tensor_scale(x.to(torch.float32).cpu().numpy())
     assert float(h.mx4_tensor_scale(x)) == float(want)
+
+
+SCALES = [(165 / 128 * 2.0 ** -80, 25 / 16 * 2.0 ** -62), (2.0 ** -90, 1.5 * 2.0 ** -62), (1.5 * 2.0 ** -30, 2.0 ** -118), (2.0 ** 70, 1.25 * 2.0 ** 60),
+          (1.5 * 2.0 ** 100, 2.0 ** -120)]
+
+
+@pytest.mark.parametrize("ga,gb", SCALES)
+@pytest.mark.parametrize("rows,k,n", [(1, 500, 300), (40, 320, 200), (300, 256, 300), (1100, 256, 2080), (1100, 256, 2085)])
+def test_product_of_tensor_scales_out_of_range(h, rows, k, n, ga, gb):
+    """The product of the two tensor scales may be subnormal, 0 or infinite in fp32 although the results are not.
+
+    Tolerance: that of the sums (test_gpu_score.py), two roundings by the scales, the last one among subnormals."""
+    gen = torch.Generator().manual_seed(71)
+    xa, xb = torch.randn((rows, k), generator=gen).numpy() * 64, torch.randn((n, k), generator=gen).numpy() * 64
+    xa[rows // 2:rows // 2 + 1, :] = 0 if rows > 1 else xa[0]
+    xb[n // 2] = 0
+    xa, xb = (xa * np.float64(ga)).astype(np.float32), (xb * np.float64(gb)).astype(np.float32)
+    qa, qb = so.quantize(xa, "e4m3_16", ga), so.quantize(xb, "e4m3_16", gb)
+    ma = binding.Mx4Matrix(torch.from_numpy(so.pack(*qa, "e4m3_16")).to(DEV), rows, k, "e4m3_16", device_scale(ga))
+    mb = binding.Mx4Matrix(torch.from_numpy(so.pack(*qb, "e4m3_16")).to(DEV), n, k, "e4m3_16", device_scale(gb))
+    a, b = so.values(*qa, "e4m3_16", ga), so.values(*qb, "e4m3_16", gb)
+    want, mag = a @ b.T, np.abs(a) @ np.abs(b).T
+    tol = (-(-k // 64) + 16) * 2.0 ** -22 * mag + 3 * 2.0 ** -24 * np.abs(want) + 2.0 ** -148
+    most = float(np.finfo(np.float32).max)
+    for y in (h.mx4_matmul(ma, mb, dtype=torch.float32), h.mx4_linear(torch.from_numpy(xa).to(DEV), mb, tensor_scale=device_scale(ga))):
+        got = y.cpu().numpy().astype(np.float64)
+        over = np.abs(want) > 1.01 * most
+        assert np.array_equal(got[over], np.copysign(np.inf, want[over]))
+        fits = np.abs(want) < 0.99 * most
+        assert np.isfinite(got[fits]).all()
+        worst = (np.abs(got - want)[fits] / tol[fits]).max(initial=0.0)
+        assert worst <= 1.0, worst
+    h.score_status()
