@@ -455,7 +455,8 @@ excp_status excp_token_logprobs(excp_handle h, const void* logits, int dtype, si
 /* The gradient of sum_i g_logprob[i] logprob[i] + g_entropy[i] entropy[i] with respect to the logits, in their type:
  *   scale * (g_logprob ([v = token] - p_v) - g_entropy p_v (log p_v + entropy))
  * g_logprob, g_entropy: device fp32 [rows], NULL = 0; row_stats: what excp_token_logprobs wrote for the same logits,
- * tokens and scale.  An ignored token's g_logprob counts as 0.  grad_out may be the logits themselves (same stride). */
+ * tokens and scale.  An ignored token's g_logprob counts as 0; a token >= vocab, whose log probability is NaN, makes its row NaN,
+ * but not where g_logprob is NULL.  grad_out may be the logits themselves (same stride). */
 excp_status excp_token_logprobs_grad(excp_handle h, const void* logits, int dtype, size_t rows, size_t vocab, size_t row_stride,
                                      const long long* tokens, float scale, const float* row_stats, const float* g_logprob,
                                      const float* g_entropy, void* grad_out, size_t grad_row_stride, void* cuda_stream);

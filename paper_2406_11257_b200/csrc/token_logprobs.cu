@@ -474,8 +474,8 @@ __global__ void __launch_bounds__(GRAD_BLOCK) grad_kernel(const T* logits, u64 r
     const u32 chunk = blockIdx.x - (u32)from_end * chunks;
     const float4 st = __ldg(reinterpret_cast<const float4*>(row_stats) + row);
     const long long t = tokens[row];
-    float gl = g_logprob && t >= 0 ? __ldg(g_logprob + row) : 0.f;
-    if (t >= (long long)vocab) gl = __uint_as_float(0x7fffffffu);
+    // nothing without g_logprob, whatever the token; NaN for one past the vocabulary
+    const float gl = !g_logprob || t < 0 ? 0.f : t < (long long)vocab ? __ldg(g_logprob + row) : __uint_as_float(0x7fffffffu);
     const float gh = g_entropy ? __ldg(g_entropy + row) : 0.f;
     const bool empty = st.x == NEG_INF && st.y == 0.f;
     const float c = scale * LOG2E, inv = scale / st.y;

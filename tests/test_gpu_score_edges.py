@@ -135,3 +135,23 @@ def test_product_of_tensor_scales_out_of_range(h, rows, k, n, ga, gb):
         worst = (np.abs(got - want)[fits] / tol[fits]).max(initial=0.0)
         assert worst <= 1.0, worst
     h.score_status()
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_gradient_of_a_token_past_the_vocabulary(h, dtype):
+    """Its log probability is NaN, and so is the gradient of its row where there is a g_logprob; the entropy does not
+    depend on the token."""
+    vocab = 903
+    x = (torch.randn((5, vocab), generator=torch.Generator().manual_seed(81)) * 3).to(DT[dtype]).to(DEV)
+    tokens = torch.tensor([3, vocab, -1, 1 << 40, 7], device=DEV)
+    inside = torch.tensor([3, 0, -1, 0, 7], device=DEV)
+    gl, gh = torch.randn(5, device=DEV), torch.randn(5, device=DEV)
+    r, s = h.token_logprobs(x, tokens), h.token_logprobs(x, inside)
+    assert torch.isnan(r.logprob).tolist() == [False, True, False, True, False]
+    assert torch.equal(r.entropy, s.entropy)
+    assert torch.equal(h.token_logprobs_grad(x, tokens, r, None, gh), h.token_logprobs_grad(x, inside, s, None, gh))
+    assert not h.token_logprobs_grad(x, tokens, r, None, None).any()
+    got, other = h.token_logprobs_grad(x, tokens, r, gl, gh), h.token_logprobs_grad(x, inside, s, gl, gh)
+    assert torch.isnan(got[1]).all() and torch.isnan(got[3]).all()
+    for i in (0, 2, 4):
+        assert torch.equal(got[i], other[i])
