@@ -444,10 +444,12 @@ excp_status excp_mx4_linear(excp_handle h, const void* x, int x_dtype, size_t ro
  *   entropy_out[i]   - sum p log p (may be NULL)
  *   top_*_out        [rows, top], top <= 64 and <= vocab: the largest logits' log probabilities and indices,
  *                    in descending order; equal logits (-0 and 0 are equal) by ascending index
- *   row_stats_out    [rows, 4], 16-byte aligned, for the gradient (may be NULL): m, S, entropy, 0
+ *   row_stats_out    [rows, 4], 16-byte aligned, for the gradient (may be NULL): the largest logit as it is (m / scale, not m),
+ *                    S, entropy, 0
  * A logit of -infinity has probability 0 and adds nothing to the entropy.  A row of nothing else has log
  * probabilities -infinity, entropy 0 and gradient 0.  A row with a NaN or +infinity gives NaN; a NaN counts as the largest
- * logit.  tokens: device int64 [rows]. */
+ * logit.  Differences of logits are taken before they are scaled: one past fp32's range (a row that holds values beyond 1.7e38 of
+ * both signs) counts as infinite.  tokens: device int64 [rows]. */
 excp_status excp_token_logprobs(excp_handle h, const void* logits, int dtype, size_t rows, size_t vocab, size_t row_stride,
                                 const long long* tokens, float scale, int top, float* logprob_out, float* entropy_out,
                                 float* row_stats_out, float* top_logprob_out, long long* top_index_out, void* cuda_stream);

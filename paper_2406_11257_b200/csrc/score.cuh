@@ -82,7 +82,7 @@ bool launch_mx4_matmul_wide(int sms, cudaStream_t s, const Mx4Operand& a, const 
 struct LogprobsOut {
     float* logprob;
     float* entropy;
-    float* row_stats;                // 4 per row: maximum, sum of exp, entropy, 0
+    float* row_stats;                // 4 per row: largest logit (not scaled), sum of exp, entropy, 0
     int top;
     float* top_logprob;
     long long* top_index;

@@ -155,3 +155,17 @@ def test_gradient_of_a_token_past_the_vocabulary(h, dtype):
     assert torch.isnan(got[1]).all() and torch.isnan(got[3]).all()
     for i in (0, 2, 4):
         assert torch.equal(got[i], other[i])
+
+
+@pytest.mark.parametrize("rows,vocab", [(3, 901), (2, 131072), (1500, 300)])
+def test_row_statistics_are_of_the_logits_before_scaling(h, rows, vocab):
+    """What a C caller may read: the largest logit itself, the sum of exp(scale (x - largest)), the entropy, 0."""
+    x = torch.randn((rows, vocab), generator=torch.Generator().manual_seed(83)).to(DEV) * 4
+    r = h.token_logprobs(x, torch.zeros(rows, dtype=torch.int64, device=DEV), scale=0.6)
+    stats = r.row_stats.cpu()
+    xd = x.double().cpu()
+    assert torch.equal(stats[:, 0], x.max(1).values.cpu())
+    want = torch.exp(float(np.float32(0.6)) * (xd - xd.max(1, keepdim=True).values)).sum(1)
+    # a sum of positive terms: exp of a rounded argument of at most 40, and the chain of additions
+    assert ((stats[:, 1].double() - want).abs() <= want * (40 * 2.0 ** -22 + (vocab / 256 + 64) * 2.0 ** -24)).all()
+    assert torch.equal(stats[:, 2], r.entropy.cpu()) and not stats[:, 3].any()
