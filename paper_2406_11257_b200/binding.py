@@ -5,6 +5,7 @@ the library cannot be loaded the import of this module's handle fails loudly."""
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 from dataclasses import dataclass
 
@@ -69,12 +70,23 @@ class Params:
 _SCORE_CALLS = ["excp_mx4_bytes", "excp_mx4_tensor_scale", "excp_mx4_quantize", "excp_mx4_dequantize", "excp_mx4_matmul",
                 "excp_mx4_linear_scratch", "excp_mx4_linear", "excp_token_logprobs", "excp_token_logprobs_grad"]
 _lib = None
-_score = None
+
+
+class _NotLoaded:
+    """Stands for the native half of the binding until a scoring call asks for it."""
+
+    def __getattr__(self, name: str):
+        if name.startswith("__"):
+            raise AttributeError(name)
+        return getattr(load_scoring(), name)
+
+
+_score = _NotLoaded()
 
 
 def load_library() -> C.CDLL:
     """Loads (building first if the sources are newer) libexcp.so and declares the prototypes."""
-    global _lib, _score
+    global _lib
     if _lib is not None:
         return _lib
     path = _build.build()
@@ -137,12 +149,22 @@ def load_library() -> C.CDLL:
     for name in EXPORTS:
         if getattr(lib, name).restype is C.c_int:
             getattr(lib, name).restype = C.c_int
-    _build.build_binding()
-    from . import _score as native
-    native.bind(*[C.cast(getattr(lib, name), vp).value for name in _SCORE_CALLS], ExcpError)
-    _score = native
     _lib = lib
     return lib
+
+
+def load_scoring():
+    """Loads (compiling it first if need be) the native half of the binding, which the scoring calls go through.  The first of them
+    does so by itself; what compresses and restores needs neither it nor a host compiler."""
+    global _score
+    if isinstance(_score, _NotLoaded):
+        lib = load_library()
+        spec = importlib.util.spec_from_file_location(__package__ + "._score", _build.build_binding())
+        native = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(native)
+        native.bind(*[C.cast(getattr(lib, name), C.c_void_p).value for name in _SCORE_CALLS], ExcpError)
+        _score = native
+    return _score
 
 
 def _ptr(t: torch.Tensor | None) -> int:

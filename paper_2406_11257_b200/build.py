@@ -1,5 +1,5 @@
 """Builds the CUDA library in-tree: csrc/*.cu -> libexcp.so (sm_100a only), and the native half of the Python
-binding: csrc/score_binding.cpp -> _score.so (against the installed torch)."""
+binding of the scoring calls: csrc/score_binding.cpp -> _score-<hash>.so (against the installed torch)."""
 from __future__ import annotations
 
 import hashlib
@@ -42,10 +42,18 @@ def _stale(lib: str) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
-def build_binding(force: bool = False) -> str:
-    """Compiles _score.so if it is missing or older than its sources; returns its path."""
+def binding_path() -> str:
+    """The native half of the scoring calls' binding.  Its name carries what it is compiled against: under another Python
+    or torch it is another file, and neither takes the other's."""
     import torch
-    out = os.path.join(HERE, "_score.so")
+    key = f"{sysconfig.get_config_var('SOABI')} {torch.__version__} {int(torch._C._GLIBCXX_USE_CXX11_ABI)}"
+    return os.path.join(HERE, "_score-" + hashlib.sha1(key.encode()).hexdigest()[:8] + ".so")
+
+
+def build_binding(force: bool = False) -> str:
+    """Compiles binding_path() if it is missing or older than its sources; returns it."""
+    import torch
+    out = binding_path()
     deps = [os.path.join(CSRC, "score_binding.cpp"), os.path.join(os.path.dirname(HERE), "include", "excp.h")]
     if not force and os.path.exists(out) and all(os.path.getmtime(d) <= os.path.getmtime(out) for d in deps):
         return out
