@@ -169,3 +169,12 @@ def test_row_statistics_are_of_the_logits_before_scaling(h, rows, vocab):
     # a sum of positive terms: exp of a rounded argument of at most 40, and the chain of additions
     assert ((stats[:, 1].double() - want).abs() <= want * (40 * 2.0 ** -22 + (vocab / 256 + 64) * 2.0 ** -24)).all()
     assert torch.equal(stats[:, 2], r.entropy.cpu()) and not stats[:, 3].any()
+
+
+def test_results_hold_no_more_memory_than_their_own(h):
+    x = torch.randn((50, 700), device=DEV)
+    r = h.token_logprobs(x, torch.zeros(50, dtype=torch.int64, device=DEV), top=20)
+    for name in ("logprob", "entropy", "top_logprob", "top_index", "row_stats"):
+        t = getattr(r, name)
+        assert t.untyped_storage().nbytes() == t.numel() * t.element_size(), name
+        assert t.storage_offset() == 0 and t.is_contiguous()
