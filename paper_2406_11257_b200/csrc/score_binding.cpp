@@ -11,6 +11,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <climits>
 #include <stdexcept>
 #include <string>
 
@@ -197,6 +198,7 @@ PyObject* logprobs(PyObject* const* a) {
     const int64_t r = (int64_t)x.rows;
     const long long* tokens = static_cast<long long*>(vector(a[3], device, at::kLong, r, "tokens"));
     const int64_t k = top > 0 && top <= (1 << 20) ? top : 0;
+    const int number = top < 0 || top > INT_MAX ? -1 : (int)top;           // what does not fit is refused, not cut
     at::Tensor stats, lp, h, tl, ti;
     if (r * (24 + 12 * k) <= ONE_BLOCK) {
         // one allocation: row statistics first (16 bytes a row), then 8-byte places, then the other floats
@@ -218,7 +220,7 @@ PyObject* logprobs(PyObject* const* a) {
         lp = fresh({r}, at::kFloat, device);
         h = fresh({r}, at::kFloat, device);
     }
-    check(api.token_logprobs(handle(a[0]), x.p, x.dtype, x.rows, x.cols, x.stride, tokens, (float)scale, (int)top, static_cast<float*>(lp.data_ptr()),
+    check(api.token_logprobs(handle(a[0]), x.p, x.dtype, x.rows, x.cols, x.stride, tokens, (float)scale, number, static_cast<float*>(lp.data_ptr()),
                              static_cast<float*>(h.data_ptr()), static_cast<float*>(stats.data_ptr()), tl.defined() ? static_cast<float*>(tl.data_ptr()) : nullptr,
                              ti.defined() ? static_cast<long long*>(ti.data_ptr()) : nullptr, stream(device)), "excp_token_logprobs");
     PyObject* out = PyTuple_New(5);

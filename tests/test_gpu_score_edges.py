@@ -178,3 +178,10 @@ def test_results_hold_no_more_memory_than_their_own(h):
         t = getattr(r, name)
         assert t.untyped_storage().nbytes() == t.numel() * t.element_size(), name
         assert t.storage_offset() == 0 and t.is_contiguous()
+
+
+@pytest.mark.parametrize("top", [1 << 32, (1 << 32) + 3, -(1 << 32), 1 << 40, (1 << 31) + 1])
+def test_numbers_of_alternatives_past_32_bits_are_refused(h, top):
+    with pytest.raises(binding.ExcpError) as e:
+        h.token_logprobs(torch.ones((4, 64), device=DEV), torch.zeros(4, dtype=torch.int64, device=DEV), top=top)
+    assert e.value.status == -1
