@@ -185,3 +185,27 @@ def test_numbers_of_alternatives_past_32_bits_are_refused(h, top):
     with pytest.raises(binding.ExcpError) as e:
         h.token_logprobs(torch.ones((4, 64), device=DEV), torch.zeros(4, dtype=torch.int64, device=DEV), top=top)
     assert e.value.status == -1
+
+
+def test_gradient_past_32_bit_offsets(h):
+    """2.2e9 half-precision logits: the last rows lie past element 2^31 and byte 2^32 of what is read and of what is written."""
+    rows, vocab = 17000, 131000
+    x = torch.zeros((rows, vocab), dtype=torch.float16, device=DEV)
+    gen = torch.Generator().manual_seed(91)
+    x[-2:] = (torch.randn((2, vocab), generator=gen) * 3).to(torch.float16).to(DEV)
+    tokens = torch.full((rows,), 77, device=DEV)
+    last = x[-2:].to(torch.float32).cpu().numpy()
+    r = h.token_logprobs(x, tokens)
+    gl, gh = torch.ones(rows, device=DEV), torch.full((rows,), 0.5, device=DEV)
+    h.token_logprobs_grad(x, tokens, r, gl, gh, out=x)
+    wg = so.logprobs_grad(last, [77, 77], 1.0, [1.0, 1.0], [0.5, 0.5])
+    p = so.logprobs(last, [77, 77])["p"]
+    # fp32: log p and the entropy are off by (chain + reach) 2^-22, p by as much of itself; then half an ulp of fp16
+    tol = np.abs(wg) * 2.0 ** -11 + p * 40 * (vocab / 256 + 100) * 2.0 ** -24 + 2.0 ** -25
+    tol[:, 77] += 2.0 ** -22
+    got = x[-2:].to(torch.float32).cpu().numpy().astype(np.float64)
+    assert (np.abs(got - wg) <= tol).all()
+    even = so.logprobs_grad(np.zeros((1, vocab)), [77], 1.0, [1.0], [0.5])
+    for i in (0, 100, 16390):                      # 16390: the row that holds element 2^31
+        assert (np.abs(x[i:i + 1].to(torch.float32).cpu().numpy() - even) <= np.abs(even) * 2.0 ** -10 + 2.0 ** -24).all()
+    del x
