@@ -28,9 +28,11 @@ constexpr int STAGES = 3;
 constexpr u32 CODES = MX4_ROWS * 128;
 constexpr u32 MAX_SPLIT = 8;
 constexpr u32 RAW_TASKS = 24;                      // plain rows x column tiles that a CTA quantises itself
-constexpr u32 SMEM_MAX = 227 * 1024 - 1024;      // dynamic shared memory of a block, beside what the kernel has of its own
-constexpr u32 RAW_MAX = 96 * 1024;                 // shared memory for plain rows that are quantised in the product
 constexpr u32 RAW_ROWS = 16;                       // and at most so many (at most 32: one column of tensor memory holds their scales)
+constexpr u32 SMEM_MAX = 227 * 1024 - 1024;        // dynamic shared memory of a block, beside what the kernel has of its own
+// Shared memory that the rows a CTA quantises take at most: rounding up to 8 makes them 8 times as many where there is one.
+constexpr u32 RAW_BYTES = 8 * RAW_TASKS * (128 + mx4_pieces(MX4_E4M3_16) * 4);
+static_assert(STAGES * (CODES + mx4_scale_bytes(MX4_E4M3_16)) + 1024 + (RAW_ROWS + MAX_SPLIT) * MX4_ROWS * 4 + 1024 + RAW_BYTES <= SMEM_MAX, "shared memory of the fused product");
 
 struct NarrowArgs {
     Mx4Operand m;                                  // M side
@@ -432,10 +434,10 @@ bool launch_mx4_matmul(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Op
     return launch_narrow(sms, s, a, nullptr, b, cols, fmt, r, wait_ns, flag, behind);
 }
 
-bool mx4_linear_in_one(int sms, u64 rows, u64 w_rows, u64 cols, int fmt) {
+bool mx4_linear_in_one(int sms, u64 rows, u64 w_rows, u64 cols) {
     if (rows > RAW_ROWS) return false;
     const u32 nt = (u32)((rows + 7) & ~7ull), ct = mx4_col_tiles(cols), parts = split(sms, mx4_row_tiles(w_rows), 1, nt, ct);
-    return rows * ((ct + parts - 1) / parts) <= RAW_TASKS && raw_bytes(nt, ct, parts, fmt) <= RAW_MAX;
+    return rows * ((ct + parts - 1) / parts) <= RAW_TASKS;
 }
 
 bool launch_mx4_linear(int sms, cudaStream_t s, const RowsIn& x, const float* x_scale, const Mx4Operand& w, int fmt,

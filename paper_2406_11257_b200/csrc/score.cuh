@@ -72,8 +72,8 @@ struct Mx4Result {
 bool launch_mx4_matmul(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
                        const Mx4Result& r, u64 wait_ns, u32* flag, bool behind);
 
-// x quantised within the product: where mx4_linear_in_one says so (few rows, and their columns fit shared memory).
-bool mx4_linear_in_one(int sms, u64 rows, u64 w_rows, u64 cols, int fmt);
+// x quantised within the product: where mx4_linear_in_one says so (few rows of few columns to a CTA).
+bool mx4_linear_in_one(int sms, u64 rows, u64 w_rows, u64 cols);
 bool launch_mx4_linear(int sms, cudaStream_t s, const RowsIn& x, const float* x_scale, const Mx4Operand& w, int fmt,
                        const Mx4Result& r, u64 wait_ns, u32* flag);
 bool launch_mx4_matmul_wide(int sms, cudaStream_t s, const Mx4Operand& a, const Mx4Operand& b, u64 cols, int fmt,
@@ -110,18 +110,6 @@ __device__ __forceinline__ void load8(const T* p, float v[8]) {
     const T* h = reinterpret_cast<const T*>(&a);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = wget(h, k);
-}
-__device__ __forceinline__ void store8(float* p, const float v[8]) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float v[8]) {
-    uint4 a;
-    T* h = reinterpret_cast<T*>(&a);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) wput(h, k, v[k]);
-    *reinterpret_cast<uint4*>(p) = a;
 }
 
 // 16 bytes from byte `shift` (0 .. 15) of the 32 that a and b hold.

@@ -143,7 +143,7 @@ excp_status excp_mx4_matmul(excp_handle h, const void* a, size_t a_rows, const f
 }
 
 size_t excp_mx4_linear_scratch(excp_handle h, size_t rows, size_t w_rows, size_t cols, int format) {
-    if (!h || !rows || !w_rows || mx4_linear_in_one(h->sms, rows, w_rows, cols, format)) return 0;
+    if (!h || !rows || !w_rows || mx4_linear_in_one(h->sms, rows, w_rows, cols)) return 0;
     return excp_mx4_bytes(rows, cols, format);
 }
 
@@ -154,7 +154,7 @@ excp_status excp_mx4_linear(excp_handle h, const void* x, int x_dtype, size_t ro
         !packed_ok(w, w_rows, cols, format) || !product_ok(rows, w_rows, x_scale, w_scale, bias, y, y_dtype, y_row_stride))
         return EXCP_ERR_INVALID_ARG;
     if (rows == 0 || w_rows == 0) return EXCP_OK;
-    const bool direct = mx4_linear_in_one(h->sms, rows, w_rows, cols, format);     // no packed x: x_packed is not looked at
+    const bool direct = mx4_linear_in_one(h->sms, rows, w_rows, cols);     // no packed x: x_packed is not looked at
     if (!direct && !packed_ok(x_packed, rows, cols, format)) return EXCP_ERR_INVALID_ARG;
     DeviceGuard guard(h->device);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);

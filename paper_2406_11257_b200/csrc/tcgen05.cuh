@@ -39,15 +39,6 @@ __device__ __forceinline__ void tm_commit(unsigned long long* bar) {
 __device__ __forceinline__ uint64_t desc_swizzled(uint32_t addr) {
     return (uint64_t)((addr >> 4) & 0x3fffu) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-// 32 rows of 16 bytes one after another (eight-row groups 128 bytes apart): scales on their way to tensor memory.
-__device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
-    return (uint64_t)((addr >> 4) & 0x3fffu) | (1ull << 16) | (8ull << 32) | (1ull << 46);
-}
-
-// 512 bytes of scales -> four columns of tensor memory, repeated in its four groups of 32 lanes.
-__device__ __forceinline__ void tm_copy_scales(uint32_t tmem, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-}
 
 // D (+)= A B^T over 64 columns of 4-bit floats with their scales: 4 x 8-bit floats (blocks of 16) per row ...
 __device__ __forceinline__ void tm_mma_block16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t add) {

@@ -165,7 +165,7 @@ struct Joint {                                     // shared memory of a block
     float m[BLOCK / 32], s[BLOCK / 32], t[BLOCK / 32];
     u32 warp_bound[BLOCK / 32];
     Sums sums;                                     // the block's
-    u32 owners[2], count[2];                       // of this row and, being reset, of the next
+    u32 owners, count;                             // slots that hold candidates, candidates
     unsigned short step_key[SLOTS][BLOCK];         // upper half of the key of every slot's (one or more steps') maximum
     unsigned short owner[OWNERS];                  // slot << 8 | thread of the slots that hold candidates
 };
@@ -270,8 +270,8 @@ struct Walk {
     }
 
     // Joins the block: a becomes its sums, and with k > 0 its alternatives are either in list[0..count), to be ranked, or (true)
-    // in best[].  `turn`: which of the counters.
-    __device__ __forceinline__ bool join(Joint<BLOCK>& j, u32 k, float c, u32 turn, u32& count) {
+    // in best[].
+    __device__ __forceinline__ bool join(Joint<BLOCK>& j, u32 k, float c, u32& count) {
         constexpr u32 WARPS = BLOCK / 32;
         const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
         if (has_head) { const float v[1] = {head}; add_many(a, v, head, c); }
@@ -305,7 +305,7 @@ struct Walk {
         auto push = [&](float v, u32 i) {
             const u64 key = order_key(v, i);
             if ((u32)(key >> 48) < bound) return;
-            const u32 at = atomicAdd(&j.count[turn], 1u);
+            const u32 at = atomicAdd(&j.count, 1u);
             if (at < LIST) j.list[at] = key;
         };
         const u32 tail = w.body + w.nvec * N;
@@ -314,10 +314,9 @@ struct Walk {
                 bound = 0xffffu;
                 for (u32 i = 0; i < full; ++i) bound = min(bound, j.warp_bound[i]);
             }
-            if (tid == 0) j.owners[turn ^ 1] = j.count[turn ^ 1] = 0;
             for (u32 o = 0; (u64)o * per_slot * STEP + tid < w.nvec; ++o) {
                 if (j.step_key[o][tid] < bound) continue;
-                const u32 at = atomicAdd(&j.owners[turn], 1u);
+                const u32 at = atomicAdd(&j.owners, 1u);
                 if (at < OWNERS) j.owner[at] = (unsigned short)(o << 8 | tid);
             }
             if (has_head) push(head, w.lo + tid);
@@ -331,7 +330,7 @@ struct Walk {
         if (!k) return false;
         // the slots that reach the bound are read again, all their words at once
         const uint4* body = reinterpret_cast<const uint4*>(w.x + w.body);
-        const u32 owners = j.owners[turn], per = per_slot * U, total = min(owners, (u32)OWNERS) * per;
+        const u32 owners = j.owners, per = per_slot * U, total = min(owners, (u32)OWNERS) * per;
         for (u32 it = tid; it < total; it += BLOCK) {
             const u32 o = it / per, r = it - o * per, who = j.owner[o];
             const u32 i = ((who >> 8) * per_slot * U + r) * BLOCK + (who & 255u);
@@ -343,7 +342,7 @@ struct Walk {
             for (u32 e = 0; e < N; ++e) push(v[e], w.body + i * N + e);
         }
         __syncthreads();
-        count = j.count[turn];
+        count = j.count;
         if (a.s == a.s && owners <= OWNERS && count <= LIST) return false;
         top_by_rounds<T, BLOCK>(j, w.x, w.lo, w.hi, k);
         return true;
@@ -393,7 +392,7 @@ __global__ void __launch_bounds__(BLOCK, BLOCK == 128 ? 7 : 768 / BLOCK) logprob
         token = tokens[row];
         at_token = token_logit(x, token, vocab);
     }
-    if (tid == 0) j.owners[0] = j.count[0] = 0;
+    if (tid == 0) j.owners = j.count = 0;
     for (u32 i = tid; i < k; i += BLOCK) j.best[i] = 0;
     Walk<T, BLOCK, U> walk;
     walk.start(share_of(x, vocab, part, parts), c);
@@ -413,7 +412,7 @@ __global__ void __launch_bounds__(BLOCK, BLOCK == 128 ? 7 : 768 / BLOCK) logprob
         for (int u = 0; u < U; ++u) q[u] = next[u];
     }
     u32 count = 0;
-    bool listed = !walk.join(j, k, c, 0, count);
+    bool listed = !walk.join(j, k, c, count);
     Sums a = walk.a;
     if constexpr (CLUSTER) {
         cg::cluster_group cluster = cg::this_cluster();
