@@ -241,7 +241,9 @@ class Mx4Matrix:
 
 class TokenLogprobs:
     """What token_logprobs returns: logprob and entropy (float32 [rows]), top_logprob (float32) and top_index (int64,
-    [rows, top]; None without alternatives), row_stats (float32 [rows, 4]) and scale for the gradient."""
+    [rows, top]; None without alternatives), row_stats (float32 [rows, 4]) and scale for the gradient.  logprob and entropy
+    share their memory, top_logprob and top_index share theirs, and of a few rows (512 bytes in all) everything does: a clone
+    takes one out."""
     __slots__ = ("logprob", "entropy", "top_logprob", "top_index", "row_stats", "scale")
 
     def __init__(self, logprob, entropy, top_logprob, top_index, row_stats, scale):
