@@ -132,7 +132,7 @@ __device__ __forceinline__ void add_many(Sums& a, const float (&v)[N], float top
 
 // Order of the alternatives: larger logit first, of equal ones the lower index; -0 counts as 0, NaN as largest.
 __device__ __forceinline__ u32 value_key(float v) {
-    if (v != v) return 0xffffffffu;
+    if (v != v) return 0xfffffffeu;                // above infinity, and no order key is ~0
     const u32 b = __float_as_uint(v + 0.f);
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;   // never 0: -infinity gives 0x007fffff
 }

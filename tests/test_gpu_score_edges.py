@@ -224,3 +224,14 @@ def test_gradient_past_32_bit_offsets(h):
     for i in (0, 100, 16390):                      # 16390: the row that holds element 2^31
         assert (np.abs(x[i:i + 1].to(torch.float32).cpu().numpy() - even) <= np.abs(even) * 2.0 ** -10 + 2.0 ** -24).all()
     del x
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("rows,vocab", [(5, 7), (1500, 40), (300, 901), (3, 60001)])
+def test_a_nan_at_either_end_of_a_row_is_its_first_alternative(h, rows, vocab, dtype):
+    x = (torch.randn((rows, vocab), generator=torch.Generator().manual_seed(97)) * 3).to(DT[dtype])
+    x[0, 0] = x[1, vocab - 1] = x[2, 0] = x[2, 3] = x[2, vocab - 1] = float("nan")
+    xn = x.to(torch.float32).numpy()
+    r = h.token_logprobs(x.to(DEV), torch.zeros(rows, dtype=torch.int64, device=DEV), top=5)
+    assert np.array_equal(r.top_index[:3].cpu().numpy(), so.logprobs(xn[:3], [0, 0, 0], 1.0, 5)["top_index"])
+    assert torch.isnan(r.top_logprob[:3]).all() and torch.isfinite(r.top_logprob[3:]).all()
