@@ -252,7 +252,11 @@ class TokenLogprobs:
 
 
 class Handle:
-    """Owns the library's scratch workspace on one device (excp_create / excp_destroy)."""
+    """Owns the library's scratch workspace on one device (excp_create / excp_destroy).
+
+    Calls on one handle share that workspace: they must be ordered on the device, on one stream or with events between
+    streams (two tensor scales at once on two streams can both come out wrong).  Programs that score on several streams at
+    once keep a handle for each."""
 
     def __init__(self, workspace_numel: int, device: int | None = None):
         self.lib = load_library()
@@ -439,6 +443,8 @@ class Handle:
     # ---- scoring a restored checkpoint -------------------------------------
     # Only enqueued on the current stream; results are allocated by torch where the caller gives no `out`.  The arguments
     # are marshalled by csrc/score_binding.cpp: TypeError for tensors of the wrong kind, ExcpError for a status.
+    # torch's autograd sees none of these calls: results carry no graph, also of inputs that require a gradient.  The
+    # gradient of the log probabilities is token_logprobs_grad; through a packed matrix there is none.
     def mx4_tensor_scale(self, x: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
         """excp_mx4_tensor_scale: the tensor scale of a matrix, as a float32 tensor of one value."""
         return _score.mx4_tensor_scale(self._h.value, self.device, x, out)

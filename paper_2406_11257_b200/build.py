@@ -19,8 +19,8 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 
 
 def extra_flags() -> list[str]:
-    """Extra nvcc flags from the environment (EXCP_NVCC_FLAGS), e.g. -DEXCP_DEBUG_BOUNDS for the build whose
-    kernels check every index they form and report through the call's status instead of faulting."""
+    """Extra nvcc flags from the environment (EXCP_NVCC_FLAGS), e.g. -DEXCP_DEBUG_BOUNDS for the build in which what
+    compresses and restores checks every index it forms and reports through the call's status instead of faulting."""
     return os.environ.get("EXCP_NVCC_FLAGS", "").split()
 
 

@@ -224,7 +224,9 @@ __device__ __forceinline__ bool call_aborted(const CallState* call) { return (ca
 
 // The checked build (-DEXCP_DEBUG_BOUNDS): every index that depends on data is tested before it is
 // used; a violation raises FLAG_INTERNAL (the call returns EXCP_ERR_CUDA) and the access is skipped.
-// Nothing traps.  In the normal build the test is the constant `true`.
+// Nothing traps.  In the normal build the test is the constant `true`.  (The kernels that compress and
+// restore.  Those that score have no flag of a call to raise: what they index by data, a token and the
+// places of candidates, they test in every build.)
 #ifdef EXCP_DEBUG_BOUNDS
 __device__ __forceinline__ bool bounds_ok(const CallState* call, bool in_bounds) {
     if (!in_bounds) atomicOr(const_cast<u32*>(&call->flags), FLAG_INTERNAL);

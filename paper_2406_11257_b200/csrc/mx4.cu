@@ -163,7 +163,7 @@ struct Place {
     }
 };
 
-// 16 bits: about thirteen instructions per value, so as many warps as 42 registers allow (11008 x 4096 bf16, blocks of 16: 23.9 us
+// 16 bits: 14.9 instructions per value, so as many warps as 42 registers allow (11008 x 4096 bf16, blocks of 16: 23.9 us
 // with six blocks per SM, 25.9 with four).
 template <typename T, int FMT, int REACH>
 __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 2 ? 6 : 4) quantize_kernel(const T* __restrict__ x, u64 rows, u64 cols, u64 stride, u32 col_tiles,

@@ -12,7 +12,9 @@
 // instructions; warps 0..3 bring the block scales to tensor memory and write the result.  Where the few rows come as plain
 // values (linear), warps 0..3 first quantise them into shared memory, each CTA the columns it needs, while the first tiles
 // are on their way: a launch less.
-// Every wait is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and leaves.
+// Every wait for a copy, a product or another warp is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and
+// leaves.  The two that hardware gives no limit, for tensor memory and at the cluster's barrier, depend only on CTAs whose own
+// waits are bounded.
 #include <type_traits>
 
 #include "mx4_codes.cuh"

@@ -14,9 +14,10 @@
 // threads' maxima; the smallest of these is a lower bound of the k-th largest logit.  Each thread also notes the maximum of
 // every step, so that only the few steps that reach the bound are read again, and what reaches it is ranked.
 //
-// Bound: instruction issue (8.4 instructions per logit at 16 bits, 62 % of the issue slots) with the exponentials (16 per SM and
-// cycle, 31 us of these) behind it; at fp32 the bytes.  4096 x 32000 bf16 50 us, with five alternatives 61 us (40.6 us at the copy
-// rate); 2048 x 50304 fp32 63 us (63.7); one row of 50304 fp32 with twenty 8 us (latency).
+// Bound at 16 bits: no unit by itself.  4096 x 32000 bf16 takes 50 us, with five alternatives 63-65; of the latter, issue alone
+// would take 37 (10.5 instructions per logit), the exponentials 31 (16 per SM and cycle), the bytes 40.6 at the copy rate, and 63 %
+// of the issue slots are taken.  78 registers a thread leave a third of the SM's warp slots filled: too few to overlap the three.
+// At fp32 the bytes: 2048 x 50304 63 us (63.7).  One row of 50304 fp32 with twenty 8 us (latency).
 // A block takes a row; where there are too few rows to fill the card, a cluster of blocks takes one and joins its sums and
 // alternatives through distributed shared memory.  (Persistent blocks with a ring of chunks that bulk copies keep filled were
 // slower, 4096 x 32000 bf16 58 us: what they hide is not what is missing.)
