@@ -235,3 +235,27 @@ def test_a_nan_at_either_end_of_a_row_is_its_first_alternative(h, rows, vocab, d
     r = h.token_logprobs(x.to(DEV), torch.zeros(rows, dtype=torch.int64, device=DEV), top=5)
     assert np.array_equal(r.top_index[:3].cpu().numpy(), so.logprobs(xn[:3], [0, 0, 0], 1.0, 5)["top_index"])
     assert torch.isnan(r.top_logprob[:3]).all() and torch.isfinite(r.top_logprob[3:]).all()
+
+
+@pytest.mark.parametrize("fmt", ["e8m0_32", "e4m3_16"])
+@pytest.mark.parametrize("cols", [33000, 32800])
+def test_quantisation_past_32_bit_offsets(h, cols, fmt):
+    """2.2e9 values: the last rows lie past element 2^31 and byte 2^32 of the matrix, and past 2^30 bytes of the packed one (rows
+    that start on 32 bytes, and others)."""
+    rows, tail = 66000, 66000 % 128
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device=DEV)
+    x[-tail:] = (torch.randn((tail, cols), generator=torch.Generator().manual_seed(99)) * 3).to(torch.bfloat16).to(DEV)
+    last = x[-tail:].to(torch.float32).cpu().numpy()
+    g = h.mx4_tensor_scale(x) if fmt == "e4m3_16" else None
+    gf = None if g is None else float(g)
+    assert g is None or gf == float(so.tensor_scale(last))
+    m = h.mx4_quantize(x, fmt, tensor_scale=g)
+    codes, scales = so.quantize(last, fmt, gf)
+    packed = so.pack(codes, scales, fmt)               # the last row tile alone has the layout of a matrix of its own
+    assert np.array_equal(m.data[-packed.size:].cpu().numpy(), packed)
+    x.fill_(7.0)
+    h.mx4_dequantize(m, out=x)
+    want = torch.from_numpy(so.values(codes, scales, fmt, gf).astype(np.float32)).to(torch.bfloat16)
+    assert torch.equal(x[-tail:].cpu(), want)
+    assert not x[:-tail].any()
+    del x, m
