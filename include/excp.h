@@ -463,6 +463,83 @@ excp_status excp_token_logprobs_grad(excp_handle h, const void* logits, int dtyp
                                      const long long* tokens, float scale, const float* row_stats, const float* g_logprob,
                                      const float* g_entropy, void* grad_out, size_t grad_row_stride, void* cuda_stream);
 
+/* ---- The layers before the logits, and the way back through them ---------------------------------------
+ * (The paper's chain restores weights and goes on training from them, and leaves the training to others.)  Products with restored weights
+ * themselves, held in 16 bits as excp_decompress_checkpoint_w16 leaves them; the norms before them; and the gradients of both, for
+ * which activations can be kept in 8 bits.
+ *
+ * As the scoring calls, these only enqueue work and can be captured in a graph (of the products: after one ordinary call of a product on
+ * the handle).  They use none of the handle's workspace but its flag: calls that are not ordered on the device may share a handle, though not
+ * scratch.  `scratch` is device memory on 16 bytes, of what the call's _scratch function says (NULL where that is 0), and its contents
+ * afterwards are unspecified.
+ *
+ * A matrix in these calls: `rows` rows of `cols` values, `row_stride` values apart (>= cols; of one row it is not looked at), aligned to
+ * its element.  Its type is an excp_dtype, or, where that is said, EXCP_ACT8: then `data` is a packed 8-bit matrix and the stride is not
+ * looked at.  A null pointer to an optional matrix: absent.  Results may not overlap inputs, but where that is said. */
+typedef struct {
+    void* data;
+    int dtype;
+    size_t rows, cols, row_stride;
+} excp_matrix;
+
+/* Values in 8 bits.  Blocks of 32 consecutive columns of a row share a scale s: with A the block's largest magnitude, fl(A / 127) rounded up
+ * to 8 significant bits, and at least 2^-126.  A code is fl(x fl(1 / s)) rounded to the nearest whole number, ties to the even one, and
+ * stands for code times s.  A block that holds a NaN or an infinity has the scale NaN and codes 0: all its values are NaN.
+ * Packed, R rows and C columns with B = ceil(C / 32): R rows of 32 B codes (signed bytes; 0 past column C), then R rows of B scales as
+ * bfloat16.  excp_act8_bytes: rounded up to 16 bytes; 0 for more than 2^30 rows or columns. */
+#define EXCP_ACT8 3
+size_t excp_act8_bytes(size_t rows, size_t cols);
+excp_status excp_act8_quantize(excp_handle h, const excp_matrix* x, void* packed_out, void* cuda_stream);
+excp_status excp_act8_restore(excp_handle h, const void* packed, const excp_matrix* out, void* cuda_stream);
+
+/* Activations.  gelu: x Phi(x) with the normal distribution function; gelu_tanh: x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2;
+ * silu: x / (1 + exp(-x)).  Where a formula has 0 times infinity the result is NaN. */
+typedef enum {
+    EXCP_ACT_NONE = 0,
+    EXCP_ACT_GELU = 1,
+    EXCP_ACT_GELU_TANH = 2,
+    EXCP_ACT_SILU = 3
+} excp_activation;
+
+/* The way back through an activation, from what went into it: dpre = dy act'(pre), again = act(pre) (what a weight gradient of the
+ * next product needs), dbias = the sum of dpre's rows before they are rounded (fp32 [cols]).  pre: dy's type or EXCP_ACT8.  The three
+ * results are optional, and dpre and again have dy's type; dpre may be dy itself.  EXCP_ACT_NONE: dpre = dy, and pre and again are NULL (for the
+ * bias gradient of a product without activation). */
+size_t excp_act_grad_scratch(excp_handle h, size_t rows, size_t cols);
+excp_status excp_act_grad(excp_handle h, int act, const excp_matrix* dy, const excp_matrix* pre, const excp_matrix* dpre_out,
+                          const excp_matrix* again_out, float* dbias_out, void* scratch, void* cuda_stream);
+
+/* Norm of every row: y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(mean((x - mean)^2) + eps); rms != 0: mean is 0 and there is no bias.
+ * y has x's type; weight and bias (device, [cols], NULL = 1 and 0) are both EXCP_F32 or x's type.  y may be x.
+ *   row_stats_out  [rows, 2], 8-byte aligned, for the gradient (may be NULL): mean, rstd
+ *   kept_out       x in 8 bits, for the gradient (may be NULL; excp_act8_bytes, 16-byte aligned)
+ *
+ * The gradient, with xh = (x - mean) rstd and g = dy weight:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)) + add   (rms: without mean(g)),   dweight = sum over rows of dy xh,   dbias = sum over rows of dy
+ * x: what excp_layer_norm was given, or EXCP_ACT8; row_stats: what it wrote.  add (what reaches x by other ways), dx and the fp32 [cols]
+ * vectors dweight and dbias are optional; add and dx have dy's type, and dx may be dy or add.  Without rows, dweight and dbias are 0. */
+excp_status excp_layer_norm(excp_handle h, const excp_matrix* x, const void* weight, const void* bias, int vector_dtype, float eps, int rms,
+                            const excp_matrix* y_out, float* row_stats_out, void* kept_out, void* cuda_stream);
+size_t excp_layer_norm_grad_scratch(excp_handle h, size_t rows, size_t cols);
+excp_status excp_layer_norm_grad(excp_handle h, const excp_matrix* dy, const excp_matrix* x, const void* weight, int vector_dtype, int rms,
+                                 const float* row_stats, const excp_matrix* add, const excp_matrix* dx_out, float* dweight_out, float* dbias_out,
+                                 void* scratch, void* cuda_stream);
+
+/* Products with plain matrices, both EXCP_F16 or both EXCP_BF16; sums in fp32, rounded once to the result's type, which may be any.
+ *   excp_linear              p = x w^T + bias (of any type, [w rows], NULL = 0); kept = p, in any type or EXCP_ACT8; y = act(p) + residual
+ *   excp_linear_grad_input   dx = dy w + add
+ *   excp_linear_grad_weight  dw = dy^T x + add
+ * residual, add and kept are optional; y may be the residual, and dx or dw may be add (gradients that are summed over several calls).
+ * excp_linear_scratch: for the two operands of any of the three; 0 where both start on 16 bytes and their strides are multiples of 8 (or they
+ * have one row): others are laid out in the scratch first.  A wait that ran out is reported by excp_score_status. */
+size_t excp_linear_scratch(const excp_matrix* a, const excp_matrix* b);
+excp_status excp_linear(excp_handle h, const excp_matrix* x, const excp_matrix* w, const void* bias, int bias_dtype, int act,
+                        const excp_matrix* residual, const excp_matrix* y_out, const excp_matrix* kept_out, void* scratch, void* cuda_stream);
+excp_status excp_linear_grad_input(excp_handle h, const excp_matrix* dy, const excp_matrix* w, const excp_matrix* add, const excp_matrix* dx_out,
+                                   void* scratch, void* cuda_stream);
+excp_status excp_linear_grad_weight(excp_handle h, const excp_matrix* dy, const excp_matrix* x, const excp_matrix* add, const excp_matrix* dw_out,
+                                    void* scratch, void* cuda_stream);
+
 /* Synchronises the stream and reports whether a bounded wait of a product since the last report ran out
  * (excp_set_wait_limit; EXCP_ERR_TIMEOUT: that product's result is unspecified). */
 excp_status excp_score_status(excp_handle h, void* cuda_stream);

@@ -27,7 +27,9 @@ EXPORTS = ["excp_create", "excp_destroy", "excp_record_bytes", "excp_compress_bo
            "excp_decompress_dense_tensor", "excp_decompress_dense_checkpoint", "excp_profile_enable", "excp_profile_stage_count", "excp_profile_stage_name", "excp_profile_read",
            "excp_set_kmeans_margin", "excp_set_wait_limit", "excp_selftest_wait_timeout", "excp_set_report_sse",
            "excp_mx4_bytes", "excp_mx4_tensor_scale", "excp_mx4_quantize", "excp_mx4_dequantize", "excp_mx4_matmul", "excp_mx4_linear", "excp_mx4_linear_scratch",
-           "excp_token_logprobs", "excp_token_logprobs_grad", "excp_score_status"]
+           "excp_token_logprobs", "excp_token_logprobs_grad", "excp_score_status",
+           "excp_act8_bytes", "excp_act8_quantize", "excp_act8_restore", "excp_act_grad_scratch", "excp_act_grad", "excp_layer_norm",
+           "excp_layer_norm_grad_scratch", "excp_layer_norm_grad", "excp_linear_scratch", "excp_linear", "excp_linear_grad_input", "excp_linear_grad_weight"]
 
 
 class ExcpError(RuntimeError):
@@ -46,6 +48,10 @@ class CStats(C.Structure):
                 ("blob_bytes", C.c_ulonglong), ("median", C.c_float), ("mean_abs_ea", C.c_float),
                 ("thr_w", C.c_float), ("thr_o", C.c_float),
                 ("sse_w", C.c_double), ("sse_ea", C.c_double), ("sse_eas", C.c_double)]
+
+
+class CMatrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int), ("rows", C.c_size_t), ("cols", C.c_size_t), ("row_stride", C.c_size_t)]
 
 
 FLAG_NO_W2M, FLAG_NO_M2W, FLAG_NO_RESIDUAL, FLAG_NO_PRUNE, FLAG_NO_QUANT = 1, 2, 4, 8, 16
@@ -68,7 +74,10 @@ class Params:
 
 # what the native half of the binding calls (csrc/score_binding.cpp, in the order of its table)
 _SCORE_CALLS = ["excp_mx4_bytes", "excp_mx4_tensor_scale", "excp_mx4_quantize", "excp_mx4_dequantize", "excp_mx4_matmul",
-                "excp_mx4_linear_scratch", "excp_mx4_linear", "excp_token_logprobs", "excp_token_logprobs_grad"]
+                "excp_mx4_linear_scratch", "excp_mx4_linear", "excp_token_logprobs", "excp_token_logprobs_grad",
+                "excp_act8_bytes", "excp_act8_quantize", "excp_act8_restore", "excp_act_grad_scratch", "excp_act_grad", "excp_layer_norm",
+                "excp_layer_norm_grad_scratch", "excp_layer_norm_grad", "excp_linear_scratch", "excp_linear", "excp_linear_grad_input",
+                "excp_linear_grad_weight"]
 _lib = None
 
 
@@ -146,6 +155,23 @@ def load_library() -> C.CDLL:
     lib.excp_token_logprobs.argtypes = [vp, vp, C.c_int, sz, sz, sz, vp, C.c_float, C.c_int, vp, vp, vp, vp, vp, vp]
     lib.excp_token_logprobs_grad.argtypes = [vp, vp, C.c_int, sz, sz, sz, vp, C.c_float, vp, vp, vp, vp, sz, vp]
     lib.excp_score_status.argtypes = [vp, vp]
+    mat = C.POINTER(CMatrix)
+    lib.excp_act8_bytes.argtypes = [sz, sz]
+    lib.excp_act8_bytes.restype = sz
+    lib.excp_act8_quantize.argtypes = [vp, mat, vp, vp]
+    lib.excp_act8_restore.argtypes = [vp, vp, mat, vp]
+    lib.excp_act_grad_scratch.argtypes = [vp, sz, sz]
+    lib.excp_act_grad_scratch.restype = sz
+    lib.excp_act_grad.argtypes = [vp, C.c_int, mat, mat, mat, mat, vp, vp, vp]
+    lib.excp_layer_norm.argtypes = [vp, mat, vp, vp, C.c_int, C.c_float, C.c_int, mat, vp, vp, vp]
+    lib.excp_layer_norm_grad_scratch.argtypes = [vp, sz, sz]
+    lib.excp_layer_norm_grad_scratch.restype = sz
+    lib.excp_layer_norm_grad.argtypes = [vp, mat, mat, vp, C.c_int, C.c_int, vp, mat, mat, vp, vp, vp, vp]
+    lib.excp_linear_scratch.argtypes = [mat, mat]
+    lib.excp_linear_scratch.restype = sz
+    lib.excp_linear.argtypes = [vp, mat, mat, vp, C.c_int, C.c_int, mat, mat, mat, vp, vp]
+    lib.excp_linear_grad_input.argtypes = [vp, mat, mat, mat, mat, vp, vp]
+    lib.excp_linear_grad_weight.argtypes = [vp, mat, mat, mat, mat, vp, vp]
     for name in EXPORTS:
         if getattr(lib, name).restype is C.c_int:
             getattr(lib, name).restype = C.c_int
@@ -249,6 +275,57 @@ class TokenLogprobs:
     def __init__(self, logprob, entropy, top_logprob, top_index, row_stats, scale):
         self.logprob, self.entropy, self.top_logprob, self.top_index = logprob, entropy, top_logprob, top_index
         self.row_stats, self.scale = row_stats, scale
+
+
+# ---- the layers before the logits, and the way back -------------------------------
+ACTIVATIONS = {"none": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
+
+
+def act8_bytes(rows: int, cols: int) -> int:
+    """Size of a packed 8-bit matrix (layout: include/excp.h)."""
+    return load_library().excp_act8_bytes(rows, cols)
+
+
+class Act8Matrix:
+    """Values kept in 8 bits: `data` (uint8, act8_bytes) and the shape."""
+    __slots__ = ("data", "rows", "cols")
+
+    def __init__(self, data: torch.Tensor, rows: int, cols: int):
+        self.data, self.rows, self.cols = data, rows, cols
+
+
+class Norm:
+    """What layer_norm returns: y, row_stats (float32 [rows, 2]: mean and 1 / deviation), kept (x as an Act8Matrix, or None) and rms."""
+    __slots__ = ("y", "row_stats", "kept", "rms")
+
+    def __init__(self, y, row_stats, kept, rms):
+        self.y, self.row_stats, self.kept, self.rms = y, row_stats, kept, rms
+
+
+class NormGrad:
+    """What layer_norm_grad returns: dx, and dweight and dbias (float32; None where not wanted, dbias also for rms)."""
+    __slots__ = ("dx", "dweight", "dbias")
+
+    def __init__(self, dx, dweight, dbias):
+        self.dx, self.dweight, self.dbias = dx, dweight, dbias
+
+
+class ActGrad:
+    """What act_grad returns: dpre, a (the activation's value; None where not wanted) and dbias (float32)."""
+    __slots__ = ("dpre", "a", "dbias")
+
+    def __init__(self, dpre, a, dbias):
+        self.dpre, self.a, self.dbias = dpre, a, dbias
+
+
+def _kept(m):
+    """The tensor of a plain or packed matrix, and whether it is packed."""
+    return (m.data, True) if isinstance(m, Act8Matrix) else (m, False)
+
+
+def _same_shape(m, like: torch.Tensor, what: str) -> None:
+    if isinstance(m, Act8Matrix) and (m.rows, m.cols) != tuple(like.shape):
+        raise TypeError(f"{what}: expected the shape {list(like.shape)}")
 
 
 class Handle:
@@ -485,6 +562,68 @@ class Handle:
         """excp_token_logprobs_grad: the gradient with respect to the logits, from what token_logprobs returned for them.
         `out` may be `logits`."""
         return _score.token_logprobs_grad(self._h.value, self.device, logits, tokens, r.row_stats, r.scale, g_logprob, g_entropy, out)
+
+    # ---- the layers before the logits, and the way back ----------------------
+    # As the scoring calls: only enqueued, marshalled natively, and torch's autograd sees none of them.
+    def act8_quantize(self, x: torch.Tensor, out: torch.Tensor | None = None) -> Act8Matrix:
+        """excp_act8_quantize: x [rows, cols] in 8 bits (into `out`, uint8, if given)."""
+        data = _score.act8_quantize(self._h.value, self.device, x, out)
+        rows, cols = x.shape
+        return Act8Matrix(data, rows, cols)
+
+    def act8_restore(self, m: Act8Matrix, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
+        """excp_act8_restore: the values that the codes stand for."""
+        return _score.act8_restore(self._h.value, self.device, m.data, m.rows, m.cols, dtype, out)
+
+    def act_grad(self, dy: torch.Tensor, pre: torch.Tensor | Act8Matrix, act: str, again: bool = False, bias: bool = True,
+                 out: torch.Tensor | None = None) -> ActGrad:
+        """excp_act_grad: the gradient through an activation ("gelu", "gelu_tanh", "silu") from what went into it (`pre`, plain or in 8 bits),
+        the bias's gradient, and with `again` the activation's value.  `out` (for dpre) may be dy."""
+        _same_shape(pre, dy, "pre")
+        data, is_packed = _kept(pre)
+        return ActGrad(*_score.act_grad(self._h.value, self.device, dy, data, is_packed, ACTIVATIONS[act], True, again, bias, out))
+
+    def bias_grad(self, dy: torch.Tensor) -> torch.Tensor:
+        """excp_act_grad without an activation: the sum of dy's rows, float32."""
+        return _score.act_grad(self._h.value, self.device, dy, None, False, 0, False, False, True, None)[2]
+
+    def layer_norm(self, x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5, rms: bool = False,
+                   keep: bool = False, out: torch.Tensor | None = None) -> Norm:
+        """excp_layer_norm: the norm of every row of x (rms: without mean and bias); with `keep` also x in 8 bits.  `out` may be x."""
+        y, stats, data = _score.layer_norm(self._h.value, self.device, x, weight, bias, eps, rms, keep, out)
+        return Norm(y, stats, None if data is None else Act8Matrix(data, *x.shape), rms)
+
+    def layer_norm_grad(self, dy: torch.Tensor, x: torch.Tensor | Act8Matrix, weight: torch.Tensor | None, r: Norm, add: torch.Tensor | None = None,
+                        out: torch.Tensor | None = None, vectors: bool = True) -> NormGrad:
+        """excp_layer_norm_grad: the gradients of x (plus `add`), weight and bias, from what layer_norm returned for them; x may be r.kept.
+        `out` (for dx) may be dy or add."""
+        _same_shape(x, dy, "x")
+        data, is_packed = _kept(x)
+        return NormGrad(*_score.layer_norm_grad(self._h.value, self.device, dy, data, is_packed, weight, r.rms, r.row_stats, add, out, vectors))
+
+    def linear(self, x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, act: str = "none", residual: torch.Tensor | None = None,
+               out: torch.Tensor | None = None, dtype: torch.dtype | None = None) -> torch.Tensor:
+        """excp_linear: act(x w^T + bias) + residual of 16-bit matrices; the result has x's type unless `dtype` or `out` says otherwise.
+        `out` may be the residual."""
+        return _score.linear(self._h.value, self.device, x, w, bias, ACTIVATIONS[act], residual, dtype, out, None)[0]
+
+    def linear_kept(self, x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, act: str = "none", residual: torch.Tensor | None = None,
+                    keep: str | torch.dtype = "act8", out: torch.Tensor | None = None, dtype: torch.dtype | None = None):
+        """The same, and what goes into the activation: an Act8Matrix for keep="act8", else a tensor of that type."""
+        if isinstance(keep, str) and keep != "act8":
+            raise ValueError('keep: "act8" or a torch.dtype')
+        y, data = _score.linear(self._h.value, self.device, x, w, bias, ACTIVATIONS[act], residual, dtype, out, True if keep == "act8" else keep)
+        return y, Act8Matrix(data, x.shape[0], w.shape[0]) if keep == "act8" else data
+
+    def linear_grad_input(self, dy: torch.Tensor, w: torch.Tensor, add: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                          dtype: torch.dtype | None = None) -> torch.Tensor:
+        """excp_linear_grad_input: dy w (+ add), in dy's type unless `dtype` or `out` says otherwise.  `out` may be add."""
+        return _score.linear_grad_input(self._h.value, self.device, dy, w, add, dtype, out)
+
+    def linear_grad_weight(self, dy: torch.Tensor, x: torch.Tensor, add: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                           dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        """excp_linear_grad_weight: dy^T x (+ add).  `out` may be add (gradients summed over several calls)."""
+        return _score.linear_grad_weight(self._h.value, self.device, dy, x, add, dtype, out)
 
     def score_status(self) -> None:
         """excp_score_status: synchronises; raises if a product's bounded wait ran out since the last report."""

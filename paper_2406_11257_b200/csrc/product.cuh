@@ -1,0 +1,269 @@
+// The product with plain 16-bit operands: c[i, j] = sum over k of a[i, k] b[j, k], and what is done to it on the way out.
+// Shared by the kernels for few rows (product.cu) and for many (product_wide.cu): operands, tensor maps, epilogue.
+#pragma once
+#include <cuda.h>
+
+#include "layers.cuh"
+#include "mx4_pipe.cuh"
+
+namespace excp {
+
+constexpr u32 PR_TILE = 128;                       // rows of an operand tile = lanes of tensor memory
+constexpr u32 PR_K = 64;                           // columns of a stage: 128 bytes, one swizzle span
+constexpr u32 PR_CHUNK = 64;                       // rows of a box of an operand that lies the other way round
+constexpr u32 PR_CHUNK_BYTES = PR_CHUNK * PR_K * 2;
+
+// One operand: `rows` x `k`.  along_k: its k values are neighbours in memory, rows `stride` apart; else the rows are neighbours
+// and k values `stride` apart (a transposed matrix).  On 16 bytes, like its stride.
+struct ProductOperand {
+    const void* p;
+    u64 rows, k, stride;
+    bool along_k;
+};
+
+// What becomes of a sum v of c[i, j]: p = v + bias[j]; kept = p; y = act(p) + residual[i, j].
+struct ProductEnd {
+    Matrix y;                                      // rows, cols: of c
+    ColumnVector bias;
+    int act = ACT_NONE;
+    Matrix residual;                               // p null: none
+    Matrix kept;                                   // p null: none
+};
+
+struct ProductCall {
+    ProductOperand a, b;
+    ProductEnd end;
+    int dtype;                                     // of both operands: DT_F16 or DT_BF16
+    int sms;
+    u64 wait_ns;
+    u32* flag;
+};
+bool launch_product(cudaStream_t s, const ProductCall& c);
+bool launch_product_wide(cudaStream_t s, const ProductCall& c);
+
+// Rows that a tensor map cannot describe (not on 16 bytes) -> rows of `pitch` values in `to`.
+u64 tidy_pitch(u64 cols);
+void launch_tidy(int sms, cudaStream_t s, const Matrix& m, void* to);
+
+// A map of an operand in boxes of `box_rows` rows (64 where the rows are neighbours) and PR_K columns.
+bool product_map(CUtensorMap* map, const ProductOperand& o, u32 box_rows, int dtype);
+
+// The epilogue as the kernels take it.
+struct EndArgs {
+    void* y;
+    u64 stride, rows, cols;
+    const void* bias;
+    const void* residual;
+    u64 residual_stride;
+    void* kept;
+    u64 kept_stride;
+    Kept k8;
+    int bias_dtype, act, residual_dtype, kept_dtype;
+    // rows that start on 32 bytes (y, kept) or 16 bytes (residual)
+    u32 y_vec, residual_vec, kept_vec;
+};
+EndArgs end_args(const ProductEnd& e);
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, u32 x, u32 y, unsigned long long* bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// Descriptor of an operand tile in shared memory, and what 16 columns further on adds to it.
+//   along k   rows of 128 bytes in 128-byte swizzle, eight-row groups 1024 bytes apart; 16 columns are 32 bytes
+//   else      boxes of 64 rows (128 bytes) x 64 columns, the same swizzle: eight columns are 1024 bytes, the next 64 rows 8192
+__device__ __forceinline__ u64 product_desc(u32 addr, bool along_k) {
+    return (u64)((addr >> 4) & 0x3fffu) | ((u64)(along_k ? 1u : PR_CHUNK_BYTES >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ u32 product_desc_step(bool along_k) { return along_k ? 32 >> 4 : 2048 >> 4; }
+// fp32 sums, 16-bit operands of one type.
+__device__ __forceinline__ u32 product_idesc(bool bf16, bool m_along_k, bool n_along_k, u32 m, u32 n) {
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (m_along_k ? 0u : 1u << 15) | (n_along_k ? 0u : 1u << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+__device__ __forceinline__ void tm_mma_f16(u32 d, u64 a, u64 b, u32 idesc, u32 add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void tm2_mma_f16(u32 d, u64 a, u64 b, u32 idesc, u32 add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+
+// ---- epilogue ---------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float any_value(const void* p, int dtype, u64 i) {
+    if (dtype == DT_F32) return __ldg(static_cast<const float*>(p) + i);
+    if (dtype == DT_F16) return __half2float(__ldg(static_cast<const __half*>(p) + i));
+    return __bfloat162float(__ldg(static_cast<const __nv_bfloat16*>(p) + i));
+}
+template <u32 W>
+__device__ __forceinline__ void activate(float (&f)[W], int act) {
+    if (act == ACT_GELU) {
+#pragma unroll
+        for (u32 e = 0; e < W; ++e) f[e] = act_value<ACT_GELU>(f[e]);
+    } else if (act == ACT_GELU_TANH) {
+#pragma unroll
+        for (u32 e = 0; e < W; ++e) f[e] = act_value<ACT_GELU_TANH>(f[e]);
+    } else if (act == ACT_SILU) {
+#pragma unroll
+        for (u32 e = 0; e < W; ++e) f[e] = act_value<ACT_SILU>(f[e]);
+    }
+}
+__device__ __forceinline__ void store32(void* p, const u32 v[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ u32 word_of(const float* f) {       // 4 bytes of results
+    if constexpr (sizeof(T) == 4) {
+        return __float_as_uint(f[0]);
+    } else {
+        u32 w;
+        T* h = reinterpret_cast<T*>(&w);
+        wput(h, 0, f[0]);
+        wput(h, 1, f[1]);
+        return w;
+    }
+}
+// The first `n` of W results to neighbouring places.
+template <typename T, u32 W>
+__device__ __forceinline__ void put_row(T* y, const float (&f)[W], u32 n, bool on32) {
+    constexpr u32 PER = 4 / sizeof(T), STEP = 8 * PER;
+#pragma unroll
+    for (u32 i = 0; i < W; i += STEP) {
+        if (on32 && i + STEP <= n) {
+            u32 w[8];
+#pragma unroll
+            for (u32 k = 0; k < 8; ++k) w[k] = word_of<T>(f + i + k * PER);
+            store32(y + i, w);
+        } else {
+#pragma unroll
+            for (u32 e = i; e < i + STEP; ++e) if (e < n) wput(y, e, f[e]);
+        }
+    }
+}
+template <u32 W>
+__device__ __forceinline__ void put_row_any(void* p, int dtype, u64 at, const float (&f)[W], u32 n, bool on32) {
+    if (dtype == DT_F32) put_row(static_cast<float*>(p) + at, f, n, on32);
+    else if (dtype == DT_F16) put_row(static_cast<__half*>(p) + at, f, n, on32);
+    else put_row(static_cast<__nv_bfloat16*>(p) + at, f, n, on32);
+}
+template <typename T, u32 W>
+__device__ __forceinline__ void add_row(const T* r, float (&f)[W], u32 n, bool on16) {
+    constexpr u32 PER = 16 / sizeof(T);
+#pragma unroll
+    for (u32 i = 0; i < W; i += PER) {
+        if (on16 && i + PER <= n) {
+            const uint4 q = *reinterpret_cast<const uint4*>(r + i);
+            const T* h = reinterpret_cast<const T*>(&q);
+#pragma unroll
+            for (u32 e = 0; e < PER; ++e) f[i + e] += wget(h, e);
+        } else {
+#pragma unroll
+            for (u32 e = i; e < i + PER; ++e) if (e < n) f[e] += wget(r, e);
+        }
+    }
+}
+
+// 32 neighbouring sums of row i, columns j ..
+template <int DT>
+__device__ __forceinline__ void end_row(const EndArgs& g, u64 i, u64 j, float (&f)[32]) {
+    typedef typename ElemOf<DT>::type T;
+    if (i >= g.rows || j >= g.cols) return;
+    const u32 n = (u32)min((u64)32, g.cols - j);
+    if (g.bias) {
+#pragma unroll
+        for (u32 e = 0; e < 32; ++e) if (e < n) f[e] += any_value(g.bias, g.bias_dtype, j + e);
+    }
+    if (g.kept) {
+        if (g.kept_dtype == DT_ACT8) {             // a thread has a whole block of 32
+            u32 top = 0;
+#pragma unroll
+            for (u32 e = 0; e < 32; ++e) {
+                if (e >= n) f[e] = 0.f;
+                top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+            }
+            const float s = a8_scale(top), inverse = a8_inverse(s);
+            u32 q[8];
+#pragma unroll
+            for (u32 k = 0; k < 8; ++k) q[k] = top >= 0x7f800000u ? 0u : a8_codes(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3], inverse);
+            const u64 block = i * g.k8.blocks + j / A8_BLOCK;
+            if (g.kept_vec) {
+                store32(g.k8.codes + block * A8_BLOCK, q);
+            } else {                               // the buffer starts on 16 bytes
+                uint4* p = reinterpret_cast<uint4*>(g.k8.codes + block * A8_BLOCK);
+                p[0] = make_uint4(q[0], q[1], q[2], q[3]);
+                p[1] = make_uint4(q[4], q[5], q[6], q[7]);
+            }
+            g.k8.scales[block] = (unsigned short)(__float_as_uint(s) >> 16);
+        } else {
+            put_row_any(g.kept, g.kept_dtype, i * g.kept_stride + j, f, n, g.kept_vec);
+        }
+    }
+    activate(f, g.act);
+    if (g.residual) {
+        const u64 at = i * g.residual_stride + j;
+        if (g.residual_dtype == DT_F32) add_row(static_cast<const float*>(g.residual) + at, f, n, g.residual_vec);
+        else if (g.residual_dtype == DT_F16) add_row(static_cast<const __half*>(g.residual) + at, f, n, g.residual_vec);
+        else add_row(static_cast<const __nv_bfloat16*>(g.residual) + at, f, n, g.residual_vec);
+    }
+    put_row(static_cast<T*>(g.y) + i * g.stride + j, f, n, g.y_vec);
+}
+
+// W sums of column j (a lane has one; the lanes of a warp have neighbouring ones, the first a multiple of 32), rows i .. i + n - 1.
+template <int DT, u32 W>
+__device__ __forceinline__ void end_column(const EndArgs& g, u64 i, u64 j, u32 n, float (&f)[W]) {
+    typedef typename ElemOf<DT>::type T;
+    const bool there = j < g.cols;
+    if (g.bias) {
+        const float b = there ? any_value(g.bias, g.bias_dtype, j) : 0.f;
+#pragma unroll
+        for (u32 e = 0; e < W; ++e) f[e] += b;
+    }
+    if (g.kept && g.kept_dtype == DT_ACT8) {       // a block is the warp's 32 columns
+        const u32 lane = threadIdx.x & 31;
+        const u64 block = j / A8_BLOCK;
+#pragma unroll
+        for (u32 e = 0; e < W; ++e) {
+            const float v = there && e < n ? f[e] : 0.f;
+            const u32 top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu);
+            const float s = a8_scale(top);
+            if (e < n && block < g.k8.blocks) {
+                const u64 at = (i + e) * g.k8.blocks + block;
+                g.k8.codes[at * A8_BLOCK + lane] = top >= 0x7f800000u ? 0 : (unsigned char)a8_codes(v, 0.f, 0.f, 0.f, a8_inverse(s));
+                if (lane == 0) g.k8.scales[at] = (unsigned short)(__float_as_uint(s) >> 16);
+            }
+        }
+    }
+    if (!there) return;
+    if (g.kept && g.kept_dtype != DT_ACT8) {
+#pragma unroll
+        for (u32 e = 0; e < W; ++e) {
+            if (e >= n) continue;
+            const u64 at = (i + e) * g.kept_stride + j;
+            if (g.kept_dtype == DT_F32) wput(static_cast<float*>(g.kept), at, f[e]);
+            else if (g.kept_dtype == DT_F16) wput(static_cast<__half*>(g.kept), at, f[e]);
+            else wput(static_cast<__nv_bfloat16*>(g.kept), at, f[e]);
+        }
+    }
+    activate(f, g.act);
+    if (g.residual) {
+        // not through the read-only cache: y may be the residual
+        const u64 at = i * g.residual_stride + j;
+#pragma unroll
+        for (u32 e = 0; e < W; ++e) {
+            if (e >= n) continue;
+            if (g.residual_dtype == DT_F32) f[e] += wget(static_cast<const float*>(g.residual), at + e * g.residual_stride);
+            else if (g.residual_dtype == DT_F16) f[e] += wget(static_cast<const __half*>(g.residual), at + e * g.residual_stride);
+            else f[e] += wget(static_cast<const __nv_bfloat16*>(g.residual), at + e * g.residual_stride);
+        }
+    }
+    T* y = static_cast<T*>(g.y) + i * g.stride + j;
+#pragma unroll
+    for (u32 e = 0; e < W; ++e) if (e < n) wput(y, e * g.stride, f[e]);
+}
+#endif
+
+}  // namespace excp

@@ -1,0 +1,239 @@
+// The product with plain 16-bit operands, many rows on both sides (product.cu: few).
+//
+// Bound: the tensor cores.  A pair of CTAs works on a tile of 256 x 256 (tcgen05 cta_group::2): each holds 128 rows of the M side and
+// half of the N side's 256, so that a step of 64 columns costs a CTA 32 KB of shared memory for 512 cycles of products.  The
+// accumulators of two tiles fit tensor memory: one is written out while the next is summed.
+//
+// Persistent pairs: pair p computes tiles p, p + pairs, ...  Roles in each CTA: warps 0..7 write the result, warps 8 and 9 fetch the
+// two operands (tensor maps; what lies past an edge comes as 0), warp 10 of the even CTA issues the products, and that of the odd
+// CTA tells it of its own copies' landing.
+// Every wait for a copy, a product or another warp is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and
+// leaves (the partner's waits run out in turn).  The two that hardware gives no limit, for tensor memory and at the pair's barrier,
+// depend only on CTAs whose own waits are bounded.
+#include "product.cuh"
+
+namespace excp {
+namespace {
+
+constexpr int STORE_WARPS = 8;
+constexpr u32 FETCH_WARP = STORE_WARPS, PRODUCT_WARP = FETCH_WARP + 2;
+constexpr int THREADS = (PRODUCT_WARP + 1) * 32;
+constexpr int STAGES = 6;
+constexpr u32 SPAN = 2 * PR_TILE;                  // rows of m and of n per pair
+constexpr u32 HALF = PR_TILE * PR_K * 2, STAGE = 2 * HALF;
+constexpr u32 SMEM = STAGES * STAGE + 1024;
+constexpr u32 GROUP = 16;                          // tiles of m that are visited before the next tile of n
+
+struct WideArgs {
+    CUtensorMap m, n;                              // on the M side (lanes of tensor memory) and the N side (columns)
+    u32 m_along_k, n_along_k, bf16;
+    u32 k_tiles, m_tiles, n_tiles;
+    // Usually a is m: a lane has a row of c.  Where rows of y do not start on 32 bytes the operands change places: a lane has a column, and
+    // neighbouring lanes write neighbouring results.
+    u32 turned;
+    EndArgs end;
+    u64 wait_ns;
+    u32* flag;
+};
+
+struct Shared {
+    unsigned long long full[STAGES];               // own copies have landed
+    unsigned long long peer[STAGES];               // even CTA: the partner's have
+    unsigned long long empty[STAGES];              // the stage has been multiplied
+    unsigned long long acc_full[2], acc_empty[2];
+    unsigned long long last;                       // everything that was issued is done; one turn only
+    u32 tmem;
+    volatile u32 abort;
+};
+
+__device__ __forceinline__ void place(const WideArgs& g, u32 t, u32& mt, u32& nt) {
+    const u32 per_group = GROUP * g.n_tiles;
+    const u32 group = t / per_group, inside = t - group * per_group;
+    const u32 rows = min(GROUP, g.m_tiles - group * GROUP);
+    nt = inside / rows;
+    mt = group * GROUP + inside - nt * rows;
+}
+
+// Releases what the partner's copies wrote before the arrival (the thread has no stores of its own to wait for).
+__device__ __forceinline__ void mbar_arrive_cluster_release(u32 address) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
+}
+
+template <int DT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_product_kernel(const __grid_constant__ WideArgs g) {
+    constexpr u32 TMEM_COLS = 512;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ Shared sh;
+    // the swizzle goes by address: stages start on 1024 bytes (the same offset in both CTAs)
+    unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const u32 base = smem_u32(smem);
+    const u32 warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const u32 rank = cluster_rank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const u32 tiles = g.m_tiles * g.n_tiles;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&sh.full[s], 2); mbar_init(&sh.peer[s], 1); mbar_init(&sh.empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&sh.acc_full[b], 1); mbar_init(&sh.acc_empty[b], 2 * STORE_WARPS); }
+        mbar_init(&sh.last, 1);
+        sh.abort = 0;
+        mbar_fence_init();
+    }
+    if (warp == PRODUCT_WARP) tm2_alloc(&sh.tmem, TMEM_COLS);
+    if (warp == FETCH_WARP && elect_one()) { tma_prefetch_map(&g.m); tma_prefetch_map(&g.n); }
+    __syncwarp();
+    wait_for_previous();
+    let_next_start();
+    tm_fence_before();
+    __syncthreads();
+    cluster_barrier();                             // the partner's barriers are ready
+    tm_fence_after();
+    const u32 tmem = sh.tmem;
+
+    if (warp == FETCH_WARP || warp == FETCH_WARP + 1) {
+        const bool is_n = warp != FETCH_WARP;
+        const CUtensorMap* map = is_n ? &g.n : &g.m;
+        const bool along_k = is_n ? g.n_along_k : g.m_along_k;
+        Ring<STAGES> ring;
+        u32 filled = 0;
+        bool ok = true;
+        for (u32 t = pair; ok && t < tiles; t += pairs) {
+            u32 mt, nt;
+            place(g, t, mt, nt);
+            const u32 row = ((is_n ? nt : mt) * 2 + rank) * PR_TILE;
+            for (u32 k = 0; k < g.k_tiles; ++k) {
+                if (filled >= STAGES && !wait_warp(&sh, &sh.empty[ring.s], ring.parity ^ 1, g.wait_ns, g.flag)) { ok = false; break; }
+                unsigned char* to = smem + ring.s * STAGE + (is_n ? HALF : 0);
+                unsigned long long* bar = &sh.full[ring.s];
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(bar, HALF);
+                    if (along_k) {
+                        tma_load_2d(to, map, k * PR_K, row, bar);
+                    } else {
+                        tma_load_2d(to, map, row, k * PR_K, bar);
+                        tma_load_2d(to + PR_CHUNK_BYTES, map, row + PR_CHUNK, k * PR_K, bar);
+                    }
+                }
+                __syncwarp();
+                ++filled;
+                ring.next();
+            }
+        }
+        // no copy may be in flight when the CTA leaves: the last turn of every stage that was filled
+        for (u32 i = 0; i < STAGES && i < filled; ++i) {
+            if (ring.s == 0) { ring.s = STAGES; ring.parity ^= 1; }
+            --ring.s;
+            drain_warp(&sh.full[ring.s], ring.parity);
+        }
+    } else if (warp == PRODUCT_WARP && rank == 0) {
+        const u32 idesc = product_idesc(g.bf16, g.m_along_k, g.n_along_k, SPAN, SPAN);
+        const u32 step_m = product_desc_step(g.m_along_k), step_n = product_desc_step(g.n_along_k);
+        Ring<STAGES> ring;
+        u32 turn = 0;
+        bool ok = true;
+        for (u32 t = pair; ok && t < tiles; t += pairs, ++turn) {
+            const u32 b = turn & 1, acc = tmem + b * SPAN;
+            if (turn >= 2 && !wait_warp(&sh, &sh.acc_empty[b], ((turn >> 1) - 1) & 1, g.wait_ns, g.flag)) { ok = false; break; }
+            tm_fence_after();
+            for (u32 k = 0; k < g.k_tiles; ++k) {
+                if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag) ||
+                    !wait_warp(&sh, &sh.peer[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
+                tm_fence_after();
+                const u32 st = base + ring.s * STAGE;
+                const u64 dm = product_desc(st, g.m_along_k), dn = product_desc(st + HALF, g.n_along_k);
+                if (elect_one()) {
+#pragma unroll
+                    for (u32 i = 0; i < PR_K / 16; ++i) tm2_mma_f16(acc, dm + i * step_m, dn + i * step_n, idesc, k || i);
+                    tm2_commit(&sh.empty[ring.s]);
+                    if (k + 1 == g.k_tiles) tm2_commit(&sh.acc_full[b]);
+                }
+                __syncwarp();
+                ring.next();
+            }
+        }
+        if (elect_one()) tm2_commit(&sh.last);
+        __syncwarp();
+    } else if (warp == PRODUCT_WARP) {
+        Ring<STAGES> ring;
+        bool ok = true;
+        for (u32 t = pair; ok && t < tiles; t += pairs) {
+            for (u32 k = 0; k < g.k_tiles; ++k) {
+                if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
+                if (elect_one()) mbar_arrive_cluster_release(cluster_address(&sh.peer[ring.s], 0));
+                __syncwarp();
+                ring.next();
+            }
+        }
+    } else {
+        const u32 quarter = warp & 3, c0 = (warp >> 2) * PR_TILE;          // a warp reads the tensor-memory lanes of its place
+        u32 turn = 0;
+        for (u32 t = pair; t < tiles; t += pairs, ++turn) {
+            u32 mt, nt;
+            place(g, t, mt, nt);
+            const u32 b = turn & 1;
+            __syncwarp();
+            if (!wait_warp(&sh, &sh.acc_full[b], (turn >> 1) & 1, g.wait_ns, g.flag)) break;
+            tm_fence_after();
+            const u64 m = (u64)(2 * mt + rank) * PR_TILE + quarter * 32 + lane;
+            const u64 n0 = (u64)nt * SPAN + c0;
+            const u32 from = tmem + ((quarter * 32) << 16) + b * SPAN + c0;
+            const u64 n_rows = g.turned ? g.end.rows : g.end.cols;
+#pragma unroll 1
+            for (u32 p = 0; p < PR_TILE; p += 32) {
+                u32 v[32];
+                __syncwarp();
+                tm_load32(from + p, v);
+                tm_wait_load();
+                if (p + 32 == PR_TILE) {           // the accumulator is free again
+                    tm_fence_before();
+                    __syncwarp();
+                    if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.acc_empty[b], 0));
+                    __syncwarp();
+                }
+                if (n0 + p >= n_rows) continue;
+                float f[32];
+#pragma unroll
+                for (u32 e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]);
+                if (g.turned) end_column<DT, 32>(g.end, n0 + p, m, (u32)min((u64)32, n_rows - n0 - p), f);
+                else end_row<DT>(g.end, m, n0 + p, f);
+            }
+        }
+    }
+    __syncwarp();
+    tm_fence_before();
+    __syncthreads();
+    // What has been issued is done before tensor memory and the CTAs go, also where only the warps that wait for it gave up.
+    if (warp == PRODUCT_WARP) drain_warp(&sh.last, 0);
+    cluster_barrier();                             // neither CTA's memory is needed any more
+    if (warp == PRODUCT_WARP) tm2_dealloc(tmem, TMEM_COLS);
+}
+
+template <int DT>
+bool launch_as(int sms, cudaStream_t s, const WideArgs& g) {
+    static std::atomic<u64> allowed{0};
+    if (!allow_smem(wide_product_kernel<DT>, allowed, SMEM)) return false;
+    const u64 tiles = (u64)g.m_tiles * g.n_tiles;
+    const u32 pairs = (u32)(tiles < (u64)(sms / 2) ? tiles : (u64)(sms / 2));
+    return launch_chained(wide_product_kernel<DT>, pairs * 2, THREADS, SMEM, 0, s, g);
+}
+
+}  // namespace
+
+bool launch_product_wide(cudaStream_t s, const ProductCall& c) {
+    WideArgs g;
+    g.end = end_args(c.end);
+    g.turned = !g.end.y_vec;
+    const ProductOperand& m = g.turned ? c.b : c.a;
+    const ProductOperand& n = g.turned ? c.a : c.b;
+    if (!product_map(&g.m, m, PR_TILE, c.dtype) || !product_map(&g.n, n, PR_TILE, c.dtype)) return false;
+    g.m_along_k = m.along_k;
+    g.n_along_k = n.along_k;
+    g.bf16 = c.dtype == DT_BF16;
+    g.k_tiles = (u32)((m.k + PR_K - 1) / PR_K);
+    g.m_tiles = (u32)((m.rows + SPAN - 1) / SPAN);
+    g.n_tiles = (u32)((n.rows + SPAN - 1) / SPAN);
+    g.wait_ns = c.wait_ns;
+    g.flag = c.flag;
+    return c.end.y.dtype == DT_F32 ? launch_as<DT_F32>(c.sms, s, g) : c.end.y.dtype == DT_F16 ? launch_as<DT_F16>(c.sms, s, g) : launch_as<DT_BF16>(c.sms, s, g);
+}
+
+}  // namespace excp

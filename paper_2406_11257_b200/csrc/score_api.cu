@@ -2,8 +2,7 @@
 // launches.  No arithmetic lives here.
 #include <cmath>
 
-#include "excp_handle.cuh"
-#include "score.cuh"
+#include "api_checks.cuh"
 
 using namespace excp;
 
@@ -13,11 +12,6 @@ void score_release(ScoreWorkspace& w) {
     if (w.h_flag) cudaFreeHost(w.h_flag);
     w = ScoreWorkspace{};
 }
-}  // namespace excp
-
-namespace {
-
-constexpr int SCORE_TOP_MAX = 64;
 
 // The workspace, allocated once and cleared on the stream of the call that needs it first.  That call waits for the clearing, so
 // that calls on other streams, which nothing orders behind this one, find it done.
@@ -40,29 +34,18 @@ bool ensure_score(excp_handle h, cudaStream_t stream) {
     }
     return ok && check(h, cudaHostGetDevicePointer(reinterpret_cast<void**>(&w.d_flag), w.h_flag, 0));   // last: marks it as ready
 }
+}  // namespace excp
 
-bool dtype_ok(int d) { return d == DT_F32 || d == DT_F16 || d == DT_BF16; }
+namespace {
+
+constexpr int SCORE_TOP_MAX = 64;
+
 bool format_ok(int f) { return f == MX4_E8M0_32 || f == MX4_E4M3_16; }
-size_t elem_bytes(int d) { return d == DT_F32 ? 4 : 2; }
-bool on_element(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) % elem_bytes(dtype)) == 0; }
-bool on_float(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
-// A matrix in ordinary layout: known type, aligned to its elements, rows that do not overlap.
-bool rows_ok(const void* p, int dtype, size_t rows, size_t cols, size_t stride) {
-    if (!dtype_ok(dtype) || rows > MX4_MAX_DIM || cols > MX4_MAX_DIM || stride > (1ull << 40)) return false;
-    if (rows == 0 || cols == 0) return true;
-    return p && on_element(p, dtype) && (rows == 1 || stride >= cols);
-}
 bool packed_ok(const void* p, size_t rows, size_t cols, int format) {
     if (!format_ok(format) || rows > MX4_MAX_DIM || cols > MX4_MAX_DIM) return false;
     // one launch covers the matrix: its 4-row groups of tiles are counted in 32 bits
     if ((u64)mx4_row_tiles(rows) * mx4_col_tiles(cols) > (1ull << 28)) return false;
     return rows == 0 || cols == 0 || (p && aligned16(p));
-}
-
-excp_status finish(excp_handle h) {
-    if (!check(h, cudaGetLastError())) return EXCP_ERR_CUDA;
-    return EXCP_OK;
 }
 
 excp_status matmul_impl(excp_handle h, const void* a, size_t a_rows, const float* a_scale, const void* b, size_t b_rows,

@@ -1,4 +1,4 @@
-// The marshalling of binding.Handle's scoring calls, natively: a decoding step's call takes a few microseconds on the
+// The marshalling of binding.Handle's scoring calls and layers, natively: a decoding step's call takes a few microseconds on the
 // GPU, and reading a tensor's attributes, allocating the result and converting arguments from Python took more than
 // that.  Checks of tensors (TypeError), allocation of results, the current stream, one call through the C ABI, its status
 // (binding.ExcpError).  The addresses of the C functions come from the library that binding.py has loaded.
@@ -29,6 +29,18 @@ struct Api {
     decltype(&excp_mx4_linear) mx4_linear;
     decltype(&excp_token_logprobs) token_logprobs;
     decltype(&excp_token_logprobs_grad) token_logprobs_grad;
+    decltype(&excp_act8_bytes) act8_bytes;
+    decltype(&excp_act8_quantize) act8_quantize;
+    decltype(&excp_act8_restore) act8_restore;
+    decltype(&excp_act_grad_scratch) act_grad_scratch;
+    decltype(&excp_act_grad) act_grad;
+    decltype(&excp_layer_norm) layer_norm;
+    decltype(&excp_layer_norm_grad_scratch) layer_norm_grad_scratch;
+    decltype(&excp_layer_norm_grad) layer_norm_grad;
+    decltype(&excp_linear_scratch) linear_scratch;
+    decltype(&excp_linear) linear;
+    decltype(&excp_linear_grad_input) linear_grad_input;
+    decltype(&excp_linear_grad_weight) linear_grad_weight;
 } api;
 PyObject* excp_error;                              // binding.ExcpError
 
@@ -243,6 +255,199 @@ PyObject* logprobs_grad(PyObject* const* a) {
     return wrap(out);
 }
 
+// ---- the layers before the logits --------------------------------------------------------------------------------------------------
+excp_matrix matrix(const at::Tensor& t, int device, const char* what) {
+    const Rows r = rows(t, device, what);
+    return excp_matrix{r.p, r.dtype, r.rows, r.cols, r.stride};
+}
+excp_matrix shaped(const at::Tensor& t, int device, const char* what, size_t r, size_t c) {
+    const excp_matrix m = matrix(t, device, what);
+    if (m.rows != r || m.cols != c) throw Refused(std::string(what) + ": expected the shape [" + std::to_string(r) + ", " + std::to_string(c) + "]");
+    return m;
+}
+// None, or a matrix of that shape.
+const excp_matrix* optional(PyObject* o, int device, const char* what, size_t r, size_t c, excp_matrix& room) {
+    if (o == Py_None) return nullptr;
+    room = shaped(tensor(o, what), device, what, r, c);
+    return &room;
+}
+// A plain matrix, or the data of a packed one of 8 bits (where `is_packed`).
+excp_matrix kept(PyObject* o, bool is_packed, int device, const char* what, size_t r, size_t c) {
+    const at::Tensor& t = tensor(o, what);
+    if (!is_packed) return shaped(t, device, what, r, c);
+    return excp_matrix{packed(t, device, api.act8_bytes(r, c), what), EXCP_ACT8, r, c, c};
+}
+// One value per column, of type float32 or any 16-bit one.
+void* columns(PyObject* o, int device, int64_t n, int& dtype, const char* what) {
+    dtype = EXCP_F32;
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, what);
+    dtype = dtype_code(t.scalar_type());
+    if (dtype < 0 || t.dim() != 1 || t.numel() != n || !on(t, device) || !t.is_contiguous())
+        throw Refused(std::string(what) + ": expected " + std::to_string(n) + " contiguous float32, float16 or bfloat16 values on cuda:" + std::to_string(device));
+    return t.data_ptr();
+}
+// Scratch from torch's allocator, which hands it out again only behind this call's work.
+struct Scratch {
+    at::Tensor t;
+    void* p = nullptr;
+    Scratch(size_t need, int device) {
+        if (need) p = (t = fresh({(int64_t)need}, at::kByte, device)).data_ptr();
+    }
+};
+bool flag(PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw PythonError{};
+    return v != 0;
+}
+PyObject* or_none(const at::Tensor& t) { return t.defined() ? wrap(t) : Py_NewRef(Py_None); }
+template <typename... O>
+PyObject* tuple(O... items) {
+    PyObject* out = PyTuple_New(sizeof...(items));
+    if (!out) throw PythonError{};
+    Py_ssize_t i = 0;
+    (PyTuple_SET_ITEM(out, i++, items), ...);
+    return out;
+}
+
+// (handle, device, x, out or None)
+PyObject* act8_quantize(PyObject* const* a) {
+    const int device = (int)integer(a[1]);
+    const excp_matrix x = matrix(tensor(a[2], "x"), device, "x");
+    const size_t need = api.act8_bytes(x.rows, x.cols);
+    const at::Tensor out = a[3] == Py_None ? fresh({(int64_t)need}, at::kByte, device) : tensor(a[3], "out");
+    check(api.act8_quantize(handle(a[0]), &x, packed(out, device, need, "out"), stream(device)), "excp_act8_quantize");
+    return wrap(out);
+}
+
+// (handle, device, data, rows, cols, dtype, out or None)
+PyObject* act8_restore(PyObject* const* a) {
+    const int device = (int)integer(a[1]);
+    const long long r = integer(a[3]), c = integer(a[4]);
+    void* p = packed(tensor(a[2], "m"), device, api.act8_bytes(r, c), "m");
+    const at::Tensor out = result(a[6], device, wanted(a[5]), r, c);
+    const excp_matrix y = matrix(out, device, "out");
+    check(api.act8_restore(handle(a[0]), p, &y, stream(device)), "excp_act8_restore");
+    return wrap(out);
+}
+
+// (handle, device, dy, pre or None, pre is packed, act, dpre wanted, again wanted, dbias wanted, out or None) -> (dpre, a, dbias), each or None
+PyObject* act_grad(PyObject* const* a) {
+    const excp_handle h = handle(a[0]);
+    const int device = (int)integer(a[1]), act = (int)integer(a[5]);
+    const at::Tensor& t = tensor(a[2], "dy");
+    const excp_matrix dy = matrix(t, device, "dy");
+    excp_matrix pre, dpre, again;
+    const bool has_pre = a[3] != Py_None;
+    if (has_pre) pre = kept(a[3], flag(a[4]), device, "pre", dy.rows, dy.cols);
+    const int64_t r = (int64_t)dy.rows, c = (int64_t)dy.cols;
+    at::Tensor out, value, db;
+    if (flag(a[6])) dpre = shaped(out = result(a[9], device, t.scalar_type(), r, c), device, "out", r, c);
+    if (flag(a[7])) again = shaped(value = fresh({r, c}, t.scalar_type(), device), device, "again", r, c);
+    if (flag(a[8])) db = fresh({c}, at::kFloat, device);
+    const Scratch room(db.defined() ? api.act_grad_scratch(h, dy.rows, dy.cols) : 0, device);
+    check(api.act_grad(h, act, &dy, has_pre ? &pre : nullptr, out.defined() ? &dpre : nullptr, value.defined() ? &again : nullptr,
+                       db.defined() ? static_cast<float*>(db.data_ptr()) : nullptr, room.p, stream(device)), "excp_act_grad");
+    return tuple(or_none(out), or_none(value), or_none(db));
+}
+
+// (handle, device, x, weight or None, bias or None, eps, rms, kept wanted, out or None) -> (y, row_stats, kept or None)
+PyObject* layer_norm(PyObject* const* a) {
+    const int device = (int)integer(a[1]);
+    const at::Tensor& t = tensor(a[2], "x");
+    const excp_matrix x = matrix(t, device, "x");
+    int wt, bt;
+    void* w = columns(a[3], device, (int64_t)x.cols, wt, "weight");
+    void* b = columns(a[4], device, (int64_t)x.cols, bt, "bias");
+    if (w && b && wt != bt) throw Refused("weight, bias: expected the same type");
+    const double eps = PyFloat_AsDouble(a[5]);
+    if (eps == -1.0 && PyErr_Occurred()) throw PythonError{};
+    const int64_t r = (int64_t)x.rows;
+    const at::Tensor out = result(a[8], device, t.scalar_type(), r, (int64_t)x.cols);
+    const excp_matrix y = matrix(out, device, "out");
+    const at::Tensor stats = fresh({r, 2}, at::kFloat, device);
+    at::Tensor k;
+    if (flag(a[7])) k = fresh({(int64_t)api.act8_bytes(x.rows, x.cols)}, at::kByte, device);
+    check(api.layer_norm(handle(a[0]), &x, w, b, w ? wt : bt, (float)eps, flag(a[6]), &y, static_cast<float*>(stats.data_ptr()), k.defined() ? k.data_ptr() : nullptr,
+                         stream(device)), "excp_layer_norm");
+    return tuple(wrap(out), wrap(stats), or_none(k));
+}
+
+// (handle, device, dy, x, x is packed, weight or None, rms, row_stats, add or None, out or None, vectors wanted) -> (dx, dweight, dbias), the last two or None
+PyObject* layer_norm_grad(PyObject* const* a) {
+    const excp_handle h = handle(a[0]);
+    const int device = (int)integer(a[1]);
+    const at::Tensor& t = tensor(a[2], "dy");
+    const excp_matrix dy = matrix(t, device, "dy"), x = kept(a[3], flag(a[4]), device, "x", dy.rows, dy.cols);
+    const int64_t r = (int64_t)dy.rows, c = (int64_t)dy.cols;
+    int wt;
+    void* w = columns(a[5], device, c, wt, "weight");
+    const bool rms = flag(a[6]), vectors = flag(a[10]);
+    excp_matrix add_room;
+    const excp_matrix* add = optional(a[8], device, "add", dy.rows, dy.cols, add_room);
+    const at::Tensor out = result(a[9], device, t.scalar_type(), r, c);
+    const excp_matrix dx = matrix(out, device, "out");
+    at::Tensor dw, db;
+    if (vectors) dw = fresh({c}, at::kFloat, device);
+    if (vectors && !rms) db = fresh({c}, at::kFloat, device);
+    const Scratch room(api.layer_norm_grad_scratch(h, dy.rows, dy.cols), device);
+    check(api.layer_norm_grad(h, &dy, &x, w, wt, rms, static_cast<float*>(vector(a[7], device, at::kFloat, 2 * r, "row_stats")), add, &dx,
+                              dw.defined() ? static_cast<float*>(dw.data_ptr()) : nullptr, db.defined() ? static_cast<float*>(db.data_ptr()) : nullptr, room.p,
+                              stream(device)), "excp_layer_norm_grad");
+    return tuple(wrap(out), or_none(dw), or_none(db));
+}
+
+// (handle, device, x, w, bias or None, act, residual or None, dtype or None, out or None, keep: None, a dtype or True for 8 bits) -> (y, kept or None)
+PyObject* plain_linear(PyObject* const* a) {
+    const int device = (int)integer(a[1]), act = (int)integer(a[5]);
+    const at::Tensor& t = tensor(a[2], "x");
+    const excp_matrix x = matrix(t, device, "x"), w = matrix(tensor(a[3], "w"), device, "w");
+    int bt;
+    void* b = columns(a[4], device, (int64_t)w.rows, bt, "bias");
+    const int64_t r = (int64_t)x.rows, n = (int64_t)w.rows;
+    excp_matrix residual_room, keep;
+    const excp_matrix* residual = optional(a[6], device, "residual", x.rows, w.rows, residual_room);
+    const at::Tensor out = result(a[8], device, a[7] == Py_None ? t.scalar_type() : wanted(a[7]), r, n);
+    const excp_matrix y = matrix(out, device, "out");
+    at::Tensor k;
+    if (a[9] == Py_True) {
+        k = fresh({(int64_t)api.act8_bytes(x.rows, w.rows)}, at::kByte, device);
+        keep = excp_matrix{k.data_ptr(), EXCP_ACT8, x.rows, w.rows, w.rows};
+    } else if (a[9] != Py_None) {
+        keep = matrix(k = fresh({r, n}, wanted(a[9]), device), device, "kept");
+    }
+    const Scratch room(api.linear_scratch(&x, &w), device);
+    check(api.linear(handle(a[0]), &x, &w, b, bt, act, residual, &y, k.defined() ? &keep : nullptr, room.p, stream(device)), "excp_linear");
+    return tuple(wrap(out), or_none(k));
+}
+
+// (handle, device, dy, w, add or None, dtype or None, out or None)
+PyObject* linear_grad_input(PyObject* const* a) {
+    const int device = (int)integer(a[1]);
+    const at::Tensor& t = tensor(a[2], "dy");
+    const excp_matrix dy = matrix(t, device, "dy"), w = matrix(tensor(a[3], "w"), device, "w");
+    excp_matrix add_room;
+    const excp_matrix* add = optional(a[4], device, "add", dy.rows, w.cols, add_room);
+    const at::Tensor out = result(a[6], device, a[5] == Py_None ? t.scalar_type() : wanted(a[5]), (int64_t)dy.rows, (int64_t)w.cols);
+    const excp_matrix dx = matrix(out, device, "out");
+    const Scratch room(api.linear_scratch(&dy, &w), device);
+    check(api.linear_grad_input(handle(a[0]), &dy, &w, add, &dx, room.p, stream(device)), "excp_linear_grad_input");
+    return wrap(out);
+}
+
+// (handle, device, dy, x, add or None, dtype, out or None)
+PyObject* linear_grad_weight(PyObject* const* a) {
+    const int device = (int)integer(a[1]);
+    const excp_matrix dy = matrix(tensor(a[2], "dy"), device, "dy"), x = matrix(tensor(a[3], "x"), device, "x");
+    excp_matrix add_room;
+    const excp_matrix* add = optional(a[4], device, "add", dy.cols, x.cols, add_room);
+    const at::Tensor out = result(a[6], device, wanted(a[5]), (int64_t)dy.cols, (int64_t)x.cols);
+    const excp_matrix dw = matrix(out, device, "out");
+    const Scratch room(api.linear_scratch(&dy, &x), device);
+    check(api.linear_grad_weight(handle(a[0]), &dy, &x, add, &dw, room.p, stream(device)), "excp_linear_grad_weight");
+    return wrap(out);
+}
+
 // Python's side: argument count, and no C++ exception leaves.
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -301,6 +506,14 @@ PyMethodDef methods[] = {
     EXCP_ENTRY("mx4_linear", linear, 13),
     EXCP_ENTRY("token_logprobs", logprobs, 6),
     EXCP_ENTRY("token_logprobs_grad", logprobs_grad, 9),
+    EXCP_ENTRY("act8_quantize", act8_quantize, 4),
+    EXCP_ENTRY("act8_restore", act8_restore, 7),
+    EXCP_ENTRY("act_grad", act_grad, 10),
+    EXCP_ENTRY("layer_norm", layer_norm, 9),
+    EXCP_ENTRY("layer_norm_grad", layer_norm_grad, 11),
+    EXCP_ENTRY("linear", plain_linear, 10),
+    EXCP_ENTRY("linear_grad_input", linear_grad_input, 7),
+    EXCP_ENTRY("linear_grad_weight", linear_grad_weight, 7),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_score", "Native marshalling of the scoring calls.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
