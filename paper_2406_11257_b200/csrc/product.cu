@@ -1,13 +1,13 @@
 // The product with plain 16-bit operands: c[i, j] = sum over k of a[i, k] b[j, k], fp32 sums, and its epilogue.
 // This file: few rows on one side (the tokens of a decoding step), or too few tiles for the kernel of many (product_wide.cu).
 //
-// Bound: with few rows the bytes of the larger operand.  Its rows go on the M side of the tensor core (128 per tile), the few rows on the
-// N side, which takes them in steps of 16.  Two CTAs share an SM, and the columns of a tile are split over a cluster so that
-// every SM streams; each CTA sends its part of a column of the accumulator to the CTA that owns the column (distributed
-// shared memory), which adds them in a fixed order.
+// Bound: with few rows the bytes of the larger operand, else what an SM can fetch (about 120 bytes a ns).  The larger operand's rows go on
+// the M side of the tensor core (128 per tile), the few rows on the N side, which takes them in steps of 16.  Where there are too few
+// tiles for the SMs the columns of a tile are split over a cluster: each CTA sends its part of the accumulator to the CTAs that own its
+// columns (bulk copies between their shared memories), which add the parts in a fixed order.
 //
-// Roles: warp 4 fetches both operands (tensor maps; what lies past an edge comes as 0), warp 5 issues the products, warps 0..3
-// write the result.
+// Roles: warps 0..3 fetch the operands (tensor maps; what lies past an edge comes as 0), warp 8 issues the products, and at the end
+// warps 0..7 write the result.
 // Every wait for a copy or a product is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and
 // leaves.  The two that hardware gives no limit, for tensor memory and at the cluster's barrier, depend only on CTAs whose own
 // waits are bounded.
@@ -16,10 +16,12 @@
 namespace excp {
 namespace {
 
-constexpr int WORK_WARPS = 4;
-constexpr u32 FETCH_WARP = WORK_WARPS, PRODUCT_WARP = WORK_WARPS + 1;
-constexpr int THREADS = (WORK_WARPS + 2) * 32;
-constexpr int STAGES_MAX = 12;
+constexpr int WORK_WARPS = 8;
+constexpr u32 PRODUCT_WARP = WORK_WARPS;
+constexpr int THREADS = (PRODUCT_WARP + 1) * 32;
+constexpr int BOUND_THREADS = 320;                 // 96 registers a thread: five of the 18 warps of two CTAs share a quarter of the registers
+constexpr int STAGES_MAX = 8;
+constexpr u32 BOXES_MAX = 2;                       // boxes of 64 columns in a stage
 constexpr u32 MAX_SPLIT = 8;
 constexpr u32 M_BYTES = PR_TILE * PR_K * 2;
 constexpr u32 SMEM_MAX = 227 * 1024 - 1024;        // dynamic shared memory of a block, beside what the kernel has of its own
@@ -27,9 +29,11 @@ constexpr u32 SMEM_MAX = 227 * 1024 - 1024;        // dynamic shared memory of a
 struct NarrowArgs {
     CUtensorMap m, n;
     u32 m_along_k, n_along_k, bf16;
-    u32 k_tiles, n_tiles;
+    u32 k_boxes, n_tiles;
+    u32 boxes;                                     // of a stage
     u32 nt;                                        // rows of n per CTA: a multiple of 16, at most 256
     u32 n_bytes, stages, tmem_cols;
+    u32 ring_bytes;                                // of the stages; afterwards the accumulator lies there
     u32 per_owner;                                 // columns of the accumulator that a CTA of the cluster joins
     u32 turned;                                    // m is b: a lane has a column of c
     EndArgs end;
@@ -41,6 +45,7 @@ struct Shared {
     unsigned long long full[STAGES_MAX];           // copies have landed
     unsigned long long empty[STAGES_MAX];          // the stage has been multiplied
     unsigned long long done;
+    unsigned long long parts;                      // the other CTAs' parts of the own columns have landed
     u32 tmem;
     volatile u32 abort;
 };
@@ -52,8 +57,15 @@ struct Turn {                                      // the place in the ring of s
     }
 };
 
+__device__ __forceinline__ void work_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// Shared memory of this CTA -> that of another of the cluster (addresses within the cluster), arriving at a barrier there.
+__device__ __forceinline__ void bulk_s2s(u32 to, const void* from, u32 bytes, u32 bar) {
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(to), "r"(smem_u32(from)), "r"(bytes), "r"(bar) : "memory");
+}
+
 template <int DT>
-__global__ void __launch_bounds__(THREADS, 2) product_kernel(const __grid_constant__ NarrowArgs g) {
+__global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_constant__ NarrowArgs g) {
     extern __shared__ unsigned char smem_raw[];
     __shared__ Shared sh;
     const u32 part = cluster_rank(), parts = cluster_size();
@@ -61,69 +73,74 @@ __global__ void __launch_bounds__(THREADS, 2) product_kernel(const __grid_consta
     unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const u32 warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const u32 tile = blockIdx.x / parts, mt = tile / g.n_tiles, ntile = tile - mt * g.n_tiles;
-    const u32 k0 = (u32)((u64)g.k_tiles * part / parts), k1 = (u32)((u64)g.k_tiles * (part + 1) / parts);
-    const u32 stage = M_BYTES + g.n_bytes;
-    float* const joined = reinterpret_cast<float*>(smem + g.stages * stage);       // [part][own column][row]
+    const u32 k_steps = (g.k_boxes + g.boxes - 1) / g.boxes;
+    const u32 k0 = (u32)((u64)k_steps * part / parts), k1 = (u32)((u64)k_steps * (part + 1) / parts);
+    const u32 box = M_BYTES + g.n_bytes, stage = g.boxes * box;
+    const u64 n0 = (u64)ntile * g.nt, n_rows = g.turned ? g.end.rows : g.end.cols;
+    const u32 cols = (u32)min((u64)g.nt, n_rows - n0);         // of the accumulator that are results
+    // the CTA's own columns of the accumulator, and the others' parts of them: [part][column][row]
+    const u32 own = part * g.per_owner, own_cols = own < cols ? min(g.per_owner, cols - own) : 0;
+    float* const received = reinterpret_cast<float*>(smem + g.ring_bytes);
+    float* const acc = reinterpret_cast<float*>(smem);         // [column][row], once the stages are not needed any more
 
     if (threadIdx.x == 0) {
-        for (u32 s = 0; s < g.stages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
+        for (u32 s = 0; s < g.stages; ++s) { mbar_init(&sh.full[s], 2 * g.boxes); mbar_init(&sh.empty[s], 1); }
         mbar_init(&sh.done, 1);
+        mbar_init(&sh.parts, 1);
         sh.abort = 0;
         mbar_fence_init();
+        if (parts > 1) mbar_arrive_expect_tx(&sh.parts, (parts - 1) * own_cols * PR_TILE * 4);
     }
     if (warp == PRODUCT_WARP) tm_alloc(&sh.tmem, g.tmem_cols);
-    if (warp == FETCH_WARP && g.k_tiles && elect_one()) { tma_prefetch_map(&g.m); tma_prefetch_map(&g.n); }
+    if (warp == 0 && g.k_boxes && elect_one()) { tma_prefetch_map(&g.m); tma_prefetch_map(&g.n); }
     __syncwarp();
     wait_for_previous();
     let_next_start();
     tm_fence_before();
     __syncthreads();
-    if (parts > 1) cluster_arrive();
+    if (parts > 1) cluster_arrive_release();
     tm_fence_after();
     const u32 tmem = sh.tmem;
-    bool ok = true;                                // this warp's waits were all met
 
-    if (warp == FETCH_WARP) {
-        Turn ring;
-        u32 filled = 0;
-        const u32 m_row = mt * PR_TILE, n_row = ntile * g.nt;
-        for (u32 k = k0; k < k1; ++k) {
-            if (filled >= g.stages && !(ok = wait_warp(&sh, &sh.empty[ring.s], ring.parity ^ 1, g.wait_ns, g.flag))) break;
-            unsigned char* st = smem + ring.s * stage;
-            unsigned long long* bar = &sh.full[ring.s];
+    if (warp < 2 * BOXES_MAX) {                    // two warps for each operand, which take turns at its boxes
+        const bool is_n = warp >= BOXES_MAX;
+        const CUtensorMap* map = is_n ? &g.n : &g.m;
+        const bool along_k = is_n ? g.n_along_k : g.m_along_k;
+        const u32 first = is_n ? ntile * g.nt : mt * PR_TILE, rows = is_n ? g.nt : PR_TILE, bytes = is_n ? g.n_bytes : M_BYTES;
+        u32 turns = k1 - k0;                       // of the ring that are filled
+        for (u32 i = warp % BOXES_MAX; i < turns * g.boxes; i += BOXES_MAX) {
+            const u32 turn = g.boxes == 1 ? i : i / BOXES_MAX, lap = turn / g.stages, s = turn - lap * g.stages;
+            if (lap && !wait_warp(&sh, &sh.empty[s], (lap - 1) & 1, g.wait_ns, g.flag)) { turns = turn; break; }
+            unsigned char* to = smem + s * stage + (g.boxes == 1 ? 0 : warp % BOXES_MAX * box) + (is_n ? M_BYTES : 0);
+            unsigned long long* bar = &sh.full[s];
+            const u32 k = k0 * g.boxes + i, col = k * PR_K;
             if (elect_one()) {
-                mbar_arrive_expect_tx(bar, stage);
-                if (g.m_along_k) {
-                    tma_load_2d(st, &g.m, k * PR_K, m_row, bar);
-                } else {
-                    tma_load_2d(st, &g.m, m_row, k * PR_K, bar);
-                    tma_load_2d(st + PR_CHUNK_BYTES, &g.m, m_row + PR_CHUNK, k * PR_K, bar);
+                mbar_arrive_expect_tx(bar, k < g.k_boxes ? bytes : 0);
+                if (k < g.k_boxes) {
+                    if (along_k) tma_load_2d(to, map, col, first, bar);
+                    else for (u32 c = 0; c < rows; c += PR_CHUNK) tma_load_2d(to + c / PR_CHUNK * PR_CHUNK_BYTES, map, first + c, col, bar);
                 }
-                if (g.n_along_k) tma_load_2d(st + M_BYTES, &g.n, k * PR_K, n_row, bar);
-                else for (u32 c = 0; c < g.nt; c += PR_CHUNK) tma_load_2d(st + M_BYTES + c / PR_CHUNK * PR_CHUNK_BYTES, &g.n, n_row + c, k * PR_K, bar);
             }
             __syncwarp();
-            ++filled;
-            ring.next(g.stages);
         }
         // no copy may be in flight when the CTA leaves: the last turn of every stage that was filled
-        for (u32 i = 0; i < g.stages && i < filled; ++i) {
-            if (ring.s == 0) { ring.s = g.stages; ring.parity ^= 1; }
-            --ring.s;
-            drain_warp(&sh.full[ring.s], ring.parity);
-        }
+        for (u32 t = turns > g.stages ? turns - g.stages : 0; t < turns; ++t) drain_warp(&sh.full[t % g.stages], t / g.stages & 1);
     } else if (warp == PRODUCT_WARP) {
         const u32 idesc = product_idesc(g.bf16, g.m_along_k, g.n_along_k, PR_TILE, g.nt);
         const u32 step_m = product_desc_step(g.m_along_k), step_n = product_desc_step(g.n_along_k);
         Turn ring;
         for (u32 k = k0; k < k1; ++k) {
-            if (!(ok = wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag))) break;
-            tm_fence_after();
+            if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag)) break;
             const u32 st = smem_u32(smem) + ring.s * stage;
             const u64 dm = product_desc(st, g.m_along_k), dn = product_desc(st + M_BYTES, g.n_along_k);
             if (elect_one()) {
 #pragma unroll
-                for (u32 i = 0; i < PR_K / 16; ++i) tm_mma_f16(tmem, dm + i * step_m, dn + i * step_n, idesc, k > k0 || i);
+                for (u32 u = 0; u < BOXES_MAX; ++u) {
+                    if (u >= g.boxes || k * g.boxes + u >= g.k_boxes) break;
+#pragma unroll
+                    for (u32 i = 0; i < PR_K / 16; ++i)
+                        tm_mma_f16(tmem, dm + u * (box >> 4) + i * step_m, dn + u * (box >> 4) + i * step_n, idesc, k > k0 || u || i);
+                }
                 tm_commit(&sh.empty[ring.s]);
             }
             __syncwarp();
@@ -132,75 +149,96 @@ __global__ void __launch_bounds__(THREADS, 2) product_kernel(const __grid_consta
         if (elect_one()) tm_commit(&sh.done);
         __syncwarp();
         drain_warp(&sh.done, 0);                   // what has been issued is done before tensor memory goes
-    } else {
-        ok = wait_warp(&sh, &sh.done, 0, g.wait_ns, g.flag);
-        tm_fence_after();
     }
-
-    const u32 t = threadIdx.x;
-    const u64 m = (u64)mt * PR_TILE + t, n0 = (u64)ntile * g.nt, n_rows = g.turned ? g.end.rows : g.end.cols;
-    const u32 cols = (u32)min((u64)g.nt, n_rows - n0);         // of the accumulator that are results
-    // Columns c .. c + W - 1 of the accumulator, complete.  Whole warps.
-    auto put = [&](auto width, u32 c, float (&f)[decltype(width)::value]) {
-        constexpr u32 W = decltype(width)::value;
-        if (c >= cols) return;
-        if (g.turned) end_column<DT, W>(g.end, n0 + c, m, min(W, cols - c), f);
-        else if constexpr (W == 32) end_row<DT>(g.end, m, n0 + c, f);
-    };
-    auto take = [&](auto width, u32 c) {
-        constexpr u32 W = decltype(width)::value;
-        u32 v[W];
-        __syncwarp();
-        if constexpr (W == 32) tm_load32(tmem + ((warp * 32) << 16) + c, v);
-        else { tm_load8(tmem + ((warp * 32) << 16) + c, v); tm_load8(tmem + ((warp * 32) << 16) + c + 8, v + 8); }
-        tm_wait_load();
-        float f[W];
-#pragma unroll
-        for (u32 e = 0; e < W; ++e) f[e] = k0 < k1 ? __uint_as_float(v[e]) : 0.f;
-        if (parts == 1) {
-            put(width, c, f);
-        } else {
-            // column c belongs to CTA c / per_owner, which has a place for this CTA's part of it
-            u32 owner = c / g.per_owner, place = c - owner * g.per_owner;
-#pragma unroll
-            for (u32 e = 0; e < W; ++e) {
-                if (c + e < cols) st_cluster(cluster_address(joined + (part * g.per_owner + place) * PR_TILE + t, owner), f[e]);
-                if (++place == g.per_owner) { place = 0; ++owner; }
-            }
-        }
-    };
-    if (parts > 1) cluster_wait();                 // every CTA of the cluster has started
+    if (parts > 1) cluster_wait();                 // every CTA of the cluster has started, its barriers are ready
     if (warp < WORK_WARPS) {
-        if (g.nt >= 32) {
-            for (u32 c = 0; c < cols; c += 32) take(std::integral_constant<u32, 32>(), c);
+        // warps w and w + 4 read the same lanes of tensor memory, every other chunk of columns
+        const u32 quarter = warp & 3, half = warp >> 2, row = quarter * 32 + (threadIdx.x & 31);
+        const u32 lanes = tmem + ((quarter * 32) << 16);
+        const u64 m = (u64)mt * PR_TILE + row;
+        const float bias = g.turned ? column_bias(g.end, m) : 0.f;
+        const bool ok = wait_warp(&sh, &sh.done, 0, g.wait_ns, g.flag);
+        tm_fence_after();
+        auto put = [&](auto width, u32 c, u32 count, float (&f)[decltype(width)::value]) {     // columns c .. of the tile, complete
+            constexpr u32 W = decltype(width)::value;
+            if (g.turned) end_column<DT, W>(g.end, n0 + c, m, min(W, count), bias, f);
+            else if constexpr (W == 32) end_row<DT>(g.end, m, n0 + c, f);
+        };
+        auto take = [&](auto width, u32 c, float (&f)[decltype(width)::value]) {
+            constexpr u32 W = decltype(width)::value;
+            u32 v[W];
+            __syncwarp();
+            if constexpr (W == 32) {
+                tm_load32(lanes + c, v);
+            } else {
+#pragma unroll
+                for (u32 i = 0; i < W; i += 8) tm_load8(lanes + c + i, v + i);
+            }
+            tm_wait_load();
+#pragma unroll
+            for (u32 e = 0; e < W; ++e) f[e] = k0 < k1 ? __uint_as_float(v[e]) : 0.f;
+        };
+        auto whole = [&](auto width) {
+            constexpr u32 W = decltype(width)::value;
+            for (u32 c = half * W; c < cols; c += 2 * W) {
+                float f[W];
+                take(width, c, f);
+                put(width, c, cols - c, f);
+            }
+        };
+        auto send = [&](auto width) {              // the accumulator to shared memory
+            constexpr u32 W = decltype(width)::value;
+            for (u32 c = half * W; c < cols; c += 2 * W) {
+                float f[W];
+                take(width, c, f);
+#pragma unroll
+                for (u32 e = 0; e < W; ++e) if (c + e < g.nt) acc[(c + e) * PR_TILE + row] = f[e];
+            }
+        };
+        auto join = [&](auto width) {              // own columns: their parts in ascending order
+            constexpr u32 W = decltype(width)::value;
+            for (u32 c = half * W; c < own_cols; c += 2 * W) {
+                float f[W];
+                for (u32 p = 0; p < parts; ++p) {
+                    const float* from = p == part ? acc + (own + c) * PR_TILE + row : received + (p * g.per_owner + c) * PR_TILE + row;
+#pragma unroll
+                    for (u32 e = 0; e < W; ++e) {
+                        const float v = c + e < own_cols ? from[e * PR_TILE] : 0.f;
+                        f[e] = p ? f[e] + v : v;
+                    }
+                }
+                put(width, own + c, own_cols - c, f);
+            }
+        };
+        if (parts == 1) {
+            if (!g.turned) whole(std::integral_constant<u32, 32>());
+            else if (g.nt > 16) whole(std::integral_constant<u32, 16>());
+            else whole(std::integral_constant<u32, 8>());
         } else {
-            take(std::integral_constant<u32, 16>(), 0);
+            send(std::integral_constant<u32, 8>());
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the copies read what was just written
+            work_barrier();
+            if (warp == 0 && ok && elect_one()) {
+                for (u32 i = 1; i < parts; ++i) {
+                    const u32 to = part + i < parts ? part + i : part + i - parts, first = to * g.per_owner;
+                    const u32 count = first < cols ? min(g.per_owner, cols - first) : 0;
+                    if (count)
+                        bulk_s2s(cluster_address(received + part * g.per_owner * PR_TILE, to), acc + first * PR_TILE, count * PR_TILE * 4,
+                                 cluster_address(&sh.parts, to));
+                }
+            }
+            __syncwarp();
+            if (own_cols && !wait_warp(&sh, &sh.parts, 0, g.wait_ns, g.flag)) drain_warp(&sh.parts, 0);    // what is on its way lands
+            if (!g.turned) join(std::integral_constant<u32, 32>());
+            else join(std::integral_constant<u32, 8>());
         }
         tm_fence_before();
     }
     __syncwarp();
-    if (parts > 1) {
-        cluster_arrive_release();
+    if (parts > 1) {                               // the others have what this CTA sent
+        cluster_arrive();
         cluster_wait();
-        if (warp < WORK_WARPS) {
-            const u32 first = part * g.per_owner, count = first < cols ? min(g.per_owner, cols - first) : 0;
-            auto join = [&](auto width, u32 c) {   // own columns c ..: their parts in ascending order
-                constexpr u32 W = decltype(width)::value;
-                float f[W];
-#pragma unroll
-                for (u32 e = 0; e < W; ++e) f[e] = joined[min(c + e, g.per_owner - 1) * PR_TILE + t];
-                for (u32 p = 1; p < parts; ++p) {
-#pragma unroll
-                    for (u32 e = 0; e < W; ++e) f[e] += joined[(p * g.per_owner + min(c + e, g.per_owner - 1)) * PR_TILE + t];
-                }
-                if (g.turned) end_column<DT, W>(g.end, n0 + first + c, m, min(W, count - c), f);
-                else if constexpr (W == 32) end_row<DT>(g.end, m, n0 + first + c, f);
-            };
-            if (!g.turned) for (u32 c = 0; c < count; c += 32) join(std::integral_constant<u32, 32>(), c);
-            else for (u32 c = 0; c < count; c += 8) join(std::integral_constant<u32, 8>(), c);
-        }
     }
-    __syncwarp();
     __syncthreads();
     tm_fence_after();
     if (warp == PRODUCT_WARP) tm_dealloc(tmem, g.tmem_cols);
@@ -213,44 +251,145 @@ bool launch_as(cudaStream_t s, const NarrowArgs& g, u32 blocks, u32 parts, u32 s
     return launch_chained(product_kernel<DT>, blocks, THREADS, smem, parts, s, g);
 }
 
-bool launch_narrow(cudaStream_t s, const ProductCall& c) {
+// How a product is cut: which operand is on which side, rows of n per CTA, CTAs that share the columns of a tile.
+struct Cut {
+    bool turned;
+    u32 nt, parts, boxes, stages, smem, ring_bytes, per_owner;
+    float us;
+};
+
+// Blocks that run at once in clusters of `parts`, `beside` of them on an SM.  Clusters stay within a group of SMs, whose sizes only the
+// driver knows (which counts one block to an SM of a kernel that uses tensor memory, however little).
+u32 at_once(int sms, u32 parts, u32 beside) {
+    if (parts == 1) return (u32)sms * beside;
+    static std::atomic<u32> known[MAX_SPLIT + 1];
+    u32 n = known[parts].load(std::memory_order_relaxed);
+    if (n) return n * beside;
+    static std::atomic<u64> allowed{0};
+    int clusters = 0;
+    if (allow_smem(product_kernel<DT_F32>, allowed, SMEM_MAX)) {
+        cudaLaunchConfig_t cfg{};
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = parts;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.gridDim = dim3((u32)sms / parts * parts);
+        cfg.blockDim = dim3(THREADS);
+        cfg.dynamicSmemBytes = SMEM_MAX;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&clusters, product_kernel<DT_F32>, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            clusters = 0;
+        }
+    }
+    n = clusters > 0 ? (u32)clusters * parts : 1;  // 1: nothing is split so
+    known[parts].store(n, std::memory_order_relaxed);
+    return n * beside;
+}
+
+// About how long a cut takes, in us, as measured: 3.2 for a launch, its first copies and the end; what an SM fetches, 135 bytes a ns (a CTA
+// alone 75 where it comes from memory, which gives 6500 in all, or 5600 to fewer than three CTAs on two SMs; L2 15000), and at least the
+// products (1.05 ns for a row of n and 64 columns); 10 ns for a column of the accumulator that lanes write across rows of y and 4 along
+// them; 1 and 0.25 a part and 6 ns a column for the exchange within a cluster; 6 for a further turn of the SMs.
+Cut find_cut(const ProductCall& c, bool y_vec) {
+    Cut best{};
+    best.us = 1e30f;
+    const u32 k_boxes = (u32)((c.a.k + PR_K - 1) / PR_K);
+    const float memory = (float)(c.a.rows + c.b.rows) * (float)c.a.k * 2.f, alone = memory > 60e6f ? 75e3f : 135e3f, all = memory > 60e6f ? 6.5e6f : 15e6f;
+    for (int side = 0; side < 2; ++side) {
+        const bool turned = side == 0;
+        if (!turned && !y_vec) break;              // rows of y that start anywhere are written across
+        const ProductOperand& m = turned ? c.b : c.a;
+        const ProductOperand& n = turned ? c.a : c.b;
+        const u64 m_tiles = (m.rows + PR_TILE - 1) / PR_TILE;
+        for (u32 want : {16u, 32u, 48u, 64u, 96u, 128u}) {
+            if (!turned && want % 32) continue;    // whole blocks of 32 columns
+            if (want > 16 && want >= n.rows + 32) break;
+            const u64 tiles = m_tiles * ((n.rows + want - 1) / want);
+            const u32 n_bytes = n.along_k ? want * PR_K * 2 : (want + PR_CHUNK - 1) / PR_CHUNK * PR_CHUNK_BYTES;
+            for (u32 parts = 1; parts <= MAX_SPLIT && (parts == 1 || (k_boxes >= parts && tiles * parts <= (u64)c.sms * 2)); ++parts) {
+                Cut cut{turned, want, parts, BOXES_MAX, 0, 0, 0, 0, 0.f};
+                cut.per_owner = (want + parts - 1) / parts;
+                if (!turned) cut.per_owner = (cut.per_owner + 31) & ~31u;
+                const u32 sums = parts > 1 ? parts * cut.per_owner * PR_TILE * 4 : 0, own = parts > 1 ? want * PR_TILE * 4 : 0;
+                const u32 box = M_BYTES + n_bytes;
+                auto room_for = [&](u32 room, u32 boxes) { return room > sums + 1024 ? (room - sums - 1024) / (box * boxes) : 0u; };
+                auto steps_of = [&](u32 boxes) { return (k_boxes + boxes - 1) / boxes / parts + ((k_boxes + boxes - 1) / boxes % parts != 0); };
+                // Two CTAs to an SM where there are more than one each; two boxes of 64 columns to a stage (waiting for one and handing it back
+                // cost 250 cycles, whatever it holds), or one: the first of these that leaves enough stages.
+                bool two = false;
+                u32 stages = 0;
+                for (u32 way = tiles * parts > (u64)c.sms ? 0 : 2; way < 4; ++way) {
+                    two = way < 2;
+                    cut.boxes = way % 2 ? 1 : BOXES_MAX;
+                    stages = room_for(two ? SMEM_MAX / 2 - 1024 : SMEM_MAX, cut.boxes);
+                    if (stages >= (cut.boxes == 1 ? 4 : 3) || stages >= steps_of(cut.boxes)) break;
+                }
+                if (!stages) continue;
+                if (stages > STAGES_MAX) stages = STAGES_MAX;
+                const u32 steps = steps_of(cut.boxes);
+                if (parts > 1 && (k_boxes + cut.boxes - 1) / cut.boxes < parts) continue;
+                cut.stages = stages < steps ? stages : steps ? steps : 1;
+                cut.ring_bytes = cut.stages * cut.boxes * box > own ? cut.stages * cut.boxes * box : own;
+                cut.smem = cut.ring_bytes + sums + 1024;
+                if (cut.smem > SMEM_MAX) continue;
+                const u64 room = at_once(c.sms, parts, two ? 2 : 1), blocks = tiles * parts;
+                if (parts > 1 && blocks > room) continue;
+                const u64 per_sm = (blocks + c.sms - 1) / c.sms, turns = (blocks + room - 1) / room;
+                const float beside = two && per_sm > 1 ? 2.f : 1.f, rate = fminf(alone, 135e3f / beside);
+                const float step = cut.boxes * fmaxf((float)box / rate, beside * want * 1.05e-3f);
+                const float whole = memory > 60e6f && blocks * 2 < (u64)c.sms * 3 ? 1.16f * memory / all : memory / all;
+                cut.us = 3.2f + fmaxf((float)turns * steps * step, whole) + (turns - 1) * 6.f +
+                         (float)turns * want / parts * (turned ? 0.010f : 0.004f) + (parts > 1 ? 1.f + 0.25f * parts + 0.006f * want : 0.f);
+                if (cut.us < best.us) best = cut;
+            }
+        }
+    }
+    return best;
+}
+
+// The search takes 10 us of host time: the cuts of the last shapes are kept (a function of the sizes alone).
+Cut best_cut(const ProductCall& c, bool y_vec) {
+    struct Entry {
+        u64 a_rows = 0, b_rows = 0, k = 0;
+        u32 how = 0;
+        Cut cut;
+    };
+    thread_local Entry kept[32];
+    const u32 how = 1u | (c.a.along_k ? 2u : 0u) | (c.b.along_k ? 4u : 0u) | (y_vec ? 8u : 0u) | (u32)c.sms << 4;
+    Entry& e = kept[((c.a.rows * 31 + c.b.rows) * 31 + c.a.k * 7 + how) * 0x9e3779b97f4a7c15ull >> 59];
+    if (e.how != how || e.a_rows != c.a.rows || e.b_rows != c.b.rows || e.k != c.a.k) e = Entry{c.a.rows, c.b.rows, c.a.k, how, find_cut(c, y_vec)};
+    return e.cut;
+}
+
+bool launch_narrow(cudaStream_t s, const ProductCall& c, const EndArgs& end, const Cut& cut) {
     NarrowArgs g;
-    g.end = end_args(c.end);
-    // The fewer rows on the N side: b's rows on the M side where that leaves fewer tiles, or rows of y do not start on 32 bytes.
-    const bool few_a = c.a.rows <= c.b.rows;
-    const u64 few = few_a ? c.a.rows : c.b.rows;
-    g.turned = few <= PR_TILE ? few_a : !g.end.y_vec;
+    g.end = end;
+    g.turned = cut.turned;
     const ProductOperand& m = g.turned ? c.b : c.a;
     const ProductOperand& n = g.turned ? c.a : c.b;
-    g.nt = n.rows >= PR_TILE ? PR_TILE : (u32)((n.rows + 15) & ~15ull);
-    if (!g.turned && g.nt < PR_TILE) g.nt = (g.nt + 31) & ~31u;        // whole blocks of 32 columns
+    g.nt = cut.nt;
     g.n_tiles = (u32)((n.rows + g.nt - 1) / g.nt);
-    g.k_tiles = (u32)((m.k + PR_K - 1) / PR_K);
+    g.k_boxes = (u32)((m.k + PR_K - 1) / PR_K);
     const u64 m_tiles = (m.rows + PR_TILE - 1) / PR_TILE;
-    u32 parts = 1;
-    while (parts < MAX_SPLIT && m_tiles * g.n_tiles * (parts + 1) <= (u64)c.sms * 2 && g.k_tiles >= 4 * (parts + 1)) ++parts;
     g.n_bytes = n.along_k ? g.nt * PR_K * 2 : (g.nt + PR_CHUNK - 1) / PR_CHUNK * PR_CHUNK_BYTES;
-    g.per_owner = (g.nt + parts - 1) / parts;
-    if (!g.turned) g.per_owner = (g.per_owner + 31) & ~31u;
-    const u32 sums = parts > 1 ? parts * g.per_owner * PR_TILE * 4 : 0, stage = M_BYTES + g.n_bytes;
-    const u32 room = SMEM_MAX / 2 - 1024 - 1024;   // two CTAs to an SM
-    u32 stages = (room > sums ? room - sums : 0) / stage;
-    if (stages < 3) stages = (SMEM_MAX - 1024 - sums) / stage;
-    if (stages > STAGES_MAX) stages = STAGES_MAX;
-    if (stages > (g.k_tiles + parts - 1) / parts) stages = (g.k_tiles + parts - 1) / parts;
-    g.stages = stages ? stages : 1;
+    g.boxes = cut.boxes;
+    g.per_owner = cut.per_owner;
+    g.stages = cut.stages;
+    g.ring_bytes = cut.ring_bytes;
     g.tmem_cols = 32;
     while (g.tmem_cols < g.nt) g.tmem_cols *= 2;
-    if (g.k_tiles && (!product_map(&g.m, m, PR_TILE, c.dtype) || !product_map(&g.n, n, g.nt, c.dtype))) return false;
+    if (g.k_boxes && (!product_map(&g.m, m, PR_TILE, c.dtype) || !product_map(&g.n, n, g.nt, c.dtype))) return false;
     g.m_along_k = m.along_k;
     g.n_along_k = n.along_k;
     g.bf16 = c.dtype == DT_BF16;
     g.wait_ns = c.wait_ns;
     g.flag = c.flag;
-    const u32 smem = g.stages * stage + sums + 1024, blocks = (u32)(m_tiles * g.n_tiles) * parts;
-    return c.end.y.dtype == DT_F32 ? launch_as<DT_F32>(s, g, blocks, parts, smem)
-         : c.end.y.dtype == DT_F16 ? launch_as<DT_F16>(s, g, blocks, parts, smem)
-                                   : launch_as<DT_BF16>(s, g, blocks, parts, smem);
+    const u32 blocks = (u32)(m_tiles * g.n_tiles) * cut.parts;
+    return c.end.y.dtype == DT_F32 ? launch_as<DT_F32>(s, g, blocks, cut.parts, cut.smem)
+         : c.end.y.dtype == DT_F16 ? launch_as<DT_F16>(s, g, blocks, cut.parts, cut.smem)
+                                   : launch_as<DT_BF16>(s, g, blocks, cut.parts, cut.smem);
 }
 
 // Eight values of a row at a time: 16 bytes of the result, cut out of the two aligned words that hold them.
@@ -320,17 +459,20 @@ EndArgs end_args(const ProductEnd& e) {
     g.kept_stride = e.kept.stride;
     g.kept_dtype = e.kept.dtype;
     if (e.kept.p && e.kept.dtype == DT_ACT8) g.k8 = Kept(e.kept.p, e.y.rows, e.y.cols);
-    g.y_vec = on(e.y, 32);
+    auto level = [&](const Matrix& m) { return on(m, 32) ? 2u : on(m, 16) ? 1u : 0u; };
+    g.y_vec = level(e.y);
+    g.bias_vec = e.bias.p && (reinterpret_cast<uintptr_t>(e.bias.p) & 15) == 0;
     g.residual_vec = e.residual.p && on(e.residual, 16);
-    g.kept_vec = e.kept.p && (e.kept.dtype == DT_ACT8 ? (reinterpret_cast<uintptr_t>(e.kept.p) & 31) == 0 : on(e.kept, 32));
+    g.kept_vec = !e.kept.p ? 0 : e.kept.dtype == DT_ACT8 ? ((reinterpret_cast<uintptr_t>(e.kept.p) & 31) == 0 ? 2 : 1) : level(e.kept);
     return g;
 }
 
 bool launch_product(cudaStream_t s, const ProductCall& c) {
-    // 256 x 256 tiles only where they are enough for half the pairs of SMs
-    const u64 wide_tiles = ((c.a.rows + 255) / 256) * ((c.b.rows + 255) / 256);
-    if (c.a.k && c.a.rows > PR_TILE && c.b.rows > PR_TILE && wide_tiles * 4 >= (u64)c.sms) return launch_product_wide(s, c);
-    return launch_narrow(s, c);
+    const EndArgs end = end_args(c.end);
+    const Cut cut = best_cut(c, end.y_vec != 0);
+    // tiles of 256 x 256 where both sides have more than one of 128
+    if (c.a.k && c.a.rows > PR_TILE && c.b.rows > PR_TILE && product_wide_us(c) < cut.us) return launch_product_wide(s, c);
+    return launch_narrow(s, c, end, cut);
 }
 
 }  // namespace excp

@@ -9,7 +9,7 @@
 namespace excp {
 
 constexpr u32 PR_TILE = 128;                       // rows of an operand tile = lanes of tensor memory
-constexpr u32 PR_K = 64;                           // columns of a stage: 128 bytes, one swizzle span
+constexpr u32 PR_K = 64;                           // columns of a box: 128 bytes, one swizzle span
 constexpr u32 PR_CHUNK = 64;                       // rows of a box of an operand that lies the other way round
 constexpr u32 PR_CHUNK_BYTES = PR_CHUNK * PR_K * 2;
 
@@ -40,6 +40,7 @@ struct ProductCall {
 };
 bool launch_product(cudaStream_t s, const ProductCall& c);
 bool launch_product_wide(cudaStream_t s, const ProductCall& c);
+float product_wide_us(const ProductCall& c);       // about how long it takes
 
 // Rows that a tensor map cannot describe (not on 16 bytes) -> rows of `pitch` values in `to`.
 u64 tidy_pitch(u64 cols);
@@ -59,8 +60,8 @@ struct EndArgs {
     u64 kept_stride;
     Kept k8;
     int bias_dtype, act, residual_dtype, kept_dtype;
-    // rows that start on 32 bytes (y, kept) or 16 bytes (residual)
-    u32 y_vec, residual_vec, kept_vec;
+    // y, kept: rows start on 32 bytes (2), 16 bytes (1) or anywhere (0); residual, bias: on 16 bytes (1)
+    u32 y_vec, residual_vec, kept_vec, bias_vec;
 };
 EndArgs end_args(const ProductEnd& e);
 
@@ -115,6 +116,15 @@ __device__ __forceinline__ void activate(float (&f)[W], int act) {
 __device__ __forceinline__ void store32(void* p, const u32 v[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
+// Eight words to a place on 32 bytes (vec = 2) or 16.
+__device__ __forceinline__ void store_words(void* p, const u32 (&w)[8], u32 vec) {
+    if (vec == 2) {
+        store32(p, w);
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
 template <typename T>
 __device__ __forceinline__ u32 word_of(const float* f) {       // 4 bytes of results
     if constexpr (sizeof(T) == 4) {
@@ -129,15 +139,15 @@ __device__ __forceinline__ u32 word_of(const float* f) {       // 4 bytes of res
 }
 // The first `n` of W results to neighbouring places.
 template <typename T, u32 W>
-__device__ __forceinline__ void put_row(T* y, const float (&f)[W], u32 n, bool on32) {
+__device__ __forceinline__ void put_row(T* y, const float (&f)[W], u32 n, u32 vec) {
     constexpr u32 PER = 4 / sizeof(T), STEP = 8 * PER;
 #pragma unroll
     for (u32 i = 0; i < W; i += STEP) {
-        if (on32 && i + STEP <= n) {
+        if (vec && i + STEP <= n) {
             u32 w[8];
 #pragma unroll
             for (u32 k = 0; k < 8; ++k) w[k] = word_of<T>(f + i + k * PER);
-            store32(y + i, w);
+            store_words(y + i, w, vec);
         } else {
 #pragma unroll
             for (u32 e = i; e < i + STEP; ++e) if (e < n) wput(y, e, f[e]);
@@ -145,10 +155,10 @@ __device__ __forceinline__ void put_row(T* y, const float (&f)[W], u32 n, bool o
     }
 }
 template <u32 W>
-__device__ __forceinline__ void put_row_any(void* p, int dtype, u64 at, const float (&f)[W], u32 n, bool on32) {
-    if (dtype == DT_F32) put_row(static_cast<float*>(p) + at, f, n, on32);
-    else if (dtype == DT_F16) put_row(static_cast<__half*>(p) + at, f, n, on32);
-    else put_row(static_cast<__nv_bfloat16*>(p) + at, f, n, on32);
+__device__ __forceinline__ void put_row_any(void* p, int dtype, u64 at, const float (&f)[W], u32 n, u32 vec) {
+    if (dtype == DT_F32) put_row(static_cast<float*>(p) + at, f, n, vec);
+    else if (dtype == DT_F16) put_row(static_cast<__half*>(p) + at, f, n, vec);
+    else put_row(static_cast<__nv_bfloat16*>(p) + at, f, n, vec);
 }
 template <typename T, u32 W>
 __device__ __forceinline__ void add_row(const T* r, float (&f)[W], u32 n, bool on16) {
@@ -174,8 +184,9 @@ __device__ __forceinline__ void end_row(const EndArgs& g, u64 i, u64 j, float (&
     if (i >= g.rows || j >= g.cols) return;
     const u32 n = (u32)min((u64)32, g.cols - j);
     if (g.bias) {
-#pragma unroll
-        for (u32 e = 0; e < 32; ++e) if (e < n) f[e] += any_value(g.bias, g.bias_dtype, j + e);
+        if (g.bias_dtype == DT_F32) add_row(static_cast<const float*>(g.bias) + j, f, n, g.bias_vec);
+        else if (g.bias_dtype == DT_F16) add_row(static_cast<const __half*>(g.bias) + j, f, n, g.bias_vec);
+        else add_row(static_cast<const __nv_bfloat16*>(g.bias) + j, f, n, g.bias_vec);
     }
     if (g.kept) {
         if (g.kept_dtype == DT_ACT8) {             // a thread has a whole block of 32
@@ -190,13 +201,7 @@ __device__ __forceinline__ void end_row(const EndArgs& g, u64 i, u64 j, float (&
 #pragma unroll
             for (u32 k = 0; k < 8; ++k) q[k] = top >= 0x7f800000u ? 0u : a8_codes(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3], inverse);
             const u64 block = i * g.k8.blocks + j / A8_BLOCK;
-            if (g.kept_vec) {
-                store32(g.k8.codes + block * A8_BLOCK, q);
-            } else {                               // the buffer starts on 16 bytes
-                uint4* p = reinterpret_cast<uint4*>(g.k8.codes + block * A8_BLOCK);
-                p[0] = make_uint4(q[0], q[1], q[2], q[3]);
-                p[1] = make_uint4(q[4], q[5], q[6], q[7]);
-            }
+            store_words(g.k8.codes + block * A8_BLOCK, q, g.kept_vec);
             g.k8.scales[block] = (unsigned short)(__float_as_uint(s) >> 16);
         } else {
             put_row_any(g.kept, g.kept_dtype, i * g.kept_stride + j, f, n, g.kept_vec);
@@ -212,57 +217,80 @@ __device__ __forceinline__ void end_row(const EndArgs& g, u64 i, u64 j, float (&
     put_row(static_cast<T*>(g.y) + i * g.stride + j, f, n, g.y_vec);
 }
 
+// The bias of a column, for end_column.
+__device__ __forceinline__ float column_bias(const EndArgs& g, u64 j) { return g.bias && j < g.cols ? any_value(g.bias, g.bias_dtype, j) : 0.f; }
+
+template <typename T, u32 W, bool FULL>
+__device__ __forceinline__ void put_column(T* y, u64 stride, u32 n, const float (&f)[W]) {
+#pragma unroll
+    for (u32 e = 0; e < W; ++e) {
+        if (FULL || e < n) wput(y, 0, f[e]);
+        y += stride;
+    }
+}
+// Not through the read-only cache: y may be the residual.
+template <typename T, u32 W, bool FULL>
+__device__ __forceinline__ void add_column(const T* r, u64 stride, u32 n, float (&f)[W]) {
+    float v[W];
+#pragma unroll
+    for (u32 e = 0; e < W; ++e) {
+        v[e] = FULL || e < n ? wget(r, 0) : 0.f;
+        r += stride;
+    }
+#pragma unroll
+    for (u32 e = 0; e < W; ++e) f[e] += v[e];
+}
+
 // W sums of column j (a lane has one; the lanes of a warp have neighbouring ones, the first a multiple of 32), rows i .. i + n - 1.
-template <int DT, u32 W>
-__device__ __forceinline__ void end_column(const EndArgs& g, u64 i, u64 j, u32 n, float (&f)[W]) {
+template <int DT, u32 W, bool FULL>
+__device__ __forceinline__ void end_column_of(const EndArgs& g, u64 i, u64 j, u32 n, float bias, float (&f)[W]) {
     typedef typename ElemOf<DT>::type T;
     const bool there = j < g.cols;
     if (g.bias) {
-        const float b = there ? any_value(g.bias, g.bias_dtype, j) : 0.f;
 #pragma unroll
-        for (u32 e = 0; e < W; ++e) f[e] += b;
+        for (u32 e = 0; e < W; ++e) f[e] += bias;
     }
     if (g.kept && g.kept_dtype == DT_ACT8) {       // a block is the warp's 32 columns
         const u32 lane = threadIdx.x & 31;
         const u64 block = j / A8_BLOCK;
+        if (block < g.k8.blocks) {
+            const u64 at = i * g.k8.blocks + block;
+            unsigned char* codes = g.k8.codes + at * A8_BLOCK + lane;
+            unsigned short* scales = g.k8.scales + at;
 #pragma unroll
-        for (u32 e = 0; e < W; ++e) {
-            const float v = there && e < n ? f[e] : 0.f;
-            const u32 top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu);
-            const float s = a8_scale(top);
-            if (e < n && block < g.k8.blocks) {
-                const u64 at = (i + e) * g.k8.blocks + block;
-                g.k8.codes[at * A8_BLOCK + lane] = top >= 0x7f800000u ? 0 : (unsigned char)a8_codes(v, 0.f, 0.f, 0.f, a8_inverse(s));
-                if (lane == 0) g.k8.scales[at] = (unsigned short)(__float_as_uint(s) >> 16);
+            for (u32 e = 0; e < W; ++e) {
+                const float v = there && (FULL || e < n) ? f[e] : 0.f;
+                const u32 top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu);
+                const float s = a8_scale(top);
+                if (FULL || e < n) {
+                    *codes = top >= 0x7f800000u ? 0 : (unsigned char)a8_codes(v, 0.f, 0.f, 0.f, a8_inverse(s));
+                    if (lane == 0) *scales = (unsigned short)(__float_as_uint(s) >> 16);
+                }
+                codes += g.k8.blocks * A8_BLOCK;
+                scales += g.k8.blocks;
             }
         }
     }
     if (!there) return;
     if (g.kept && g.kept_dtype != DT_ACT8) {
-#pragma unroll
-        for (u32 e = 0; e < W; ++e) {
-            if (e >= n) continue;
-            const u64 at = (i + e) * g.kept_stride + j;
-            if (g.kept_dtype == DT_F32) wput(static_cast<float*>(g.kept), at, f[e]);
-            else if (g.kept_dtype == DT_F16) wput(static_cast<__half*>(g.kept), at, f[e]);
-            else wput(static_cast<__nv_bfloat16*>(g.kept), at, f[e]);
-        }
+        const u64 at = i * g.kept_stride + j;
+        if (g.kept_dtype == DT_F32) put_column<float, W, FULL>(static_cast<float*>(g.kept) + at, g.kept_stride, n, f);
+        else if (g.kept_dtype == DT_F16) put_column<__half, W, FULL>(static_cast<__half*>(g.kept) + at, g.kept_stride, n, f);
+        else put_column<__nv_bfloat16, W, FULL>(static_cast<__nv_bfloat16*>(g.kept) + at, g.kept_stride, n, f);
     }
     activate(f, g.act);
     if (g.residual) {
-        // not through the read-only cache: y may be the residual
         const u64 at = i * g.residual_stride + j;
-#pragma unroll
-        for (u32 e = 0; e < W; ++e) {
-            if (e >= n) continue;
-            if (g.residual_dtype == DT_F32) f[e] += wget(static_cast<const float*>(g.residual), at + e * g.residual_stride);
-            else if (g.residual_dtype == DT_F16) f[e] += wget(static_cast<const __half*>(g.residual), at + e * g.residual_stride);
-            else f[e] += wget(static_cast<const __nv_bfloat16*>(g.residual), at + e * g.residual_stride);
-        }
+        if (g.residual_dtype == DT_F32) add_column<float, W, FULL>(static_cast<const float*>(g.residual) + at, g.residual_stride, n, f);
+        else if (g.residual_dtype == DT_F16) add_column<__half, W, FULL>(static_cast<const __half*>(g.residual) + at, g.residual_stride, n, f);
+        else add_column<__nv_bfloat16, W, FULL>(static_cast<const __nv_bfloat16*>(g.residual) + at, g.residual_stride, n, f);
     }
-    T* y = static_cast<T*>(g.y) + i * g.stride + j;
-#pragma unroll
-    for (u32 e = 0; e < W; ++e) if (e < n) wput(y, e * g.stride, f[e]);
+    put_column<T, W, FULL>(static_cast<T*>(g.y) + i * g.stride + j, g.stride, n, f);
+}
+template <int DT, u32 W>
+__device__ __forceinline__ void end_column(const EndArgs& g, u64 i, u64 j, u32 n, float bias, float (&f)[W]) {
+    if (n >= W) end_column_of<DT, W, true>(g, i, j, W, bias, f);
+    else end_column_of<DT, W, false>(g, i, j, n, bias, f);
 }
 #endif
 

@@ -4,8 +4,8 @@
 // half of the N side's 256, so that a step of 64 columns costs a CTA 32 KB of shared memory for 512 cycles of products.  The
 // accumulators of two tiles fit tensor memory: one is written out while the next is summed.
 //
-// Persistent pairs: pair p computes tiles p, p + pairs, ...  Roles in each CTA: warps 0..7 write the result, warps 8 and 9 fetch the
-// two operands (tensor maps; what lies past an edge comes as 0), warp 10 of the even CTA issues the products, and that of the odd
+// Persistent pairs: pair p computes tiles p, p + pairs, ...  Roles in each CTA: warps 0..7 write the result, warps 8 to 11 fetch the
+// two operands (tensor maps; what lies past an edge comes as 0), warp 12 of the even CTA issues the products, and that of the odd
 // CTA tells it of its own copies' landing.
 // Every wait for a copy, a product or another warp is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and
 // leaves (the partner's waits run out in turn).  The two that hardware gives no limit, for tensor memory and at the pair's barrier,
@@ -16,7 +16,8 @@ namespace excp {
 namespace {
 
 constexpr int STORE_WARPS = 8;
-constexpr u32 FETCH_WARP = STORE_WARPS, PRODUCT_WARP = FETCH_WARP + 2;
+constexpr u32 FETCH_WARPS = 2;                     // per operand, every other stage
+constexpr u32 FETCH_WARP = STORE_WARPS, PRODUCT_WARP = FETCH_WARP + 2 * FETCH_WARPS;
 constexpr int THREADS = (PRODUCT_WARP + 1) * 32;
 constexpr int STAGES = 6;
 constexpr u32 SPAN = 2 * PR_TILE;                  // rows of m and of n per pair
@@ -28,8 +29,8 @@ struct WideArgs {
     CUtensorMap m, n;                              // on the M side (lanes of tensor memory) and the N side (columns)
     u32 m_along_k, n_along_k, bf16;
     u32 k_tiles, m_tiles, n_tiles;
-    // Usually a is m: a lane has a row of c.  Where rows of y do not start on 32 bytes the operands change places: a lane has a column, and
-    // neighbouring lanes write neighbouring results.
+    // Usually a is m: a lane has a row of c.  Where rows of y do not start on 16 bytes the operands change places: a lane has a column,
+    // and neighbouring lanes write neighbouring results.
     u32 turned;
     EndArgs end;
     u64 wait_ns;
@@ -52,11 +53,6 @@ __device__ __forceinline__ void place(const WideArgs& g, u32 t, u32& mt, u32& nt
     const u32 rows = min(GROUP, g.m_tiles - group * GROUP);
     nt = inside / rows;
     mt = group * GROUP + inside - nt * rows;
-}
-
-// Releases what the partner's copies wrote before the arrival (the thread has no stores of its own to wait for).
-__device__ __forceinline__ void mbar_arrive_cluster_release(u32 address) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
 }
 
 template <int DT>
@@ -89,18 +85,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_pro
     tm_fence_after();
     const u32 tmem = sh.tmem;
 
-    if (warp == FETCH_WARP || warp == FETCH_WARP + 1) {
-        const bool is_n = warp != FETCH_WARP;
+    if (warp >= FETCH_WARP && warp < PRODUCT_WARP) {
+        const bool is_n = warp >= FETCH_WARP + FETCH_WARPS;
         const CUtensorMap* map = is_n ? &g.n : &g.m;
         const bool along_k = is_n ? g.n_along_k : g.m_along_k;
+        const u32 mine = (warp - FETCH_WARP) % FETCH_WARPS;
         Ring<STAGES> ring;
-        u32 filled = 0;
+        u32 filled = 0;                            // stages so far, the other warps' among them
         bool ok = true;
         for (u32 t = pair; ok && t < tiles; t += pairs) {
             u32 mt, nt;
             place(g, t, mt, nt);
             const u32 row = ((is_n ? nt : mt) * 2 + rank) * PR_TILE;
-            for (u32 k = 0; k < g.k_tiles; ++k) {
+            for (u32 k = 0; k < g.k_tiles; ++k, ++filled, ring.next()) {
+                if (filled % FETCH_WARPS != mine) continue;
                 if (filled >= STAGES && !wait_warp(&sh, &sh.empty[ring.s], ring.parity ^ 1, g.wait_ns, g.flag)) { ok = false; break; }
                 unsigned char* to = smem + ring.s * STAGE + (is_n ? HALF : 0);
                 unsigned long long* bar = &sh.full[ring.s];
@@ -114,8 +112,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_pro
                     }
                 }
                 __syncwarp();
-                ++filled;
-                ring.next();
             }
         }
         // no copy may be in flight when the CTA leaves: the last turn of every stage that was filled
@@ -137,7 +133,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_pro
             for (u32 k = 0; k < g.k_tiles; ++k) {
                 if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag) ||
                     !wait_warp(&sh, &sh.peer[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
-                tm_fence_after();
                 const u32 st = base + ring.s * STAGE;
                 const u64 dm = product_desc(st, g.m_along_k), dn = product_desc(st + HALF, g.n_along_k);
                 if (elect_one()) {
@@ -158,7 +153,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_pro
         for (u32 t = pair; ok && t < tiles; t += pairs) {
             for (u32 k = 0; k < g.k_tiles; ++k) {
                 if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
-                if (elect_one()) mbar_arrive_cluster_release(cluster_address(&sh.peer[ring.s], 0));
+                if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.peer[ring.s], 0));
                 __syncwarp();
                 ring.next();
             }
@@ -177,6 +172,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_pro
             const u64 n0 = (u64)nt * SPAN + c0;
             const u32 from = tmem + ((quarter * 32) << 16) + b * SPAN + c0;
             const u64 n_rows = g.turned ? g.end.rows : g.end.cols;
+            const float bias = g.turned ? column_bias(g.end, m) : 0.f;
 #pragma unroll 1
             for (u32 p = 0; p < PR_TILE; p += 32) {
                 u32 v[32];
@@ -193,7 +189,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_pro
                 float f[32];
 #pragma unroll
                 for (u32 e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]);
-                if (g.turned) end_column<DT, 32>(g.end, n0 + p, m, (u32)min((u64)32, n_rows - n0 - p), f);
+                if (g.turned) end_column<DT, 32>(g.end, n0 + p, m, (u32)min((u64)32, n_rows - n0 - p), bias, f);
                 else end_row<DT>(g.end, m, n0 + p, f);
             }
         }
@@ -217,6 +213,14 @@ bool launch_as(int sms, cudaStream_t s, const WideArgs& g) {
 }
 
 }  // namespace
+
+// Measured: a step of 64 columns takes a pair 0.275 us, a tile's epilogue 2 us at 16 bits and 4 at 32, half of which the last one does
+// not hide, and a launch 4.5.
+float product_wide_us(const ProductCall& c) {
+    const u64 tiles = ((c.a.rows + SPAN - 1) / SPAN) * ((c.b.rows + SPAN - 1) / SPAN), pairs = (u64)(c.sms / 2);
+    const float end = c.end.y.dtype == DT_F32 ? 4.f : 2.f, sum = (float)((c.a.k + PR_K - 1) / PR_K) * 0.275f;
+    return 4.5f + (float)((tiles + pairs - 1) / pairs) * (sum > end ? sum : end) + 0.5f * end;
+}
 
 bool launch_product_wide(cudaStream_t s, const ProductCall& c) {
     WideArgs g;
