@@ -33,6 +33,7 @@ struct NarrowArgs {
     u32 boxes;                                     // of a stage
     u32 nt;                                        // rows of n per CTA: a multiple of 16, at most 256
     u32 n_bytes, stages, tmem_cols;
+    u32 runs;                                      // accumulators, nt columns of tensor memory each: the columns are split among them
     u32 ring_bytes;                                // of the stages; afterwards the accumulator lies there
     u32 per_owner;                                 // columns of the accumulator that a CTA of the cluster joins
     u32 turned;                                    // m is b: a lane has a column of c
@@ -76,6 +77,7 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
     const u32 k_steps = (g.k_boxes + g.boxes - 1) / g.boxes;
     const u32 k0 = (u32)((u64)k_steps * part / parts), k1 = (u32)((u64)k_steps * (part + 1) / parts);
     const u32 box = M_BYTES + g.n_bytes, stage = g.boxes * box;
+    const u32 run = max((k1 - k0 + g.runs - 1) / g.runs, 1u), runs = (k1 - k0 + run - 1) / run;      // stages of an accumulator, those in use
     const u64 n0 = (u64)ntile * g.nt, n_rows = g.turned ? g.end.rows : g.end.cols;
     const u32 cols = (u32)min((u64)g.nt, n_rows - n0);         // of the accumulator that are results
     // the CTA's own columns of the accumulator, and the others' parts of them: [part][column][row]
@@ -133,13 +135,14 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
             if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag)) break;
             const u32 st = smem_u32(smem) + ring.s * stage;
             const u64 dm = product_desc(st, g.m_along_k), dn = product_desc(st + M_BYTES, g.n_along_k);
+            const u32 which = (k - k0) / run, d = tmem + which * g.nt;
             if (elect_one()) {
 #pragma unroll
                 for (u32 u = 0; u < BOXES_MAX; ++u) {
                     if (u >= g.boxes || k * g.boxes + u >= g.k_boxes) break;
 #pragma unroll
                     for (u32 i = 0; i < PR_K / 16; ++i)
-                        tm_mma_f16(tmem, dm + u * (box >> 4) + i * step_m, dn + u * (box >> 4) + i * step_n, idesc, k > k0 || u || i);
+                        tm_mma_f16(d, dm + u * (box >> 4) + i * step_m, dn + u * (box >> 4) + i * step_n, idesc, k - k0 > which * run || u || i);
                 }
                 tm_commit(&sh.empty[ring.s]);
             }
@@ -166,17 +169,21 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
         };
         auto take = [&](auto width, u32 c, float (&f)[decltype(width)::value]) {
             constexpr u32 W = decltype(width)::value;
-            u32 v[W];
-            __syncwarp();
-            if constexpr (W == 32) {
-                tm_load32(lanes + c, v);
-            } else {
 #pragma unroll
-                for (u32 i = 0; i < W; i += 8) tm_load8(lanes + c + i, v + i);
+            for (u32 e = 0; e < W; ++e) f[e] = 0.f;
+            for (u32 r = 0; r < runs; ++r) {
+                u32 v[W];
+                __syncwarp();
+                if constexpr (W == 32) {
+                    tm_load32(lanes + r * g.nt + c, v);
+                } else {
+#pragma unroll
+                    for (u32 i = 0; i < W; i += 8) tm_load8(lanes + r * g.nt + c + i, v + i);
+                }
+                tm_wait_load();
+#pragma unroll
+                for (u32 e = 0; e < W; ++e) f[e] += __uint_as_float(v[e]);
             }
-            tm_wait_load();
-#pragma unroll
-            for (u32 e = 0; e < W; ++e) f[e] = k0 < k1 ? __uint_as_float(v[e]) : 0.f;
         };
         auto whole = [&](auto width) {
             constexpr u32 W = decltype(width)::value;
@@ -254,7 +261,7 @@ bool launch_as(cudaStream_t s, const NarrowArgs& g, u32 blocks, u32 parts, u32 s
 // How a product is cut: which operand is on which side, rows of n per CTA, CTAs that share the columns of a tile.
 struct Cut {
     bool turned;
-    u32 nt, parts, boxes, stages, smem, ring_bytes, per_owner;
+    u32 nt, parts, beside, boxes, stages, smem, ring_bytes, per_owner;
     float us;
 };
 
@@ -309,7 +316,7 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
             const u64 tiles = m_tiles * ((n.rows + want - 1) / want);
             const u32 n_bytes = n.along_k ? want * PR_K * 2 : (want + PR_CHUNK - 1) / PR_CHUNK * PR_CHUNK_BYTES;
             for (u32 parts = 1; parts <= MAX_SPLIT && (parts == 1 || (k_boxes >= parts && tiles * parts <= (u64)c.sms * 2)); ++parts) {
-                Cut cut{turned, want, parts, BOXES_MAX, 0, 0, 0, 0, 0.f};
+                Cut cut{turned, want, parts, 1, BOXES_MAX, 0, 0, 0, 0, 0.f};
                 cut.per_owner = (want + parts - 1) / parts;
                 if (!turned) cut.per_owner = (cut.per_owner + 31) & ~31u;
                 const u32 sums = parts > 1 ? parts * cut.per_owner * PR_TILE * 4 : 0, own = parts > 1 ? want * PR_TILE * 4 : 0;
@@ -342,6 +349,7 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
                 const float whole = memory > 60e6f && blocks * 2 < (u64)c.sms * 3 ? 1.16f * memory / all : memory / all;
                 cut.us = 3.2f + fmaxf((float)turns * steps * step, whole) + (turns - 1) * 6.f +
                          (float)turns * want / parts * (turned ? 0.010f : 0.004f) + (parts > 1 ? 1.f + 0.25f * parts + 0.006f * want : 0.f);
+                cut.beside = two ? 2 : 1;
                 if (cut.us < best.us) best = cut;
             }
         }
@@ -378,8 +386,13 @@ bool launch_narrow(cudaStream_t s, const ProductCall& c, const EndArgs& end, con
     g.per_owner = cut.per_owner;
     g.stages = cut.stages;
     g.ring_bytes = cut.ring_bytes;
+    g.runs = 1;
+    if (c.end.y.dtype == DT_F32) {                 // as many runs as a CTA's tensor memory holds, a power of two of them
+        const u32 cols = (g.k_boxes + cut.parts - 1) / cut.parts * PR_K, room = cut.beside > 1 ? 256 : 512;
+        while (cols > g.runs * PR_RUN && (g.runs * 2) * g.nt <= room) g.runs *= 2;
+    }
     g.tmem_cols = 32;
-    while (g.tmem_cols < g.nt) g.tmem_cols *= 2;
+    while (g.tmem_cols < g.nt * g.runs) g.tmem_cols *= 2;
     if (g.k_boxes && (!product_map(&g.m, m, PR_TILE, c.dtype) || !product_map(&g.n, n, g.nt, c.dtype))) return false;
     g.m_along_k = m.along_k;
     g.n_along_k = n.along_k;

@@ -18,7 +18,13 @@ namespace {
 constexpr int STORE_WARPS = 8;
 constexpr u32 FETCH_WARPS = 2;                     // per operand, every other stage
 constexpr u32 FETCH_WARP = STORE_WARPS, PRODUCT_WARP = FETCH_WARP + 2 * FETCH_WARPS;
-constexpr int THREADS = (PRODUCT_WARP + 1) * 32;
+// Where the result has 32 bits the store warps hold the sum of the runs, 128 columns a thread: they take the registers that the others (and
+// three warps that do nothing) do without.
+template <int DT> __host__ __device__ constexpr bool in_runs() { return DT == DT_F32; }
+template <int DT> __host__ __device__ constexpr int threads() { return in_runs<DT>() ? 512 : (int)(PRODUCT_WARP + 1) * 32; }
+constexpr int UP = 200, DOWN = 56;                 // registers a thread, of 128 at launch
+static_assert(256 * UP + 256 * DOWN <= 512 * 128, "registers");
+constexpr u32 RUN = PR_RUN / PR_K;                 // stages
 constexpr int STAGES = 6;
 constexpr u32 SPAN = 2 * PR_TILE;                  // rows of m and of n per pair
 constexpr u32 HALF = PR_TILE * PR_K * 2, STAGE = 2 * HALF;
@@ -56,7 +62,7 @@ __device__ __forceinline__ void place(const WideArgs& g, u32 t, u32& mt, u32& nt
 }
 
 template <int DT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_product_kernel(const __grid_constant__ WideArgs g) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<DT>(), 1) wide_product_kernel(const __grid_constant__ WideArgs g) {
     constexpr u32 TMEM_COLS = 512;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Shared sh;
@@ -84,8 +90,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_pro
     cluster_barrier();                             // the partner's barriers are ready
     tm_fence_after();
     const u32 tmem = sh.tmem;
-
+    // stages that are added up in one accumulator
+    const u32 run = in_runs<DT>() ? RUN : g.k_tiles;
     if (warp >= FETCH_WARP && warp < PRODUCT_WARP) {
+        if constexpr (in_runs<DT>()) registers_down<DOWN>();
         const bool is_n = warp >= FETCH_WARP + FETCH_WARPS;
         const CUtensorMap* map = is_n ? &g.n : &g.m;
         const bool along_k = is_n ? g.n_along_k : g.m_along_k;
@@ -120,77 +128,124 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) wide_pro
             --ring.s;
             drain_warp(&sh.full[ring.s], ring.parity);
         }
-    } else if (warp == PRODUCT_WARP && rank == 0) {
-        const u32 idesc = product_idesc(g.bf16, g.m_along_k, g.n_along_k, SPAN, SPAN);
-        const u32 step_m = product_desc_step(g.m_along_k), step_n = product_desc_step(g.n_along_k);
-        Ring<STAGES> ring;
-        u32 turn = 0;
-        bool ok = true;
-        for (u32 t = pair; ok && t < tiles; t += pairs, ++turn) {
-            const u32 b = turn & 1, acc = tmem + b * SPAN;
-            if (turn >= 2 && !wait_warp(&sh, &sh.acc_empty[b], ((turn >> 1) - 1) & 1, g.wait_ns, g.flag)) { ok = false; break; }
-            tm_fence_after();
-            for (u32 k = 0; k < g.k_tiles; ++k) {
-                if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag) ||
-                    !wait_warp(&sh, &sh.peer[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
-                const u32 st = base + ring.s * STAGE;
-                const u64 dm = product_desc(st, g.m_along_k), dn = product_desc(st + HALF, g.n_along_k);
-                if (elect_one()) {
+    } else if (warp >= PRODUCT_WARP) {
+        if constexpr (in_runs<DT>()) registers_down<DOWN>();
+        if (warp > PRODUCT_WARP) {                 // nothing
+        } else if (rank == 0) {
+            const u32 idesc = product_idesc(g.bf16, g.m_along_k, g.n_along_k, SPAN, SPAN);
+            const u32 step_m = product_desc_step(g.m_along_k), step_n = product_desc_step(g.n_along_k);
+            Ring<STAGES> ring;
+            u32 turn = 0;
+            bool ok = true;
+            for (u32 t = pair; ok && t < tiles; t += pairs) {
+                u32 b = 0, left = 0;                   // the accumulator, stages that it still takes
+                for (u32 k = 0; k < g.k_tiles; ++k) {
+                    const bool first = left == 0;
+                    if (first) {
+                        b = turn & 1;
+                        left = min(run, g.k_tiles - k);
+                        if (turn >= 2 && !wait_warp(&sh, &sh.acc_empty[b], ((turn >> 1) - 1) & 1, g.wait_ns, g.flag)) { ok = false; break; }
+                        tm_fence_after();
+                        ++turn;
+                    }
+                    if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag) ||
+                        !wait_warp(&sh, &sh.peer[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
+                    const u32 st = base + ring.s * STAGE, acc = tmem + b * SPAN;
+                    const u64 dm = product_desc(st, g.m_along_k), dn = product_desc(st + HALF, g.n_along_k);
+                    --left;
+                    if (elect_one()) {
 #pragma unroll
-                    for (u32 i = 0; i < PR_K / 16; ++i) tm2_mma_f16(acc, dm + i * step_m, dn + i * step_n, idesc, k || i);
-                    tm2_commit(&sh.empty[ring.s]);
-                    if (k + 1 == g.k_tiles) tm2_commit(&sh.acc_full[b]);
+                        for (u32 i = 0; i < PR_K / 16; ++i) tm2_mma_f16(acc, dm + i * step_m, dn + i * step_n, idesc, !first || i);
+                        tm2_commit(&sh.empty[ring.s]);
+                        if (left == 0) tm2_commit(&sh.acc_full[b]);
+                    }
+                    __syncwarp();
+                    ring.next();
                 }
-                __syncwarp();
-                ring.next();
             }
-        }
-        if (elect_one()) tm2_commit(&sh.last);
-        __syncwarp();
-    } else if (warp == PRODUCT_WARP) {
-        Ring<STAGES> ring;
-        bool ok = true;
-        for (u32 t = pair; ok && t < tiles; t += pairs) {
-            for (u32 k = 0; k < g.k_tiles; ++k) {
-                if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
-                if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.peer[ring.s], 0));
-                __syncwarp();
-                ring.next();
+            if (elect_one()) tm2_commit(&sh.last);
+            __syncwarp();
+        } else {
+            Ring<STAGES> ring;
+            bool ok = true;
+            for (u32 t = pair; ok && t < tiles; t += pairs) {
+                for (u32 k = 0; k < g.k_tiles; ++k) {
+                    if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag)) { ok = false; break; }
+                    if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.peer[ring.s], 0));
+                    __syncwarp();
+                    ring.next();
+                }
             }
         }
     } else {
+        if constexpr (in_runs<DT>()) registers_up<UP>();
         const u32 quarter = warp & 3, c0 = (warp >> 2) * PR_TILE;          // a warp reads the tensor-memory lanes of its place
+        const u32 lanes = tmem + ((quarter * 32) << 16) + c0;
+        const u64 n_rows = g.turned ? g.end.rows : g.end.cols;
+        auto put = [&](u64 m, u64 n, float bias, float (&f)[32]) {         // 32 neighbouring columns of the accumulator
+            if (n >= n_rows) return;
+            if (g.turned) end_column<DT, 32>(g.end, n, m, (u32)min((u64)32, n_rows - n), bias, f);
+            else end_row<DT>(g.end, m, n, f);
+        };
+        auto release = [&](u32 b) {                // the accumulator is free again
+            tm_fence_before();
+            __syncwarp();
+            if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.acc_empty[b], 0));
+            __syncwarp();
+        };
         u32 turn = 0;
-        for (u32 t = pair; t < tiles; t += pairs, ++turn) {
+        bool ok = true;
+        for (u32 t = pair; ok && t < tiles; t += pairs) {
             u32 mt, nt;
             place(g, t, mt, nt);
-            const u32 b = turn & 1;
-            __syncwarp();
-            if (!wait_warp(&sh, &sh.acc_full[b], (turn >> 1) & 1, g.wait_ns, g.flag)) break;
-            tm_fence_after();
-            const u64 m = (u64)(2 * mt + rank) * PR_TILE + quarter * 32 + lane;
-            const u64 n0 = (u64)nt * SPAN + c0;
-            const u32 from = tmem + ((quarter * 32) << 16) + b * SPAN + c0;
-            const u64 n_rows = g.turned ? g.end.rows : g.end.cols;
+            const u64 m = (u64)(2 * mt + rank) * PR_TILE + quarter * 32 + lane, n0 = (u64)nt * SPAN + c0;
             const float bias = g.turned ? column_bias(g.end, m) : 0.f;
-#pragma unroll 1
-            for (u32 p = 0; p < PR_TILE; p += 32) {
-                u32 v[32];
-                __syncwarp();
-                tm_load32(from + p, v);
-                tm_wait_load();
-                if (p + 32 == PR_TILE) {           // the accumulator is free again
-                    tm_fence_before();
-                    __syncwarp();
-                    if (elect_one()) mbar_arrive_cluster(cluster_address(&sh.acc_empty[b], 0));
-                    __syncwarp();
-                }
-                if (n0 + p >= n_rows) continue;
-                float f[32];
+            if constexpr (in_runs<DT>()) {
+                float sum[PR_TILE];
 #pragma unroll
-                for (u32 e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]);
-                if (g.turned) end_column<DT, 32>(g.end, n0 + p, m, (u32)min((u64)32, n_rows - n0 - p), bias, f);
-                else end_row<DT>(g.end, m, n0 + p, f);
+                for (u32 e = 0; e < PR_TILE; ++e) sum[e] = 0.f;
+                for (u32 k = 0; k < g.k_tiles; k += run, ++turn) {
+                    const u32 b = turn & 1;
+                    __syncwarp();
+                    if (!(ok = wait_warp(&sh, &sh.acc_full[b], (turn >> 1) & 1, g.wait_ns, g.flag))) break;
+                    tm_fence_after();
+#pragma unroll
+                    for (u32 p = 0; p < PR_TILE; p += 16) {
+                        u32 v[16];
+                        tm_load8(lanes + b * SPAN + p, v);
+                        tm_load8(lanes + b * SPAN + p + 8, v + 8);
+                        tm_wait_load();
+#pragma unroll
+                        for (u32 e = 0; e < 16; ++e) sum[p + e] += __uint_as_float(v[e]);
+                    }
+                    release(b);
+                }
+                if (!ok) break;
+#pragma unroll
+                for (u32 p = 0; p < PR_TILE; p += 32) {
+                    float f[32];
+#pragma unroll
+                    for (u32 e = 0; e < 32; ++e) f[e] = sum[p + e];
+                    put(m, n0 + p, bias, f);
+                }
+            } else {
+                const u32 b = turn & 1;
+                __syncwarp();
+                if (!wait_warp(&sh, &sh.acc_full[b], (turn >> 1) & 1, g.wait_ns, g.flag)) break;
+                tm_fence_after();
+                ++turn;
+#pragma unroll 1
+                for (u32 p = 0; p < PR_TILE; p += 32) {
+                    u32 v[32];
+                    __syncwarp();
+                    tm_load32(lanes + b * SPAN + p, v);
+                    tm_wait_load();
+                    if (p + 32 == PR_TILE) release(b);
+                    float f[32];
+#pragma unroll
+                    for (u32 e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]);
+                    put(m, n0 + p, bias, f);
+                }
             }
         }
     }
@@ -209,7 +264,7 @@ bool launch_as(int sms, cudaStream_t s, const WideArgs& g) {
     if (!allow_smem(wide_product_kernel<DT>, allowed, SMEM)) return false;
     const u64 tiles = (u64)g.m_tiles * g.n_tiles;
     const u32 pairs = (u32)(tiles < (u64)(sms / 2) ? tiles : (u64)(sms / 2));
-    return launch_chained(wide_product_kernel<DT>, pairs * 2, THREADS, SMEM, 0, s, g);
+    return launch_chained(wide_product_kernel<DT>, pairs * 2, threads<DT>(), SMEM, 0, s, g);
 }
 
 }  // namespace
