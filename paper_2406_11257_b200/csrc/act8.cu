@@ -21,8 +21,15 @@ template <int U, typename F>
 __device__ __forceinline__ void for_pieces(u64 rows, u32 cols, F&& f) {
     const u32 per_row = (cols + SPAN - 1) / SPAN;
     const u64 first = ((u64)blockIdx.x * WARPS + threadIdx.x / 32) * U;
-    u64 row = first / per_row;
-    u32 piece = (u32)(first - row * per_row);
+    u64 row;
+    u32 piece;
+    if ((first >> 32) == 0) {                      // 32 bits: a division of 64 costs as much as eight values
+        row = (u32)first / per_row;
+        piece = (u32)first - (u32)row * per_row;
+    } else {
+        row = first / per_row;
+        piece = (u32)(first - row * per_row);
+    }
     u64 at[U];
     u32 base[U];
     u32 n = 0;
@@ -48,9 +55,9 @@ __global__ void __launch_bounds__(THREADS) quantize_kernel(const T* __restrict__
 #pragma unroll
         for (u32 u = 0; u < U; ++u) {
             if (u >= n) break;
-            float v[8];
+            Eight v;
             raw[u].values(v);
-            store_kept<VEC>(k, row[u], base[u], lane, cols, v);
+            store_kept<VEC>(k, row[u], base[u], lane, v);
         }
     });
 }
@@ -63,11 +70,11 @@ __global__ void __launch_bounds__(THREADS) restore_kernel(Kept k, T* out, u64 ro
     for_pieces<U>(rows, cols, [&](const u64 (&row)[U], const u32 (&base)[U], u32 n) {
         RawKept<VEC> raw[U];
 #pragma unroll
-        for (u32 u = 0; u < U; ++u) if (u < n) raw[u].load(k, row[u], base[u], lane, cols);
+        for (u32 u = 0; u < U; ++u) if (u < n) raw[u].load(k, row[u], base[u], lane);
 #pragma unroll
         for (u32 u = 0; u < U; ++u) {
             if (u >= n) break;
-            float v[8];
+            Eight v;
             raw[u].values(v);
             store_cols<T, VEC>(out + row[u] * stride, base[u], lane, cols, v);
         }
@@ -100,42 +107,65 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) act_grad_kern
     let_next_start();
     const u32 warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const u32 strip = blockIdx.x / g.groups, group = blockIdx.x - strip * g.groups, base = strip * SPAN;
-    float total[8] = {};
+    Eight total = {};
     const u64 step = (u64)g.groups * WARPS;
-    for (u64 row = (u64)group * WARPS + warp; row < g.rows; row += U * step) {
-        Raw<T, VEC> dy[U], pre[KEPT || ACT == ACT_NONE ? 1 : U];
-        RawKept<VEC> kept[KEPT ? U : 1];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const u64 r = row + u * step;
-            if (r >= g.rows) break;
-            dy[u].load(g.dy + r * g.dy_stride, base, lane, g.cols);
-            if constexpr (ACT != ACT_NONE) {
-                if constexpr (KEPT) kept[u].load(g.kept, r, base, lane, g.cols);
-                else pre[u].load(g.pre + r * g.pre_stride, base, lane, g.cols);
+    u64 row = (u64)group * WARPS + warp;
+    // pointers to the warp's rows, moved by whole steps: products of 64 bits for each would cost as much as the values
+    const T* dy_row = g.dy + row * g.dy_stride;
+    const T* pre_row = KEPT || ACT == ACT_NONE ? nullptr : g.pre + row * g.pre_stride;
+    const u32 per_row = g.kept.blocks;             // blocks of 32 columns
+    const unsigned char* code_row = KEPT ? g.kept.codes + row * per_row * A8_BLOCK : nullptr;
+    const unsigned short* scale_row = KEPT ? g.kept.scales + row * per_row : nullptr;
+    T* dpre_row = g.dpre + row * g.dpre_stride;
+    T* again_row = g.again + row * g.again_stride;
+    Raw<T, VEC> dy[U], pre[KEPT || ACT == ACT_NONE ? 1 : U];
+    RawKept<VEC> kept[KEPT ? U : 1];
+    auto fetch = [&](int u) {                      // the next row of the warp
+        dy[u].load(dy_row, base, lane, g.cols);
+        dy_row += step * g.dy_stride;
+        if constexpr (ACT != ACT_NONE) {
+            if constexpr (KEPT) {
+                kept[u].load(code_row, scale_row, per_row, base, lane);
+                code_row += step * per_row * A8_BLOCK;
+                scale_row += step * per_row;
+            } else {
+                pre[u].load(pre_row, base, lane, g.cols);
+                pre_row += step * g.pre_stride;
             }
         }
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) if (row + u * step < g.rows) fetch(u);
+    for (; row < g.rows; row += U * step) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const u64 r = row + u * step;
-            if (r >= g.rows) break;
-            float d[8], a[8], p[8];
+            if (row + u * step >= g.rows) break;
+            Eight d, a, p;
             dy[u].values(d);
             if constexpr (ACT != ACT_NONE) {
                 if constexpr (KEPT) kept[u].values(p);
                 else pre[u].values(p);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] *= act_slope<ACT>(p[e], a[e]);
-                if (g.again) store_cols<T, VEC>(g.again + r * g.again_stride, base, lane, g.cols, a);
             }
-            if (g.dpre) store_cols<T, VEC>(g.dpre + r * g.dpre_stride, base, lane, g.cols, d);
+            if (row + (u + U) * step < g.rows) fetch(u);         // on its way while this row is worked on
+            if constexpr (ACT != ACT_NONE) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) total[e] += d[e];
+                for (int i = 0; i < 4; ++i) {
+                    f32x2 slope;
+                    a[i] = act_of<ACT, true>(p[i], slope);
+                    d[i] = mul_2(d[i], slope);
+                }
+                if (g.again) store_cols<T, VEC>(again_row, base, lane, g.cols, a);
+                again_row += step * g.again_stride;
+            }
+            if (g.dpre) store_cols<T, VEC>(dpre_row, base, lane, g.cols, d);
+            dpre_row += step * g.dpre_stride;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) total[i] = add_2(total[i], d[i]);
         }
     }
     if (!g.sums) return;
 #pragma unroll
-    for (u32 e = 0; e < 8; ++e) part[warp][lane_col<VEC>(0, lane, e)] = total[e];
+    for (u32 e = 0; e < 8; ++e) part[warp][lane_col<VEC>(0, lane, e)] = e % 2 ? high_2(total[e / 2]) : low_2(total[e / 2]);
     __syncthreads();
     float s = 0.f;
 #pragma unroll
@@ -175,9 +205,6 @@ __global__ void __launch_bounds__(THREADS) column_sums_kernel(const float* __res
     else if (out1) out1[c - split] = s;
 }
 
-bool on16(const void* p, u64 stride_bytes, u64 rows) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (rows == 1 || (stride_bytes & 15) == 0); }
-u64 size_of(int dtype) { return dtype == DT_F32 ? 4 : 2; }
-bool vec(const Matrix& m) { return !m.p || m.dtype == DT_ACT8 || on16(m.p, m.stride * size_of(m.dtype), m.rows); }
 
 template <typename T, bool VEC>
 void quantize_as(cudaStream_t s, const Matrix& x, const Kept& k) {
@@ -198,14 +225,13 @@ struct Split {
     u32 groups, cluster;
 };
 Split act_split(int sms, u64 rows, u64 cols) {
-    const u64 strips = (cols + SPAN - 1) / SPAN;
-    u64 groups = ((u64)sms * 3 + strips - 1) / strips;
-    const u64 most = (rows + 2 * WARPS - 1) / (2 * WARPS);
+    const u64 strips = (cols + SPAN - 1) / SPAN, most = (rows + 2 * WARPS - 1) / (2 * WARPS);
+    u64 groups = (u64)sms * 3 / strips;            // no more than find room at once
     if (groups > most) groups = most;
+    if (groups < 1) groups = 1;
     Split r{1, 1};
-    while (r.cluster < 8 && r.cluster < groups) r.cluster *= 2;
-    if (groups > 8) r.cluster = 4;
-    r.groups = (u32)((groups + r.cluster - 1) / r.cluster * r.cluster);
+    while (r.cluster * 2 <= groups && r.cluster < (groups <= 8 ? 8u : 4u)) r.cluster *= 2;
+    r.groups = (u32)(groups / r.cluster * r.cluster);
     return r;
 }
 
@@ -222,7 +248,7 @@ void act_grad_as(int sms, cudaStream_t s, int act, const Matrix& dy, const Matri
     const bool kept = pre.dtype == DT_ACT8;
     const Args<T> g{static_cast<const T*>(dy.p), dy.stride, static_cast<const T*>(pre.p), pre.stride, Kept(pre.p, dy.rows, dy.cols), dy.rows, (u32)dy.cols,
                     static_cast<T*>(dpre.p), dpre.stride, static_cast<T*>(again.p), again.stride, dbias ? (rows_of_sums > 1 ? scratch : dbias) : nullptr, p.groups};
-    const bool v = vec(dy) && vec(pre) && vec(dpre) && vec(again);
+    const bool v = in_words(dy) && in_words(pre) && in_words(dpre) && in_words(again);
 #define EXCP_AG(ACT) (kept ? (v ? act_grad_launch<T, true, true, ACT>(s, g, p) : act_grad_launch<T, true, false, ACT>(s, g, p)) \
                            : (v ? act_grad_launch<T, false, true, ACT>(s, g, p) : act_grad_launch<T, false, false, ACT>(s, g, p)))
     if (act == ACT_GELU) EXCP_AG(ACT_GELU);
@@ -242,7 +268,7 @@ void launch_column_sums(cudaStream_t s, const float* rows, u32 parts, u64 n, u64
 
 void launch_act8_quantize(int, cudaStream_t s, const Matrix& x, unsigned char* packed) {
     const Kept k(packed, x.rows, x.cols);
-#define EXCP_Q(T) (vec(x) ? quantize_as<T, true>(s, x, k) : quantize_as<T, false>(s, x, k))
+#define EXCP_Q(T) (in_words(x) ? quantize_as<T, true>(s, x, k) : quantize_as<T, false>(s, x, k))
     if (x.dtype == DT_F32) EXCP_Q(float);
     else if (x.dtype == DT_F16) EXCP_Q(__half);
     else EXCP_Q(__nv_bfloat16);
@@ -251,7 +277,7 @@ void launch_act8_quantize(int, cudaStream_t s, const Matrix& x, unsigned char* p
 
 void launch_act8_restore(int, cudaStream_t s, const unsigned char* packed, const Matrix& y) {
     const Kept k(const_cast<unsigned char*>(packed), y.rows, y.cols);
-#define EXCP_R(T) (vec(y) ? restore_as<T, true>(s, k, y) : restore_as<T, false>(s, k, y))
+#define EXCP_R(T) (in_words(y) ? restore_as<T, true>(s, k, y) : restore_as<T, false>(s, k, y))
     if (y.dtype == DT_F32) EXCP_R(float);
     else if (y.dtype == DT_F16) EXCP_R(__half);
     else EXCP_R(__nv_bfloat16);

@@ -5,11 +5,16 @@
 //   g = dy weight, dx = rstd (g - mean g - xh mean(g xh)) + add  (RMS: without mean g)
 //   dweight = sum over rows of dy xh, dbias = sum over rows of dy
 //
-// A row is held in registers by a group of 32 .. 512 threads, eight columns to a thread and piece: the squares are summed after
-// the mean is known, which costs no second read.  Rows past 16384 columns are read again instead.  Sums are fp32.
+// A row is held in registers, as it lies in memory, by a group of 32 .. 512 threads, eight columns to a thread and piece: the squares are
+// summed after the mean is known, which costs no second read.  Where there are rows enough a warp takes a row of up to 4096 16-bit
+// values: no barrier, one set of shuffles for 128 values a lane, and a dozen rows on their way to every SM.  (8192 x 4096 bf16: 512
+// threads to a row 85 us, 256 threads with the rows in a ring in shared memory 45.)  Rows past what registers hold are read again.
+// Sums are fp32.
 //
-// The gradients of weight and bias are summed in the registers of blocks that walk over the rows; the groups of a block and the
-// blocks of a cluster join through (distributed) shared memory in a fixed order, the clusters through a second launch.
+// The gradient of few rows is one kernel: blocks walk over the rows and sum the gradients of weight and bias in registers.  With
+// many rows that costs two barriers a row and half the registers (8192 x 4096 bf16 103 us); there, dx is one kernel as above, and the
+// sums are another, which reads dy and x again: strips of 256 columns, a warp to a row.  Either way the sums of a cluster's
+// blocks join through distributed shared memory in a fixed order, the clusters' through a further launch.
 // Bound: the bytes.
 #include <cooperative_groups.h>
 
@@ -23,11 +28,18 @@ namespace {
 constexpr u32 GROUP_MAX = 512;                     // threads of a row at most
 constexpr u32 PIECE = 8;                           // columns of a thread at a time
 
-// Sums of two values over a group of `size` threads (a power of two, whole warps), the same in all of them.  `sums`: room of the
+// Sums of one or two values over a group of `size` threads (a power of two, whole warps), the same in all of them.  `room`: of the
 // group, two turns of it.
 struct GroupSums {
     float2* room;                                  // [2][warps]
     u32 warps, warp, barrier, size, turn = 0;
+    __device__ __forceinline__ float2* meet(float a, float b) {            // behind the barrier: the warps' sums
+        float2* at = room + turn;
+        turn ^= warps;                             // a turn's room is written again only behind the next turn's barrier
+        if ((threadIdx.x & 31) == 0) at[warp] = make_float2(a, b);
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(size) : "memory");
+        return at + (threadIdx.x & (warps - 1));
+    }
     __device__ __forceinline__ void operator()(float& a, float& b) {
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
@@ -35,20 +47,35 @@ struct GroupSums {
             b += __shfl_xor_sync(0xffffffffu, b, o);
         }
         if (warps == 1) return;
-        float2* at = room + turn * warps;
-        turn ^= 1;                                 // a turn's room is written again only behind the next turn's barrier
-        if ((threadIdx.x & 31) == 0) at[warp] = make_float2(a, b);
-        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(size) : "memory");
-        a = b = 0.f;
-        for (u32 w = 0; w < warps; ++w) { const float2 v = at[w]; a += v.x; b += v.y; }
+        const float2 v = *meet(a, b);
+        a = v.x;
+        b = v.y;
+#pragma unroll
+        for (u32 o = 1; o < GROUP_MAX / 32; o *= 2) {
+            if (o >= warps) break;
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+            b += __shfl_xor_sync(0xffffffffu, b, o);
+        }
+    }
+    __device__ __forceinline__ float operator()(float a) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+        if (warps == 1) return a;
+        a = meet(a, 0.f)->x;
+#pragma unroll
+        for (u32 o = 1; o < GROUP_MAX / 32; o *= 2) {
+            if (o >= warps) break;
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+        }
+        return a;
     }
 };
-__device__ __forceinline__ GroupSums group_sums(float2* room, u32 threads) {
+__device__ __forceinline__ GroupSums group_sums(float2* room, u32 threads, u32 threads_log) {
     GroupSums s;
-    const u32 group = threadIdx.x / threads;
+    const u32 group = threadIdx.x >> threads_log;
     s.warps = threads / 32;
     s.room = room + group * 2 * s.warps;
-    s.warp = (threadIdx.x - group * threads) / 32;
+    s.warp = (threadIdx.x & (threads - 1)) / 32;
     s.barrier = 1 + group;
     s.size = threads;
     return s;
@@ -57,7 +84,7 @@ __device__ __forceinline__ GroupSums group_sums(float2* room, u32 threads) {
 template <typename T> struct NormArgs {
     const T* x;
     u64 stride, rows;
-    u32 cols, threads;                             // threads of a row
+    u32 cols, threads, threads_log, rows_log;      // threads of a row; rows of a block
     ColumnVector weight, bias;
     float eps;
     u32 rms;
@@ -68,64 +95,79 @@ template <typename T> struct NormArgs {
 };
 
 // PIECES of eight columns to a thread, or 0: the row is read again for each of the three passes.
+template <int PIECES> constexpr int block_of() { return PIECES < 2 ? (int)GROUP_MAX : 128; }      // threads of a block at most
+
 template <typename T, bool VEC, int PIECES>
-__global__ void __launch_bounds__(GROUP_MAX) norm_kernel(const __grid_constant__ NormArgs<T> g) {
+__global__ void __launch_bounds__(block_of<PIECES>(), PIECES < 2 ? 2 : 5) norm_kernel(const __grid_constant__ NormArgs<T> g) {
     __shared__ float2 room[2 * GROUP_MAX / 32];
     wait_for_previous();
     let_next_start();
-    const u32 group = threadIdx.x / g.threads, t = threadIdx.x - group * g.threads, lane = t & 31;
-    const u64 row = (u64)blockIdx.x * (blockDim.x / g.threads) + group;
+    const u32 group = threadIdx.x >> g.threads_log, t = threadIdx.x & (g.threads - 1), lane = t & 31;
+    const u64 row = ((u64)blockIdx.x << g.rows_log) + group;
     if (row >= g.rows) return;                     // a whole group
-    GroupSums sums = group_sums(room, g.threads);
+    GroupSums sums = group_sums(room, g.threads, g.threads_log);
     const T* x = g.x + row * g.stride;
     const u32 first = t / 32 * 256, step = g.threads * PIECE;
-    const float n = (float)g.cols;
-    constexpr int HELD = PIECES ? PIECES : 1;
-    float v[HELD][8];
+    const float n = (float)g.cols, inv_n = 1.f / n;
+    Raw<T, VEC> held[PIECES ? PIECES : 1];
     auto each = [&](auto&& f) {                    // f(values, first column of the warp's piece)
         if constexpr (PIECES) {
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) f(v[p], first + p * step);
+            for (int p = 0; p < PIECES; ++p) {
+                if (p && first + p * step >= g.cols) break;      // a whole warp
+                Eight v;
+                held[p].values(v);
+                f(v, first + p * step);
+            }
         } else {
-            for (u32 p0 = 0; p0 < g.cols; p0 += step) {
-                load_cols<T, VEC>(x, first + p0, lane, g.cols, v[0]);
-                f(v[0], first + p0);
+            for (u32 base = first; base < g.cols; base += step) {
+                Eight v;
+                load_cols<T, VEC>(x, base, lane, g.cols, v);
+                f(v, base);
             }
         }
     };
     if constexpr (PIECES) {
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) load_cols<T, VEC>(x, first + p * step, lane, g.cols, v[p]);
+        for (int p = 0; p < PIECES; ++p) if (!p || first + p * step < g.cols) held[p].load(x, first + p * step, lane, g.cols);
     }
-    float mean = 0.f, none = 0.f;
+    float mean = 0.f;
     if (!g.rms) {
-        each([&](const float (&a)[8], u32) {
+        f32x2 sum = 0;
+        each([&](const Eight& a, u32) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) mean += a[e];
+            for (int i = 0; i < 4; ++i) sum = add_2(sum, a[i]);
         });
-        sums(mean, none);
-        mean /= n;
+        mean = sums(low_2(sum) + high_2(sum)) / n;      // divided: the mean of equal values is that value
     }
-    float square = 0.f;
-    each([&](const float (&a)[8], u32 base) {
+    const f32x2 minus_mean = both_2(-mean);
+    f32x2 squares = 0;
+    each([&](const Eight& a, u32 base) {
+        const bool last = base + 256 > g.cols;     // a warp's last columns: those past the end do not count
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float d = a[e] - mean;
-            if (lane_col<VEC>(base, lane, e) < g.cols) square = fmaf(d, d, square);
+        for (int i = 0; i < 4; ++i) {
+            f32x2 d = add_2(a[i], minus_mean);
+            if (VEC) {                             // a lane's eight are in or out
+                if (base + lane * 8 >= g.cols) d = 0;
+            } else if (last) {
+                if (lane_col<VEC>(base, lane, 2 * i) >= g.cols) d &= ~0xffffffffull;
+                if (lane_col<VEC>(base, lane, 2 * i + 1) >= g.cols) d &= 0xffffffffull;
+            }
+            squares = fma_2(d, d, squares);
         }
     });
-    sums(square, none);
-    const float rstd = 1.f / sqrtf(square / n + g.eps);
+    const float rstd = rsqrtf(fmaf(sums(low_2(squares) + high_2(squares)), inv_n, g.eps));
     if (t == 0 && g.stats) g.stats[row] = make_float2(mean, rstd);
     T* y = g.y + row * g.y_stride;
-    each([&](const float (&a)[8], u32 base) {
+    const f32x2 both_rstd = both_2(rstd);
+    each([&](const Eight& a, u32 base) {
         if (base >= g.cols) return;                // a whole warp
-        float w[8], b[8], r[8];
+        Eight w, b, r;
         load_vector<T, VEC>(g.weight, base, lane, g.cols, 1.f, w);
         load_vector<T, VEC>(g.bias, base, lane, g.cols, 0.f, b);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = fmaf((a[e] - mean) * rstd, w[e], b[e]);
-        if (g.kept.codes) store_kept<VEC>(g.kept, row, base, lane, g.cols, a);
+        for (int i = 0; i < 4; ++i) r[i] = fma_2(mul_2(add_2(a[i], minus_mean), both_rstd), w[i], b[i]);
+        if (g.kept.codes) store_kept<VEC>(g.kept, row, base, lane, a);
         store_cols<T, VEC>(y, base, lane, g.cols, r);
     });
 }
@@ -137,7 +179,7 @@ template <typename T> struct GradArgs {
     u64 x_stride;
     Kept kept;
     u64 rows;
-    u32 cols, threads;
+    u32 cols, threads, threads_log, rows_log;
     ColumnVector weight;
     u32 rms;
     const float2* stats;
@@ -148,20 +190,20 @@ template <typename T> struct GradArgs {
     float* sums;                                   // per cluster dweight, then dbias, or null
     float* dweight;                                // where there is one cluster alone
     float* dbias;
-    float2* row_sums;                              // rows that are not held: what the first pass found
+    u32 groups;                                    // of the sums alone: blocks that share a strip of columns
 };
 
 template <typename T, bool KEPT, bool VEC>
 struct RawX {
     Raw<T, VEC> x;
     __device__ __forceinline__ void load(const GradArgs<T>& g, u64 row, u32 base, u32 lane) { x.load(g.x + row * g.x_stride, base, lane, g.cols); }
-    __device__ __forceinline__ void values(float (&v)[8]) const { x.values(v); }
+    __device__ __forceinline__ void values(Eight& v) const { x.values(v); }
 };
 template <typename T, bool VEC>
 struct RawX<T, true, VEC> {
     RawKept<VEC> x;
-    __device__ __forceinline__ void load(const GradArgs<T>& g, u64 row, u32 base, u32 lane) { x.load(g.kept, row, base, lane, g.cols); }
-    __device__ __forceinline__ void values(float (&v)[8]) const { x.values(v); }
+    __device__ __forceinline__ void load(const GradArgs<T>& g, u64 row, u32 base, u32 lane) { x.load(g.kept, row, base, lane); }
+    __device__ __forceinline__ void values(Eight& v) const { x.values(v); }
 };
 
 // Adds what the blocks of a cluster have in own[0..n) and writes it: column c < split to out0[c], the others to out1.
@@ -178,20 +220,18 @@ __device__ __forceinline__ void join_cluster(float* own, u32 n, u32 split, float
     cluster.sync();                                // the others have read this block's
 }
 
-template <typename T, bool KEPT, bool VEC, int PIECES>
-__global__ void __launch_bounds__(GROUP_MAX, PIECES == 1 ? 2 : 1) norm_grad_kernel(const __grid_constant__ GradArgs<T> g) {
+template <typename T, bool KEPT, bool VEC>
+__global__ void __launch_bounds__(GROUP_MAX, 1) norm_grad_kernel(const __grid_constant__ GradArgs<T> g) {
     extern __shared__ float own[];                 // dweight, dbias: the block's
     __shared__ float2 room[2 * GROUP_MAX / 32];
     wait_for_previous();
     let_next_start();
-    const u32 groups = blockDim.x / g.threads, group = threadIdx.x / g.threads, t = threadIdx.x - group * g.threads, lane = t & 31;
-    GroupSums sums = group_sums(room, g.threads);
+    constexpr int PIECES = 1;
+    const u32 groups = 1u << g.rows_log, group = threadIdx.x >> g.threads_log, t = threadIdx.x & (g.threads - 1), lane = t & 31;
+    GroupSums sums = group_sums(room, g.threads, g.threads_log);
     const u32 first = t / 32 * 256, step = g.threads * PIECE;
     const float inv_n = 1.f / (float)g.cols;
-    constexpr bool HOLD = PIECES == 1;             // the weight, too
-    float w[HOLD ? 1 : 1][8];
-    if (HOLD) load_vector<T, VEC>(g.weight, first, lane, g.cols, 1.f, w[0]);
-    float dw[PIECES][8] = {}, db[PIECES][8] = {};
+    Eight dw[PIECES] = {}, db[PIECES] = {};
     Raw<T, VEC> dy[PIECES];
     RawX<T, KEPT, VEC> x[PIECES];
     float2 st = make_float2(0.f, 0.f);
@@ -208,43 +248,43 @@ __global__ void __launch_bounds__(GROUP_MAX, PIECES == 1 ? 2 : 1) norm_grad_kern
     u64 row = (u64)blockIdx.x * groups + group;
     fetch(row);
     for (; row < g.rows; row += stride) {
-        float d[PIECES][8], xh[PIECES][8], s1 = 0.f, s2 = 0.f;
-        const float mean = st.x, rstd = st.y;
+        Eight d[PIECES], xh[PIECES];
+        f32x2 s1 = 0, s2 = 0;
+        const f32x2 minus_mean = both_2(-st.x), rstd = both_2(st.y);
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
+            Eight w;
             dy[p].values(d[p]);
             x[p].values(xh[p]);
-            if (!HOLD) load_vector<T, VEC>(g.weight, first + p * step, lane, g.cols, 1.f, w[0]);
+            load_vector<T, VEC>(g.weight, first + p * step, lane, g.cols, 1.f, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                xh[p][e] = (xh[p][e] - mean) * rstd;
-                db[p][e] += d[p][e];               // 0 past the last column
-                const float dxh = d[p][e] * xh[p][e];
-                dw[p][e] += dxh;
-                d[p][e] *= w[0][e];
-                s1 += d[p][e];
-                s2 = fmaf(dxh, w[0][e], s2);
+            for (int i = 0; i < 4; ++i) {
+                xh[p][i] = mul_2(add_2(xh[p][i], minus_mean), rstd);
+                db[p][i] = add_2(db[p][i], d[p][i]);       // 0 past the last column
+                dw[p][i] = fma_2(d[p][i], xh[p][i], dw[p][i]);
+                d[p][i] = mul_2(d[p][i], w[i]);
+                s1 = add_2(s1, d[p][i]);
+                s2 = fma_2(d[p][i], xh[p][i], s2);
             }
         }
         fetch(row + stride);                       // on its way while the sums are found
-        sums(s1, s2);
-        s1 = g.rms ? 0.f : s1 * inv_n;
-        s2 *= inv_n;
+        float m1 = low_2(s1) + high_2(s1), m2 = low_2(s2) + high_2(s2);
+        sums(m1, m2);
         if (g.dx) {
+            const f32x2 minus_m1 = both_2(g.rms ? 0.f : -m1 * inv_n), minus_m2 = both_2(-m2 * inv_n);
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
                 const u32 base = first + p * step;
                 if (base >= g.cols) continue;      // a whole warp
-                float r[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) r[e] = rstd * (d[p][e] - fmaf(xh[p][e], s2, s1));
+                for (int i = 0; i < 4; ++i) d[p][i] = mul_2(rstd, add_2(d[p][i], fma_2(xh[p][i], minus_m2, minus_m1)));
                 if (g.add) {
-                    float a[8];
+                    Eight a;
                     load_cols<T, VEC>(g.add + row * g.add_stride, base, lane, g.cols, a);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) r[e] += a[e];
+                    for (int i = 0; i < 4; ++i) d[p][i] = add_2(d[p][i], a[i]);
                 }
-                store_cols<T, VEC>(g.dx + row * g.dx_stride, base, lane, g.cols, r);
+                store_cols<T, VEC>(g.dx + row * g.dx_stride, base, lane, g.cols, d[p]);
             }
         }
     }
@@ -259,8 +299,9 @@ __global__ void __launch_bounds__(GROUP_MAX, PIECES == 1 ? 2 : 1) norm_grad_kern
             for (u32 e = 0; e < 8; ++e) {
                 const u32 c = lane_col<VEC>(first + p * step, lane, e);
                 if (c >= g.cols) continue;
-                own[c] = i ? own[c] + dw[p][e] : dw[p][e];
-                own[g.cols + c] = i ? own[g.cols + c] + db[p][e] : db[p][e];
+                const float a = e % 2 ? high_2(dw[p][e / 2]) : low_2(dw[p][e / 2]), b = e % 2 ? high_2(db[p][e / 2]) : low_2(db[p][e / 2]);
+                own[c] = i ? own[c] + a : a;
+                own[g.cols + c] = i ? own[g.cols + c] + b : b;
             }
         }
     }
@@ -269,200 +310,311 @@ __global__ void __launch_bounds__(GROUP_MAX, PIECES == 1 ? 2 : 1) norm_grad_kern
     else join_cluster(own, 2 * g.cols, g.cols, g.dweight, g.dbias);
 }
 
-// ---- rows that are not held ---------------------------------------------------------------------------------------------------
-// First pass: mean g and mean g xh of every row; a block of GROUP_MAX threads to a row.
-template <typename T, bool KEPT, bool VEC>
-__global__ void __launch_bounds__(GROUP_MAX) long_sums_kernel(const __grid_constant__ GradArgs<T> g) {
+// ---- many rows ------------------------------------------------------------------------------------------------------------------
+// dx alone.  PIECES as above.
+template <typename T, bool KEPT, bool VEC, int PIECES>
+__global__ void __launch_bounds__(block_of<PIECES>(), PIECES < 2 ? 2 : 4) norm_dx_kernel(const __grid_constant__ GradArgs<T> g) {
     __shared__ float2 room[2 * GROUP_MAX / 32];
     wait_for_previous();
     let_next_start();
-    const u32 lane = threadIdx.x & 31, first = threadIdx.x / 32 * 256, step = GROUP_MAX * PIECE;
-    const u64 row = blockIdx.x;
-    GroupSums sums = group_sums(room, GROUP_MAX);
+    const u32 group = threadIdx.x >> g.threads_log, t = threadIdx.x & (g.threads - 1), lane = t & 31;
+    const u64 row = ((u64)blockIdx.x << g.rows_log) + group;
+    if (row >= g.rows) return;                     // a whole group
+    GroupSums sums = group_sums(room, g.threads, g.threads_log);
+    const u32 first = t / 32 * 256, step = g.threads * PIECE;
+    const float inv_n = 1.f / (float)g.cols;
     const float2 st = __ldg(g.stats + row);
-    float s1 = 0.f, s2 = 0.f;
-    for (u32 base = first; base < g.cols; base += step) {
-        float d[8], w[8], v[8];
-        RawX<T, KEPT, VEC> x;
-        x.load(g, row, base, lane);
-        load_cols<T, VEC>(g.dy + row * g.dy_stride, base, lane, g.cols, d);
-        load_vector<T, VEC>(g.weight, base, lane, g.cols, 1.f, w);
-        x.values(v);
+    const f32x2 minus_mean = both_2(-st.x), rstd = both_2(st.y);
+    constexpr int HELD = PIECES ? PIECES : 1;
+    Raw<T, VEC> dy[HELD];
+    RawX<T, KEPT, VEC> x[HELD];
+    auto load = [&](int p, u32 base) {
+        dy[p].load(g.dy + row * g.dy_stride, base, lane, g.cols);
+        x[p].load(g, row, base, lane);
+    };
+    auto each = [&](auto&& f) {                    // f(g, xh, first column of the warp's piece)
+        auto one = [&](int p, u32 base) {
+            Eight d, xh, w;
+            dy[p].values(d);
+            x[p].values(xh);
+            load_vector<T, VEC>(g.weight, base, lane, g.cols, 1.f, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float a = d[e] * w[e];
-            s1 += a;
-            s2 = fmaf(a, (v[e] - st.x) * st.y, s2);
+            for (int i = 0; i < 4; ++i) {
+                xh[i] = mul_2(add_2(xh[i], minus_mean), rstd);
+                d[i] = mul_2(d[i], w[i]);          // 0 past the last column
+            }
+            f(d, xh, base);
+        };
+        if constexpr (PIECES) {
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                if (p && first + p * step >= g.cols) break;      // a whole warp
+                one(p, first + p * step);
+            }
+        } else {
+            for (u32 base = first; base < g.cols; base += step) {
+                load(0, base);
+                one(0, base);
+            }
         }
+    };
+    if constexpr (PIECES) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) if (!p || first + p * step < g.cols) load(p, first + p * step);
     }
-    sums(s1, s2);
-    if (threadIdx.x == 0) g.row_sums[row] = make_float2(g.rms ? 0.f : s1 / (float)g.cols, s2 / (float)g.cols);
+    f32x2 s1 = 0, s2 = 0;
+    each([&](const Eight& d, const Eight& xh, u32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s1 = add_2(s1, d[i]);
+            s2 = fma_2(d[i], xh[i], s2);
+        }
+    });
+    float m1 = low_2(s1) + high_2(s1), m2 = low_2(s2) + high_2(s2);
+    sums(m1, m2);
+    const f32x2 minus_m1 = both_2(g.rms ? 0.f : -m1 * inv_n), minus_m2 = both_2(-m2 * inv_n);
+    each([&](const Eight& d, const Eight& xh, u32 base) {
+        if (base >= g.cols) return;                // a whole warp
+        Eight r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = mul_2(rstd, add_2(d[i], fma_2(xh[i], minus_m2, minus_m1)));
+        if (g.add) {
+            Eight a;
+            load_cols<T, VEC>(g.add + row * g.add_stride, base, lane, g.cols, a);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = add_2(r[i], a[i]);
+        }
+        store_cols<T, VEC>(g.dx + row * g.dx_stride, base, lane, g.cols, r);
+    });
 }
 
-// Second pass: strips of 256 columns, a warp to a row.
-constexpr u32 LONG_WARPS = 8;
+// dweight and dbias alone: a block takes 256 columns and every groups-th set of 8 rows.
+constexpr u32 SUM_WARPS = 8;
 template <typename T, bool KEPT, bool VEC>
-__global__ void __launch_bounds__(LONG_WARPS * 32) long_grad_kernel(const __grid_constant__ GradArgs<T> g, u32 row_groups) {
-    __shared__ float part[2][LONG_WARPS][256];
+__global__ void __launch_bounds__(SUM_WARPS * 32, 4) norm_columns_kernel(const __grid_constant__ GradArgs<T> g) {
+    constexpr int U = 2;
+    __shared__ float part[SUM_WARPS][256];
+    __shared__ float own[512];
     wait_for_previous();
     let_next_start();
     const u32 warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    const u32 strip = blockIdx.x / row_groups, rg = blockIdx.x - strip * row_groups, base = strip * 256;
-    float dw[8] = {}, db[8] = {}, w[8];
-    load_vector<T, VEC>(g.weight, base, lane, g.cols, 1.f, w);
-    for (u64 row = (u64)rg * LONG_WARPS + warp; row < g.rows; row += (u64)row_groups * LONG_WARPS) {
-        float d[8], v[8], r[8];
-        RawX<T, KEPT, VEC> x;
-        x.load(g, row, base, lane);
-        load_cols<T, VEC>(g.dy + row * g.dy_stride, base, lane, g.cols, d);
-        x.values(v);
-        const float2 st = __ldg(g.stats + row), sm = g.row_sums[row];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float xh = (v[e] - st.x) * st.y;
-            dw[e] = fmaf(d[e], xh, dw[e]);
-            db[e] += d[e];
-            r[e] = st.y * (d[e] * w[e] - fmaf(xh, sm.y, sm.x));
+    const u32 strip = blockIdx.x / g.groups, group = blockIdx.x - strip * g.groups, base = strip * 256;
+    const u64 step = (u64)g.groups * SUM_WARPS;
+    u64 row = (u64)group * SUM_WARPS + warp;
+    // pointers to the warp's rows, moved by whole steps: products of 64 bits for each would cost as much as the values
+    const T* dy_row = g.dy + row * g.dy_stride;
+    const T* x_row = KEPT ? nullptr : g.x + row * g.x_stride;
+    const u32 per_row = g.kept.blocks;             // blocks of 32 columns
+    const unsigned char* code_row = KEPT ? g.kept.codes + row * per_row * A8_BLOCK : nullptr;
+    const unsigned short* scale_row = KEPT ? g.kept.scales + row * per_row : nullptr;
+    const float2* stat = g.stats + row;
+    Raw<T, VEC> dy[U];
+    RawX<T, KEPT, VEC> x[U];
+    float2 st[U];
+    auto fetch = [&](int u) {                      // the next row of the warp
+        dy[u].load(dy_row, base, lane, g.cols);
+        dy_row += step * g.dy_stride;
+        if constexpr (KEPT) {
+            x[u].x.load(code_row, scale_row, per_row, base, lane);
+            code_row += step * per_row * A8_BLOCK;
+            scale_row += step * per_row;
+        } else {
+            x[u].x.load(x_row, base, lane, g.cols);
+            x_row += step * g.x_stride;
         }
-        if (!g.dx) continue;
-        if (g.add) {
-            float a[8];
-            load_cols<T, VEC>(g.add + row * g.add_stride, base, lane, g.cols, a);
+        st[u] = __ldg(stat);
+        stat += step;
+    };
+    Eight dw = {}, db = {};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] += a[e];
+    for (int u = 0; u < U; ++u) if (row + u * step < g.rows) fetch(u);
+    for (; row < g.rows; row += U * step) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (row + u * step >= g.rows) break;
+            Eight d, xh;
+            dy[u].values(d);
+            x[u].values(xh);
+            const f32x2 minus_mean = both_2(-st[u].x), rstd = both_2(st[u].y);
+            if (row + (u + U) * step < g.rows) fetch(u);         // on its way while this row is worked on
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                db[i] = add_2(db[i], d[i]);
+                dw[i] = fma_2(d[i], mul_2(add_2(xh[i], minus_mean), rstd), dw[i]);
+            }
         }
-        store_cols<T, VEC>(g.dx + row * g.dx_stride, base, lane, g.cols, r);
     }
-    if (!g.sums) return;
 #pragma unroll
-    for (u32 e = 0; e < 8; ++e) {
-        part[0][warp][lane_col<VEC>(0, lane, e)] = dw[e];
-        part[1][warp][lane_col<VEC>(0, lane, e)] = db[e];
-    }
-    __syncthreads();
-    if (base + threadIdx.x >= g.cols) return;
+    for (int k = 0; k < 2; ++k) {
 #pragma unroll
-    for (u32 k = 0; k < 2; ++k) {
+        for (u32 e = 0; e < 8; ++e) {
+            const f32x2 v = k ? db[e / 2] : dw[e / 2];
+            part[warp][lane_col<VEC>(0, lane, e)] = e % 2 ? high_2(v) : low_2(v);
+        }
+        __syncthreads();
         float s = 0.f;
 #pragma unroll
-        for (u32 i = 0; i < LONG_WARPS; ++i) s += part[k][i][threadIdx.x];
-        g.sums[((u64)rg * 2 + k) * g.cols + base + threadIdx.x] = s;
+        for (u32 i = 0; i < SUM_WARPS; ++i) s += part[i][threadIdx.x];
+        own[k * 256 + threadIdx.x] = s;
+        __syncthreads();
     }
+    cg::cluster_group cluster = cg::this_cluster();
+    const u32 blocks = cluster.num_blocks(), rank = cluster.block_rank();
+    cluster.sync();
+    for (u32 c = rank * 256 + threadIdx.x; c < 512; c += blocks * 256) {
+        const u32 k = c / 256, col = base + c % 256;
+        float all = 0.f;
+        for (u32 b = 0; b < blocks; ++b) all += *cluster.map_shared_rank(own + c, b);
+        if (col >= g.cols) continue;
+        if (g.sums) g.sums[((u64)(group / blocks) * 2 + k) * g.cols + col] = all;
+        else if (k == 0 && g.dweight) g.dweight[col] = all;
+        else if (k == 1 && g.dbias) g.dbias[col] = all;
+    }
+    cluster.sync();                                // the others have read this block's sums
 }
 
 // ---- how rows are dealt ---------------------------------------------------------------------------------------------------------
-bool on16(const void* p, u64 stride_bytes, u64 rows) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (rows == 1 || (stride_bytes & 15) == 0); }
-bool vec(const Matrix& m) { return !m.p || m.dtype == DT_ACT8 || on16(m.p, m.stride * (m.dtype == DT_F32 ? 4 : 2), m.rows); }
-bool vec(const ColumnVector& v) { return on16(v.p, 0, 1); }
 
-constexpr u64 HELD_COLS = GROUP_MAX * PIECE * 4;   // longest row that registers hold
-u32 threads_of(u64 cols, u32 pieces) {
-    u32 t = 32;
-    while (t < GROUP_MAX && (u64)t * PIECE * pieces < cols) t *= 2;
-    return t;
-}
-
-template <typename T, bool VEC, int PIECES>
-void norm_launch(cudaStream_t s, NormArgs<T> g) {
-    g.threads = PIECES ? threads_of(g.cols, PIECES) : GROUP_MAX;
-    // four warps to a block, or one row's
-    const u32 block = g.threads > 128 ? g.threads : 128;
-    const u64 per = block / g.threads;
-    launch_chained(norm_kernel<T, VEC, PIECES>, (u32)((g.rows + per - 1) / per), block, 0, 0, s, g);
-}
-template <typename T>
-void norm_as(cudaStream_t s, const Matrix& x, const ColumnVector& weight, const ColumnVector& bias, float eps, bool rms, const Matrix& y, float* row_stats,
-             unsigned char* kept) {
-    const NormArgs<T> g{static_cast<const T*>(x.p), x.stride, x.rows, (u32)x.cols, 0, weight, bias, eps, rms, static_cast<T*>(y.p), y.stride,
-                        reinterpret_cast<float2*>(row_stats), Kept(kept, x.rows, x.cols)};
-    const bool v = vec(x) && vec(y) && vec(weight) && vec(bias);
-#define EXCP_N(P) (v ? norm_launch<T, true, P>(s, g) : norm_launch<T, false, P>(s, g))
-    if (x.cols <= GROUP_MAX * PIECE) EXCP_N(1);
-    else if (x.cols <= GROUP_MAX * PIECE * 2) EXCP_N(2);
-    else if (x.cols <= HELD_COLS) EXCP_N(4);
-    else EXCP_N(0);
-#undef EXCP_N
-}
-
-// Blocks of the gradient's kernel, and of a cluster.
-struct Deal {
-    u32 threads, block, blocks, cluster, sums;     // sums: rows of partial sums; 1: none, written at once
+// How a row is dealt: pieces of a thread (0: too long to be held), threads, threads of a block.
+struct Rows {
+    u32 pieces, threads, block;
 };
-Deal deal(int sms, u64 rows, u64 cols) {
-    Deal d{};
-    const u32 pieces = cols <= GROUP_MAX * PIECE ? 1 : cols <= GROUP_MAX * PIECE * 2 ? 2 : 4;
-    d.threads = threads_of(cols, pieces);
-    d.block = GROUP_MAX;
-    const u64 per = d.block / d.threads, most = (rows + per - 1) / per, full = (u64)sms * (pieces == 1 ? 2 : 1);
-    d.blocks = (u32)(most < full ? most : full);
-    d.cluster = 1;
-    while (d.cluster < 4 && d.cluster < d.blocks) d.cluster *= 2;
-    d.blocks = (d.blocks + d.cluster - 1) / d.cluster * d.cluster;
-    d.sums = d.blocks / d.cluster;
-    return d;
+// Few rows: as many threads to a row as it has words of eight columns.  Many, or long ones: as few as can hold it.
+constexpr u32 PIECES_MAX = 8;
+Rows rows_of(int sms, u64 rows, u64 cols) {
+    if (cols > (u64)128 * PIECE * PIECES_MAX) return Rows{0, GROUP_MAX, GROUP_MAX};
+    Rows r{1, 32, 128};
+    const bool many = rows > (u64)sms * 2 || cols > GROUP_MAX * PIECE;
+    while ((u64)r.threads * PIECE * r.pieces < cols) {
+        if (many && r.pieces < PIECES_MAX) r.pieces *= 2;
+        else r.threads *= 2;
+    }
+    if (r.threads > r.block) r.block = r.threads;
+    return r;
 }
-u32 long_row_groups(int sms, u64 rows, u64 cols) {
-    const u64 strips = (cols + 255) / 256;
-    u64 n = ((u64)sms * 4 + strips - 1) / strips;
-    const u64 most = (rows + LONG_WARPS - 1) / LONG_WARPS;
-    return (u32)(n < most ? n : most);
+u32 log2_of(u32 v) { return v <= 1 ? 0 : 1 + log2_of(v / 2); }
+template <typename T, bool VEC, int PIECES>
+void norm_launch(cudaStream_t s, NormArgs<T> g, const Rows& r) {
+    g.threads = r.threads;
+    g.threads_log = log2_of(r.threads);
+    g.rows_log = log2_of(r.block / r.threads);
+    launch_chained(norm_kernel<T, VEC, PIECES>, (u32)((g.rows + (1u << g.rows_log) - 1) >> g.rows_log), r.block, 0, 0, s, g);
+}
+template <typename T, bool VEC>
+void norm_as(int sms, cudaStream_t s, const NormArgs<T>& g) {
+    const Rows r = rows_of(sms, g.rows, g.cols);
+    if (r.pieces == 0) norm_launch<T, VEC, 0>(s, g, r);
+    else if (r.pieces == 1) norm_launch<T, VEC, 1>(s, g, r);
+    else if (r.pieces == 2) norm_launch<T, VEC, 2>(s, g, r);
+    else if (r.pieces == 4) norm_launch<T, VEC, 4>(s, g, r);
+    else norm_launch<T, VEC, 8>(s, g, r);
+}
+
+// The gradient in one kernel: while no group of threads has more than three rows.
+constexpr u64 FUSED_COLS = GROUP_MAX * PIECE;
+struct Deal {
+    Rows rows;
+    u32 blocks, cluster;
+};
+u32 cluster_of(u64 blocks) { return blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1; }
+bool deal_fused(int sms, u64 rows, u64 cols, Deal& d) {
+    if (cols > FUSED_COLS) return false;
+    d.rows = Rows{1, 32, GROUP_MAX};
+    while ((u64)d.rows.threads * PIECE < cols) d.rows.threads *= 2;
+    const u64 per = GROUP_MAX / d.rows.threads, most = (rows + per - 1) / per;
+    if (most > (u64)sms * 3) return false;
+    const u64 blocks = most < (u64)sms ? most : (u64)sms;
+    d.cluster = cluster_of(blocks);
+    d.blocks = (u32)((blocks + d.cluster - 1) / d.cluster * d.cluster);
+    return true;
+}
+// The sums alone: blocks of a strip, and of a cluster.
+Deal deal_sums(int sms, u64 rows, u64 cols) {
+    Deal d{};
+    const u64 strips = (cols + 255) / 256, most = (rows + 2 * SUM_WARPS - 1) / (2 * SUM_WARPS);
+    u64 groups = (u64)sms * 4 / strips;            // no more than find room at once
+    if (groups > most) groups = most;
+    if (groups < 1) groups = 1;
+    d.cluster = cluster_of(groups);
+    d.blocks = (u32)(groups / d.cluster * d.cluster);
+    return d;
 }
 
 template <typename T, bool KEPT, bool VEC, int PIECES>
-void grad_launch(cudaStream_t s, const GradArgs<T>& g, const Deal& d) {
-    const u32 smem = (u32)(2 * g.cols * sizeof(float));
-    static std::atomic<u64> allowed{0};
-    if (smem > 32 * 1024 && !allow_smem(norm_grad_kernel<T, KEPT, VEC, PIECES>, allowed, (u32)(2 * HELD_COLS * sizeof(float)))) return;
-    launch_chained(norm_grad_kernel<T, KEPT, VEC, PIECES>, d.blocks, d.block, smem, d.cluster, s, g);
+void dx_launch(cudaStream_t s, GradArgs<T> g, const Rows& r) {
+    g.threads = r.threads;
+    g.threads_log = log2_of(r.threads);
+    g.rows_log = log2_of(r.block / r.threads);
+    launch_chained(norm_dx_kernel<T, KEPT, VEC, PIECES>, (u32)((g.rows + (1u << g.rows_log) - 1) >> g.rows_log), r.block, 0, 0, s, g);
 }
 
 template <typename T, bool KEPT, bool VEC>
 void grad_as(int sms, cudaStream_t s, GradArgs<T> g, float* scratch) {
-    const bool wanted = g.dweight || g.dbias;
     float* const dweight = g.dweight;
     float* const dbias = g.dbias;
-    if (g.cols > HELD_COLS) {
-        const u32 rg = long_row_groups(sms, g.rows, g.cols);
-        g.row_sums = reinterpret_cast<float2*>(scratch);
-        g.sums = wanted ? scratch + 2 * g.rows : nullptr;
-        launch_chained(long_sums_kernel<T, KEPT, VEC>, (u32)g.rows, GROUP_MAX, 0, 0, s, g);
-        launch_chained(long_grad_kernel<T, KEPT, VEC>, (g.cols + 255) / 256 * rg, LONG_WARPS * 32, 0, 0, s, g, rg);
-        if (wanted) launch_column_sums(s, g.sums, rg, 2 * (u64)g.cols, g.cols, dweight, dbias);
-        return;
+    const bool wanted = dweight || dbias;
+    u32 sums = 1;                                  // rows of partial sums
+    Deal d;
+    if (wanted && g.dx && deal_fused(sms, g.rows, g.cols, d)) {
+        sums = d.blocks / d.cluster;
+        g.sums = sums > 1 ? scratch : nullptr;
+        g.threads = d.rows.threads;
+        g.threads_log = log2_of(g.threads);
+        g.rows_log = log2_of(GROUP_MAX / g.threads);
+        launch_chained(norm_grad_kernel<T, KEPT, VEC>, d.blocks, GROUP_MAX, (u32)(2 * g.cols * sizeof(float)), d.cluster, s, g);
+    } else {
+        if (wanted) {                              // first: dx may take dy's place
+            d = deal_sums(sms, g.rows, g.cols);
+            sums = d.blocks / d.cluster;
+            g.sums = sums > 1 ? scratch : nullptr;
+            g.groups = d.blocks;
+            launch_chained(norm_columns_kernel<T, KEPT, VEC>, (g.cols + 255) / 256 * d.blocks, SUM_WARPS * 32, 0, d.cluster, s, g);
+        }
+        if (g.dx) {
+            const Rows r = rows_of(sms, g.rows, g.cols);
+            if (r.pieces == 0) dx_launch<T, KEPT, VEC, 0>(s, g, r);
+            else if (r.pieces == 1) dx_launch<T, KEPT, VEC, 1>(s, g, r);
+            else if (r.pieces == 2) dx_launch<T, KEPT, VEC, 2>(s, g, r);
+            else if (r.pieces == 4) dx_launch<T, KEPT, VEC, 4>(s, g, r);
+            else dx_launch<T, KEPT, VEC, 8>(s, g, r);
+        }
     }
-    const Deal d = deal(sms, g.rows, g.cols);
-    g.threads = d.threads;
-    g.sums = wanted && d.sums > 1 ? scratch : nullptr;
-    if (g.cols <= GROUP_MAX * PIECE) grad_launch<T, KEPT, VEC, 1>(s, g, d);
-    else if (g.cols <= GROUP_MAX * PIECE * 2) grad_launch<T, KEPT, VEC, 2>(s, g, d);
-    else grad_launch<T, KEPT, VEC, 4>(s, g, d);
-    if (g.sums) launch_column_sums(s, g.sums, d.sums, 2 * (u64)g.cols, g.cols, dweight, dbias);
+    if (sums > 1) launch_column_sums(s, scratch, sums, 2 * (u64)g.cols, g.cols, dweight, dbias);
 }
 
 }  // namespace
 
-void launch_layer_norm(int, cudaStream_t s, const Matrix& x, const ColumnVector& weight, const ColumnVector& bias, float eps, bool rms, const Matrix& y,
+void launch_layer_norm(int sms, cudaStream_t s, const Matrix& x, const ColumnVector& weight, const ColumnVector& bias, float eps, bool rms, const Matrix& y,
                        float* row_stats, unsigned char* kept) {
-    if (x.dtype == DT_F32) norm_as<float>(s, x, weight, bias, eps, rms, y, row_stats, kept);
-    else if (x.dtype == DT_F16) norm_as<__half>(s, x, weight, bias, eps, rms, y, row_stats, kept);
-    else norm_as<__nv_bfloat16>(s, x, weight, bias, eps, rms, y, row_stats, kept);
+    const bool v = in_words(x) && in_words(y) && in_words(weight) && in_words(bias);
+    auto with = [&](auto type) {
+        typedef decltype(type) T;
+        const NormArgs<T> g{static_cast<const T*>(x.p), x.stride, x.rows, (u32)x.cols, 0, 0, 0, weight, bias, eps, rms, static_cast<T*>(y.p), y.stride,
+                            reinterpret_cast<float2*>(row_stats), Kept(kept, x.rows, x.cols)};
+        v ? norm_as<T, true>(sms, s, g) : norm_as<T, false>(sms, s, g);
+    };
+    if (x.dtype == DT_F32) with(float());
+    else if (x.dtype == DT_F16) with(__half());
+    else with(__nv_bfloat16());
 }
 
 u64 layer_norm_grad_scratch(int sms, u64 rows, u64 cols) {
     if (!rows || !cols) return 0;
-    if (cols > HELD_COLS) return (2 * rows + (u64)long_row_groups(sms, rows, cols) * 2 * cols) * sizeof(float);
-    const Deal d = deal(sms, rows, cols);
-    return d.sums > 1 ? d.sums * 2 * cols * sizeof(float) : 0;
+    Deal d, fused;
+    d = deal_sums(sms, rows, cols);
+    u32 sums = d.blocks / d.cluster;
+    if (deal_fused(sms, rows, cols, fused) && fused.blocks / fused.cluster > sums) sums = fused.blocks / fused.cluster;
+    return sums > 1 ? sums * 2 * cols * sizeof(float) : 0;
 }
 
 void launch_layer_norm_grad(int sms, cudaStream_t s, const Matrix& dy, const Matrix& x, const ColumnVector& weight, bool rms, const float* row_stats,
                             const Matrix& add, const Matrix& dx, float* dweight, float* dbias, float* scratch) {
-    const bool v = vec(dy) && vec(x) && vec(weight) && vec(add) && vec(dx);
+    const bool v = in_words(dy) && in_words(x) && in_words(weight) && in_words(add) && in_words(dx);
     auto with = [&](auto type) {
         typedef decltype(type) T;
-        const GradArgs<T> g{static_cast<const T*>(dy.p), dy.stride, static_cast<const T*>(x.p), x.stride, Kept(x.p, dy.rows, dy.cols), dy.rows, (u32)dy.cols, 0,
+        const GradArgs<T> g{static_cast<const T*>(dy.p), dy.stride, static_cast<const T*>(x.p), x.stride, Kept(x.p, dy.rows, dy.cols), dy.rows, (u32)dy.cols, 0, 0, 0,
                             weight, rms, reinterpret_cast<const float2*>(row_stats), static_cast<const T*>(add.p), add.stride, static_cast<T*>(dx.p),
-                            dx.stride, nullptr, dweight, dbias, nullptr};
+                            dx.stride, nullptr, dweight, dbias, 0};
         if (x.dtype == DT_ACT8) v ? grad_as<T, true, true>(sms, s, g, scratch) : grad_as<T, true, false>(sms, s, g, scratch);
         else v ? grad_as<T, false, true>(sms, s, g, scratch) : grad_as<T, false, false>(sms, s, g, scratch);
     };

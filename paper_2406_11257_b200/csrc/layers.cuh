@@ -27,6 +27,11 @@ constexpr u32 A8_BLOCK = 32;
 __host__ __device__ inline u64 a8_blocks(u64 cols) { return (cols + A8_BLOCK - 1) / A8_BLOCK; }
 __host__ __device__ inline u64 a8_bytes(u64 rows, u64 cols) { return (rows * a8_blocks(cols) * (A8_BLOCK + 2) + 15) & ~15ull; }
 
+// Whether a kernel may take a matrix (or vector) in 16-byte words.
+inline bool on_words(const void* p, u64 stride_bytes, u64 rows) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (rows == 1 || (stride_bytes & 15) == 0); }
+inline bool in_words(const Matrix& m) { return !m.p || (m.cols % 8 == 0 && (m.dtype == DT_ACT8 || on_words(m.p, m.stride * (m.dtype == DT_F32 ? 4 : 2), m.rows))); }
+inline bool in_words(const ColumnVector& v) { return on_words(v.p, 0, 1); }
+
 // ---- launch wrappers ---------------------------------------------------------------------------------------------------
 void launch_act8_quantize(int sms, cudaStream_t s, const Matrix& x, unsigned char* packed);
 void launch_act8_restore(int sms, cudaStream_t s, const unsigned char* packed, const Matrix& out);
@@ -47,14 +52,35 @@ void launch_column_sums(cudaStream_t s, const float* rows, u32 parts, u64 n, u64
 
 #ifdef __CUDACC__
 // ---- how a warp holds 256 consecutive columns of a row, eight to a lane -------------------------------------------------
-// VEC: eight neighbours, fetched in 16-byte words (rows on 16 bytes).  Else column 32 e + lane for e = 0 .. 7, so that the lanes of
+// VEC: eight neighbours, fetched in 16-byte words (rows on 16 bytes, of a multiple of eight columns: an edge inside a word would double the
+// code of every piece, and these kernels wait for instructions before they wait for memory).  Else column 32 e + lane for e = 0 .. 7, so that the lanes of
 // one access are neighbours whatever the alignment.  Either way 32 lanes x 8 values are eight whole blocks of an 8-bit matrix.
 template <bool VEC>
 __device__ __forceinline__ u32 lane_col(u32 base, u32 lane, u32 e) {
     return VEC ? base + lane * 8 + e : base + e * 32 + lane;
 }
 
-// Sixteen bytes of values as they lie in memory, and as fp32.
+// A lane's eight values, two to a word: neighbours (VEC), or those of columns 32 e + lane and 32 (e + 1) + lane.
+typedef f32x2 Eight[4];
+
+template <typename T> __device__ __forceinline__ f32x2 two_values(const void* p);          // of a 4-byte word (fp32: of 8 bytes)
+template <> __device__ __forceinline__ f32x2 two_values<float>(const void* p) { return *static_cast<const f32x2*>(p); }
+template <> __device__ __forceinline__ f32x2 two_values<__half>(const void* p) {
+    const float2 f = __half22float2(*static_cast<const __half2*>(p));
+    return pack_2(f.x, f.y);
+}
+template <> __device__ __forceinline__ f32x2 two_values<__nv_bfloat16>(const void* p) {
+    const u32 w = *static_cast<const u32*>(p);
+    return (u64)(w << 16) | (u64)(w & 0xffff0000u) << 32;
+}
+template <typename T>
+__device__ __forceinline__ void put_two(void* p, f32x2 v) {
+    if constexpr (sizeof(T) == 4) *static_cast<f32x2*>(p) = v;
+    else if constexpr (std::is_same<T, __half>::value) *static_cast<__half2*>(p) = __floats2half2_rn(low_2(v), high_2(v));
+    else *static_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(low_2(v), high_2(v));
+}
+
+// Eight values as they lie in memory, and as fp32.
 template <typename T, bool VEC>
 struct Raw {
     static constexpr int N = VEC ? (int)sizeof(T) / 2 : 8;
@@ -64,15 +90,9 @@ struct Raw {
     __device__ __forceinline__ void load(const T* row, u32 base, u32 lane, u32 cols) {
         if constexpr (VEC) {
             const u32 c = base + lane * 8;
-            if (c + 8 <= cols) {
-                const uint4* p = reinterpret_cast<const uint4*>(row + c);
+            const uint4* p = reinterpret_cast<const uint4*>(row + c);
 #pragma unroll
-                for (int i = 0; i < N; ++i) q[i] = __ldg(p + i);
-            } else {
-                T* h = reinterpret_cast<T*>(q);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) wput(h, e, c + e < cols ? wget(row, c + e) : 0.f);
-            }
+            for (int i = 0; i < N; ++i) q[i] = c < cols ? __ldg(p + i) : make_uint4(0u, 0u, 0u, 0u);
         } else {
 #pragma unroll
             for (u32 e = 0; e < 8; ++e) {
@@ -82,49 +102,49 @@ struct Raw {
             }
         }
     }
-    __device__ __forceinline__ void values(float (&v)[8]) const {
-        const T* h = reinterpret_cast<const T*>(q);
+    __device__ __forceinline__ void values(Eight& v) const {
+        if constexpr (VEC) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = wget(h, e);
+            for (int i = 0; i < 4; ++i) v[i] = two_values<T>(reinterpret_cast<const char*>(q) + i * 2 * sizeof(T));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = pack_2(wget(q, 2 * i), wget(q, 2 * i + 1));
+        }
     }
 };
 
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_cols(const T* row, u32 base, u32 lane, u32 cols, float (&v)[8]) {
+__device__ __forceinline__ void load_cols(const T* row, u32 base, u32 lane, u32 cols, Eight& v) {
     Raw<T, VEC> r;
     r.load(row, base, lane, cols);
     r.values(v);
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store_cols(T* row, u32 base, u32 lane, u32 cols, const float (&v)[8]) {
+__device__ __forceinline__ void store_cols(T* row, u32 base, u32 lane, u32 cols, const Eight& v) {
     if constexpr (VEC) {
         const u32 c = base + lane * 8;
-        if (c + 8 <= cols) {
+        if (c < cols) {
             uint4 q[sizeof(T) / 2];
-            T* h = reinterpret_cast<T*>(q);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) wput(h, e, v[e]);
+            for (int i = 0; i < 4; ++i) put_two<T>(reinterpret_cast<char*>(q) + i * 2 * sizeof(T), v[i]);
 #pragma unroll
             for (int i = 0; i < (int)sizeof(T) / 2; ++i) __stcs(reinterpret_cast<uint4*>(row + c) + i, q[i]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) if (c + e < cols) wput(row, c + e, v[e]);
         }
     } else {
 #pragma unroll
         for (u32 e = 0; e < 8; ++e) {
             const u32 c = base + e * 32 + lane;
-            if (c < cols) wput(row, c, v[e]);
+            if (c < cols) wput(row, c, e % 2 ? high_2(v[e / 2]) : low_2(v[e / 2]));
         }
     }
 }
 // One value per column, 32-bit floats or T (runtime: the branch is the same for all).
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_vector(const ColumnVector& w, u32 base, u32 lane, u32 cols, float absent, float (&v)[8]) {
+__device__ __forceinline__ void load_vector(const ColumnVector& w, u32 base, u32 lane, u32 cols, float absent, Eight& v) {
     if (!w.p) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = absent;
-    } else if (w.dtype == DT_F32) {
+        for (int i = 0; i < 4; ++i) v[i] = both_2(absent);
+    } else if (sizeof(T) != 4 && w.dtype == DT_F32) {
         load_cols<float, VEC>(static_cast<const float*>(w.p), base, lane, cols, v);
     } else {
         load_cols<T, VEC>(static_cast<const T*>(w.p), base, lane, cols, v);
@@ -132,12 +152,16 @@ __device__ __forceinline__ void load_vector(const ColumnVector& w, u32 base, u32
 }
 
 // ---- blocks of 32 values in 8 bits ------------------------------------------------------------------------------------------
-// The scale of a block from its largest magnitude (as bits): A / 127 rounded up to 8 significant bits, at least 2^-126; NaN where the
+// The scale of a block from its largest magnitude A (as bits): fl(A / 127) rounded up to 8 significant bits, at least 2^-126; NaN where the
 // block holds one or an infinity.  It has the bits of a bfloat16.
+// That is the smallest number s of 8 bits with 127 s >= A: the product is exact in fp32, and where A is above it by one unit in its last
+// place, A / 127 is above s by more than half of one of its own (127 s has 1.984 or 0.992 times the significand of s), so the quotient
+// does not round down to s.  A times a little less than 1 / 127 gives s or the number before it.
 __device__ __forceinline__ float a8_scale(u32 largest) {
     if (largest >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
-    const u32 b = (__float_as_uint(__fdiv_rn(__uint_as_float(largest), 127.f)) + 0xffffu) & 0xffff0000u;
-    return __uint_as_float(max(b, 0x00800000u));
+    const float a = __uint_as_float(largest);
+    const u32 b = max((__float_as_uint(a * 0.0078740126f) + 0xffffu) & 0xffff0000u, 0x00800000u);
+    return __uint_as_float(127.f * __uint_as_float(b) < a ? b + 0x10000u : b);
 }
 // Four codes in a word.  1.5 * 2^23 added: the nearest whole number (ties to even) in the low byte, in two's complement.
 __device__ __forceinline__ u32 a8_codes(float a, float b, float c, float d, float inverse) {
@@ -148,9 +172,32 @@ __device__ __forceinline__ u32 a8_codes(float a, float b, float c, float d, floa
 }
 // 1 / scale; of NaN: 0 where that makes every code 0.
 __device__ __forceinline__ float a8_inverse(float scale) { return __frcp_rn(scale); }
-// The value of byte `i` of a word of codes that was turned to 0 .. 255 (^ 0x80808080).
-__device__ __forceinline__ float a8_value(u32 turned, u32 i, float scale) {
-    return (__uint_as_float(__byte_perm(turned, 0x4b000000u, 0x7440u + i)) - 8388736.f) * scale;
+// (The products one by one: a product and a sum of two lanes each become one fused instruction, whatever their rounding says, and a
+// code depends on the product's own rounding.)
+__device__ __forceinline__ f32x2 a8_steps(f32x2 v, float inverse) {
+    return add_2(pack_2(__fmul_rn(low_2(v), inverse), __fmul_rn(high_2(v), inverse)), both_2(12582912.f));
+}
+__device__ __forceinline__ u32 a8_codes(f32x2 ab, f32x2 cd, float inverse) {
+    const f32x2 p = a8_steps(ab, inverse), q = a8_steps(cd, inverse);
+    return __byte_perm(__byte_perm((u32)p, (u32)(p >> 32), 0x0040), __byte_perm((u32)q, (u32)(q >> 32), 0x0040), 0x5410);
+}
+// Bytes i and j of words of codes that were turned to 0 .. 255 (^ 0x80808080), times their scales.
+__device__ __forceinline__ f32x2 a8_values(u32 turned_a, u32 i, u32 turned_b, u32 j, f32x2 scale) {
+    const u32 a = __byte_perm(turned_a, 0x4b000000u, 0x7440u + i), b = __byte_perm(turned_b, 0x4b000000u, 0x7440u + j);
+    return mul_2(add_2((u64)a | (u64)b << 32, both_2(-8388736.f)), scale);
+}
+__device__ __forceinline__ void a8_eight(u32 first, u32 second, float scale, Eight& v) {
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+        const u32 w = (i < 2 ? first : second) ^ 0x80808080u;
+        v[i] = a8_values(w, (2 * i) % 4, w, (2 * i + 1) % 4, both_2(scale));
+    }
+}
+// The larger magnitude; NaN if one is.
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
 }
 
 struct Kept {                                      // an 8-bit matrix
@@ -165,17 +212,19 @@ struct Kept {                                      // an 8-bit matrix
 
 // The lane's eight values -> codes and scales.  Whole warp; values past `cols` are 0.
 template <bool VEC>
-__device__ __forceinline__ void store_kept(const Kept& k, u64 row, u32 base, u32 lane, u32 cols, const float (&v)[8]) {
+__device__ __forceinline__ void store_kept(const Kept& k, u64 row, u32 base, u32 lane, const Eight& v) {
     unsigned char* codes = k.codes + row * k.blocks * A8_BLOCK;
     unsigned short* scales = k.scales + row * k.blocks;
     if constexpr (VEC) {
-        u32 top = 0;
+        float m = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+        for (int i = 0; i < 4; ++i) m = larger(larger(m, low_2(v[i])), high_2(v[i]));
+        u32 top = __float_as_uint(m) & 0x7fffffffu;
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const float s = a8_scale(top), inverse = a8_inverse(s);
-        uint2 q = make_uint2(a8_codes(v[0], v[1], v[2], v[3], inverse), a8_codes(v[4], v[5], v[6], v[7], inverse));
+        const float s = a8_scale(top);
+        const float inverse = a8_inverse(s);
+        uint2 q = make_uint2(a8_codes(v[0], v[1], inverse), a8_codes(v[2], v[3], inverse));
         if (top >= 0x7f800000u) q = make_uint2(0u, 0u);
         const u32 c = base + lane * 8;
         if (c / A8_BLOCK < k.blocks) {
@@ -187,9 +236,10 @@ __device__ __forceinline__ void store_kept(const Kept& k, u64 row, u32 base, u32
         for (u32 e = 0; e < 8; ++e) {
             const u32 b = base / A8_BLOCK + e;
             if (b >= k.blocks) break;
-            const u32 top = __reduce_max_sync(0xffffffffu, __float_as_uint(v[e]) & 0x7fffffffu);
+            const float x = e % 2 ? high_2(v[e / 2]) : low_2(v[e / 2]);
+            const u32 top = __reduce_max_sync(0xffffffffu, __float_as_uint(x) & 0x7fffffffu);
             const float s = a8_scale(top);
-            const u32 q = top >= 0x7f800000u ? 0u : a8_codes(v[e], 0.f, 0.f, 0.f, a8_inverse(s));
+            const u32 q = top >= 0x7f800000u ? 0u : a8_codes(x, 0.f, 0.f, 0.f, a8_inverse(s));
             codes[b * A8_BLOCK + lane] = (unsigned char)q;
             if (lane == 0) scales[b] = (unsigned short)(__float_as_uint(s) >> 16);
         }
@@ -200,12 +250,11 @@ template <bool VEC>
 struct RawKept {                                   // a lane's eight codes and their scales as they lie in memory
     u32 q[VEC ? 2 : 8];
     unsigned short s[VEC ? 1 : 8];
-    __device__ __forceinline__ void load(const Kept& k, u64 row, u32 base, u32 lane, u32) {
-        const unsigned char* codes = k.codes + row * k.blocks * A8_BLOCK;
-        const unsigned short* scales = k.scales + row * k.blocks;
+    // codes, scales: of the row
+    __device__ __forceinline__ void load(const unsigned char* codes, const unsigned short* scales, u32 blocks, u32 base, u32 lane) {
         if constexpr (VEC) {
             const u32 c = base + lane * 8;
-            const bool there = c / A8_BLOCK < k.blocks;
+            const bool there = c / A8_BLOCK < blocks;
             const uint2 w = there ? __ldg(reinterpret_cast<const uint2*>(codes + c)) : make_uint2(0u, 0u);
             q[0] = w.x;
             q[1] = w.y;
@@ -214,19 +263,21 @@ struct RawKept {                                   // a lane's eight codes and t
 #pragma unroll
             for (u32 e = 0; e < 8; ++e) {
                 const u32 b = base / A8_BLOCK + e;
-                q[e] = b < k.blocks ? codes[b * A8_BLOCK + lane] : 0u;
-                s[e] = b < k.blocks ? scales[b] : 0;
+                q[e] = b < blocks ? codes[b * A8_BLOCK + lane] : 0u;
+                s[e] = b < blocks ? scales[b] : 0;
             }
         }
     }
-    __device__ __forceinline__ void values(float (&v)[8]) const {
+    __device__ __forceinline__ void load(const Kept& k, u64 row, u32 base, u32 lane) {
+        load(k.codes + row * k.blocks * A8_BLOCK, k.scales + row * k.blocks, k.blocks, base, lane);
+    }
+    __device__ __forceinline__ void values(Eight& v) const {
         if constexpr (VEC) {
-            const float scale = __uint_as_float((u32)s[0] << 16);
-#pragma unroll
-            for (u32 e = 0; e < 8; ++e) v[e] = a8_value(q[e / 4] ^ 0x80808080u, e % 4, scale);
+            a8_eight(q[0], q[1], __uint_as_float((u32)s[0] << 16), v);
         } else {
 #pragma unroll
-            for (u32 e = 0; e < 8; ++e) v[e] = a8_value(q[e] ^ 0x80u, 0, __uint_as_float((u32)s[e] << 16));
+            for (u32 i = 0; i < 4; ++i)
+                v[i] = a8_values(q[2 * i] ^ 0x80u, 0, q[2 * i + 1] ^ 0x80u, 0, (u64)((u32)s[2 * i] << 16) | (u64)((u32)s[2 * i + 1] << 16) << 32);
         }
     }
 };

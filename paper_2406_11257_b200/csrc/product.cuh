@@ -106,16 +106,9 @@ __device__ __forceinline__ float any_value(const void* p, int dtype, u64 i) {
 }
 template <u32 W>
 __device__ __forceinline__ void activate(float (&f)[W], int act) {
-    if (act == ACT_GELU) {
-#pragma unroll
-        for (u32 e = 0; e < W; ++e) f[e] = act_value<ACT_GELU>(f[e]);
-    } else if (act == ACT_GELU_TANH) {
-#pragma unroll
-        for (u32 e = 0; e < W; ++e) f[e] = act_value<ACT_GELU_TANH>(f[e]);
-    } else if (act == ACT_SILU) {
-#pragma unroll
-        for (u32 e = 0; e < W; ++e) f[e] = act_value<ACT_SILU>(f[e]);
-    }
+    if (act == ACT_GELU) act_values<ACT_GELU>(f);
+    else if (act == ACT_GELU_TANH) act_values<ACT_GELU_TANH>(f);
+    else if (act == ACT_SILU) act_values<ACT_SILU>(f);
 }
 __device__ __forceinline__ void store32(void* p, const u32 v[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
