@@ -109,7 +109,8 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) act_grad_kern
     const u32 strip = blockIdx.x / g.groups, group = blockIdx.x - strip * g.groups, base = strip * SPAN;
     Eight total = {};
     const u64 step = (u64)g.groups * WARPS;
-    u64 row = (u64)group * WARPS + warp;
+    const u64 row = (u64)group * WARPS + warp;
+    const u32 mine = row < g.rows ? (u32)((g.rows - row + step - 1) / step) : 0;       // rows of the warp
     // pointers to the warp's rows, moved by whole steps: products of 64 bits for each would cost as much as the values
     const T* dy_row = g.dy + row * g.dy_stride;
     const T* pre_row = KEPT || ACT == ACT_NONE ? nullptr : g.pre + row * g.pre_stride;
@@ -135,18 +136,18 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) act_grad_kern
         }
     };
 #pragma unroll
-    for (int u = 0; u < U; ++u) if (row + u * step < g.rows) fetch(u);
-    for (; row < g.rows; row += U * step) {
+    for (u32 u = 0; u < U; ++u) if (u < mine) fetch(u);
+    for (u32 at = 0; at < mine; at += U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (row + u * step >= g.rows) break;
+        for (u32 u = 0; u < U; ++u) {
+            if (at + u >= mine) break;
             Eight d, a, p;
             dy[u].values(d);
             if constexpr (ACT != ACT_NONE) {
                 if constexpr (KEPT) kept[u].values(p);
                 else pre[u].values(p);
             }
-            if (row + (u + U) * step < g.rows) fetch(u);         // on its way while this row is worked on
+            if (at + u + U < mine) fetch(u);       // on its way while this row is worked on
             if constexpr (ACT != ACT_NONE) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -238,7 +239,7 @@ Split act_split(int sms, u64 rows, u64 cols) {
 template <typename T, bool KEPT, bool VEC, int ACT>
 void act_grad_launch(cudaStream_t s, const Args<T>& g, const Split& p) {
     const u32 strips = (g.cols + SPAN - 1) / SPAN;
-    launch_chained(act_grad_kernel<T, KEPT, VEC, ACT, 2>, strips * p.groups, THREADS, 0, g.sums ? p.cluster : 0, s, g);
+    launch_chained(act_grad_kernel<T, KEPT, VEC, ACT, ACT == ACT_NONE ? 6 : 2>, strips * p.groups, THREADS, 0, g.sums ? p.cluster : 0, s, g);
 }
 
 template <typename T>

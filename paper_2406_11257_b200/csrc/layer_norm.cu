@@ -143,18 +143,17 @@ __global__ void __launch_bounds__(block_of<PIECES>(), PIECES < 2 ? 2 : 5) norm_k
     const f32x2 minus_mean = both_2(-mean);
     f32x2 squares = 0;
     each([&](const Eight& a, u32 base) {
-        const bool last = base + 256 > g.cols;     // a warp's last columns: those past the end do not count
+        f32x2 piece = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             f32x2 d = add_2(a[i], minus_mean);
-            if (VEC) {                             // a lane's eight are in or out
-                if (base + lane * 8 >= g.cols) d = 0;
-            } else if (last) {
+            if (!VEC) {
                 if (lane_col<VEC>(base, lane, 2 * i) >= g.cols) d &= ~0xffffffffull;
                 if (lane_col<VEC>(base, lane, 2 * i + 1) >= g.cols) d &= 0xffffffffull;
             }
-            squares = fma_2(d, d, squares);
+            piece = fma_2(d, d, piece);
         }
+        if (!VEC || base + lane * 8 < g.cols) squares = add_2(squares, piece);         // VEC: a lane's eight are in or out
     });
     const float rstd = rsqrtf(fmaf(sums(low_2(squares) + high_2(squares)), inv_n, g.eps));
     if (t == 0 && g.stats) g.stats[row] = make_float2(mean, rstd);
@@ -313,7 +312,7 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) norm_grad_kernel(const __grid_co
 // ---- many rows ------------------------------------------------------------------------------------------------------------------
 // dx alone.  PIECES as above.
 template <typename T, bool KEPT, bool VEC, int PIECES>
-__global__ void __launch_bounds__(block_of<PIECES>(), PIECES < 2 ? 2 : 4) norm_dx_kernel(const __grid_constant__ GradArgs<T> g) {
+__global__ void __launch_bounds__(PIECES == 2 ? 128 : GROUP_MAX, PIECES == 2 ? 6 : PIECES == 1 ? 2 : 1) norm_dx_kernel(const __grid_constant__ GradArgs<T> g) {
     __shared__ float2 room[2 * GROUP_MAX / 32];
     wait_for_previous();
     let_next_start();
@@ -326,41 +325,44 @@ __global__ void __launch_bounds__(block_of<PIECES>(), PIECES < 2 ? 2 : 4) norm_d
     const float2 st = __ldg(g.stats + row);
     const f32x2 minus_mean = both_2(-st.x), rstd = both_2(st.y);
     constexpr int HELD = PIECES ? PIECES : 1;
+    Eight held_g[HELD], held_xh[HELD];
     Raw<T, VEC> dy[HELD];
     RawX<T, KEPT, VEC> x[HELD];
     auto load = [&](int p, u32 base) {
         dy[p].load(g.dy + row * g.dy_stride, base, lane, g.cols);
         x[p].load(g, row, base, lane);
     };
-    auto each = [&](auto&& f) {                    // f(g, xh, first column of the warp's piece)
-        auto one = [&](int p, u32 base) {
-            Eight d, xh, w;
-            dy[p].values(d);
-            x[p].values(xh);
-            load_vector<T, VEC>(g.weight, base, lane, g.cols, 1.f, w);
+    auto take = [&](int p, u32 base) {
+        Eight w;
+        dy[p].values(held_g[p]);
+        x[p].values(held_xh[p]);
+        load_vector<T, VEC>(g.weight, base, lane, g.cols, 1.f, w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                xh[i] = mul_2(add_2(xh[i], minus_mean), rstd);
-                d[i] = mul_2(d[i], w[i]);          // 0 past the last column
-            }
-            f(d, xh, base);
-        };
+        for (int i = 0; i < 4; ++i) {
+            held_xh[p][i] = mul_2(add_2(held_xh[p][i], minus_mean), rstd);
+            held_g[p][i] = mul_2(held_g[p][i], w[i]);            // 0 past the last column
+        }
+    };
+    auto each = [&](auto&& f) {                    // f(g, xh, first column of the warp's piece)
         if constexpr (PIECES) {
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
                 if (p && first + p * step >= g.cols) break;      // a whole warp
-                one(p, first + p * step);
+                f(held_g[p], held_xh[p], first + p * step);
             }
         } else {
             for (u32 base = first; base < g.cols; base += step) {
                 load(0, base);
-                one(0, base);
+                take(0, base);
+                f(held_g[0], held_xh[0], base);
             }
         }
     };
     if constexpr (PIECES) {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) if (!p || first + p * step < g.cols) load(p, first + p * step);
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) if (!p || first + p * step < g.cols) take(p, first + p * step);
     }
     f32x2 s1 = 0, s2 = 0;
     each([&](const Eight& d, const Eight& xh, u32) {
@@ -399,8 +401,8 @@ __global__ void __launch_bounds__(SUM_WARPS * 32, 4) norm_columns_kernel(const _
     let_next_start();
     const u32 warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const u32 strip = blockIdx.x / g.groups, group = blockIdx.x - strip * g.groups, base = strip * 256;
-    const u64 step = (u64)g.groups * SUM_WARPS;
-    u64 row = (u64)group * SUM_WARPS + warp;
+    const u64 step = (u64)g.groups * SUM_WARPS, row = (u64)group * SUM_WARPS + warp;
+    const u32 mine = row < g.rows ? (u32)((g.rows - row + step - 1) / step) : 0;       // rows of the warp
     // pointers to the warp's rows, moved by whole steps: products of 64 bits for each would cost as much as the values
     const T* dy_row = g.dy + row * g.dy_stride;
     const T* x_row = KEPT ? nullptr : g.x + row * g.x_stride;
@@ -427,16 +429,16 @@ __global__ void __launch_bounds__(SUM_WARPS * 32, 4) norm_columns_kernel(const _
     };
     Eight dw = {}, db = {};
 #pragma unroll
-    for (int u = 0; u < U; ++u) if (row + u * step < g.rows) fetch(u);
-    for (; row < g.rows; row += U * step) {
+    for (u32 u = 0; u < U; ++u) if (u < mine) fetch(u);
+    for (u32 at = 0; at < mine; at += U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (row + u * step >= g.rows) break;
+        for (u32 u = 0; u < U; ++u) {
+            if (at + u >= mine) break;
             Eight d, xh;
             dy[u].values(d);
             x[u].values(xh);
             const f32x2 minus_mean = both_2(-st[u].x), rstd = both_2(st[u].y);
-            if (row + (u + U) * step < g.rows) fetch(u);         // on its way while this row is worked on
+            if (at + u + U < mine) fetch(u);       // on its way while this row is worked on
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 db[i] = add_2(db[i], d[i]);
@@ -480,13 +482,12 @@ struct Rows {
     u32 pieces, threads, block;
 };
 // Few rows: as many threads to a row as it has words of eight columns.  Many, or long ones: as few as can hold it.
-constexpr u32 PIECES_MAX = 8;
-Rows rows_of(int sms, u64 rows, u64 cols) {
-    if (cols > (u64)128 * PIECE * PIECES_MAX) return Rows{0, GROUP_MAX, GROUP_MAX};
+Rows rows_of(int sms, u64 rows, u64 cols, u32 most_pieces, u32 most_threads) {
+    if (cols > (u64)most_threads * PIECE * most_pieces) return Rows{0, GROUP_MAX, GROUP_MAX};
     Rows r{1, 32, 128};
     const bool many = rows > (u64)sms * 2 || cols > GROUP_MAX * PIECE;
     while ((u64)r.threads * PIECE * r.pieces < cols) {
-        if (many && r.pieces < PIECES_MAX) r.pieces *= 2;
+        if (many && r.pieces < most_pieces) r.pieces *= 2;
         else r.threads *= 2;
     }
     if (r.threads > r.block) r.block = r.threads;
@@ -502,7 +503,7 @@ void norm_launch(cudaStream_t s, NormArgs<T> g, const Rows& r) {
 }
 template <typename T, bool VEC>
 void norm_as(int sms, cudaStream_t s, const NormArgs<T>& g) {
-    const Rows r = rows_of(sms, g.rows, g.cols);
+    const Rows r = rows_of(sms, g.rows, g.cols, 8, 128);
     if (r.pieces == 0) norm_launch<T, VEC, 0>(s, g, r);
     else if (r.pieces == 1) norm_launch<T, VEC, 1>(s, g, r);
     else if (r.pieces == 2) norm_launch<T, VEC, 2>(s, g, r);
@@ -571,12 +572,11 @@ void grad_as(int sms, cudaStream_t s, GradArgs<T> g, float* scratch) {
             launch_chained(norm_columns_kernel<T, KEPT, VEC>, (g.cols + 255) / 256 * d.blocks, SUM_WARPS * 32, 0, d.cluster, s, g);
         }
         if (g.dx) {
-            const Rows r = rows_of(sms, g.rows, g.cols);
+            const Rows r = rows_of(sms, g.rows, g.cols, 4, GROUP_MAX);
             if (r.pieces == 0) dx_launch<T, KEPT, VEC, 0>(s, g, r);
             else if (r.pieces == 1) dx_launch<T, KEPT, VEC, 1>(s, g, r);
             else if (r.pieces == 2) dx_launch<T, KEPT, VEC, 2>(s, g, r);
-            else if (r.pieces == 4) dx_launch<T, KEPT, VEC, 4>(s, g, r);
-            else dx_launch<T, KEPT, VEC, 8>(s, g, r);
+            else dx_launch<T, KEPT, VEC, 4>(s, g, r);
         }
     }
     if (sums > 1) launch_column_sums(s, scratch, sums, 2 * (u64)g.cols, g.cols, dweight, dbias);

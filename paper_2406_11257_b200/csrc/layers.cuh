@@ -80,19 +80,26 @@ __device__ __forceinline__ void put_two(void* p, f32x2 v) {
     else *static_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(low_2(v), high_2(v));
 }
 
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+    uint4 q;
+    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(p));
+    return q;
+}
+
 // Eight values as they lie in memory, and as fp32.
 template <typename T, bool VEC>
 struct Raw {
     static constexpr int N = VEC ? (int)sizeof(T) / 2 : 8;
     typename std::conditional<VEC, uint4, T>::type q[N];
 
-    // Columns past `cols` are left 0.
+    // Columns past `cols` are left 0.  STREAM: read once (it leaves the first-level cache to what every row reads).
+    template <bool STREAM = true>
     __device__ __forceinline__ void load(const T* row, u32 base, u32 lane, u32 cols) {
         if constexpr (VEC) {
             const u32 c = base + lane * 8;
             const uint4* p = reinterpret_cast<const uint4*>(row + c);
 #pragma unroll
-            for (int i = 0; i < N; ++i) q[i] = c < cols ? __ldg(p + i) : make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < N; ++i) q[i] = c < cols ? (STREAM ? load_once(p + i) : __ldg(p + i)) : make_uint4(0u, 0u, 0u, 0u);
         } else {
 #pragma unroll
             for (u32 e = 0; e < 8; ++e) {
@@ -113,10 +120,10 @@ struct Raw {
     }
 };
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool STREAM = true>
 __device__ __forceinline__ void load_cols(const T* row, u32 base, u32 lane, u32 cols, Eight& v) {
     Raw<T, VEC> r;
-    r.load(row, base, lane, cols);
+    r.template load<STREAM>(row, base, lane, cols);
     r.values(v);
 }
 template <typename T, bool VEC>
@@ -145,9 +152,9 @@ __device__ __forceinline__ void load_vector(const ColumnVector& w, u32 base, u32
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = both_2(absent);
     } else if (sizeof(T) != 4 && w.dtype == DT_F32) {
-        load_cols<float, VEC>(static_cast<const float*>(w.p), base, lane, cols, v);
+        load_cols<float, VEC, false>(static_cast<const float*>(w.p), base, lane, cols, v);
     } else {
-        load_cols<T, VEC>(static_cast<const T*>(w.p), base, lane, cols, v);
+        load_cols<T, VEC, false>(static_cast<const T*>(w.p), base, lane, cols, v);
     }
 }
 

@@ -357,3 +357,219 @@ def test_infinities_and_nan_stay_in_their_rows(h):
         y = h.linear(x, w)
         keep = [i for i in range(rows) if i not in (2, 3)]
         assert torch.equal(y[keep], clean[keep]) and torch.isnan(y[2]).all() and not torch.isfinite(y[3]).any()
+
+
+# ---- how the calls are made ----------------------------------------------------------------------------------
+def mlp_step(h, x, w, b, nw, nb, dy, run=None):
+    """A residual MLP block forward and backward as a training step runs it, activations kept in 8 bits."""
+    n = h.layer_norm(x, nw, nb, keep=True)
+    a, pre = h.linear_kept(n.y, w[0], b[0], act="gelu", keep="act8")
+    y = h.linear(a, w[1], b[1], residual=x)
+    g = {"y": y, "w1": h.linear_grad_weight(dy, a), "b1": h.bias_grad(dy)}
+    r = h.act_grad(h.linear_grad_input(dy, w[1]), pre, "gelu")
+    g["b0"], g["w0"] = r.dbias, h.linear_grad_weight(r.dpre, n.y)
+    ng = h.layer_norm_grad(h.linear_grad_input(r.dpre, w[0]), n.kept, nw, n, add=dy)
+    return {**g, "x": ng.dx, "nw": ng.dweight, "nb": ng.dbias}
+
+
+def mlp_inputs(tokens, d, f, seed=1, dtype="bf16"):
+    return dict(x=make(tokens, d, dtype, seed), w=[make(f, d, dtype, seed + 1, size=0.05), make(d, f, dtype, seed + 2, size=0.05)],
+                b=[vector(f, dtype, seed + 3, 0.1), vector(d, dtype, seed + 4, 0.1)], nw=vector(d, dtype, seed + 5, 0.2, 1.0), nb=vector(d, dtype, seed + 6, 0.1),
+                dy=make(tokens, d, dtype, seed + 7, size=0.1))
+
+
+@pytest.mark.parametrize("tokens,d,f", [(1, 64, 256), (200, 256, 1024), (777, 200, 1000)])
+def test_an_mlp_block_forward_and_backward(h, tokens, d, f):
+    """Against torch's autograd in 64 bits.  Between the operators values are rounded to 16 and 8 bits, so a gradient is compared as a
+    whole: the relative error of a sum of products whose factors are each off by at most r is about r.  Three 16-bit roundings
+    (2^-8) and two 8-bit ones (half of 1 / 127 of a block's largest magnitude, some three deviations) in the chain make at most
+    3 * 2^-8 + 2 * 1.5 / 127 = 0.036; a wrong term makes more than 0.1 of any gradient here."""
+    i = mlp_inputs(tokens, d, f)
+    got = mlp_step(h, **i)
+    leaf = lambda t: t.double().requires_grad_()
+    x, w, b, nw, nb = leaf(i["x"]), [leaf(t) for t in i["w"]], [leaf(t) for t in i["b"]], leaf(i["nw"]), leaf(i["nb"])
+    n = torch.nn.functional.layer_norm(x, (d,), nw, nb)
+    y = torch.nn.functional.gelu(n @ w[0].T + b[0]) @ w[1].T + b[1] + x
+    grads = torch.autograd.grad(y, [x, w[0], b[0], w[1], b[1], nw, nb], i["dy"].double())
+    for name, want in zip(["y", "x", "w0", "b0", "w1", "b1", "nw", "nb"], [y.detach(), *grads]):
+        assert (got[name].double() - want).norm() <= 0.036 * want.norm(), name
+
+
+def test_captured_and_replayed(h):
+    """A graph of a training step: replayed on new contents of the same tensors, it gives what the calls give; two graphs on one
+    handle, replayed at once on two streams, do not disturb each other."""
+    a, b = mlp_inputs(130, 128, 512, 1), mlp_inputs(700, 1024, 512, 20)
+    eager = [mlp_step(h, **a), mlp_step(h, **b)]
+    torch.cuda.synchronize()
+    graphs, results = [], []
+    for i in (a, b):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            results.append(mlp_step(h, **i))
+        graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for r, e in zip(results, eager):
+        for k in e:
+            assert torch.equal(r[k], e[k]), k
+    new = mlp_inputs(130, 128, 512, 50)
+    want = mlp_step(h, **new)
+    for k in ("x", "nw", "nb", "dy"):
+        a[k].copy_(new[k])
+    for k in ("w", "b"):
+        for t, u in zip(a[k], new[k]):
+            t.copy_(u)
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    for k in want:
+        assert torch.equal(results[0][k], want[k]), k
+
+
+def test_same_bits_every_time(h):
+    i = mlp_inputs(1000, 512, 2048, 3)
+    first = mlp_step(h, **i)
+    for _ in range(3):
+        again = mlp_step(h, **i)
+        for k in first:
+            assert torch.equal(first[k], again[k]), k
+
+
+def test_on_another_stream_and_a_fresh_handle():
+    other = binding.Handle(workspace_numel=4096, device=0)
+    i = mlp_inputs(64, 128, 256, 4)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = mlp_step(other, **i)
+    s.synchronize()
+    want = mlp_step(other, **i)
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    other.score_status()
+    other.close()
+
+
+def test_rows_past_the_last_stay_as_they_are(h):
+    """Results into the first rows and columns of a larger buffer."""
+    for rows, k, n in ((5, 96, 100), (130, 64, 257), (300, 200, 520)):
+        x, w = make(rows, k, "bf16", 1), make(n, k, "bf16", 2)
+        room = torch.full((rows + 3, n + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+        h.linear(x, w, out=room[:rows, :n])
+        assert torch.equal(room[:rows, :n], h.linear(x, w)) and bool((room[rows:] == 7).all()) and bool((room[:, n:] == 7).all())
+        t = make(rows, n, "bf16", 3)
+        room.fill_(7.0)
+        h.layer_norm(t, out=room[:rows, :n])
+        assert torch.equal(room[:rows, :n], h.layer_norm(t).y) and bool((room[rows:] == 7).all()) and bool((room[:, n:] == 7).all())
+        room.fill_(7.0)
+        h.act_grad(t, t, "silu", out=room[:rows, :n])
+        assert torch.equal(room[:rows, :n], h.act_grad(t, t, "silu").dpre) and bool((room[rows:] == 7).all()) and bool((room[:, n:] == 7).all())
+
+
+def test_waits_that_run_out():
+    """No time at all: the products report it and the handle stays usable."""
+    other = binding.Handle(workspace_numel=4096, device=0)
+    shapes = ((4, 512, 300), (64, 4096, 1024), (2304, 256, 2304))
+    for rows, k, n in shapes:
+        x, w = make(rows, k, "bf16", 1), make(n, k, "bf16", 2)
+        want = other.linear(x, w)
+        other.score_status()
+        other.set_wait_limit(0)
+        other.linear(x, w)
+        with pytest.raises(binding.ExcpError) as e:
+            other.score_status()
+        assert e.value.status == -7
+        other.set_wait_limit(2_000_000_000)
+        assert torch.equal(other.linear(x, w), want)
+        other.score_status()
+    other.close()
+
+
+def test_offsets_past_32_bits(h):
+    """Rows whose bytes and elements lie past 2^32 and 2^31 of their buffer."""
+    cols, rows = 65536 + 64, 33000                 # 2.16e9 elements of 2 bytes
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device=DEV)
+    last = make(8, cols, "bf16", 1)
+    x[-8:] = last
+    y = torch.empty_like(x)
+    r = h.layer_norm(x, out=y)
+    want, mean, rstd = lo.norm(last)
+    near(r.y[-8:], want, (last.double().abs() + mean.abs()[:, None]) * rstd[:, None] * adds(cols) * U * 2)
+    g = h.layer_norm_grad(x, x, None, r, out=y)
+    dx, _, _ = lo.norm_grad(last, last, None, r.row_stats[-8:, 0], r.row_stats[-8:, 1])
+    near(g.dx[-8:], dx, rstd[:, None] * last.double().abs().amax(1, keepdim=True) * adds(cols) * U * 8 * (1 + last.double().abs()))
+    near(g.dbias, x[-8:].double().sum(0), x[-8:].double().abs().sum(0) * 64 * U)
+    m = h.act8_quantize(x)
+    codes, scales = lo.act8_codes(last)
+    b = cols // 32
+    assert torch.equal(m.data[(rows - 8) * cols:rows * cols].view(torch.int8).view(8, -1), codes)
+    assert torch.equal(m.data[rows * cols + (rows - 8) * b * 2:rows * cols + rows * b * 2].view(torch.bfloat16).view(8, b).float(), scales)
+    h.act8_restore(m, out=y)
+    assert torch.equal(y[-8:].double(), lo.act8_round_trip(last).bfloat16().double())
+    got = h.act_grad(x, m, "silu", out=y)
+    v = lo.act8_round_trip(last)
+    near(got.dpre[-8:], last.double() * lo.act_slope(v, "silu"), last.double().abs() * 2.0 ** -17)
+    del m, y, g, r, got
+    # as an operand: few rows of a long matrix, and its gradients
+    w = make(16, cols, "bf16", 2, size=0.1)
+    p = h.linear(x, w, dtype=torch.float32)
+    near(p[-8:], last.double() @ w.double().T, product_tol(last, w))
+    assert not p[:-8].any()
+    dw = h.linear_grad_weight(p.bfloat16(), x)
+    near(dw, p[-8:].bfloat16().double().T @ last.double(), product_tol(p[-8:].bfloat16().T, last.T) * 4)
+    big = h.linear_grad_input(p.bfloat16(), w)
+    near(big[-8:], p[-8:].bfloat16().double() @ w.double(), product_tol(p[-8:].bfloat16(), w.T))
+
+
+def test_refusals(h):
+    x, w = make(4, 64, "bf16", 1), make(8, 64, "bf16", 2)
+    y = make(4, 8, "bf16", 3)
+    r = h.layer_norm(x)
+    q = h.act8_quantize(x)
+    bad = [
+        lambda: h.linear(x.float(), w.float()),                            # operands of 32 bits
+        lambda: h.linear(x, w.half()),                                     # two types
+        lambda: h.linear(x, make(8, 63, "bf16", 4)),                       # another number of columns
+        lambda: h.linear(x, w, torch.zeros(7, device=DEV)),                # a bias of another length
+        lambda: h.linear(x, w, torch.zeros(8, device=DEV, dtype=torch.float64)),
+        lambda: h.linear(x, w, residual=make(5, 8, "bf16", 5)),
+        lambda: h.linear(x, w, out=make(4, 9, "bf16", 6)),
+        lambda: h.linear(x.cpu(), w),
+        lambda: h.linear(x[0], w),
+        lambda: h.linear(x.T, w),
+        lambda: h.linear(x, w, dtype=torch.float64),
+        lambda: h.linear_grad_input(y, make(7, 64, "bf16", 7)),
+        lambda: h.linear_grad_weight(y, make(5, 64, "bf16", 8)),
+        lambda: h.linear_grad_weight(y, x, add=torch.zeros(8, 65, device=DEV)),
+        lambda: h.layer_norm(x, torch.ones(64, device=DEV, dtype=torch.float16)),      # neither x's type nor 32 bits
+        lambda: h.layer_norm(x, torch.ones(64, device=DEV), torch.ones(64, device=DEV, dtype=torch.bfloat16)),
+        lambda: h.layer_norm(x, bias=torch.ones(64, device=DEV), rms=True),
+        lambda: h.layer_norm(x, eps=-1.0),
+        lambda: h.layer_norm(x, eps=math.nan),
+        lambda: h.layer_norm(x, out=x.float()),
+        lambda: h.layer_norm_grad(x, x.float(), None, r),
+        lambda: h.layer_norm_grad(x[:3], x, None, r),
+        lambda: h.layer_norm_grad(x[:3], q, None, r),
+        lambda: h.layer_norm_grad(x[:3], x[:3], None, r),                  # statistics of other rows
+        lambda: h.layer_norm_grad(x, x, None, r, add=x.float()),
+        lambda: h.act_grad(x, x.float(), "gelu"),
+        lambda: h.act_grad(x, x[:3], "gelu"),
+        lambda: h.act_grad(x, binding.Act8Matrix(q.data[:100], 4, 64), "gelu"),
+        lambda: h.act8_quantize(x, out=torch.zeros(100, dtype=torch.uint8, device=DEV)),
+        lambda: h.act8_quantize(x, out=torch.zeros(1000, dtype=torch.uint8, device=DEV)[1:]),
+        lambda: h.act8_quantize(x.double()),
+        lambda: h.act8_restore(binding.Act8Matrix(q.data, 8, 64)),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises((TypeError, binding.ExcpError)):
+            f()
+            pytest.fail(f"call {i} was taken")
+    for f in (lambda: h.linear(x, w, act="relu"), lambda: h.act_grad(x, x, "relu")):
+        with pytest.raises(KeyError):
+            f()
+    with pytest.raises(ValueError):
+        h.linear_kept(x, w, keep="fp8")
+    torch.cuda.synchronize()
