@@ -1,5 +1,6 @@
-"""Scores a text with a checkpoint's output embedding before and after it went through the compressor, the
-restored one also held at 4 bits, and takes the gradient of the score.
+"""Scores a text with a checkpoint's final norm and output embedding before and after it went through the compressor, the
+restored one held in 16 bits and at 4 bits, and takes the gradient of the score: with respect to the logits, and through the
+16-bit weights to the embedding, the norm and the hidden states.
 
     python examples/score_checkpoint.py [--shape tiny|pythia-410m|pythia-1.4b|llama-7b] [--tokens N] [--format e8m0_32|e4m3_16]
 
@@ -33,6 +34,11 @@ def score(shape: str = "tiny", tokens: int = 256, fmt: str = "e4m3_16", seed: in
     gen = torch.Generator(device="cuda").manual_seed(seed)
     hidden = torch.randn(tokens, d, generator=gen, device="cuda").to(torch.bfloat16)
     text = torch.randint(0, v, (tokens,), generator=gen, device="cuda")
+    # the final norm: with mean and bias for the neox shapes, without for the llama ones; the input is kept in 8 bits for its gradient
+    rms = cfg.family == "llama"
+    norm_w = torch.ones(d, device="cuda")
+    norm = h.layer_norm(hidden, norm_w, None if rms else torch.zeros(d, device="cuda"), rms=rms, keep=True)
+    hidden, states = norm.y, hidden
     scale_x = h.mx4_tensor_scale(hidden) if fmt == "e4m3_16" else None
 
     def run(weights: torch.Tensor):
@@ -44,14 +50,22 @@ def score(shape: str = "tiny", tokens: int = 256, fmt: str = "e4m3_16", seed: in
     _, before = run(w_t)
     logits, after = run(restored)
     grad = h.token_logprobs_grad(logits, text, after, torch.full((tokens,), -1.0 / tokens, device="cuda"))
+    # the same with the restored weights themselves, in 16 bits, and the way back to them
+    w16 = restored.view(v, d).to(torch.bfloat16)
+    logits16 = h.linear(hidden, w16)
+    exact = h.token_logprobs(logits16, text)
+    dlogits = h.token_logprobs_grad(logits16, text, exact, torch.full((tokens,), -1.0 / tokens, device="cuda"))
+    dw = h.linear_grad_weight(dlogits, hidden)
+    back = h.layer_norm_grad(h.linear_grad_input(dlogits, w16), norm.kept, norm_w, norm)
     plain = torch.log_softmax(hidden.float() @ restored.view(v, d).T, 1).gather(1, text[:, None])[:, 0]
     h.score_status()
     out = {"record_bytes": nbytes, "weights_bytes": 4 * n, "packed_bytes": binding.mx4_bytes(v, d, fmt),
            "mean_logprob_original": before.logprob.mean().item(), "mean_logprob_restored": after.logprob.mean().item(),
-           "mean_logprob_restored_fp32": plain.mean().item(), "mean_entropy": after.entropy.mean().item(),
+           "mean_logprob_restored_16bit": exact.logprob.mean().item(), "mean_logprob_restored_fp32": plain.mean().item(), "mean_entropy": after.entropy.mean().item(),
            "largest_change": (before.logprob - after.logprob).abs().max().item(),
            "same_first_choice": (before.top_index[:, 0] == after.top_index[:, 0]).float().mean().item(),
-           "gradient_sum": grad.float().sum().item()}
+           "gradient_sum": grad.float().sum().item(), "embedding_gradient_norm": dw.norm().item(), "embedding_gradient_column_sum": dw.sum(0).abs().max().item(),
+           "norm_gradient_norm": back.dweight.norm().item(), "state_gradient_along_states": (back.dx.float() * states.float()).sum(1).abs().max().item()}
     h.close()
     return out
 

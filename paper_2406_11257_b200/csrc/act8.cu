@@ -229,6 +229,7 @@ Split act_split(int sms, u64 rows, u64 cols) {
     const u64 strips = (cols + SPAN - 1) / SPAN, most = (rows + 2 * WARPS - 1) / (2 * WARPS);
     u64 groups = (u64)sms * 3 / strips;            // no more than find room at once
     if (groups > most) groups = most;
+    if (groups > 8 && rows <= 8 * 6 * WARPS) groups = 8;         // six rows to a warp cost less than the second launch
     if (groups < 1) groups = 1;
     Split r{1, 1};
     while (r.cluster * 2 <= groups && r.cluster < (groups <= 8 ? 8u : 4u)) r.cluster *= 2;

@@ -485,7 +485,7 @@ struct Rows {
 Rows rows_of(int sms, u64 rows, u64 cols, u32 most_pieces, u32 most_threads) {
     if (cols > (u64)most_threads * PIECE * most_pieces) return Rows{0, GROUP_MAX, GROUP_MAX};
     Rows r{1, 32, 128};
-    const bool many = rows > (u64)sms * 2 || cols > GROUP_MAX * PIECE;
+    const bool many = rows > (u64)sms * 4 || cols > GROUP_MAX * PIECE;
     while ((u64)r.threads * PIECE * r.pieces < cols) {
         if (many && r.pieces < most_pieces) r.pieces *= 2;
         else r.threads *= 2;
