@@ -15,6 +15,7 @@ namespace {
 
 constexpr u32 SPAN = 256;                          // columns of a warp
 constexpr u32 WARPS = 8, THREADS = WARPS * 32;
+constexpr u32 ACT_BLOCKS = 3;                      // of the gradient that an SM holds
 
 // A warp takes U pieces of 256 columns, one after the other in the matrix, all fetched before the first is worked on.
 template <int U, typename F>
@@ -100,7 +101,7 @@ template <typename T> struct Args {
 // A block takes 256 columns and every groups-th set of 8 rows; the column sums of the blocks of a cluster, which share a strip,
 // are added through distributed shared memory in the order of the blocks.
 template <typename T, bool KEPT, bool VEC, int ACT, int U>
-__global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) act_grad_kernel(const __grid_constant__ Args<T> g) {
+__global__ void __launch_bounds__(THREADS, ACT_BLOCKS) act_grad_kernel(const __grid_constant__ Args<T> g) {
     __shared__ float part[WARPS][SPAN];
     __shared__ float sum[SPAN];
     wait_for_previous();
@@ -227,7 +228,7 @@ struct Split {
 };
 Split act_split(int sms, u64 rows, u64 cols) {
     const u64 strips = (cols + SPAN - 1) / SPAN, most = (rows + 2 * WARPS - 1) / (2 * WARPS);
-    u64 groups = (u64)sms * 3 / strips;            // no more than find room at once
+    u64 groups = (u64)sms * ACT_BLOCKS / strips;            // no more than find room at once
     if (groups > most) groups = most;
     if (groups > 8 && rows <= 8 * 6 * WARPS) groups = 8;         // six rows to a warp cost less than the second launch
     if (groups < 1) groups = 1;

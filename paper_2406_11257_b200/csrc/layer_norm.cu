@@ -171,6 +171,76 @@ __global__ void __launch_bounds__(block_of<PIECES>(), PIECES < 2 ? 2 : 5) norm_k
     });
 }
 
+// The same for many rows in 16-byte words, with all that can be known when it is compiled: THREADS of a row (so that a piece's place
+// is a constant), and what vectors there are (VECTORS: 1 the weight, 2 the bias too, both of T).  Half the instructions of the kernel above,
+// which is what bounds it (8192 x 4096 bf16: 43 us there, 27 here).
+__host__ __device__ constexpr int rows_block(int threads) { return threads > 128 ? threads : 128; }
+__host__ __device__ constexpr u32 const_log(u32 v) { return v <= 1 ? 0 : 1 + const_log(v / 2); }
+template <typename T, int PIECES, int THREADS, int VECTORS>
+__global__ void __launch_bounds__(rows_block(THREADS), 512 / rows_block(THREADS)) norm_rows_kernel(const __grid_constant__ NormArgs<T> g) {
+    constexpr u32 BLOCK = rows_block(THREADS), STEP = THREADS * PIECE, LOG = const_log(THREADS);
+    __shared__ float2 room[2 * BLOCK / 32];
+    wait_for_previous();
+    let_next_start();
+    const u32 t = threadIdx.x % THREADS, lane = t & 31, at = t * PIECE;
+    const u64 row = (u64)blockIdx.x * (BLOCK / THREADS) + threadIdx.x / THREADS;
+    if (row >= g.rows) return;                     // a whole group
+    GroupSums sums = group_sums(room, THREADS, LOG);
+    const T* x = g.x + row * g.stride + at;
+    const float n = (float)g.cols, inv_n = 1.f / n;
+    Raw<T, true> raw[PIECES];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) raw[p].load_at(x + p * STEP, at + p * STEP < g.cols);
+    Eight v[PIECES];
+    f32x2 sum = 0;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        raw[p].values(v[p]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = add_2(sum, v[p][i]);
+    }
+    float mean = 0.f;
+    if (!g.rms) mean = sums(low_2(sum) + high_2(sum)) / n;       // divided: the mean of equal values is that value
+    const f32x2 minus_mean = both_2(-mean);
+    f32x2 squares = 0;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        f32x2 piece = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 d = add_2(v[p][i], minus_mean);
+            piece = fma_2(d, d, piece);
+        }
+        if (at + p * STEP < g.cols) squares = add_2(squares, piece);
+    }
+    const float rstd = rsqrtf(fmaf(sums(low_2(squares) + high_2(squares)), inv_n, g.eps));
+    if (t == 0 && g.stats) g.stats[row] = make_float2(mean, rstd);
+    const f32x2 both_rstd = both_2(rstd);
+    T* y = g.y + row * g.y_stride + at;
+    const T* weight = static_cast<const T*>(g.weight.p) + at;
+    const T* bias = static_cast<const T*>(g.bias.p) + at;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        const bool there = at + p * STEP < g.cols;
+        if (g.kept.codes && p * STEP + at - lane * PIECE < g.cols) store_kept<true>(g.kept, row, p * STEP + at - lane * PIECE, lane, v[p]);
+        if (!there) continue;
+        Raw<T, true> w, b;
+        Eight we, be;
+        w.template load_at<false>(weight + p * STEP, true);
+        w.values(we);
+        if (VECTORS == 2) {
+            b.template load_at<false>(bias + p * STEP, true);
+            b.values(be);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 xh = mul_2(add_2(v[p][i], minus_mean), both_rstd);
+            v[p][i] = VECTORS == 2 ? fma_2(xh, we[i], be[i]) : mul_2(xh, we[i]);
+        }
+        store_eight(y + p * STEP, v[p]);
+    }
+}
+
 template <typename T> struct GradArgs {
     const T* dy;
     u64 dy_stride;
@@ -390,17 +460,96 @@ __global__ void __launch_bounds__(PIECES == 2 ? 128 : GROUP_MAX, PIECES == 2 ? 6
     });
 }
 
-// dweight and dbias alone: a block takes 256 columns and every groups-th set of 8 rows.
-constexpr u32 SUM_WARPS = 8;
+// The same as above (norm_rows_kernel), with a weight of T.
+template <typename T, bool KEPT, int PIECES, int THREADS>
+__global__ void __launch_bounds__(rows_block(THREADS), 512 / rows_block(THREADS)) norm_dx_rows_kernel(const __grid_constant__ GradArgs<T> g) {
+    constexpr u32 BLOCK = rows_block(THREADS), STEP = THREADS * PIECE, LOG = const_log(THREADS);
+    __shared__ float2 room[2 * BLOCK / 32];
+    wait_for_previous();
+    let_next_start();
+    const u32 t = threadIdx.x % THREADS, at = t * PIECE;
+    const u64 row = (u64)blockIdx.x * (BLOCK / THREADS) + threadIdx.x / THREADS;
+    if (row >= g.rows) return;                     // a whole group
+    GroupSums sums = group_sums(room, THREADS, LOG);
+    const T* dy = g.dy + row * g.dy_stride + at;
+    const float inv_n = 1.f / (float)g.cols;
+    Raw<T, true> raw[PIECES], x[KEPT ? 1 : PIECES];
+    uint2 codes[KEPT ? PIECES : 1];
+    float scale[KEPT ? PIECES : 1];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) raw[p].load_at(dy + p * STEP, at + p * STEP < g.cols);
+    if constexpr (KEPT) {
+        const unsigned char* c = g.kept.codes + row * g.kept.blocks * A8_BLOCK + at;
+        const unsigned short* s = g.kept.scales + row * g.kept.blocks + at / A8_BLOCK;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const bool there = at + p * STEP < g.cols;
+            codes[p] = there ? __ldg(reinterpret_cast<const uint2*>(c + p * STEP)) : make_uint2(0u, 0u);
+            scale[p] = there ? __uint_as_float((u32)__ldg(s + p * STEP / A8_BLOCK) << 16) : 0.f;
+        }
+    } else {
+        const T* from = g.x + row * g.x_stride + at;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) x[p].load_at(from + p * STEP, at + p * STEP < g.cols);
+    }
+    const float2 st = __ldg(g.stats + row);
+    const f32x2 minus_mean = both_2(-st.x), rstd = both_2(st.y);
+    const T* weight = static_cast<const T*>(g.weight.p) + at;
+    Eight d[PIECES], xh[PIECES];
+    f32x2 s1 = 0, s2 = 0;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        Raw<T, true> w;
+        Eight we;
+        w.template load_at<false>(weight + p * STEP, at + p * STEP < g.cols);
+        w.values(we);
+        raw[p].values(d[p]);
+        if constexpr (KEPT) a8_eight(codes[p].x, codes[p].y, scale[p], xh[p]);
+        else x[p].values(xh[p]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            xh[p][i] = mul_2(add_2(xh[p][i], minus_mean), rstd);
+            d[p][i] = mul_2(d[p][i], we[i]);       // 0 past the last column
+            s1 = add_2(s1, d[p][i]);
+            s2 = fma_2(d[p][i], xh[p][i], s2);
+        }
+    }
+    float m1 = low_2(s1) + high_2(s1), m2 = low_2(s2) + high_2(s2);
+    sums(m1, m2);
+    const f32x2 minus_m1 = both_2(g.rms ? 0.f : -m1 * inv_n), minus_m2 = both_2(-m2 * inv_n);
+    T* dx = g.dx + row * g.dx_stride + at;
+    const T* add = g.add ? g.add + row * g.add_stride + at : nullptr;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        if (at + p * STEP >= g.cols) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[p][i] = mul_2(rstd, add_2(d[p][i], fma_2(xh[p][i], minus_m2, minus_m1)));
+        if (add) {
+            Raw<T, true> r;
+            Eight a;
+            r.load_at(add + p * STEP, true);
+            r.values(a);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[p][i] = add_2(d[p][i], a[i]);
+        }
+        store_eight(dx + p * STEP, d[p]);
+    }
+}
+
+// dweight and dbias alone: a block takes 256 columns and every groups-th set of 8 rows, a warp a row, COLUMN_ROWS of them on their way.
+// (512 columns to a warp: 8192 x 4096 38 us against 35, 16384 x 1024 37 against 24.)
+constexpr int COLUMN_ROWS = 4;                     // (8192 x 4096: two rows 34 us, four 24)
+constexpr u32 SUM_WARPS = 8, SUM_BLOCKS = 3;       // blocks that an SM holds
 template <typename T, bool KEPT, bool VEC>
-__global__ void __launch_bounds__(SUM_WARPS * 32, 4) norm_columns_kernel(const __grid_constant__ GradArgs<T> g) {
-    constexpr int U = 2;
+__global__ void __launch_bounds__(SUM_WARPS * 32, SUM_BLOCKS) norm_columns_kernel(const __grid_constant__ GradArgs<T> g) {
+    constexpr int U = COLUMN_ROWS;
+    constexpr u32 SPAN = 256;
     __shared__ float part[SUM_WARPS][256];
-    __shared__ float own[512];
+    __shared__ float own[2 * SPAN];
     wait_for_previous();
     let_next_start();
     const u32 warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    const u32 strip = blockIdx.x / g.groups, group = blockIdx.x - strip * g.groups, base = strip * 256;
+    const u32 strip = blockIdx.x / g.groups, group = blockIdx.x - strip * g.groups, base = strip * SPAN;
     const u64 step = (u64)g.groups * SUM_WARPS, row = (u64)group * SUM_WARPS + warp;
     const u32 mine = row < g.rows ? (u32)((g.rows - row + step - 1) / step) : 0;       // rows of the warp
     // pointers to the warp's rows, moved by whole steps: products of 64 bits for each would cost as much as the values
@@ -410,19 +559,20 @@ __global__ void __launch_bounds__(SUM_WARPS * 32, 4) norm_columns_kernel(const _
     const unsigned char* code_row = KEPT ? g.kept.codes + row * per_row * A8_BLOCK : nullptr;
     const unsigned short* scale_row = KEPT ? g.kept.scales + row * per_row : nullptr;
     const float2* stat = g.stats + row;
+    const u64 dy_step = step * g.dy_stride, x_step = step * g.x_stride, code_step = step * per_row * A8_BLOCK, scale_step = step * per_row;
     Raw<T, VEC> dy[U];
     RawX<T, KEPT, VEC> x[U];
     float2 st[U];
     auto fetch = [&](int u) {                      // the next row of the warp
         dy[u].load(dy_row, base, lane, g.cols);
-        dy_row += step * g.dy_stride;
+        dy_row += dy_step;
         if constexpr (KEPT) {
             x[u].x.load(code_row, scale_row, per_row, base, lane);
-            code_row += step * per_row * A8_BLOCK;
-            scale_row += step * per_row;
+            code_row += code_step;
+            scale_row += scale_step;
         } else {
             x[u].x.load(x_row, base, lane, g.cols);
-            x_row += step * g.x_stride;
+            x_row += x_step;
         }
         st[u] = __ldg(stat);
         stat += step;
@@ -435,14 +585,14 @@ __global__ void __launch_bounds__(SUM_WARPS * 32, 4) norm_columns_kernel(const _
         for (u32 u = 0; u < U; ++u) {
             if (at + u >= mine) break;
             Eight d, xh;
+            const f32x2 minus_mean = both_2(-st[u].x), rstd = both_2(st[u].y);
             dy[u].values(d);
             x[u].values(xh);
-            const f32x2 minus_mean = both_2(-st[u].x), rstd = both_2(st[u].y);
             if (at + u + U < mine) fetch(u);       // on its way while this row is worked on
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                db[i] = add_2(db[i], d[i]);
-                dw[i] = fma_2(d[i], mul_2(add_2(xh[i], minus_mean), rstd), dw[i]);
+            for (int k = 0; k < 4; ++k) {
+                db[k] = add_2(db[k], d[k]);
+                dw[k] = fma_2(d[k], mul_2(add_2(xh[k], minus_mean), rstd), dw[k]);
             }
         }
     }
@@ -463,8 +613,8 @@ __global__ void __launch_bounds__(SUM_WARPS * 32, 4) norm_columns_kernel(const _
     cg::cluster_group cluster = cg::this_cluster();
     const u32 blocks = cluster.num_blocks(), rank = cluster.block_rank();
     cluster.sync();
-    for (u32 c = rank * 256 + threadIdx.x; c < 512; c += blocks * 256) {
-        const u32 k = c / 256, col = base + c % 256;
+    for (u32 c = rank * 256 + threadIdx.x; c < 2 * SPAN; c += blocks * 256) {
+        const u32 k = c / SPAN, col = base + c % SPAN;
         float all = 0.f;
         for (u32 b = 0; b < blocks; ++b) all += *cluster.map_shared_rank(own + c, b);
         if (col >= g.cols) continue;
@@ -501,8 +651,47 @@ void norm_launch(cudaStream_t s, NormArgs<T> g, const Rows& r) {
     g.rows_log = log2_of(r.block / r.threads);
     launch_chained(norm_kernel<T, VEC, PIECES>, (u32)((g.rows + (1u << g.rows_log) - 1) >> g.rows_log), r.block, 0, 0, s, g);
 }
+// The kernels of many rows: four words to a thread (eight: 8192 x 4096 bf16 47 us against 27), as few threads as hold a row, or two
+// words where a warp holds it so.  False where they do not take it.
+template <typename T> constexpr int code_of() { return std::is_same<T, float>::value ? DT_F32 : std::is_same<T, __half>::value ? DT_F16 : DT_BF16; }
+constexpr u64 ROWS_COLS = 512 * PIECE * 4;
+template <typename T, int PIECES, int THREADS>
+void norm_rows_launch(cudaStream_t s, const NormArgs<T>& g) {
+    constexpr u32 block = rows_block(THREADS), per = block / THREADS;
+    const u32 blocks = (u32)((g.rows + per - 1) / per);
+    if (g.bias.p) launch_chained(norm_rows_kernel<T, PIECES, THREADS, 2>, blocks, block, 0, 0, s, g);
+    else launch_chained(norm_rows_kernel<T, PIECES, THREADS, 1>, blocks, block, 0, 0, s, g);
+}
+template <typename T>
+bool norm_rows(int sms, cudaStream_t s, const NormArgs<T>& g) {
+    if (g.rows <= (u64)sms * 4 || g.cols > ROWS_COLS || !g.weight.p || g.weight.dtype != code_of<T>() || (g.bias.p && g.bias.dtype != code_of<T>())) return false;
+    if (g.cols <= 32 * PIECE * 2) norm_rows_launch<T, 2, 32>(s, g);
+    else if (g.cols <= 32 * PIECE * 4) norm_rows_launch<T, 4, 32>(s, g);
+    else if (g.cols <= 64 * PIECE * 4) norm_rows_launch<T, 4, 64>(s, g);
+    else if (g.cols <= 128 * PIECE * 4) norm_rows_launch<T, 4, 128>(s, g);
+    else if (g.cols <= 256 * PIECE * 4) norm_rows_launch<T, 4, 256>(s, g);
+    else norm_rows_launch<T, 4, 512>(s, g);
+    return true;
+}
+template <typename T, bool KEPT, int PIECES, int THREADS>
+void dx_rows_launch(cudaStream_t s, const GradArgs<T>& g) {
+    constexpr u32 block = rows_block(THREADS), per = block / THREADS;
+    launch_chained(norm_dx_rows_kernel<T, KEPT, PIECES, THREADS>, (u32)((g.rows + per - 1) / per), block, 0, 0, s, g);
+}
+template <typename T, bool KEPT>
+bool dx_rows(int sms, cudaStream_t s, const GradArgs<T>& g) {
+    if (g.rows <= (u64)sms * 4 || g.cols > ROWS_COLS || !g.weight.p || g.weight.dtype != code_of<T>()) return false;
+    if (g.cols <= 32 * PIECE * 2) dx_rows_launch<T, KEPT, 2, 32>(s, g);
+    else if (g.cols <= 32 * PIECE * 4) dx_rows_launch<T, KEPT, 4, 32>(s, g);
+    else if (g.cols <= 64 * PIECE * 4) dx_rows_launch<T, KEPT, 4, 64>(s, g);
+    else if (g.cols <= 128 * PIECE * 4) dx_rows_launch<T, KEPT, 4, 128>(s, g);
+    else if (g.cols <= 256 * PIECE * 4) dx_rows_launch<T, KEPT, 4, 256>(s, g);
+    else dx_rows_launch<T, KEPT, 4, 512>(s, g);
+    return true;
+}
 template <typename T, bool VEC>
 void norm_as(int sms, cudaStream_t s, const NormArgs<T>& g) {
+    if constexpr (VEC) if (norm_rows<T>(sms, s, g)) return;
     const Rows r = rows_of(sms, g.rows, g.cols, 8, 128);
     if (r.pieces == 0) norm_launch<T, VEC, 0>(s, g, r);
     else if (r.pieces == 1) norm_launch<T, VEC, 1>(s, g, r);
@@ -533,7 +722,7 @@ bool deal_fused(int sms, u64 rows, u64 cols, Deal& d) {
 Deal deal_sums(int sms, u64 rows, u64 cols) {
     Deal d{};
     const u64 strips = (cols + 255) / 256, most = (rows + 2 * SUM_WARPS - 1) / (2 * SUM_WARPS);
-    u64 groups = (u64)sms * 4 / strips;            // no more than find room at once
+    u64 groups = (u64)sms * SUM_BLOCKS / strips;       // no more than find room at once
     if (groups > most) groups = most;
     if (groups < 1) groups = 1;
     d.cluster = cluster_of(groups);
@@ -571,7 +760,9 @@ void grad_as(int sms, cudaStream_t s, GradArgs<T> g, float* scratch) {
             g.groups = d.blocks;
             launch_chained(norm_columns_kernel<T, KEPT, VEC>, (g.cols + 255) / 256 * d.blocks, SUM_WARPS * 32, 0, d.cluster, s, g);
         }
-        if (g.dx) {
+        bool done = !g.dx;
+        if constexpr (VEC) done = done || dx_rows<T, KEPT>(sms, s, g);
+        if (!done) {
             const Rows r = rows_of(sms, g.rows, g.cols, 4, GROUP_MAX);
             if (r.pieces == 0) dx_launch<T, KEPT, VEC, 0>(s, g, r);
             else if (r.pieces == 1) dx_launch<T, KEPT, VEC, 1>(s, g, r);

@@ -109,6 +109,15 @@ struct Raw {
             }
         }
     }
+    // VEC: eight at p, or 0.
+    template <bool STREAM = true>
+    __device__ __forceinline__ void load_at(const T* p, bool there) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint4* w = reinterpret_cast<const uint4*>(p) + i;
+            q[i] = there ? (STREAM ? load_once(w) : __ldg(w)) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
     __device__ __forceinline__ void values(Eight& v) const {
         if constexpr (VEC) {
 #pragma unroll
@@ -126,17 +135,19 @@ __device__ __forceinline__ void load_cols(const T* row, u32 base, u32 lane, u32 
     r.template load<STREAM>(row, base, lane, cols);
     r.values(v);
 }
+template <typename T>
+__device__ __forceinline__ void store_eight(T* p, const Eight& v) {
+    uint4 q[sizeof(T) / 2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put_two<T>(reinterpret_cast<char*>(q) + i * 2 * sizeof(T), v[i]);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) __stcs(reinterpret_cast<uint4*>(p) + i, q[i]);
+}
 template <typename T, bool VEC>
 __device__ __forceinline__ void store_cols(T* row, u32 base, u32 lane, u32 cols, const Eight& v) {
     if constexpr (VEC) {
         const u32 c = base + lane * 8;
-        if (c < cols) {
-            uint4 q[sizeof(T) / 2];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) put_two<T>(reinterpret_cast<char*>(q) + i * 2 * sizeof(T), v[i]);
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) __stcs(reinterpret_cast<uint4*>(row + c) + i, q[i]);
-        }
+        if (c < cols) store_eight(row + c, v);
     } else {
 #pragma unroll
         for (u32 e = 0; e < 8; ++e) {
