@@ -468,9 +468,9 @@ excp_status excp_token_logprobs_grad(excp_handle h, const void* logits, int dtyp
  * themselves, held in 16 bits as excp_decompress_checkpoint_w16 leaves them; the norms before them; and the gradients of both, for
  * which activations can be kept in 8 bits.
  *
- * As the scoring calls, these only enqueue work and can be captured in a graph (of the products: after one ordinary call of a product on
- * the handle).  They use none of the handle's workspace but its flag: calls that are not ordered on the device may share a handle, though not
- * scratch.  `scratch` is device memory on 16 bytes, of what the call's _scratch function says (NULL where that is 0), and its contents
+ * As the scoring calls, these only enqueue work and can be captured in a graph (products after one ordinary product or scoring call on
+ * the handle, which allocates the word that their waits report to).  They use nothing else of the handle: calls that are not ordered on the
+ * device may share one, though not scratch.  `scratch` is device memory on 16 bytes, of what the call's _scratch function says (NULL where that is 0), and its contents
  * afterwards are unspecified.
  *
  * A matrix in these calls: `rows` rows of `cols` values, `row_stride` values apart (>= cols; of one row it is not looked at), aligned to

@@ -3,7 +3,9 @@
 //   blocks of 32 columns: A = max |x|, s = A / 127 rounded up to 8 significant bits, code = nearest whole number of x (1 / s)
 //   dpre = dy act'(pre), again = act(pre), dbias = sum over rows of dpre
 //
-// A warp takes 256 columns of a row, eight to a lane: a block is four lanes' (two shuffles find A).  Bound: the bytes.
+// A warp takes 256 columns of a row, eight to a lane: a block is four lanes' (two shuffles find A).
+// Bound: of values in 8 bits and back the bytes (4096 x 11008 bf16 28 us, 5.0 TB/s; back 30 us, 4.6 TB/s).  Of the gradient instructions: a
+// gelu and its slope are 13 of the 28 a value takes (4096 x 11008 bf16 from 8 bits, value again: 75 us, 4.2 TB/s; silu 63).
 #include <cooperative_groups.h>
 
 #include "layers.cuh"
