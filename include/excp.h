@@ -475,7 +475,8 @@ excp_status excp_token_logprobs_grad(excp_handle h, const void* logits, int dtyp
  *
  * A matrix in these calls: `rows` rows of `cols` values, `row_stride` values apart (>= cols; of one row it is not looked at), aligned to
  * its element.  Its type is an excp_dtype, or, where that is said, EXCP_ACT8: then `data` is a packed 8-bit matrix and the stride is not
- * looked at.  A null pointer to an optional matrix: absent.  Results may not overlap inputs, but where that is said. */
+ * looked at.  A null pointer to an optional matrix: absent.  Results may not overlap inputs, but where it is
+ * said that one may be the other: then both have the same type and stride. */
 typedef struct {
     void* data;
     int dtype;

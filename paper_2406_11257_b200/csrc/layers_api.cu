@@ -32,6 +32,10 @@ bool kept_ok(const excp_matrix* m) {
 bool optional_ok(const excp_matrix* m, const excp_matrix* of, int dtype) {
     return !m || (plain_ok(m) && same_shape(m, of) && (dtype < 0 || m->dtype == dtype));
 }
+// A result may take an input's place where that is said, but then value by value.
+bool in_place_ok(const excp_matrix* in, const excp_matrix* out) {
+    return !in || !out || empty(out) || in->data != out->data || (in->dtype == out->dtype && (out->rows == 1 || in->row_stride == out->row_stride));
+}
 bool vector_ok(const void* p, int dtype) { return !p || (dtype_ok(dtype) && on_element(p, dtype)); }
 bool act_ok(int act) { return act >= ACT_NONE && act <= ACT_SILU; }
 
@@ -107,7 +111,7 @@ size_t excp_act_grad_scratch(excp_handle h, size_t rows, size_t cols) { return h
 
 excp_status excp_act_grad(excp_handle h, int act, const excp_matrix* dy, const excp_matrix* pre, const excp_matrix* dpre_out, const excp_matrix* again_out,
                           float* dbias_out, void* scratch, void* cuda_stream) {
-    if (!h || !act_ok(act) || !plain_ok(dy) || !optional_ok(dpre_out, dy, dy->dtype) || !optional_ok(again_out, dy, dy->dtype) || !on_float(dbias_out))
+    if (!h || !act_ok(act) || !plain_ok(dy) || !optional_ok(dpre_out, dy, dy->dtype) || !optional_ok(again_out, dy, dy->dtype) || !in_place_ok(dy, dpre_out) || !on_float(dbias_out))
         return EXCP_ERR_INVALID_ARG;
     if (act == ACT_NONE) {
         if (pre || again_out) return EXCP_ERR_INVALID_ARG;
@@ -126,7 +130,7 @@ excp_status excp_act_grad(excp_handle h, int act, const excp_matrix* dy, const e
 
 excp_status excp_layer_norm(excp_handle h, const excp_matrix* x, const void* weight, const void* bias, int vector_dtype, float eps, int rms,
                             const excp_matrix* y_out, float* row_stats_out, void* kept_out, void* cuda_stream) {
-    if (!h || !plain_ok(x) || !plain_ok(y_out) || !same_shape(x, y_out) || x->dtype != y_out->dtype || !(eps >= 0.f) || eps > 1e30f ||
+    if (!h || !plain_ok(x) || !plain_ok(y_out) || !same_shape(x, y_out) || x->dtype != y_out->dtype || !in_place_ok(x, y_out) || !(eps >= 0.f) || eps > 1e30f ||
         !vector_ok(weight, vector_dtype) || !vector_ok(bias, vector_dtype) || ((weight || bias) && vector_dtype != EXCP_F32 && vector_dtype != x->dtype) ||
         (rms && bias) || !on8(row_stats_out) || !aligned16(kept_out))
         return EXCP_ERR_INVALID_ARG;
@@ -145,7 +149,7 @@ excp_status excp_layer_norm_grad(excp_handle h, const excp_matrix* dy, const exc
                                  void* cuda_stream) {
     if (!h || !plain_ok(dy) || !kept_ok(x) || !same_shape(x, dy) || (x->dtype != EXCP_ACT8 && x->dtype != dy->dtype) || !vector_ok(weight, vector_dtype) ||
         (weight && vector_dtype != EXCP_F32 && vector_dtype != dy->dtype) || !optional_ok(add, dy, dy->dtype) || !optional_ok(dx_out, dy, dy->dtype) ||
-        (add && !dx_out) || !on_float(dweight_out) || !on_float(dbias_out) || !on8(row_stats))
+        (add && !dx_out) || !in_place_ok(dy, dx_out) || !in_place_ok(add, dx_out) || !on_float(dweight_out) || !on_float(dbias_out) || !on8(row_stats))
         return EXCP_ERR_INVALID_ARG;
     if (dy->cols == 0) return EXCP_OK;
     DeviceGuard guard(h->device);
@@ -170,7 +174,7 @@ size_t excp_linear_scratch(const excp_matrix* a, const excp_matrix* b) {
 excp_status excp_linear(excp_handle h, const excp_matrix* x, const excp_matrix* w, const void* bias, int bias_dtype, int act, const excp_matrix* residual,
                         const excp_matrix* y_out, const excp_matrix* kept_out, void* scratch, void* cuda_stream) {
     if (!h || !operand_ok(x) || !operand_ok(w) || x->dtype != w->dtype || x->cols != w->cols || !plain_ok(y_out) || y_out->rows != x->rows ||
-        y_out->cols != w->rows || !vector_ok(bias, bias_dtype) || !act_ok(act) || !optional_ok(residual, y_out, -1) ||
+        y_out->cols != w->rows || !vector_ok(bias, bias_dtype) || !act_ok(act) || !optional_ok(residual, y_out, -1) || !in_place_ok(residual, y_out) ||
         (kept_out && (!kept_ok(kept_out) || !same_shape(kept_out, y_out))))
         return EXCP_ERR_INVALID_ARG;
     if (empty(y_out)) return EXCP_OK;
@@ -180,7 +184,7 @@ excp_status excp_linear(excp_handle h, const excp_matrix* x, const excp_matrix* 
 excp_status excp_linear_grad_input(excp_handle h, const excp_matrix* dy, const excp_matrix* w, const excp_matrix* add, const excp_matrix* dx_out, void* scratch,
                                    void* cuda_stream) {
     if (!h || !operand_ok(dy) || !operand_ok(w) || dy->dtype != w->dtype || dy->cols != w->rows || !plain_ok(dx_out) || dx_out->rows != dy->rows ||
-        dx_out->cols != w->cols || !optional_ok(add, dx_out, -1))
+        dx_out->cols != w->cols || !optional_ok(add, dx_out, -1) || !in_place_ok(add, dx_out))
         return EXCP_ERR_INVALID_ARG;
     if (empty(dx_out)) return EXCP_OK;
     return product(h, dy, true, w, false, ProductEnd{matrix(dx_out), ColumnVector{}, ACT_NONE, matrix(add), Matrix{}}, scratch, cuda_stream);
@@ -189,7 +193,7 @@ excp_status excp_linear_grad_input(excp_handle h, const excp_matrix* dy, const e
 excp_status excp_linear_grad_weight(excp_handle h, const excp_matrix* dy, const excp_matrix* x, const excp_matrix* add, const excp_matrix* dw_out, void* scratch,
                                     void* cuda_stream) {
     if (!h || !operand_ok(dy) || !operand_ok(x) || dy->dtype != x->dtype || dy->rows != x->rows || !plain_ok(dw_out) || dw_out->rows != dy->cols ||
-        dw_out->cols != x->cols || !optional_ok(add, dw_out, -1))
+        dw_out->cols != x->cols || !optional_ok(add, dw_out, -1) || !in_place_ok(add, dw_out))
         return EXCP_ERR_INVALID_ARG;
     if (empty(dw_out)) return EXCP_OK;
     return product(h, dy, false, x, false, ProductEnd{matrix(dw_out), ColumnVector{}, ACT_NONE, matrix(add), Matrix{}}, scratch, cuda_stream);

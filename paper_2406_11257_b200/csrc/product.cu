@@ -28,6 +28,11 @@ constexpr u32 BOXES_MAX = 2;                       // boxes of 64 columns in a s
 constexpr u32 MAX_SPLIT = 8;
 constexpr u32 M_BYTES = PR_TILE * PR_K * 2;
 constexpr u32 SMEM_MAX = 227 * 1024 - 1024;        // dynamic shared memory of a block, beside what the kernel has of its own
+// Tensor memory is given out without a limit on the wait, and a CTA that holds some waits for its cluster: two launches on two streams
+// whose CTAs held it from one another would wait for good.  So a CTA takes shared memory in proportion to its columns of tensor memory
+// (all of an SM's for 512), and never so little that it fits beside two CTAs of the 4-bit product, which take 256 columns each with 75 KB or
+// more: whatever finds room on an SM finds tensor memory.
+constexpr u32 SMEM_SM = 228 * 1024, SMEM_LEAST = 76 * 1024;
 
 struct NarrowArgs {
     CUtensorMap m, n;
@@ -80,7 +85,8 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
     const u32 k_steps = (g.k_boxes + g.boxes - 1) / g.boxes;
     const u32 k0 = (u32)((u64)k_steps * part / parts), k1 = (u32)((u64)k_steps * (part + 1) / parts);
     const u32 box = M_BYTES + g.n_bytes, stage = g.boxes * box;
-    const u32 run = max((k1 - k0 + g.runs - 1) / g.runs, 1u), runs = (k1 - k0 + run - 1) / run;      // stages of an accumulator, those in use
+    constexpr bool RUNS = DT == DT_F32;            // stages of an accumulator, accumulators in use
+    const u32 run = RUNS ? max((k1 - k0 + g.runs - 1) / g.runs, 1u) : k1 - k0, runs = RUNS ? (k1 - k0 + run - 1) / run : k1 > k0;
     const u64 n0 = (u64)ntile * g.nt, n_rows = g.turned ? g.end.rows : g.end.cols;
     const u32 cols = (u32)min((u64)g.nt, n_rows - n0);         // of the accumulator that are results
     // the CTA's own columns of the accumulator, and the others' parts of them: [part][column][row]
@@ -134,22 +140,29 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
         const u32 idesc = product_idesc(g.bf16, g.m_along_k, g.n_along_k, PR_TILE, g.nt);
         const u32 step_m = product_desc_step(g.m_along_k), step_n = product_desc_step(g.n_along_k);
         Turn ring;
+        u32 left = run, d = tmem, begun = 0;
         for (u32 k = k0; k < k1; ++k) {
             if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag)) break;
             const u32 st = smem_u32(smem) + ring.s * stage;
             const u64 dm = product_desc(st, g.m_along_k), dn = product_desc(st + M_BYTES, g.n_along_k);
-            const u32 which = (k - k0) / run, d = tmem + which * g.nt;
+            if (RUNS && left == 0) {               // the next accumulator
+                left = run;
+                d += g.nt;
+                begun = 0;
+            }
+            if (RUNS) --left;
             if (elect_one()) {
 #pragma unroll
                 for (u32 u = 0; u < BOXES_MAX; ++u) {
                     if (u >= g.boxes || k * g.boxes + u >= g.k_boxes) break;
 #pragma unroll
                     for (u32 i = 0; i < PR_K / 16; ++i)
-                        tm_mma_f16(d, dm + u * (box >> 4) + i * step_m, dn + u * (box >> 4) + i * step_n, idesc, k - k0 > which * run || u || i);
+                        tm_mma_f16(d, dm + u * (box >> 4) + i * step_m, dn + u * (box >> 4) + i * step_n, idesc, begun | u | i);
                 }
                 tm_commit(&sh.empty[ring.s]);
             }
             __syncwarp();
+            begun = 1;
             ring.next(g.stages);
         }
         if (elect_one()) tm_commit(&sh.done);
@@ -172,20 +185,26 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
         };
         auto take = [&](auto width, u32 c, float (&f)[decltype(width)::value]) {
             constexpr u32 W = decltype(width)::value;
-#pragma unroll
-            for (u32 e = 0; e < W; ++e) f[e] = 0.f;
-            for (u32 r = 0; r < runs; ++r) {
-                u32 v[W];
+            auto load = [&](u32 at, u32 (&v)[W]) {
                 __syncwarp();
                 if constexpr (W == 32) {
-                    tm_load32(lanes + r * g.nt + c, v);
+                    tm_load32(at, v);
                 } else {
 #pragma unroll
-                    for (u32 i = 0; i < W; i += 8) tm_load8(lanes + r * g.nt + c + i, v + i);
+                    for (u32 i = 0; i < W; i += 8) tm_load8(at + i, v + i);
                 }
                 tm_wait_load();
+            };
+            u32 v[W];
+            if (runs) load(lanes + c, v);
 #pragma unroll
-                for (u32 e = 0; e < W; ++e) f[e] += __uint_as_float(v[e]);
+            for (u32 e = 0; e < W; ++e) f[e] = runs ? __uint_as_float(v[e]) : 0.f;
+            if constexpr (RUNS) {
+                for (u32 r = 1; r < runs; ++r) {
+                    load(lanes + r * g.nt + c, v);
+#pragma unroll
+                    for (u32 e = 0; e < W; ++e) f[e] += __uint_as_float(v[e]);
+                }
             }
         };
         auto whole = [&](auto width) {
@@ -264,7 +283,7 @@ bool launch_as(cudaStream_t s, const NarrowArgs& g, u32 blocks, u32 parts, u32 s
 // How a product is cut: which operand is on which side, rows of n per CTA, CTAs that share the columns of a tile.
 struct Cut {
     bool turned;
-    u32 nt, parts, beside, boxes, stages, smem, ring_bytes, per_owner;
+    u32 nt, parts, boxes, stages, runs, tmem_cols, smem, ring_bytes, per_owner;
     float us;
 };
 
@@ -319,7 +338,7 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
             const u64 tiles = m_tiles * ((n.rows + want - 1) / want);
             const u32 n_bytes = n.along_k ? want * PR_K * 2 : (want + PR_CHUNK - 1) / PR_CHUNK * PR_CHUNK_BYTES;
             for (u32 parts = 1; parts <= MAX_SPLIT && (parts == 1 || (k_boxes >= parts && tiles * parts <= (u64)c.sms * 2)); ++parts) {
-                Cut cut{turned, want, parts, 1, BOXES_MAX, 0, 0, 0, 0, 0.f};
+                Cut cut{turned, want, parts, BOXES_MAX, 0, 1, 0, 0, 0, 0, 0.f};
                 cut.per_owner = (want + parts - 1) / parts;
                 if (!turned) cut.per_owner = (cut.per_owner + 31) & ~31u;
                 const u32 sums = parts > 1 ? parts * cut.per_owner * PR_TILE * 4 : 0, own = parts > 1 ? want * PR_TILE * 4 : 0;
@@ -329,8 +348,9 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
                 // Two CTAs to an SM where there are more than one each; two boxes of 64 columns to a stage (waiting for one and handing it back
                 // cost 250 cycles, whatever it holds), or one: the first of these that leaves enough stages.
                 bool two = false;
-                u32 stages = 0;
-                for (u32 way = tiles * parts > (u64)c.sms ? 0 : 2; way < 4; ++way) {
+                u32 stages = 0, wanted_runs = 1;   // of a result of 32 bits
+                while (c.end.y.dtype == DT_F32 && (k_boxes + parts - 1) / parts * PR_K > wanted_runs * PR_RUN) wanted_runs *= 2;
+                for (u32 way = tiles * parts > (u64)c.sms && want * wanted_runs <= 128 ? 0 : 2; way < 4; ++way) {
                     two = way < 2;
                     cut.boxes = way % 2 ? 1 : BOXES_MAX;
                     stages = room_for(two ? SMEM_MAX / 2 - 1024 : SMEM_MAX, cut.boxes);
@@ -344,6 +364,14 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
                 cut.ring_bytes = cut.stages * cut.boxes * box > own ? cut.stages * cut.boxes * box : own;
                 cut.smem = cut.ring_bytes + sums + 1024;
                 if (cut.smem > SMEM_MAX) continue;
+                while (cut.runs < wanted_runs && cut.runs * 2 * want <= 512) cut.runs *= 2;
+                if (cut.runs < wanted_runs && want > 16) continue;         // a smaller tile has room for more runs
+                cut.tmem_cols = 32;
+                while (cut.tmem_cols < want * cut.runs) cut.tmem_cols *= 2;
+                const u32 least = cut.tmem_cols >= 512 ? SMEM_MAX : cut.tmem_cols * (SMEM_SM / 512);
+                if (cut.smem < least) cut.smem = least;
+                if (cut.smem < SMEM_LEAST) cut.smem = SMEM_LEAST;
+                if (cut.smem > SMEM_MAX / 2 - 1024) two = false;
                 const u64 room = at_once(c.sms, parts, two ? 2 : 1), blocks = tiles * parts;
                 if (parts > 1 && blocks > room) continue;
                 const u64 per_sm = (blocks + c.sms - 1) / c.sms, turns = (blocks + room - 1) / room;
@@ -352,7 +380,6 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
                 const float whole = memory > 60e6f && blocks * 2 < (u64)c.sms * 3 ? 1.16f * memory / all : memory / all;
                 cut.us = 3.2f + fmaxf((float)turns * steps * step, whole) + (turns - 1) * 6.f +
                          (float)turns * want / parts * (turned ? 0.010f : 0.004f) + (parts > 1 ? 1.f + 0.25f * parts + 0.006f * want : 0.f);
-                cut.beside = two ? 2 : 1;
                 if (cut.us < best.us) best = cut;
             }
         }
@@ -368,7 +395,7 @@ Cut best_cut(const ProductCall& c, bool y_vec) {
         Cut cut;
     };
     thread_local Entry kept[32];
-    const u32 how = 1u | (c.a.along_k ? 2u : 0u) | (c.b.along_k ? 4u : 0u) | (y_vec ? 8u : 0u) | (u32)c.sms << 4;
+    const u32 how = 1u | (c.a.along_k ? 2u : 0u) | (c.b.along_k ? 4u : 0u) | (y_vec ? 8u : 0u) | (c.end.y.dtype == DT_F32 ? 16u : 0u) | (u32)c.sms << 5;
     Entry& e = kept[((c.a.rows * 31 + c.b.rows) * 31 + c.a.k * 7 + how) * 0x9e3779b97f4a7c15ull >> 59];
     if (e.how != how || e.a_rows != c.a.rows || e.b_rows != c.b.rows || e.k != c.a.k) e = Entry{c.a.rows, c.b.rows, c.a.k, how, find_cut(c, y_vec)};
     return e.cut;
@@ -389,13 +416,8 @@ bool launch_narrow(cudaStream_t s, const ProductCall& c, const EndArgs& end, con
     g.per_owner = cut.per_owner;
     g.stages = cut.stages;
     g.ring_bytes = cut.ring_bytes;
-    g.runs = 1;
-    if (c.end.y.dtype == DT_F32) {                 // as many runs as a CTA's tensor memory holds, a power of two of them
-        const u32 cols = (g.k_boxes + cut.parts - 1) / cut.parts * PR_K, room = cut.beside > 1 ? 256 : 512;
-        while (cols > g.runs * PR_RUN && (g.runs * 2) * g.nt <= room) g.runs *= 2;
-    }
-    g.tmem_cols = 32;
-    while (g.tmem_cols < g.nt * g.runs) g.tmem_cols *= 2;
+    g.runs = cut.runs;
+    g.tmem_cols = cut.tmem_cols;
     if (g.k_boxes && (!product_map(&g.m, m, PR_TILE, c.dtype) || !product_map(&g.n, n, g.nt, c.dtype))) return false;
     g.m_along_k = m.along_k;
     g.n_along_k = n.along_k;

@@ -30,7 +30,7 @@ constexpr u32 RUN = PR_RUN / PR_K;                 // stages
 constexpr int STAGES = 6;
 constexpr u32 SPAN = 2 * PR_TILE;                  // rows of m and of n per pair
 constexpr u32 HALF = PR_TILE * PR_K * 2, STAGE = 2 * HALF;
-constexpr u32 SMEM = STAGES * STAGE + 1024;
+constexpr u32 SMEM = STAGES * STAGE + 1024;        // no other CTA that uses tensor memory fits beside it (product.cu: why that matters)
 constexpr u32 GROUP = 16;                          // tiles of m that are visited before the next tile of n
 
 struct WideArgs {

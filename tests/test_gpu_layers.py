@@ -529,6 +529,8 @@ def test_refusals(h):
     y = make(4, 8, "bf16", 3)
     r = h.layer_norm(x)
     q = h.act8_quantize(x)
+    room = make(8, 100, "bf16", 9)
+    other = torch.as_strided(room, (4, 64), (90, 1))
     bad = [
         lambda: h.linear(x.float(), w.float()),                            # operands of 32 bits
         lambda: h.linear(x, w.half()),                                     # two types
@@ -562,6 +564,9 @@ def test_refusals(h):
         lambda: h.act8_quantize(x, out=torch.zeros(1000, dtype=torch.uint8, device=DEV)[1:]),
         lambda: h.act8_quantize(x.double()),
         lambda: h.act8_restore(binding.Act8Matrix(q.data, 8, 64)),
+        lambda: h.layer_norm(room[:4, :64], out=other),                    # one place, two strides
+        lambda: h.linear(x, w, residual=room[:4, :8], out=torch.as_strided(room, (4, 8), (90, 1))),
+        lambda: h.act_grad(room[:4, :64], x, "silu", out=other),
     ]
     for i, f in enumerate(bad):
         with pytest.raises((TypeError, binding.ExcpError)):
@@ -573,3 +578,40 @@ def test_refusals(h):
     with pytest.raises(ValueError):
         h.linear_kept(x, w, keep="fp8")
     torch.cuda.synchronize()
+
+
+def test_products_on_several_streams_at_once(h):
+    """Products of every kind (split over clusters, many runs of a 32-bit result, pairs of CTAs) and 4-bit ones, enqueued on four streams
+    that nothing orders: each gives what it gives alone."""
+    calls = []
+    for i, (rows, k, n) in enumerate(((4, 4096, 2000), (64, 4096, 1024), (200, 2048, 1024), (2304, 256, 2304), (333, 1000, 515))):
+        x, w, dy = make(rows, k, "bf16", i), make(n, k, "bf16", i + 10), make(rows, n, "bf16", i + 20)
+        q = h.mx4_quantize(w, "e8m0_32")
+        calls += [lambda x=x, w=w: h.linear(x, w, dtype=torch.float32), lambda dy=dy, w=w: h.linear_grad_input(dy, w), lambda dy=dy, x=x: h.linear_grad_weight(dy, x),
+                  lambda x=x, q=q: h.mx4_linear(x, q)]
+    alone = [f() for f in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    results = []
+    for turn in range(6):
+        for j, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                results.append([calls[(i * 7 + 5 * j + turn) % len(calls)]() for i in range(len(calls))])
+    torch.cuda.synchronize()
+    for t, r in enumerate(results):
+        for i, y in enumerate(r):
+            assert torch.equal(y, alone[(i * 7 + 5 * (t % 4) + t // 4) % len(calls)])
+    h.score_status()
+
+
+@pytest.mark.parametrize("k", [700, 3000, 9000])
+def test_long_sums_of_32_bits(h, k):
+    """The tensor core cuts sums off: in runs of 768 columns (and no fewer than 48 additions of 16) a sum loses no more than 48 times half
+    a unit of its running value on average, so the norm of the error stays below 2^-20 of the result's whatever the length."""
+    for m, n in ((2304, 2400), (300, 200), (8, 2000), (257, 130)):
+        dy, x = make(k, m, "bf16", 1), make(k, n, "bf16", 2)
+        want = dy.double().T @ x.double()
+        assert ((h.linear_grad_weight(dy, x).double() - want).norm() <= 2.0 ** -20 * want.norm())
+        a, b = make(m, k, "bf16", 3), make(n, k, "bf16", 4)
+        want = a.double() @ b.double().T
+        assert ((h.linear(a, b, dtype=torch.float32).double() - want).norm() <= 2.0 ** -20 * want.norm())
