@@ -487,7 +487,7 @@ typedef struct {
  * to 8 significant bits, and at least 2^-126.  A code is fl(x fl(1 / s)) rounded to the nearest whole number, ties to the even one, and
  * stands for code times s.  A block that holds a NaN or an infinity has the scale NaN and codes 0: all its values are NaN.
  * Packed, R rows and C columns with B = ceil(C / 32): R rows of 32 B codes (signed bytes; 0 past column C), then R rows of B scales as
- * bfloat16.  excp_act8_bytes: rounded up to 16 bytes; 0 for more than 2^30 rows or columns. */
+ * bfloat16.  excp_act8_bytes: rounded up to 16 bytes, of which no call reads or writes what follows the last scale; 0 for more than 2^30 rows or columns. */
 #define EXCP_ACT8 3
 size_t excp_act8_bytes(size_t rows, size_t cols);
 excp_status excp_act8_quantize(excp_handle h, const excp_matrix* x, void* packed_out, void* cuda_stream);

@@ -271,11 +271,13 @@ const excp_matrix* optional(PyObject* o, int device, const char* what, size_t r,
     room = shaped(tensor(o, what), device, what, r, c);
     return &room;
 }
+// What a matrix of 8 bits says: without the bytes behind its last scale, which no call reads.
+size_t act8_said(size_t r, size_t c) { return api.act8_bytes(r, c) ? r * ((c + 31) / 32) * 34 : 0; }
 // A plain matrix, or the data of a packed one of 8 bits (where `is_packed`).
 excp_matrix kept(PyObject* o, bool is_packed, int device, const char* what, size_t r, size_t c) {
     const at::Tensor& t = tensor(o, what);
     if (!is_packed) return shaped(t, device, what, r, c);
-    return excp_matrix{packed(t, device, api.act8_bytes(r, c), what), EXCP_ACT8, r, c, c};
+    return excp_matrix{packed(t, device, act8_said(r, c), what), EXCP_ACT8, r, c, c};
 }
 // One value per column, of type float32 or any 16-bit one.
 void* columns(PyObject* o, int device, int64_t n, int& dtype, const char* what) {
@@ -324,7 +326,7 @@ PyObject* act8_quantize(PyObject* const* a) {
 PyObject* act8_restore(PyObject* const* a) {
     const int device = (int)integer(a[1]);
     const long long r = integer(a[3]), c = integer(a[4]);
-    void* p = packed(tensor(a[2], "m"), device, api.act8_bytes(r, c), "m");
+    void* p = packed(tensor(a[2], "m"), device, act8_said(r, c), "m");
     const at::Tensor out = result(a[6], device, wanted(a[5]), r, c);
     const excp_matrix y = matrix(out, device, "out");
     check(api.act8_restore(handle(a[0]), p, &y, stream(device)), "excp_act8_restore");

@@ -91,6 +91,20 @@ def test_act8_and_back(h, rows, cols, dtype):
         assert torch.equal(wide[:, :cols].double(), values) and bool((wide[:, cols:] == 7).all())
 
 
+def test_act8_without_the_bytes_behind_the_last_scale(h):
+    """3 * 3 blocks are 306 bytes, of the 320 that a buffer is given: what says all of the values is taken as it is."""
+    x = make(3, 70, "bf16", 5)
+    data = lo.act8_pack(*lo.act8_codes(x))
+    assert data.numel() == 306 and binding.act8_bytes(3, 70) == 320
+    m = binding.Act8Matrix(data, 3, 70)
+    assert torch.equal(h.act8_restore(m, torch.float32).double(), lo.act8_round_trip(x))
+    whole = h.act8_quantize(x)
+    dy = make(3, 70, "bf16", 6)
+    assert torch.equal(h.act_grad(dy, m, act="gelu").dpre, h.act_grad(dy, whole, act="gelu").dpre)
+    with pytest.raises(TypeError):
+        h.act8_restore(binding.Act8Matrix(data[:305], 3, 70), torch.float32)
+
+
 def test_act8_extreme_values(h):
     g = torch.Generator().manual_seed(5)
     x = torch.randn(64, 320, generator=g) * torch.exp(torch.randn(64, 320, generator=g) * 25)
