@@ -6,8 +6,8 @@
 // tiles for the SMs the columns of a tile are split over a cluster: each CTA sends its part of the accumulator to the CTAs that own its
 // columns (bulk copies between their shared memories), which add the parts in a fixed order.
 //
-// 1 x 4096 -> 11008 bf16 18 us from memory, 16 x 2048 -> 50304 37 us (5.6 TB/s), 333 x 1000 -> 4097 9 us, 512 x 1024 -> 1024 5.5 us, one tile
-// alone 2.4 us.
+// 1 x 4096 -> 11008 bf16 18 us from memory, 16 x 2048 -> 50304 37 us (5.6 TB/s), 333 x 1000 -> 4097 9.3 us, 512 x 1024 -> 1024 5.6 us, one tile
+// alone 2.6 us.
 //
 // Roles: warps 0..3 fetch the operands (tensor maps; what lies past an edge comes as 0), warp 8 issues the products, and at the end
 // warps 0..7 write the result.
@@ -26,6 +26,7 @@ constexpr int BOUND_THREADS = 320;                 // 96 registers a thread: fiv
 constexpr int STAGES_MAX = 8;
 constexpr u32 BOXES_MAX = 2;                       // boxes of 64 columns in a stage
 constexpr u32 MAX_SPLIT = 8;
+constexpr u32 OUT_BYTES = 8192;                  // of a warp's results on their way out
 constexpr u32 M_BYTES = PR_TILE * PR_K * 2;
 constexpr u32 SMEM_MAX = 227 * 1024 - 1024;        // dynamic shared memory of a block, beside what the kernel has of its own
 // Tensor memory is given out without a limit on the wait, and a CTA that holds some waits for its cluster: two launches on two streams
@@ -35,14 +36,14 @@ constexpr u32 SMEM_MAX = 227 * 1024 - 1024;        // dynamic shared memory of a
 constexpr u32 SMEM_SM = 228 * 1024, SMEM_LEAST = 76 * 1024;
 
 struct NarrowArgs {
-    CUtensorMap m, n;
+    CUtensorMap m, n, y;                           // y: where lanes have rows and nothing is split
     u32 m_along_k, n_along_k, bf16;
     u32 k_boxes, n_tiles;
     u32 boxes;                                     // of a stage
     u32 nt;                                        // rows of n per CTA: a multiple of 16, at most 256
     u32 n_bytes, stages, tmem_cols;
     u32 runs;                                      // accumulators, nt columns of tensor memory each: the columns are split among them
-    u32 ring_bytes;                                // of the stages; afterwards the accumulator lies there
+    u32 ring_bytes;                                // of the stages; afterwards the accumulator lies there, or the results on their way out
     u32 per_owner;                                 // columns of the accumulator that a CTA of the cluster joins
     u32 turned;                                    // m is b: a lane has a column of c
     EndArgs end;
@@ -73,7 +74,7 @@ __device__ __forceinline__ void bulk_s2s(u32 to, const void* from, u32 bytes, u3
                  ::"r"(to), "r"(smem_u32(from)), "r"(bytes), "r"(bar) : "memory");
 }
 
-template <int DT>
+template <int DT, bool RUNS>
 __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_constant__ NarrowArgs g) {
     extern __shared__ unsigned char smem_raw[];
     __shared__ Shared sh;
@@ -85,7 +86,7 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
     const u32 k_steps = (g.k_boxes + g.boxes - 1) / g.boxes;
     const u32 k0 = (u32)((u64)k_steps * part / parts), k1 = (u32)((u64)k_steps * (part + 1) / parts);
     const u32 box = M_BYTES + g.n_bytes, stage = g.boxes * box;
-    constexpr bool RUNS = DT == DT_F32;            // stages of an accumulator, accumulators in use
+    // stages of an accumulator, accumulators in use
     const u32 run = RUNS ? max((k1 - k0 + g.runs - 1) / g.runs, 1u) : k1 - k0, runs = RUNS ? (k1 - k0 + run - 1) / run : k1 > k0;
     const u64 n0 = (u64)ntile * g.nt, n_rows = g.turned ? g.end.rows : g.end.cols;
     const u32 cols = (u32)min((u64)g.nt, n_rows - n0);         // of the accumulator that are results
@@ -178,11 +179,7 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
         const float bias = g.turned ? column_bias(g.end, m) : 0.f;
         const bool ok = wait_warp(&sh, &sh.done, 0, g.wait_ns, g.flag);
         tm_fence_after();
-        auto put = [&](auto width, u32 c, u32 count, float (&f)[decltype(width)::value]) {     // columns c .. of the tile, complete
-            constexpr u32 W = decltype(width)::value;
-            if (g.turned) end_column<DT, W>(g.end, n0 + c, m, min(W, count), bias, f);
-            else if constexpr (W == 32) end_row<DT>(g.end, m, n0 + c, f);
-        };
+        u32 turn = 0;
         auto take = [&](auto width, u32 c, float (&f)[decltype(width)::value]) {
             constexpr u32 W = decltype(width)::value;
             auto load = [&](u32 at, u32 (&v)[W]) {
@@ -207,12 +204,13 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
                 }
             }
         };
-        auto whole = [&](auto width) {
+        auto whole = [&](auto width) {            // 32 columns at a time where lanes have rows of y
             constexpr u32 W = decltype(width)::value;
             for (u32 c = half * W; c < cols; c += 2 * W) {
                 float f[W];
                 take(width, c, f);
-                put(width, c, cols - c, f);
+                if constexpr (W == 32) end_rows<DT, OUT_BYTES>(g.end, &g.y, smem + warp * OUT_BYTES, turn, m, n0 + c, f);
+                else end_column<DT, W>(g.end, n0 + c, m, min(W, cols - c), bias, f);
             }
         };
         auto send = [&](auto width) {              // the accumulator to shared memory
@@ -236,7 +234,8 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
                         f[e] = p ? f[e] + v : v;
                     }
                 }
-                put(width, own + c, own_cols - c, f);
+                if constexpr (W == 32) end_row<DT>(g.end, m, n0 + own + c, f);
+                else end_column<DT, W>(g.end, n0 + own + c, m, min(W, own_cols - c), bias, f);
             }
         };
         if (parts == 1) {
@@ -261,6 +260,7 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
             if (!g.turned) join(std::integral_constant<u32, 32>());
             else join(std::integral_constant<u32, 8>());
         }
+        end_rows_done();
         tm_fence_before();
     }
     __syncwarp();
@@ -273,11 +273,11 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
     if (warp == PRODUCT_WARP) tm_dealloc(tmem, g.tmem_cols);
 }
 
-template <int DT>
+template <int DT, bool RUNS>
 bool launch_as(cudaStream_t s, const NarrowArgs& g, u32 blocks, u32 parts, u32 smem) {
     static std::atomic<u64> allowed{0};
-    if (!allow_smem(product_kernel<DT>, allowed, SMEM_MAX)) return false;
-    return launch_chained(product_kernel<DT>, blocks, THREADS, smem, parts, s, g);
+    if (!allow_smem(product_kernel<DT, RUNS>, allowed, SMEM_MAX)) return false;
+    return launch_chained(product_kernel<DT, RUNS>, blocks, THREADS, smem, parts, s, g);
 }
 
 // How a product is cut: which operand is on which side, rows of n per CTA, CTAs that share the columns of a tile.
@@ -296,7 +296,7 @@ u32 at_once(int sms, u32 parts, u32 beside) {
     if (n) return n * beside;
     static std::atomic<u64> allowed{0};
     int clusters = 0;
-    if (allow_smem(product_kernel<DT_F32>, allowed, SMEM_MAX)) {
+    if (allow_smem(product_kernel<DT_F32, true>, allowed, SMEM_MAX)) {
         cudaLaunchConfig_t cfg{};
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
@@ -307,7 +307,7 @@ u32 at_once(int sms, u32 parts, u32 beside) {
         cfg.dynamicSmemBytes = SMEM_MAX;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        if (cudaOccupancyMaxActiveClusters(&clusters, product_kernel<DT_F32>, &cfg) != cudaSuccess) {
+        if (cudaOccupancyMaxActiveClusters(&clusters, product_kernel<DT_F32, true>, &cfg) != cudaSuccess) {
             cudaGetLastError();
             clusters = 0;
         }
@@ -341,15 +341,15 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
                 Cut cut{turned, want, parts, BOXES_MAX, 0, 1, 0, 0, 0, 0, 0.f};
                 cut.per_owner = (want + parts - 1) / parts;
                 if (!turned) cut.per_owner = (cut.per_owner + 31) & ~31u;
-                const u32 sums = parts > 1 ? parts * cut.per_owner * PR_TILE * 4 : 0, own = parts > 1 ? want * PR_TILE * 4 : 0;
+                const u32 sums = parts > 1 ? parts * cut.per_owner * PR_TILE * 4 : 0, own = parts > 1 ? want * PR_TILE * 4 : turned ? 0 : WORK_WARPS * OUT_BYTES;
                 const u32 box = M_BYTES + n_bytes;
                 auto room_for = [&](u32 room, u32 boxes) { return room > sums + 1024 ? (room - sums - 1024) / (box * boxes) : 0u; };
                 auto steps_of = [&](u32 boxes) { return (k_boxes + boxes - 1) / boxes / parts + ((k_boxes + boxes - 1) / boxes % parts != 0); };
                 // Two CTAs to an SM where there are more than one each; two boxes of 64 columns to a stage (waiting for one and handing it back
                 // cost 250 cycles, whatever it holds), or one: the first of these that leaves enough stages.
                 bool two = false;
-                u32 stages = 0, wanted_runs = 1;   // of a result of 32 bits
-                while (c.end.y.dtype == DT_F32 && (k_boxes + parts - 1) / parts * PR_K > wanted_runs * PR_RUN) wanted_runs *= 2;
+                u32 stages = 0, wanted_runs = 1;
+                while ((u64)((k_boxes + parts - 1) / parts) * PR_K > (u64)wanted_runs * product_run(c.end)) wanted_runs *= 2;
                 for (u32 way = tiles * parts > (u64)c.sms && want * wanted_runs <= 128 ? 0 : 2; way < 4; ++way) {
                     two = way < 2;
                     cut.boxes = way % 2 ? 1 : BOXES_MAX;
@@ -395,7 +395,7 @@ Cut best_cut(const ProductCall& c, bool y_vec) {
         Cut cut;
     };
     thread_local Entry kept[32];
-    const u32 how = 1u | (c.a.along_k ? 2u : 0u) | (c.b.along_k ? 4u : 0u) | (y_vec ? 8u : 0u) | (c.end.y.dtype == DT_F32 ? 16u : 0u) | (u32)c.sms << 5;
+    const u32 how = 1u | (c.a.along_k ? 2u : 0u) | (c.b.along_k ? 4u : 0u) | (y_vec ? 8u : 0u) | (product_run(c.end) == PR_RUN ? 16u : product_run(c.end) == PR_RUN_KEPT ? 32u : 0u) | (u32)c.sms << 6;
     Entry& e = kept[((c.a.rows * 31 + c.b.rows) * 31 + c.a.k * 7 + how) * 0x9e3779b97f4a7c15ull >> 59];
     if (e.how != how || e.a_rows != c.a.rows || e.b_rows != c.b.rows || e.k != c.a.k) e = Entry{c.a.rows, c.b.rows, c.a.k, how, find_cut(c, y_vec)};
     return e.cut;
@@ -419,15 +419,20 @@ bool launch_narrow(cudaStream_t s, const ProductCall& c, const EndArgs& end, con
     g.runs = cut.runs;
     g.tmem_cols = cut.tmem_cols;
     if (g.k_boxes && (!product_map(&g.m, m, PR_TILE, c.dtype) || !product_map(&g.n, n, g.nt, c.dtype))) return false;
+    if (!g.turned && cut.parts == 1 && !result_map(&g.y, c.end.y)) return false;
     g.m_along_k = m.along_k;
     g.n_along_k = n.along_k;
     g.bf16 = c.dtype == DT_BF16;
     g.wait_ns = c.wait_ns;
     g.flag = c.flag;
     const u32 blocks = (u32)(m_tiles * g.n_tiles) * cut.parts;
-    return c.end.y.dtype == DT_F32 ? launch_as<DT_F32>(s, g, blocks, cut.parts, cut.smem)
-         : c.end.y.dtype == DT_F16 ? launch_as<DT_F16>(s, g, blocks, cut.parts, cut.smem)
-                                   : launch_as<DT_BF16>(s, g, blocks, cut.parts, cut.smem);
+    auto launch = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if constexpr (DT != DT_F32) if (cut.runs == 1) return launch_as<DT, false>(s, g, blocks, cut.parts, cut.smem);
+        return launch_as<DT, true>(s, g, blocks, cut.parts, cut.smem);
+    };
+    return c.end.y.dtype == DT_F32 ? launch(std::integral_constant<int, DT_F32>()) : c.end.y.dtype == DT_F16 ? launch(std::integral_constant<int, DT_F16>())
+                                                                                                           : launch(std::integral_constant<int, DT_BF16>());
 }
 
 // Eight values of a row at a time: 16 bytes of the result, cut out of the two aligned words that hold them.
@@ -465,7 +470,8 @@ void launch_tidy(int sms, cudaStream_t s, const Matrix& m, void* to) {
                    static_cast<unsigned short*>(to), pitch);
 }
 
-bool product_map(CUtensorMap* map, const ProductOperand& o, u32 box_rows, int dtype) {
+namespace {
+bool encode_map(CUtensorMap* map, CUtensorMapDataType type, const void* p, u64 inner, u64 outer, u64 pitch, u32 box_inner, u32 box_outer, CUtensorMapSwizzle swizzle) {
     static const auto encode = [] {
         void* f = nullptr;
         cudaDriverEntryPointQueryResult found;
@@ -473,10 +479,23 @@ bool product_map(CUtensorMap* map, const ProductOperand& o, u32 box_rows, int dt
         return reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(f);
     }();
     if (!encode) return false;
-    const cuuint64_t dims[2] = {o.along_k ? o.k : o.rows, o.along_k ? o.rows : o.k}, strides[1] = {o.stride * 2};
-    const cuuint32_t box[2] = {PR_K, o.along_k ? box_rows : PR_K}, one[2] = {1, 1};
-    return encode(map, dtype == DT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(o.p), dims, strides, box, one,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t dims[2] = {inner, outer}, strides[1] = {pitch};
+    const cuuint32_t box[2] = {box_inner, box_outer}, one[2] = {1, 1};
+    return encode(map, type, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+CUtensorMapDataType map_type(int dtype) {
+    return dtype == DT_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == DT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+}
+}  // namespace
+
+bool product_map(CUtensorMap* map, const ProductOperand& o, u32 box_rows, int dtype) {
+    return encode_map(map, map_type(dtype), o.p, o.along_k ? o.k : o.rows, o.along_k ? o.rows : o.k, o.stride * 2, PR_K, o.along_k ? box_rows : PR_K, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+bool result_map(CUtensorMap* map, const Matrix& y) {
+    const u64 size = y.dtype == DT_F32 ? 4 : 2, pitch = y.rows == 1 ? (y.cols * size + 15) & ~15ull : y.stride * size;
+    return encode_map(map, map_type(y.dtype), y.p, y.cols, y.rows, pitch, 32, 32, size == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 EndArgs end_args(const ProductEnd& e) {

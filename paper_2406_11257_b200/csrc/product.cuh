@@ -14,6 +14,10 @@ constexpr u32 PR_K = 64;                           // columns of a box: 128 byte
 // 4e-6, which shows in a result of 32 bits.  There the columns are added up in runs of at most about so many, and the runs' sums in
 // fp32: 7e-7 whatever the length.  (Runs of 512: 5e-7, and 4096 x 4096 x 11008 294 us against 270.)
 constexpr u32 PR_RUN = 768;
+// It shows less in codes of 8 bits: after 4096 columns seven times as many land on the other side of a border as of a plain fp32 sum, and the
+// kept values of fp16 activations are 1.7 times as far off.  Runs of 2048 columns leave 1.2 times.
+// Not shorter: while a tile with 8 bits and a gelu is written out the products can go on for two runs only.
+constexpr u32 PR_RUN_KEPT = 2048;
 constexpr u32 PR_CHUNK = 64;                       // rows of a box of an operand that lies the other way round
 constexpr u32 PR_CHUNK_BYTES = PR_CHUNK * PR_K * 2;
 
@@ -34,6 +38,12 @@ struct ProductEnd {
     Matrix kept;                                   // p null: none
 };
 
+// Columns of a run: results of 16 bits have one.  What is kept in 32 bits has the sums of what is kept in 8.
+inline u32 product_run(const ProductEnd& e) {
+    if (e.y.dtype == DT_F32) return PR_RUN;
+    return e.kept.p && (e.kept.dtype == DT_ACT8 || e.kept.dtype == DT_F32) ? PR_RUN_KEPT : ~0u;
+}
+
 struct ProductCall {
     ProductOperand a, b;
     ProductEnd end;
@@ -52,6 +62,8 @@ void launch_tidy(int sms, cudaStream_t s, const Matrix& m, void* to);
 
 // A map of an operand in boxes of `box_rows` rows (64 where the rows are neighbours) and PR_K columns.
 bool product_map(CUtensorMap* map, const ProductOperand& o, u32 box_rows, int dtype);
+// A map of a result whose rows start on 16 bytes, in boxes of 32 x 32 (end_rows).
+bool result_map(CUtensorMap* map, const Matrix& y);
 
 // The epilogue as the kernels take it.
 struct EndArgs {
@@ -174,12 +186,8 @@ __device__ __forceinline__ void add_row(const T* r, float (&f)[W], u32 n, bool o
     }
 }
 
-// 32 neighbouring sums of row i, columns j ..
-template <int DT>
-__device__ __forceinline__ void end_row(const EndArgs& g, u64 i, u64 j, float (&f)[32]) {
-    typedef typename ElemOf<DT>::type T;
-    if (i >= g.rows || j >= g.cols) return;
-    const u32 n = (u32)min((u64)32, g.cols - j);
+// 32 neighbouring sums of row i, columns j .. j + n - 1: all but the way of y to memory.
+__device__ __forceinline__ void end_values(const EndArgs& g, u64 i, u64 j, u32 n, float (&f)[32]) {
     if (g.bias) {
         if (g.bias_dtype == DT_F32) add_row(static_cast<const float*>(g.bias) + j, f, n, g.bias_vec);
         else if (g.bias_dtype == DT_F16) add_row(static_cast<const __half*>(g.bias) + j, f, n, g.bias_vec);
@@ -211,7 +219,53 @@ __device__ __forceinline__ void end_row(const EndArgs& g, u64 i, u64 j, float (&
         else if (g.residual_dtype == DT_F16) add_row(static_cast<const __half*>(g.residual) + at, f, n, g.residual_vec);
         else add_row(static_cast<const __nv_bfloat16*>(g.residual) + at, f, n, g.residual_vec);
     }
+}
+// The same with y, a lane by itself.
+template <int DT>
+__device__ __forceinline__ void end_row(const EndArgs& g, u64 i, u64 j, float (&f)[32]) {
+    typedef typename ElemOf<DT>::type T;
+    if (i >= g.rows || j >= g.cols) return;
+    const u32 n = (u32)min((u64)32, g.cols - j);
+    end_values(g, i, j, n, f);
     put_row(static_cast<T*>(g.y) + i * g.stride + j, f, n, g.y_vec);
+}
+// The same of a warp's 32 rows, which a copy takes to memory (rows past the last stay behind; of a row it writes whole 16-byte words, past the
+// last column too, so that fewer than 32 columns are left to the lanes).  Lanes that each write 32 bytes of a row of
+// their own send 17 bytes a cycle from an SM, whole lines several times that: 16 x 2048 -> 50304, the weight
+// gradient in 32 bits: 128 us, so 82.
+// `room`: BYTES of shared memory of the warp on 1024 bytes, `turn`: how often it was used.  Before the CTA leaves: end_rows_done.
+template <int DT, u32 BYTES>
+__device__ __forceinline__ void end_rows(const EndArgs& g, const CUtensorMap* map, unsigned char* room, u32& turn, u64 i, u64 j, float (&f)[32]) {
+    typedef typename ElemOf<DT>::type T;
+    constexpr u32 LINE = 32 * sizeof(T), BOX = 32 * LINE, ROOMS = BYTES / BOX, PER = 4 / sizeof(T);
+    const u32 lane = threadIdx.x & 31;
+    if (i - lane >= g.rows || j >= g.cols) return;             // the warp as one
+    const u32 n = (u32)min((u64)32, g.cols - j);
+    if (i < g.rows) end_values(g, i, j, n, f);
+    if (n < 32) {
+        if (i < g.rows) put_row(static_cast<T*>(g.y) + i * g.stride + j, f, n, g.y_vec);
+        return;
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(ROOMS - 1) : "memory");
+    __syncwarp();
+    unsigned char* to = room + turn++ % ROOMS * BOX;
+    const u32 turned = LINE == 128 ? lane & 7 : lane >> 1 & 3; // the swizzle of a row's 16-byte words
+#pragma unroll
+    for (u32 c = 0; c < LINE / 16; ++c)
+        *reinterpret_cast<uint4*>(to + lane * LINE + ((c ^ turned) << 4)) =
+            make_uint4(word_of<T>(f + c * 4 * PER), word_of<T>(f + (c * 4 + 1) * PER), word_of<T>(f + (c * 4 + 2) * PER), word_of<T>(f + (c * 4 + 3) * PER));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");           // the copy reads what was just written
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+                     ::"l"(map), "r"((u32)j), "r"((u32)i), "r"(smem_u32(to)) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+    __syncwarp();
+}
+__device__ __forceinline__ void end_rows_done() {
+    if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    __syncwarp();
 }
 
 // The bias of a column, for end_column.

@@ -20,23 +20,24 @@ namespace {
 constexpr int STORE_WARPS = 8;
 constexpr u32 FETCH_WARPS = 2;                     // per operand, every other stage
 constexpr u32 FETCH_WARP = STORE_WARPS, PRODUCT_WARP = FETCH_WARP + 2 * FETCH_WARPS;
-// Where the result has 32 bits the store warps hold the sum of the runs, 128 columns a thread: they take the registers that the others (and
+// Where sums are taken in runs the store warps hold the sum of the runs, 128 columns a thread: they take the registers that the others (and
 // three warps that do nothing) do without.
-template <int DT> __host__ __device__ constexpr bool in_runs() { return DT == DT_F32; }
-template <int DT> __host__ __device__ constexpr int threads() { return in_runs<DT>() ? 512 : (int)(PRODUCT_WARP + 1) * 32; }
+template <bool RUNS> __host__ __device__ constexpr int threads() { return RUNS ? 512 : (int)(PRODUCT_WARP + 1) * 32; }
 constexpr int UP = 200, DOWN = 56;                 // registers a thread, of 128 at launch
 static_assert(256 * UP + 256 * DOWN <= 512 * 128, "registers");
-constexpr u32 RUN = PR_RUN / PR_K;                 // stages
 constexpr int STAGES = 6;
 constexpr u32 SPAN = 2 * PR_TILE;                  // rows of m and of n per pair
 constexpr u32 HALF = PR_TILE * PR_K * 2, STAGE = 2 * HALF;
-constexpr u32 SMEM = STAGES * STAGE + 1024;        // no other CTA that uses tensor memory fits beside it (product.cu: why that matters)
+constexpr u32 OUT_BYTES = 4096;                    // of a warp's results on their way out
+constexpr u32 SMEM = STAGES * STAGE + STORE_WARPS * OUT_BYTES + 1024;        // no other CTA that uses tensor memory fits beside it (product.cu: why that matters)
 constexpr u32 GROUP = 16;                          // tiles of m that are visited before the next tile of n
 
 struct WideArgs {
     CUtensorMap m, n;                              // on the M side (lanes of tensor memory) and the N side (columns)
+    CUtensorMap y;                                 // not where they change places
     u32 m_along_k, n_along_k, bf16;
     u32 k_tiles, m_tiles, n_tiles;
+    u32 run;                                       // stages
     // Usually a is m: a lane has a row of c.  Where rows of y do not start on 16 bytes the operands change places: a lane has a column,
     // and neighbouring lanes write neighbouring results.
     u32 turned;
@@ -63,8 +64,8 @@ __device__ __forceinline__ void place(const WideArgs& g, u32 t, u32& mt, u32& nt
     mt = group * GROUP + inside - nt * rows;
 }
 
-template <int DT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<DT>(), 1) wide_product_kernel(const __grid_constant__ WideArgs g) {
+template <int DT, bool RUNS>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<RUNS>(), 1) wide_product_kernel(const __grid_constant__ WideArgs g) {
     constexpr u32 TMEM_COLS = 512;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Shared sh;
@@ -93,9 +94,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<DT>(), 1) wi
     tm_fence_after();
     const u32 tmem = sh.tmem;
     // stages that are added up in one accumulator
-    const u32 run = in_runs<DT>() ? RUN : g.k_tiles;
+    const u32 run = RUNS ? g.run : g.k_tiles;
     if (warp >= FETCH_WARP && warp < PRODUCT_WARP) {
-        if constexpr (in_runs<DT>()) registers_down<DOWN>();
+        if constexpr (RUNS) registers_down<DOWN>();
         const bool is_n = warp >= FETCH_WARP + FETCH_WARPS;
         const CUtensorMap* map = is_n ? &g.n : &g.m;
         const bool along_k = is_n ? g.n_along_k : g.m_along_k;
@@ -131,7 +132,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<DT>(), 1) wi
             drain_warp(&sh.full[ring.s], ring.parity);
         }
     } else if (warp >= PRODUCT_WARP) {
-        if constexpr (in_runs<DT>()) registers_down<DOWN>();
+        if constexpr (RUNS) registers_down<DOWN>();
         if (warp > PRODUCT_WARP) {                 // nothing
         } else if (rank == 0) {
             const u32 idesc = product_idesc(g.bf16, g.m_along_k, g.n_along_k, SPAN, SPAN);
@@ -180,14 +181,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<DT>(), 1) wi
             }
         }
     } else {
-        if constexpr (in_runs<DT>()) registers_up<UP>();
+        if constexpr (RUNS) registers_up<UP>();
         const u32 quarter = warp & 3, c0 = (warp >> 2) * PR_TILE;          // a warp reads the tensor-memory lanes of its place
         const u32 lanes = tmem + ((quarter * 32) << 16) + c0;
         const u64 n_rows = g.turned ? g.end.rows : g.end.cols;
+        u32 out = 0;
         auto put = [&](u64 m, u64 n, float bias, float (&f)[32]) {         // 32 neighbouring columns of the accumulator
             if (n >= n_rows) return;
             if (g.turned) end_column<DT, 32>(g.end, n, m, (u32)min((u64)32, n_rows - n), bias, f);
-            else end_row<DT>(g.end, m, n, f);
+            else end_rows<DT, OUT_BYTES>(g.end, &g.y, smem + STAGES * STAGE + warp * OUT_BYTES, out, m, n, f);
         };
         auto release = [&](u32 b) {                // the accumulator is free again
             tm_fence_before();
@@ -202,7 +204,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<DT>(), 1) wi
             place(g, t, mt, nt);
             const u64 m = (u64)(2 * mt + rank) * PR_TILE + quarter * 32 + lane, n0 = (u64)nt * SPAN + c0;
             const float bias = g.turned ? column_bias(g.end, m) : 0.f;
-            if constexpr (in_runs<DT>()) {
+            if constexpr (RUNS) {
                 float sum[PR_TILE];
 #pragma unroll
                 for (u32 e = 0; e < PR_TILE; ++e) sum[e] = 0.f;
@@ -223,11 +225,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<DT>(), 1) wi
                     release(b);
                 }
                 if (!ok) break;
-#pragma unroll
+                // the sums move up instead of the loop being unrolled: four epilogues are more than the instruction cache holds
+#pragma unroll 1
                 for (u32 p = 0; p < PR_TILE; p += 32) {
                     float f[32];
 #pragma unroll
-                    for (u32 e = 0; e < 32; ++e) f[e] = sum[p + e];
+                    for (u32 e = 0; e < 32; ++e) f[e] = sum[e];
+#pragma unroll
+                    for (u32 e = 0; e + 32 < PR_TILE; ++e) sum[e] = sum[e + 32];
                     put(m, n0 + p, bias, f);
                 }
             } else {
@@ -250,6 +255,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<DT>(), 1) wi
                 }
             }
         }
+        end_rows_done();
     }
     __syncwarp();
     tm_fence_before();
@@ -260,13 +266,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads<DT>(), 1) wi
     if (warp == PRODUCT_WARP) tm2_dealloc(tmem, TMEM_COLS);
 }
 
-template <int DT>
+template <int DT, bool RUNS>
 bool launch_as(int sms, cudaStream_t s, const WideArgs& g) {
     static std::atomic<u64> allowed{0};
-    if (!allow_smem(wide_product_kernel<DT>, allowed, SMEM)) return false;
+    if (!allow_smem(wide_product_kernel<DT, RUNS>, allowed, SMEM)) return false;
     const u64 tiles = (u64)g.m_tiles * g.n_tiles;
     const u32 pairs = (u32)(tiles < (u64)(sms / 2) ? tiles : (u64)(sms / 2));
-    return launch_chained(wide_product_kernel<DT>, pairs * 2, threads<DT>(), SMEM, 0, s, g);
+    return launch_chained(wide_product_kernel<DT, RUNS>, pairs * 2, threads<RUNS>(), SMEM, 0, s, g);
 }
 
 }  // namespace
@@ -286,15 +292,24 @@ bool launch_product_wide(cudaStream_t s, const ProductCall& c) {
     const ProductOperand& m = g.turned ? c.b : c.a;
     const ProductOperand& n = g.turned ? c.a : c.b;
     if (!product_map(&g.m, m, PR_TILE, c.dtype) || !product_map(&g.n, n, PR_TILE, c.dtype)) return false;
+    if (!g.turned && !result_map(&g.y, c.end.y)) return false;
     g.m_along_k = m.along_k;
     g.n_along_k = n.along_k;
     g.bf16 = c.dtype == DT_BF16;
     g.k_tiles = (u32)((m.k + PR_K - 1) / PR_K);
+    const u32 stages = product_run(c.end) / PR_K, runs = g.k_tiles / stages + (g.k_tiles % stages != 0);
+    g.run = (g.k_tiles + runs - 1) / runs;
     g.m_tiles = (u32)((m.rows + SPAN - 1) / SPAN);
     g.n_tiles = (u32)((n.rows + SPAN - 1) / SPAN);
     g.wait_ns = c.wait_ns;
     g.flag = c.flag;
-    return c.end.y.dtype == DT_F32 ? launch_as<DT_F32>(c.sms, s, g) : c.end.y.dtype == DT_F16 ? launch_as<DT_F16>(c.sms, s, g) : launch_as<DT_BF16>(c.sms, s, g);
+    auto launch = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if constexpr (DT != DT_F32) if (runs == 1) return launch_as<DT, false>(c.sms, s, g);
+        return launch_as<DT, true>(c.sms, s, g);
+    };
+    return c.end.y.dtype == DT_F32 ? launch(std::integral_constant<int, DT_F32>()) : c.end.y.dtype == DT_F16 ? launch(std::integral_constant<int, DT_F16>())
+                                                                                                           : launch(std::integral_constant<int, DT_BF16>());
 }
 
 }  // namespace excp
