@@ -629,3 +629,35 @@ def test_long_sums_of_32_bits(h, k):
         a, b = make(m, k, "bf16", 3), make(n, k, "bf16", 4)
         want = a.double() @ b.double().T
         assert ((h.linear(a, b, dtype=torch.float32).double() - want).norm() <= 2.0 ** -20 * want.norm())
+
+
+@pytest.mark.parametrize("k", [3000, 9000])
+def test_long_sums_of_what_is_kept(h, k):
+    """Kept in 32 bits or 8 beside a result of 16: runs of 2048 columns, 128 additions of 16, lose 128 / 48 times what those above do.  A
+    code is another where its value lies no further from a border than that: at most twice the error over a step (A / 127, and A is
+    above the root of the block's mean square) of all codes.  A block's codes are others where its scale is: A that close to where the
+    scale takes its next value, 2^-8 further."""
+    off = 128 / 48 * 2.0 ** -20
+    for m, n in ((2304, 2400), (300, 200), (8, 2000), (257, 130)):
+        x, w = make(m, k, "fp16", 3), make(n, k, "fp16", 4, size=0.02)
+        want = x.double() @ w.double().T
+        y, kept = h.linear_kept(x, w, keep=torch.float32)
+        assert ((kept.double() - want).norm() <= off * want.norm())
+        again, packed = h.linear_kept(x, w, keep="act8")
+        assert torch.equal(y, again)
+        near(y, want, product_tol(x, w) * 1.01, "y")
+        q, e = lo.act8_codes(want)
+        ours = packed.data[:q.numel()].view(torch.int8).view(q.shape)
+        assert int((ours.double() != q.double()).sum()) <= 2 * off * (127 + 256) * q.numel()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(1, 45), (40, 45), (300, 2397), (2500, 2397), (2500, 2400), (33, 8), (130, 4100)])
+def test_results_leave_what_lies_beside_them(h, rows, n, dtype):
+    """Rows that start on 16 bytes and end anywhere, in a part of a wider buffer, with rows behind the last."""
+    x, w = make(rows, 64, "bf16", 1), make(n, 64, "bf16", 2)
+    room = torch.full((rows + 3, (n + 31) // 8 * 8), 7.0, dtype=DT[dtype], device=DEV)
+    h.linear(x, w, out=room[:rows, 8:8 + n])
+    want = x.double() @ w.double().T
+    near(room[:rows, 8:8 + n], want, product_tol(x, w) * 1.01, "y")
+    assert bool((room[rows:] == 7).all() and (room[:, :8] == 7).all() and (room[:, 8 + n:] == 7).all())
