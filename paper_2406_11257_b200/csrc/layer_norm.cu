@@ -4,6 +4,7 @@
 //   y = xh weight + bias
 //   g = dy weight, dx = rstd (g - mean g - xh mean(g xh)) + add  (RMS: without mean g)
 //   dweight = sum over rows of dy xh, dbias = sum over rows of dy
+// Lanes past the last column have xh 0: (0 - mean) rstd can be infinite, and would spoil the sum of g xh although g is 0 there.
 //
 // A row is held in registers, as it lies in memory, by a group of 32 .. 512 threads, eight columns to a thread and piece: the squares are
 // summed after the mean is known, which costs no second read.  Where there are rows enough a warp takes a row of up to 4096 16-bit
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) norm_grad_kernel(const __grid_co
             load_vector<T, VEC>(g.weight, first + p * step, lane, g.cols, 1.f, w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                xh[p][i] = mul_2(add_2(xh[p][i], minus_mean), rstd);
+                xh[p][i] = mul_2(add_2(xh[p][i], minus_mean), where_column<VEC>(first + p * step, lane, g.cols, i, st.y));
                 db[p][i] = add_2(db[p][i], d[p][i]);       // 0 past the last column
                 dw[p][i] = fma_2(d[p][i], xh[p][i], dw[p][i]);
                 d[p][i] = mul_2(d[p][i], w[i]);
@@ -409,7 +410,7 @@ __global__ void __launch_bounds__(PIECES == 2 ? 128 : GROUP_MAX, PIECES == 2 ? 6
         load_vector<T, VEC>(g.weight, base, lane, g.cols, 1.f, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            held_xh[p][i] = mul_2(add_2(held_xh[p][i], minus_mean), rstd);
+            held_xh[p][i] = mul_2(add_2(held_xh[p][i], minus_mean), where_column<VEC>(base, lane, g.cols, i, st.y));
             held_g[p][i] = mul_2(held_g[p][i], w[i]);            // 0 past the last column
         }
     };
@@ -502,13 +503,14 @@ __global__ void __launch_bounds__(rows_block(THREADS), 512 / rows_block(THREADS)
         Raw<T, true> w;
         Eight we;
         w.template load_at<false>(weight + p * STEP, at + p * STEP < g.cols);
+        const f32x2 here = both_2(at + p * STEP < g.cols ? st.y : 0.f);
         w.values(we);
         raw[p].values(d[p]);
         if constexpr (KEPT) a8_eight(codes[p].x, codes[p].y, scale[p], xh[p]);
         else x[p].values(xh[p]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            xh[p][i] = mul_2(add_2(xh[p][i], minus_mean), rstd);
+            xh[p][i] = mul_2(add_2(xh[p][i], minus_mean), here);
             d[p][i] = mul_2(d[p][i], we[i]);       // 0 past the last column
             s1 = add_2(s1, d[p][i]);
             s2 = fma_2(d[p][i], xh[p][i], s2);

@@ -156,6 +156,12 @@ __device__ __forceinline__ void store_cols(T* row, u32 base, u32 lane, u32 cols,
         }
     }
 }
+// v for the pair i of a lane's eight columns, 0 past the last one.
+template <bool VEC>
+__device__ __forceinline__ f32x2 where_column(u32 base, u32 lane, u32 cols, u32 i, float v) {
+    if (VEC) return both_2(base + lane * 8 < cols ? v : 0.f);              // all eight are in or out
+    return pack_2(lane_col<VEC>(base, lane, 2 * i) < cols ? v : 0.f, lane_col<VEC>(base, lane, 2 * i + 1) < cols ? v : 0.f);
+}
 // One value per column, 32-bit floats or T (runtime: the branch is the same for all).
 template <typename T, bool VEC>
 __device__ __forceinline__ void load_vector(const ColumnVector& w, u32 base, u32 lane, u32 cols, float absent, Eight& v) {
