@@ -42,3 +42,16 @@ def test_gradient_of_equal_values_is_finite(h, rows, cols, slack, dtype, weighte
         g = h.layer_norm_grad(dy, v, w, r)
         assert not g.dweight.any()
         near(g.dbias, db, dy.double().abs().sum(0) * (rows + 40) * U, "dbias")
+
+
+@pytest.mark.parametrize("rows", [3000, 200])
+@pytest.mark.parametrize("cols", [256, 320, 4096, 16384, 20000])
+def test_rstd_is_rounded_once(h, rows, cols):
+    """Whole numbers, whose squares add up exactly (at most 64 * 20000 < 2^24): what is left is the rounding of the sum over cols (u, which the root
+    halves) and of 1 / root (u).  With a power of two for cols the division is exact too."""
+    g = torch.Generator().manual_seed(cols + rows)
+    x = torch.randint(-8, 9, (rows, cols), generator=g).float().to(DEV)
+    r = h.layer_norm(x, eps=0.0, rms=True)
+    want = 1.0 / torch.sqrt((x.double() ** 2).mean(1))
+    units = 1.0 if cols & (cols - 1) == 0 else 1.5
+    assert bool(((r.row_stats[:, 1].double() - want).abs() <= units * U * 1.0001 * want).all())
