@@ -58,6 +58,7 @@ struct Shared {
     unsigned long long parts;                      // the other CTAs' parts of the own columns have landed
     u32 tmem;
     volatile u32 abort;
+    volatile u32 late;                             // a CTA of the cluster has given up waiting for parts
 };
 
 struct Turn {                                      // the place in the ring of stages, and the parity of its current turn
@@ -100,6 +101,7 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
         mbar_init(&sh.done, 1);
         mbar_init(&sh.parts, 1);
         sh.abort = 0;
+        sh.late = 0;
         mbar_fence_init();
         if (parts > 1) mbar_arrive_expect_tx(&sh.parts, (parts - 1) * own_cols * PR_TILE * 4);
     }
@@ -256,7 +258,13 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
                 }
             }
             __syncwarp();
-            if (own_cols && !wait_warp(&sh, &sh.parts, 0, g.wait_ns, g.flag)) drain_warp(&sh.parts, 0);    // what is on its way lands
+            if (own_cols && !wait_warp(&sh, &sh.parts, 0, g.wait_ns, g.flag)) {
+                if (elect_one()) {
+                    for (u32 p = 0; p < parts; ++p) st_cluster_u32(cluster_address(const_cast<u32*>(&sh.late), p), 1);
+                    asm volatile("fence.acq_rel.cluster;" ::: "memory");       // the arrival below is relaxed
+                }
+                __syncwarp();
+            }
             if (!g.turned) join(std::integral_constant<u32, 32>());
             else join(std::integral_constant<u32, 8>());
         }
@@ -267,6 +275,12 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
     if (parts > 1) {                               // the others have what this CTA sent
         cluster_arrive();
         cluster_wait();
+        // Unless one gave up: then all parts that will be sent are on their way by now, and the CTAs stay until they have landed.
+        if (sh.late) {
+            if (own_cols) drain_warp(&sh.parts, 0);
+            cluster_arrive();
+            cluster_wait();
+        }
     }
     __syncthreads();
     tm_fence_after();

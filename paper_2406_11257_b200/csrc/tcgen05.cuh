@@ -107,6 +107,9 @@ __device__ __forceinline__ uint32_t cluster_size() {
     asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
     return r;
 }
+__device__ __forceinline__ void st_cluster_u32(uint32_t address, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(address), "r"(v) : "memory");
+}
 __device__ __forceinline__ void st_cluster(uint32_t address, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(address), "f"(v) : "memory");
 }

@@ -55,3 +55,27 @@ def test_rstd_is_rounded_once(h, rows, cols):
     want = 1.0 / torch.sqrt((x.double() ** 2).mean(1))
     units = 1.0 if cols & (cols - 1) == 0 else 1.5
     assert bool(((r.row_stats[:, 1].double() - want).abs() <= units * U * 1.0001 * want).all())
+
+
+# ---- products ------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,k,n", [(4, 512, 300), (64, 4096, 1024), (1, 11008, 4096)])
+def test_waits_that_some_ctas_give_up(rows, k, n):
+    """Limits at which some CTAs of a cluster give up and others do not: the product says so or is right, and the next one is right."""
+    other = binding.Handle(workspace_numel=4096, device=0)
+    x, w = make(rows, k, "bf16", 1), make(n, k, "bf16", 2)
+    want = other.linear(x, w)
+    other.score_status()
+    for limit in (1, 500, 2000, 5000, 10000):
+        for _ in range(3):
+            other.set_wait_limit(limit)
+            got = other.linear(x, w)
+            try:
+                other.score_status()
+            except binding.ExcpError as e:
+                assert e.status == -7
+            else:
+                assert torch.equal(got, want)
+            other.set_wait_limit(2_000_000_000)
+            assert torch.equal(other.linear(x, w), want)
+            other.score_status()
+    other.close()
