@@ -9,8 +9,13 @@
 // 1 x 4096 -> 11008 bf16 18 us from memory, 16 x 2048 -> 50304 37 us (5.6 TB/s), 333 x 1000 -> 4097 9.3 us, 512 x 1024 -> 1024 5.6 us, one tile
 // alone 2.6 us.
 //
-// Roles: warps 0..3 fetch the operands (tensor maps; what lies past an edge comes as 0), warp 8 issues the products, and at the end
-// warps 0..7 write the result.
+// Sums are taken in runs of at most PR_RUN columns, whatever the results' types, so that they do not depend on what is done with them.  Up to
+// four runs have an accumulator each; of more, all but the last three are added to the first by warps that have nothing else to do, while
+// the products go on in the others.  (One run, which loses more the longer it is: 1 x 4096 -> 4096 8.3 us against 8.8, 512 x 4096 -> 4096
+// 18.7 against 20.4.)
+//
+// Roles: warps 0..3 fetch the operands (tensor maps; what lies past an edge comes as 0), warps 4..7 add up runs, warp 8 issues the products, and at
+// the end warps 0..7 write the result.
 // Every wait for a copy or a product is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and
 // leaves.  The two that hardware gives no limit, for tensor memory and at the cluster's barrier, depend only on CTAs whose own
 // waits are bounded.
@@ -27,6 +32,7 @@ constexpr int STAGES_MAX = 8;
 constexpr u32 BOXES_MAX = 2;                       // boxes of 64 columns in a stage
 constexpr u32 MAX_SPLIT = 8;
 constexpr u32 OUT_BYTES = 8192;                  // of a warp's results on their way out
+constexpr u32 ACCS = 4;                            // accumulators at most
 constexpr u32 M_BYTES = PR_TILE * PR_K * 2;
 constexpr u32 SMEM_MAX = 227 * 1024 - 1024;        // dynamic shared memory of a block, beside what the kernel has of its own
 // Tensor memory is given out without a limit on the wait, and a CTA that holds some waits for its cluster: two launches on two streams
@@ -42,7 +48,7 @@ struct NarrowArgs {
     u32 boxes;                                     // of a stage
     u32 nt;                                        // rows of n per CTA: a multiple of 16, at most 256
     u32 n_bytes, stages, tmem_cols;
-    u32 runs;                                      // accumulators, nt columns of tensor memory each: the columns are split among them
+    u32 accs, runs, run;                           // accumulators, nt columns of tensor memory each; runs of a part's stages, stages of a run
     u32 ring_bytes;                                // of the stages; afterwards the accumulator lies there, or the results on their way out
     u32 per_owner;                                 // columns of the accumulator that a CTA of the cluster joins
     u32 turned;                                    // m is b: a lane has a column of c
@@ -54,6 +60,7 @@ struct NarrowArgs {
 struct Shared {
     unsigned long long full[STAGES_MAX];           // copies have landed
     unsigned long long empty[STAGES_MAX];          // the stage has been multiplied
+    unsigned long long acc_full[ACCS - 1], acc_empty[ACCS - 1];
     unsigned long long done;
     unsigned long long parts;                      // the other CTAs' parts of the own columns have landed
     u32 tmem;
@@ -87,8 +94,10 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
     const u32 k_steps = (g.k_boxes + g.boxes - 1) / g.boxes;
     const u32 k0 = (u32)((u64)k_steps * part / parts), k1 = (u32)((u64)k_steps * (part + 1) / parts);
     const u32 box = M_BYTES + g.n_bytes, stage = g.boxes * box;
-    // stages of an accumulator, accumulators in use
-    const u32 run = RUNS ? max((k1 - k0 + g.runs - 1) / g.runs, 1u) : k1 - k0, runs = RUNS ? (k1 - k0 + run - 1) / run : k1 > k0;
+    // The stages are added up in runs, about equally long.  The first has accumulator 0, the others the rest in turn; those that
+    // would find none of their own in the end (`emptied`, from the second on) are added to accumulator 0 on the way.
+    const u32 runs = RUNS ? g.runs - (g.runs && k1 - k0 <= (g.runs - 1) * g.run) : k1 > k0;      // a part is one stage shorter than another, or none
+    const u32 emptied = RUNS && runs > g.accs ? runs - g.accs : 0;
     const u64 n0 = (u64)ntile * g.nt, n_rows = g.turned ? g.end.rows : g.end.cols;
     const u32 cols = (u32)min((u64)g.nt, n_rows - n0);         // of the accumulator that are results
     // the CTA's own columns of the accumulator, and the others' parts of them: [part][column][row]
@@ -98,6 +107,7 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
 
     if (threadIdx.x == 0) {
         for (u32 s = 0; s < g.stages; ++s) { mbar_init(&sh.full[s], 2 * g.boxes); mbar_init(&sh.empty[s], 1); }
+        for (u32 i = 0; i + 1 < ACCS; ++i) { mbar_init(&sh.acc_full[i], 1); mbar_init(&sh.acc_empty[i], 4); }
         mbar_init(&sh.done, 1);
         mbar_init(&sh.parts, 1);
         sh.abort = 0;
@@ -142,35 +152,67 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
     } else if (warp == PRODUCT_WARP) {
         const u32 idesc = product_idesc(g.bf16, g.m_along_k, g.n_along_k, PR_TILE, g.nt);
         const u32 step_m = product_desc_step(g.m_along_k), step_n = product_desc_step(g.n_along_k);
-        Turn ring;
-        u32 left = run, d = tmem, begun = 0;
-        for (u32 k = k0; k < k1; ++k) {
-            if (!wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag)) break;
-            const u32 st = smem_u32(smem) + ring.s * stage;
-            const u64 dm = product_desc(st, g.m_along_k), dn = product_desc(st + M_BYTES, g.n_along_k);
-            if (RUNS && left == 0) {               // the next accumulator
-                left = run;
-                d += g.nt;
-                begun = 0;
+        Turn ring, acc;
+        u32 k = k0, d = tmem;
+        bool ok = true;
+        for (u32 r = 0; ok && r < runs; ++r) {
+            const u32 end = RUNS ? min(k + g.run, k1) : k1;
+            if (RUNS && r) {
+                if (r > 1) acc.next(g.accs - 1);
+                if (r >= g.accs && !(ok = wait_warp(&sh, &sh.acc_empty[acc.s], acc.parity ^ 1, g.wait_ns, g.flag))) break;
+                tm_fence_after();
+                d = tmem + (1 + acc.s) * g.nt;
             }
-            if (RUNS) --left;
-            if (elect_one()) {
+            for (u32 begun = 0; k < end; ++k, begun = 1) {
+                if (!(ok = wait_warp(&sh, &sh.full[ring.s], ring.parity, g.wait_ns, g.flag))) break;
+                const u32 st = smem_u32(smem) + ring.s * stage;
+                const u64 dm = product_desc(st, g.m_along_k), dn = product_desc(st + M_BYTES, g.n_along_k);
+                if (elect_one()) {
 #pragma unroll
-                for (u32 u = 0; u < BOXES_MAX; ++u) {
-                    if (u >= g.boxes || k * g.boxes + u >= g.k_boxes) break;
+                    for (u32 u = 0; u < BOXES_MAX; ++u) {
+                        if (u >= g.boxes || k * g.boxes + u >= g.k_boxes) break;
 #pragma unroll
-                    for (u32 i = 0; i < PR_K / 16; ++i)
-                        tm_mma_f16(d, dm + u * (box >> 4) + i * step_m, dn + u * (box >> 4) + i * step_n, idesc, begun | u | i);
+                        for (u32 i = 0; i < PR_K / 16; ++i)
+                            tm_mma_f16(d, dm + u * (box >> 4) + i * step_m, dn + u * (box >> 4) + i * step_n, idesc, begun | u | i);
+                    }
+                    tm_commit(&sh.empty[ring.s]);
                 }
-                tm_commit(&sh.empty[ring.s]);
+                __syncwarp();
+                ring.next(g.stages);
             }
-            __syncwarp();
-            begun = 1;
-            ring.next(g.stages);
+            if (RUNS && r && r <= emptied) {
+                if (elect_one()) tm_commit(&sh.acc_full[acc.s]);
+                __syncwarp();
+            }
         }
         if (elect_one()) tm_commit(&sh.done);
         __syncwarp();
         drain_warp(&sh.done, 0);                   // what has been issued is done before tensor memory goes
+    } else if (RUNS) {                             // warps 4..7, each its place's lanes of tensor memory
+        const u32 sum = tmem + ((warp & 3) << 21);
+        Turn acc;
+        for (u32 r = 1; r <= emptied; ++r) {
+            if (!wait_warp(&sh, &sh.acc_full[acc.s], acc.parity, g.wait_ns, g.flag)) break;
+            tm_fence_after();
+            const u32 from = sum + (1 + acc.s) * g.nt;
+            for (u32 c = 0; c < g.nt; c += 16) {
+                u32 v[16], t[16];
+                tm_load8(from + c, v);
+                tm_load8(from + c + 8, v + 8);
+                tm_load8(sum + c, t);
+                tm_load8(sum + c + 8, t + 8);
+                tm_wait_load();
+#pragma unroll
+                for (u32 e = 0; e < 16; ++e) t[e] = __float_as_uint(__uint_as_float(t[e]) + __uint_as_float(v[e]));
+                tm_store16(sum + c, t);
+            }
+            tm_wait_store();
+            tm_fence_before();
+            __syncwarp();
+            if (elect_one()) mbar_arrive_own(&sh.acc_empty[acc.s]);
+            __syncwarp();
+            acc.next(g.accs - 1);
+        }
     }
     if (parts > 1) cluster_wait();                 // every CTA of the cluster has started, its barriers are ready
     if (warp < WORK_WARPS) {
@@ -180,29 +222,40 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
         const u64 m = (u64)mt * PR_TILE + row;
         const float bias = g.turned ? column_bias(g.end, m) : 0.f;
         const bool ok = wait_warp(&sh, &sh.done, 0, g.wait_ns, g.flag);
+        if (emptied) work_barrier();               // warps 4..7 have added up theirs
         tm_fence_after();
         u32 turn = 0;
         auto take = [&](auto width, u32 c, float (&f)[decltype(width)::value]) {
             constexpr u32 W = decltype(width)::value;
-            auto load = [&](u32 at, u32 (&v)[W]) {
-                __syncwarp();
+            u32 v[W];
+            __syncwarp();
+            if (runs) {
                 if constexpr (W == 32) {
-                    tm_load32(at, v);
+                    tm_load32(lanes + c, v);
                 } else {
 #pragma unroll
-                    for (u32 i = 0; i < W; i += 8) tm_load8(at + i, v + i);
+                    for (u32 i = 0; i < W; i += 8) tm_load8(lanes + c + i, v + i);
                 }
                 tm_wait_load();
-            };
-            u32 v[W];
-            if (runs) load(lanes + c, v);
+            }
 #pragma unroll
             for (u32 e = 0; e < W; ++e) f[e] = runs ? __uint_as_float(v[e]) : 0.f;
             if constexpr (RUNS) {
-                for (u32 r = 1; r < runs; ++r) {
-                    load(lanes + r * g.nt + c, v);
+                constexpr u32 STEP = W < 16 ? W : 16;                      // more does not fit the registers
+                u32 slot = emptied % (ACCS - 1);                           // 0 where there are fewer accumulators
+                for (u32 r = emptied + 1; r < runs; ++r) {
+                    const u32 from = lanes + (1 + slot) * g.nt + c;
+                    if (++slot == g.accs - 1) slot = 0;
 #pragma unroll
-                    for (u32 e = 0; e < W; ++e) f[e] += __uint_as_float(v[e]);
+                    for (u32 h = 0; h < W; h += STEP) {
+                        u32 t[STEP];
+                        __syncwarp();
+#pragma unroll
+                        for (u32 i = 0; i < STEP; i += 8) tm_load8(from + h + i, t + i);
+                        tm_wait_load();
+#pragma unroll
+                        for (u32 e = 0; e < STEP; ++e) f[h + e] += __uint_as_float(t[e]);
+                    }
                 }
             }
         };
@@ -297,7 +350,7 @@ bool launch_as(cudaStream_t s, const NarrowArgs& g, u32 blocks, u32 parts, u32 s
 // How a product is cut: which operand is on which side, rows of n per CTA, CTAs that share the columns of a tile.
 struct Cut {
     bool turned;
-    u32 nt, parts, boxes, stages, runs, tmem_cols, smem, ring_bytes, per_owner;
+    u32 nt, parts, boxes, stages, accs, tmem_cols, smem, ring_bytes, per_owner;
     float us;
 };
 
@@ -331,8 +384,12 @@ u32 at_once(int sms, u32 parts, u32 beside) {
     return n * beside;
 }
 
+// Stages of a run; accumulators for so many stages.
+u32 run_of(u32 boxes) { return PR_RUN / (PR_K * boxes); }
+u32 accs_of(u32 steps, u32 boxes) { return steps <= run_of(boxes) ? 1 : steps <= 2 * run_of(boxes) ? 2 : ACCS; }
+
 // About how long a cut takes, in us, as measured: 3.2 for a launch, its first copies and the end; what an SM fetches, 135 bytes a ns (a CTA
-// alone 75 where it comes from memory, which gives 6500 in all, or 5600 to fewer than three CTAs on two SMs; L2 15000), and at least the
+// alone 75 of the larger operand where it comes from memory, which gives 6500 in all, or 5600 to fewer than three CTAs on two SMs; L2 15000), and at least the
 // products (1.05 ns for a row of n and 64 columns); 10 ns for a column of the accumulator that lanes write across rows of y and 4 along
 // them; 1 and 0.25 a part and 6 ns a column for the exchange within a cluster; 6 for a further turn of the SMs.
 Cut find_cut(const ProductCall& c, bool y_vec) {
@@ -362,9 +419,8 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
                 // Two CTAs to an SM where there are more than one each; two boxes of 64 columns to a stage (waiting for one and handing it back
                 // cost 250 cycles, whatever it holds), or one: the first of these that leaves enough stages.
                 bool two = false;
-                u32 stages = 0, wanted_runs = 1;
-                while ((u64)((k_boxes + parts - 1) / parts) * PR_K > (u64)wanted_runs * product_run(c.end)) wanted_runs *= 2;
-                for (u32 way = tiles * parts > (u64)c.sms && want * wanted_runs <= 128 ? 0 : 2; way < 4; ++way) {
+                u32 stages = 0;
+                for (u32 way = tiles * parts > (u64)c.sms && want * accs_of(steps_of(BOXES_MAX), BOXES_MAX) <= 128 ? 0 : 2; way < 4; ++way) {
                     two = way < 2;
                     cut.boxes = way % 2 ? 1 : BOXES_MAX;
                     stages = room_for(two ? SMEM_MAX / 2 - 1024 : SMEM_MAX, cut.boxes);
@@ -378,10 +434,9 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
                 cut.ring_bytes = cut.stages * cut.boxes * box > own ? cut.stages * cut.boxes * box : own;
                 cut.smem = cut.ring_bytes + sums + 1024;
                 if (cut.smem > SMEM_MAX) continue;
-                while (cut.runs < wanted_runs && cut.runs * 2 * want <= 512) cut.runs *= 2;
-                if (cut.runs < wanted_runs && want > 16) continue;         // a smaller tile has room for more runs
+                cut.accs = accs_of(steps, cut.boxes);
                 cut.tmem_cols = 32;
-                while (cut.tmem_cols < want * cut.runs) cut.tmem_cols *= 2;
+                while (cut.tmem_cols < want * cut.accs) cut.tmem_cols *= 2;
                 const u32 least = cut.tmem_cols >= 512 ? SMEM_MAX : cut.tmem_cols * (SMEM_SM / 512);
                 if (cut.smem < least) cut.smem = least;
                 if (cut.smem < SMEM_LEAST) cut.smem = SMEM_LEAST;
@@ -390,7 +445,8 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
                 if (parts > 1 && blocks > room) continue;
                 const u64 per_sm = (blocks + c.sms - 1) / c.sms, turns = (blocks + room - 1) / room;
                 const float beside = two && per_sm > 1 ? 2.f : 1.f, rate = fminf(alone, 135e3f / beside);
-                const float step = cut.boxes * fmaxf((float)box / rate, beside * want * 1.05e-3f);
+                const float near = 135e3f / beside, fetch = m.rows >= n.rows ? M_BYTES / rate + n_bytes / near : M_BYTES / near + n_bytes / rate;
+                const float step = cut.boxes * fmaxf(fetch, beside * want * 1.05e-3f);
                 const float whole = memory > 60e6f && blocks * 2 < (u64)c.sms * 3 ? 1.16f * memory / all : memory / all;
                 cut.us = 3.2f + fmaxf((float)turns * steps * step, whole) + (turns - 1) * 6.f +
                          (float)turns * want / parts * (turned ? 0.010f : 0.004f) + (parts > 1 ? 1.f + 0.25f * parts + 0.006f * want : 0.f);
@@ -409,7 +465,7 @@ Cut best_cut(const ProductCall& c, bool y_vec) {
         Cut cut;
     };
     thread_local Entry kept[32];
-    const u32 how = 1u | (c.a.along_k ? 2u : 0u) | (c.b.along_k ? 4u : 0u) | (y_vec ? 8u : 0u) | (product_run(c.end) == PR_RUN ? 16u : product_run(c.end) == PR_RUN_KEPT ? 32u : 0u) | (u32)c.sms << 6;
+    const u32 how = 1u | (c.a.along_k ? 2u : 0u) | (c.b.along_k ? 4u : 0u) | (y_vec ? 8u : 0u) | (u32)c.sms << 4;
     Entry& e = kept[((c.a.rows * 31 + c.b.rows) * 31 + c.a.k * 7 + how) * 0x9e3779b97f4a7c15ull >> 59];
     if (e.how != how || e.a_rows != c.a.rows || e.b_rows != c.b.rows || e.k != c.a.k) e = Entry{c.a.rows, c.b.rows, c.a.k, how, find_cut(c, y_vec)};
     return e.cut;
@@ -430,7 +486,11 @@ bool launch_narrow(cudaStream_t s, const ProductCall& c, const EndArgs& end, con
     g.per_owner = cut.per_owner;
     g.stages = cut.stages;
     g.ring_bytes = cut.ring_bytes;
-    g.runs = cut.runs;
+    g.accs = cut.accs;
+    const u32 k_steps = (g.k_boxes + cut.boxes - 1) / cut.boxes, steps = k_steps / cut.parts + (k_steps % cut.parts != 0);
+    g.runs = (steps + run_of(cut.boxes) - 1) / run_of(cut.boxes);
+    g.run = g.runs ? (steps + g.runs - 1) / g.runs : 0;
+    g.runs = g.run ? (steps + g.run - 1) / g.run : 0;
     g.tmem_cols = cut.tmem_cols;
     if (g.k_boxes && (!product_map(&g.m, m, PR_TILE, c.dtype) || !product_map(&g.n, n, g.nt, c.dtype))) return false;
     if (!g.turned && cut.parts == 1 && !result_map(&g.y, c.end.y)) return false;
@@ -442,7 +502,7 @@ bool launch_narrow(cudaStream_t s, const ProductCall& c, const EndArgs& end, con
     const u32 blocks = (u32)(m_tiles * g.n_tiles) * cut.parts;
     auto launch = [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if constexpr (DT != DT_F32) if (cut.runs == 1) return launch_as<DT, false>(s, g, blocks, cut.parts, cut.smem);
+        if constexpr (DT != DT_F32) if (cut.accs == 1) return launch_as<DT, false>(s, g, blocks, cut.parts, cut.smem);
         return launch_as<DT, true>(s, g, blocks, cut.parts, cut.smem);
     };
     return c.end.y.dtype == DT_F32 ? launch(std::integral_constant<int, DT_F32>()) : c.end.y.dtype == DT_F16 ? launch(std::integral_constant<int, DT_F16>())

@@ -11,8 +11,9 @@ namespace excp {
 constexpr u32 PR_TILE = 128;                       // rows of an operand tile = lanes of tensor memory
 constexpr u32 PR_K = 64;                           // columns of a box: 128 bytes, one swizzle span
 // The tensor core cuts its sums off instead of rounding them: 1024 columns added one after the other lose 1e-6 of a sum (measured), 4096
-// 4e-6, which shows in a result of 32 bits.  There the columns are added up in runs of at most about so many, and the runs' sums in
-// fp32: 7e-7 whatever the length.  (Runs of 512: 5e-7, and a twelfth slower.)
+// 4e-6, which shows in a result of 32 bits.  There, and in the kernel for few rows always, the columns are added up in runs of at most so many,
+// and the runs' sums in fp32: 7e-7 whatever the length, of terms of both signs.  (Runs of 512: 5e-7, and a twelfth slower.)  Where all terms have
+// one sign every addition cuts off the same way: 4e-6, or 6e-9 a column of one run.
 constexpr u32 PR_RUN = 768;
 // It shows less in codes of 8 bits: after 4096 columns seven times as many land on the other side of a border as of a plain fp32 sum, and the
 // kept values of fp16 activations are 1.7 times as far off.  Runs of 2048 columns leave 1.2 times.
@@ -38,7 +39,7 @@ struct ProductEnd {
     Matrix kept;                                   // p null: none
 };
 
-// Columns of a run: results of 16 bits have one.  What is kept in 32 bits has the sums of what is kept in 8.
+// Columns of a run of the kernel for many rows: results of 16 bits have one.  What is kept in 32 bits has the sums of what is kept in 8.
 inline u32 product_run(const ProductEnd& e) {
     if (e.y.dtype == DT_F32) return PR_RUN;
     return e.kept.p && (e.kept.dtype == DT_ACT8 || e.kept.dtype == DT_F32) ? PR_RUN_KEPT : ~0u;

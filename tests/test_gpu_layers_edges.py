@@ -79,3 +79,46 @@ def test_waits_that_some_ctas_give_up(rows, k, n):
             assert torch.equal(other.linear(x, w), want)
             other.score_status()
     other.close()
+
+
+def big(rows, cols, seed, dtype=torch.bfloat16, size=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return (torch.randn(rows, cols, generator=g, device=DEV) * size).to(dtype)
+
+
+def off(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+def test_sums_of_any_length(h):
+    """32-bit results of more columns than tensor memory has room for in runs of 768 (few rows on one side, too many tiles to be split; or so
+    long that even a part of the columns is): as exact as short ones, 2^-20 of the result's norm."""
+    for k, n, m in ((65536, 19100, 16), (131072, 19000, 8), (262144, 100, 3)):
+        dy, x = big(k, n, 1), big(k, m, 2)
+        want = torch.zeros(n, m, dtype=torch.float64, device=DEV)
+        for i in range(0, k, 8192):
+            want += dy[i:i + 8192].double().T @ x[i:i + 8192].double()
+        assert off(h.linear_grad_weight(dy, x), want) <= 2.0 ** -20, (k, n, m)
+        del dy, x
+    for rows, k, n in ((64, 50304, 11008), (1, 50304, 4096)):
+        x, w = big(rows, k, 3), big(n, k, 4)
+        want = torch.cat([x.double() @ w[i:i + 2048].double().T for i in range(0, n, 2048)], 1)
+        assert off(h.linear(x, w, dtype=torch.float32), want) <= 2.0 ** -20, (rows, k, n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,k,n", [(1, 11008, 4096), (40, 8200, 48), (64, 4096, 4096), (300, 3000, 700)])
+def test_what_is_kept_does_not_change_results(h, rows, k, n, dtype):
+    """The same y whatever is kept beside it, and what is kept in 32 bits as exact as a result of 32 bits (2^-20 of the norm)."""
+    x, w = big(rows, k, 1, DT[dtype]), big(n, k, 2, DT[dtype], 0.02)
+    bias = vector(n, dtype, 3)
+    y = h.linear(x, w, bias, act="gelu")
+    for keep in ("act8", torch.float32, torch.float16, torch.bfloat16):
+        again, kept = h.linear_kept(x, w, bias, act="gelu", keep=keep)
+        assert torch.equal(again, y), keep
+        if keep == torch.float32:
+            want = x.double() @ w.double().T + bias.double()
+            assert off(kept, want) <= 2.0 ** -20
+            q, s = lo.act8_codes(kept)
+            packed = h.linear_kept(x, w, bias, act="gelu")[1].data
+            assert torch.equal(packed[:q.numel() + 2 * s.numel()], lo.act8_pack(q, s))
