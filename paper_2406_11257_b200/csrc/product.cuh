@@ -15,10 +15,14 @@ constexpr u32 PR_K = 64;                           // columns of a box: 128 byte
 // and the runs' sums in fp32: 7e-7 whatever the length, of terms of both signs.  (Runs of 512: 5e-7, and a twelfth slower.)  Where all terms have
 // one sign every addition cuts off the same way: 4e-6, or 6e-9 a column of one run.
 constexpr u32 PR_RUN = 768;
-// It shows less in codes of 8 bits: after 4096 columns seven times as many land on the other side of a border as of a plain fp32 sum, and the
-// kept values of fp16 activations are 1.7 times as far off.  Runs of 2048 columns leave 1.2 times.
-// Not shorter: while a tile with 8 bits and a gelu is written out the products can go on for two runs only.
-constexpr u32 PR_RUN_KEPT = 2048;
+// It shows less in fewer bits, and the kernel for many rows takes longer runs where that is quicker.
+// Codes of 8 bits: after 4096 columns in one run seven times as many as of a plain fp32 sum land on the other side of a border, and the kept values of
+// fp16 activations are 1.7 times as far off; runs of 2048 columns leave 1.2 times.  Not shorter with an activation: while such a tile is written out the products
+// can go on for two runs only (4096 x 4096 -> 11008, gelu: runs of 768 columns 369 us, of 2048 317).
+// (Without one they are as short as for 32 bits, 249 -> 331 us: the result beside 8 bits is then the same as beside 32.)
+// Results of 16 bits: a run of terms of one sign loses up to a fifth of half a unit (5e-5 in 8192 columns, and bfloat16 has three bits less; fp16 results
+// of one run of 50304 columns lost 3e-4).
+constexpr u32 PR_RUN_ACT8 = 2048, PR_RUN_F16 = 8192, PR_RUN_BF16 = 65536;
 constexpr u32 PR_CHUNK = 64;                       // rows of a box of an operand that lies the other way round
 constexpr u32 PR_CHUNK_BYTES = PR_CHUNK * PR_K * 2;
 
@@ -39,10 +43,12 @@ struct ProductEnd {
     Matrix kept;                                   // p null: none
 };
 
-// Columns of a run of the kernel for many rows: results of 16 bits have one.  What is kept in 32 bits has the sums of what is kept in 8.
+// Columns of a run of the kernel for many rows.
 inline u32 product_run(const ProductEnd& e) {
-    if (e.y.dtype == DT_F32) return PR_RUN;
-    return e.kept.p && (e.kept.dtype == DT_ACT8 || e.kept.dtype == DT_F32) ? PR_RUN_KEPT : ~0u;
+    const bool kept32 = e.kept.p && e.kept.dtype == DT_F32, kept8 = e.kept.p && e.kept.dtype == DT_ACT8;
+    if (e.y.dtype == DT_F32 || kept32 || (kept8 && e.act == ACT_NONE)) return PR_RUN;
+    if (kept8) return PR_RUN_ACT8;
+    return e.y.dtype == DT_F16 ? PR_RUN_F16 : PR_RUN_BF16;
 }
 
 struct ProductCall {

@@ -122,3 +122,24 @@ def test_what_is_kept_does_not_change_results(h, rows, k, n, dtype):
             q, s = lo.act8_codes(kept)
             packed = h.linear_kept(x, w, bias, act="gelu")[1].data
             assert torch.equal(packed[:q.numel() + 2 * s.numel()], lo.act8_pack(q, s))
+
+
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,k,n", [(2304, 3000, 2400), (2304, 9000, 2400)])
+def test_kept_in_32_bits_is_as_exact_as_a_result(h, rows, k, n, dtype, act):
+    x, w = big(rows, k, 1, DT[dtype]), big(n, k, 2, DT[dtype], 0.02)
+    _, kept = h.linear_kept(x, w, act=act, keep=torch.float32)
+    assert off(kept, x.double() @ w.double().T) <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("k", [9000, 50304])
+@pytest.mark.parametrize("rows,n", [(2304, 2304), (200, 300), (1, 2304)])
+def test_long_sums_of_one_sign_in_16_bits(h, rows, n, k):
+    """Terms of one sign: an addition of 16 columns cuts off at most 2^-22 of the running sum, which is half of the last one on average, so a run of
+    8192 columns loses at most 256 * 2^-22 of it; the rounding to fp16 falls on both sides, and of rows * n of them a mean of 5 deviations
+    (2^-11 / sqrt(12) each at most) is left."""
+    g = torch.Generator(device=DEV).manual_seed(7)
+    x, w = ((torch.rand(r, k, generator=g, device=DEV) + 0.5).mul_(s).half() for r, s in ((rows, 1.0), (n, 400.0 / k)))
+    y, want = h.linear(x, w).double(), x.double() @ w.double().T
+    assert abs(((y - want) / want).mean().item()) <= 256 * 2.0 ** -22 + 5 * 2.0 ** -11 / math.sqrt(12 * rows * n)
