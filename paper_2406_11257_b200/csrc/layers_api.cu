@@ -70,7 +70,7 @@ excp_status product(excp_handle h, const excp_matrix* ma, bool a_along_k, const 
     auto operand = [](const Matrix& m, const excp_matrix* shape, bool along_k) {
         return ProductOperand{m.p, along_k ? shape->rows : shape->cols, along_k ? shape->cols : shape->rows, m.stride, along_k};
     };
-    const ProductCall c{operand(a, ma, a_along_k), operand(b, mb, b_along_k), end, ma->dtype, h->sms, h->wait_limit_ns, h->score.d_flag};
+    const ProductCall c{operand(a, ma, a_along_k), operand(b, mb, b_along_k), end, ma->dtype, h->device, h->sms, h->wait_limit_ns, h->score.d_flag};
     if (!launch_product(stream, c)) {
         check(h, cudaGetLastError());
         return EXCP_ERR_CUDA;

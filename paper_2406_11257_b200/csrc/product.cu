@@ -19,6 +19,7 @@
 // Every wait for a copy or a product is bounded; where one runs out the CTA raises the handle's flag, lets its copies land and
 // leaves.  The two that hardware gives no limit, for tensor memory and at the cluster's barrier, depend only on CTAs whose own
 // waits are bounded.
+#include "per_device.h"
 #include "product.cuh"
 
 namespace excp {
@@ -352,18 +353,17 @@ struct Cut {
     bool turned;
     u32 nt, parts, boxes, stages, accs, tmem_cols, smem, ring_bytes, per_owner;
     float us;
+    bool guess;                                    // the driver did not say how many clusters run at once
 };
 
-// Blocks that run at once in clusters of `parts`, `beside` of them on an SM.  Clusters stay within a group of SMs, whose sizes only the
-// driver knows (which counts one block to an SM of a kernel that uses tensor memory, however little).
-u32 at_once(int sms, u32 parts, u32 beside) {
-    if (parts == 1) return (u32)sms * beside;
-    static std::atomic<u32> known[MAX_SPLIT + 1];
-    u32 n = known[parts].load(std::memory_order_relaxed);
-    if (n) return n * beside;
-    static std::atomic<u64> allowed{0};
-    int clusters = 0;
-    if (allow_smem(product_kernel<DT_F32, true>, allowed, SMEM_MAX)) {
+// Blocks that run at once in clusters of `parts`, one to an SM; 0 where the driver did not say.  Clusters stay within a group of SMs, whose sizes only
+// the driver knows (which counts one block to an SM of a kernel that uses tensor memory, however little).
+u32 at_once(int device, int sms, u32 parts) {
+    if (parts == 1) return (u32)sms;
+    static PerDevice<MAX_SPLIT + 1> known;
+    return known.get(device, parts, [&]() -> u32 {
+        static std::atomic<u64> allowed{0};
+        if (!allow_smem(product_kernel<DT_F32, true>, allowed, SMEM_MAX)) return 0;
         cudaLaunchConfig_t cfg{};
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
@@ -374,14 +374,13 @@ u32 at_once(int sms, u32 parts, u32 beside) {
         cfg.dynamicSmemBytes = SMEM_MAX;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
+        int clusters = 0;
         if (cudaOccupancyMaxActiveClusters(&clusters, product_kernel<DT_F32, true>, &cfg) != cudaSuccess) {
             cudaGetLastError();
-            clusters = 0;
+            return 0;
         }
-    }
-    n = clusters > 0 ? (u32)clusters * parts : 1;  // 1: nothing is split so
-    known[parts].store(n, std::memory_order_relaxed);
-    return n * beside;
+        return clusters > 0 ? (u32)clusters * parts : 1;       // 1: nothing is split so
+    });
 }
 
 // Stages of a run; accumulators for so many stages.
@@ -395,6 +394,7 @@ u32 accs_of(u32 steps, u32 boxes) { return steps <= run_of(boxes) ? 1 : steps <=
 Cut find_cut(const ProductCall& c, bool y_vec) {
     Cut best{};
     best.us = 1e30f;
+    bool guess = false;
     const u32 k_boxes = (u32)((c.a.k + PR_K - 1) / PR_K);
     const float memory = (float)(c.a.rows + c.b.rows) * (float)c.a.k * 2.f, alone = memory > 60e6f ? 75e3f : 135e3f, all = memory > 60e6f ? 6.5e6f : 15e6f;
     for (int side = 0; side < 2; ++side) {
@@ -409,7 +409,7 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
             const u64 tiles = m_tiles * ((n.rows + want - 1) / want);
             const u32 n_bytes = n.along_k ? want * PR_K * 2 : (want + PR_CHUNK - 1) / PR_CHUNK * PR_CHUNK_BYTES;
             for (u32 parts = 1; parts <= MAX_SPLIT && (parts == 1 || (k_boxes >= parts && tiles * parts <= (u64)c.sms * 2)); ++parts) {
-                Cut cut{turned, want, parts, BOXES_MAX, 0, 1, 0, 0, 0, 0, 0.f};
+                Cut cut{turned, want, parts, BOXES_MAX, 0, 1, 0, 0, 0, 0, 0.f, false};
                 cut.per_owner = (want + parts - 1) / parts;
                 if (!turned) cut.per_owner = (cut.per_owner + 31) & ~31u;
                 const u32 sums = parts > 1 ? parts * cut.per_owner * PR_TILE * 4 : 0, own = parts > 1 ? want * PR_TILE * 4 : turned ? 0 : WORK_WARPS * OUT_BYTES;
@@ -441,7 +441,8 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
                 if (cut.smem < least) cut.smem = least;
                 if (cut.smem < SMEM_LEAST) cut.smem = SMEM_LEAST;
                 if (cut.smem > SMEM_MAX / 2 - 1024) two = false;
-                const u64 room = at_once(c.sms, parts, two ? 2 : 1), blocks = tiles * parts;
+                const u64 room = (u64)at_once(c.device, c.sms, parts) * (two ? 2 : 1), blocks = tiles * parts;
+                guess |= room == 0;
                 if (parts > 1 && blocks > room) continue;
                 const u64 per_sm = (blocks + c.sms - 1) / c.sms, turns = (blocks + room - 1) / room;
                 const float beside = two && per_sm > 1 ? 2.f : 1.f, rate = fminf(alone, 135e3f / beside);
@@ -454,21 +455,25 @@ Cut find_cut(const ProductCall& c, bool y_vec) {
             }
         }
     }
+    best.guess = guess;
     return best;
 }
 
-// The search takes 10 us of host time: the cuts of the last shapes are kept (a function of the sizes alone).
+// The search takes 10 us of host time: the cuts of the last shapes are kept (a function of the device and the sizes alone).
 Cut best_cut(const ProductCall& c, bool y_vec) {
     struct Entry {
         u64 a_rows = 0, b_rows = 0, k = 0;
         u32 how = 0;
+        int device = 0;
         Cut cut;
     };
     thread_local Entry kept[32];
     const u32 how = 1u | (c.a.along_k ? 2u : 0u) | (c.b.along_k ? 4u : 0u) | (y_vec ? 8u : 0u) | (u32)c.sms << 4;
     Entry& e = kept[((c.a.rows * 31 + c.b.rows) * 31 + c.a.k * 7 + how) * 0x9e3779b97f4a7c15ull >> 59];
-    if (e.how != how || e.a_rows != c.a.rows || e.b_rows != c.b.rows || e.k != c.a.k) e = Entry{c.a.rows, c.b.rows, c.a.k, how, find_cut(c, y_vec)};
-    return e.cut;
+    if (e.how == how && e.device == c.device && e.a_rows == c.a.rows && e.b_rows == c.b.rows && e.k == c.a.k) return e.cut;
+    const Cut cut = find_cut(c, y_vec);
+    if (!cut.guess) e = Entry{c.a.rows, c.b.rows, c.a.k, how, c.device, cut};
+    return cut;
 }
 
 bool launch_narrow(cudaStream_t s, const ProductCall& c, const EndArgs& end, const Cut& cut) {

@@ -55,7 +55,7 @@ struct ProductCall {
     ProductOperand a, b;
     ProductEnd end;
     int dtype;                                     // of both operands: DT_F16 or DT_BF16
-    int sms;
+    int device, sms;
     u64 wait_ns;
     u32* flag;
 };
