@@ -128,6 +128,12 @@ at::Tensor result(PyObject* out, int device, at::ScalarType type, int64_t r, int
     return t;
 }
 
+// A result, behind the call that wrote it.  Where it is a tensor of the caller's (`given` is not None), autograd is told that it has changed.
+PyObject* wrap_written(const at::Tensor& t, PyObject* given) {
+    if (given != Py_None && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    return wrap(t);
+}
+
 // (handle, device, x, out or None)
 PyObject* tensor_scale(PyObject* const* a) {
     const int device = (int)integer(a[1]);
@@ -135,7 +141,7 @@ PyObject* tensor_scale(PyObject* const* a) {
     const at::Tensor out = a[3] == Py_None ? fresh({}, at::kFloat, device) : tensor(a[3], "out");
     if (out.scalar_type() != at::kFloat || out.numel() != 1 || !on(out, device)) throw Refused("out: expected one float32 value on the handle's device");
     check(api.mx4_tensor_scale(handle(a[0]), x.p, x.dtype, x.rows, x.cols, x.stride, static_cast<float*>(out.data_ptr()), stream(device)), "excp_mx4_tensor_scale");
-    return wrap(out);
+    return wrap_written(out, a[3]);
 }
 
 // (handle, device, x, format, scale or None, out or None)
@@ -146,7 +152,7 @@ PyObject* quantize(PyObject* const* a) {
     const at::Tensor out = a[5] == Py_None ? fresh({(int64_t)need}, at::kByte, device) : tensor(a[5], "out");
     check(api.mx4_quantize(handle(a[0]), x.p, x.dtype, x.rows, x.cols, x.stride, format,
                            static_cast<float*>(vector(a[4], device, at::kFloat, 1, "tensor_scale")), packed(out, device, need, "out"), stream(device)), "excp_mx4_quantize");
-    return wrap(out);
+    return wrap_written(out, a[5]);
 }
 
 // (handle, device, data, rows, cols, format, scale or None, dtype, out or None)
@@ -157,7 +163,7 @@ PyObject* dequantize(PyObject* const* a) {
     const at::Tensor out = result(a[8], device, wanted(a[7]), r, c);
     const Rows y = rows(out, device, "out");
     check(api.mx4_dequantize(handle(a[0]), p, r, c, format, static_cast<float*>(vector(a[6], device, at::kFloat, 1, "scale")), y.p, y.dtype, y.stride, stream(device)), "excp_mx4_dequantize");
-    return wrap(out);
+    return wrap_written(out, a[8]);
 }
 
 // (handle, device, a, a rows, a scale, b, b rows, b scale, cols, format, bias or None, dtype, out or None)
@@ -171,7 +177,7 @@ PyObject* matmul(PyObject* const* a) {
     check(api.mx4_matmul(handle(a[0]), pa, ar, static_cast<float*>(vector(a[4], device, at::kFloat, 1, "a.scale")), pb, br,
                          static_cast<float*>(vector(a[7], device, at::kFloat, 1, "b.scale")), c, format,
                          static_cast<float*>(vector(a[10], device, at::kFloat, br, "bias")), y.p, y.dtype, y.stride, stream(device)), "excp_mx4_matmul");
-    return wrap(out);
+    return wrap_written(out, a[12]);
 }
 
 // (handle, device, x, x scale, w, w rows, w scale, cols, format, bias or None, dtype or None, out or None, room or None)
@@ -193,7 +199,7 @@ PyObject* linear(PyObject* const* a) {
     check(api.mx4_linear(h, x.p, x.dtype, x.rows, x.stride, static_cast<float*>(vector(a[3], device, at::kFloat, 1, "tensor_scale")), w, wr,
                          static_cast<float*>(vector(a[6], device, at::kFloat, 1, "w.scale")), c, format,
                          static_cast<float*>(vector(a[9], device, at::kFloat, wr, "bias")), y.p, y.dtype, y.stride, px, stream(device)), "excp_mx4_linear");
-    return wrap(out);
+    return wrap_written(out, a[11]);
 }
 
 // What torch's allocator hands out at least, so that results which fit it hold no more together than one of them alone.  Every
@@ -252,7 +258,7 @@ PyObject* logprobs_grad(PyObject* const* a) {
     check(api.token_logprobs_grad(handle(a[0]), x.p, x.dtype, x.rows, x.cols, x.stride, static_cast<long long*>(vector(a[3], device, at::kLong, r, "tokens")), (float)scale,
                                   static_cast<float*>(vector(a[4], device, at::kFloat, r * 4, "row_stats")), static_cast<float*>(vector(a[6], device, at::kFloat, r, "g_logprob")),
                                   static_cast<float*>(vector(a[7], device, at::kFloat, r, "g_entropy")), y.p, y.stride, stream(device)), "excp_token_logprobs_grad");
-    return wrap(out);
+    return wrap_written(out, a[8]);
 }
 
 // ---- the layers before the logits --------------------------------------------------------------------------------------------------
@@ -319,7 +325,7 @@ PyObject* act8_quantize(PyObject* const* a) {
     const size_t need = api.act8_bytes(x.rows, x.cols);
     const at::Tensor out = a[3] == Py_None ? fresh({(int64_t)need}, at::kByte, device) : tensor(a[3], "out");
     check(api.act8_quantize(handle(a[0]), &x, packed(out, device, need, "out"), stream(device)), "excp_act8_quantize");
-    return wrap(out);
+    return wrap_written(out, a[3]);
 }
 
 // (handle, device, data, rows, cols, dtype, out or None)
@@ -330,7 +336,7 @@ PyObject* act8_restore(PyObject* const* a) {
     const at::Tensor out = result(a[6], device, wanted(a[5]), r, c);
     const excp_matrix y = matrix(out, device, "out");
     check(api.act8_restore(handle(a[0]), p, &y, stream(device)), "excp_act8_restore");
-    return wrap(out);
+    return wrap_written(out, a[6]);
 }
 
 // (handle, device, dy, pre or None, pre is packed, act, dpre wanted, again wanted, dbias wanted, out or None) -> (dpre, a, dbias), each or None
@@ -350,7 +356,7 @@ PyObject* act_grad(PyObject* const* a) {
     const Scratch room(db.defined() ? api.act_grad_scratch(h, dy.rows, dy.cols) : 0, device);
     check(api.act_grad(h, act, &dy, has_pre ? &pre : nullptr, out.defined() ? &dpre : nullptr, value.defined() ? &again : nullptr,
                        db.defined() ? static_cast<float*>(db.data_ptr()) : nullptr, room.p, stream(device)), "excp_act_grad");
-    return tuple(or_none(out), or_none(value), or_none(db));
+    return tuple(out.defined() ? wrap_written(out, a[9]) : Py_NewRef(Py_None), or_none(value), or_none(db));
 }
 
 // (handle, device, x, weight or None, bias or None, eps, rms, kept wanted, out or None) -> (y, row_stats, kept or None)
@@ -372,7 +378,7 @@ PyObject* layer_norm(PyObject* const* a) {
     if (flag(a[7])) k = fresh({(int64_t)api.act8_bytes(x.rows, x.cols)}, at::kByte, device);
     check(api.layer_norm(handle(a[0]), &x, w, b, w ? wt : bt, (float)eps, flag(a[6]), &y, static_cast<float*>(stats.data_ptr()), k.defined() ? k.data_ptr() : nullptr,
                          stream(device)), "excp_layer_norm");
-    return tuple(wrap(out), wrap(stats), or_none(k));
+    return tuple(wrap_written(out, a[8]), wrap(stats), or_none(k));
 }
 
 // (handle, device, dy, x, x is packed, weight or None, rms, row_stats, add or None, out or None, vectors wanted) -> (dx, dweight, dbias), the last two or None
@@ -396,7 +402,7 @@ PyObject* layer_norm_grad(PyObject* const* a) {
     check(api.layer_norm_grad(h, &dy, &x, w, wt, rms, static_cast<float*>(vector(a[7], device, at::kFloat, 2 * r, "row_stats")), add, &dx,
                               dw.defined() ? static_cast<float*>(dw.data_ptr()) : nullptr, db.defined() ? static_cast<float*>(db.data_ptr()) : nullptr, room.p,
                               stream(device)), "excp_layer_norm_grad");
-    return tuple(wrap(out), or_none(dw), or_none(db));
+    return tuple(wrap_written(out, a[9]), or_none(dw), or_none(db));
 }
 
 // (handle, device, x, w, bias or None, act, residual or None, dtype or None, out or None, keep: None, a dtype or True for 8 bits) -> (y, kept or None)
@@ -420,7 +426,7 @@ PyObject* plain_linear(PyObject* const* a) {
     }
     const Scratch room(api.linear_scratch(&x, &w), device);
     check(api.linear(handle(a[0]), &x, &w, b, bt, act, residual, &y, k.defined() ? &keep : nullptr, room.p, stream(device)), "excp_linear");
-    return tuple(wrap(out), or_none(k));
+    return tuple(wrap_written(out, a[8]), or_none(k));
 }
 
 // (handle, device, dy, w, add or None, dtype or None, out or None)
@@ -434,7 +440,7 @@ PyObject* linear_grad_input(PyObject* const* a) {
     const excp_matrix dx = matrix(out, device, "out");
     const Scratch room(api.linear_scratch(&dy, &w), device);
     check(api.linear_grad_input(handle(a[0]), &dy, &w, add, &dx, room.p, stream(device)), "excp_linear_grad_input");
-    return wrap(out);
+    return wrap_written(out, a[6]);
 }
 
 // (handle, device, dy, x, add or None, dtype, out or None)
@@ -447,7 +453,7 @@ PyObject* linear_grad_weight(PyObject* const* a) {
     const excp_matrix dw = matrix(out, device, "out");
     const Scratch room(api.linear_scratch(&dy, &x), device);
     check(api.linear_grad_weight(handle(a[0]), &dy, &x, add, &dw, room.p, stream(device)), "excp_linear_grad_weight");
-    return wrap(out);
+    return wrap_written(out, a[6]);
 }
 
 // Python's side: argument count, and no C++ exception leaves.

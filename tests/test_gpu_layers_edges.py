@@ -143,3 +143,35 @@ def test_long_sums_of_one_sign_in_16_bits(h, rows, n, k):
     x, w = ((torch.rand(r, k, generator=g, device=DEV) + 0.5).mul_(s).half() for r, s in ((rows, 1.0), (n, 400.0 / k)))
     y, want = h.linear(x, w).double(), x.double() @ w.double().T
     assert abs(((y - want) / want).mean().item()) <= 256 * 2.0 ** -22 + 5 * 2.0 ** -11 / math.sqrt(12 * rows * n)
+
+
+# ---- results that the caller gives ------------------------------------------------------
+def test_results_move_their_version(h):
+    """What a call writes into a tensor of the caller's is a change that autograd sees: saved for a backward pass, it is refused there."""
+    x, w, dy = make(4, 64, "bf16", 1), make(8, 64, "bf16", 2), make(4, 8, "bf16", 3)
+    n, q = h.layer_norm(x), h.act8_quantize(x)
+    z = h.mx4_quantize(w, "e8m0_32")
+    logits = make(4, 100, "fp32", 4)
+    r = h.token_logprobs(logits, torch.zeros(4, dtype=torch.int64, device=DEV))
+    new = lambda like, dtype=torch.bfloat16: torch.empty(like.shape, dtype=dtype, device=DEV)
+    calls = [(new(dy), lambda o: h.linear(x, w, out=o)), (new(dy), lambda o: h.linear_kept(x, w, out=o)), (new(x), lambda o: h.linear_grad_input(dy, w, out=o)),
+             (new(w, torch.float32), lambda o: h.linear_grad_weight(dy, x, out=o)), (new(x), lambda o: h.layer_norm(x, out=o)),
+             (new(x), lambda o: h.layer_norm_grad(x, x, None, n, out=o)), (new(x), lambda o: h.act_grad(x, x, "gelu", out=o)),
+             (new(q.data, torch.uint8), lambda o: h.act8_quantize(x, out=o)), (new(x), lambda o: h.act8_restore(q, out=o)),
+             (new(dy), lambda o: h.mx4_linear(x, z, out=o)), (new(w), lambda o: h.mx4_dequantize(z, out=o)),
+             (new(logits, torch.float32), lambda o: h.token_logprobs_grad(logits, torch.zeros(4, dtype=torch.int64, device=DEV), r, torch.ones(4, device=DEV), out=o))]
+    for i, (out, f) in enumerate(calls):
+        before, inputs = out._version, [t._version for t in (x, w, dy)]
+        f(out)
+        assert out._version == before + 1, i
+        assert [t._version for t in (x, w, dy)] == inputs, i
+    leaf = torch.ones(4, 8, device=DEV, requires_grad=True)
+    y = torch.zeros(4, 8, device=DEV)
+    product = leaf * y                             # saves y
+    h.linear(x, w, out=y)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        product.sum().backward()
+    with torch.inference_mode():
+        out = new(dy)
+        h.linear(x, w, out=out)                    # has no version
+        assert torch.equal(out, h.linear(x, w))
