@@ -472,6 +472,9 @@ excp_status excp_token_logprobs_grad(excp_handle h, const void* logits, int dtyp
  * the handle, which allocates the word that their waits report to).  They use nothing else of the handle: calls that are not ordered on the
  * device may share one, though not scratch.  `scratch` is device memory on 16 bytes, of what the call's _scratch function says (NULL where that is 0), and its contents
  * afterwards are unspecified.
+ * Products wait for room in the tensor cores' memory without a limit.  Among this library's launches, on however many streams, none can wait for one another
+ * in a circle.  A kernel of another library that takes such memory beside little shared memory, and itself waits for something, can hold them up: order
+ * such kernels with the products.
  *
  * A matrix in these calls: `rows` rows of `cols` values, `row_stride` values apart (>= cols; of one row it is not looked at), aligned to
  * its element.  Its type is an excp_dtype, or, where that is said, EXCP_ACT8: then `data` is a packed 8-bit matrix and the stride is not
@@ -518,7 +521,8 @@ excp_status excp_act_grad(excp_handle h, int act, const excp_matrix* dy, const e
  * The gradient, with xh = (x - mean) rstd and g = dy weight:
  *   dx = rstd (g - mean(g) - xh mean(g xh)) + add   (rms: without mean(g)),   dweight = sum over rows of dy xh,   dbias = sum over rows of dy
  * x: what excp_layer_norm was given, or EXCP_ACT8; row_stats: what it wrote.  add (what reaches x by other ways), dx and the fp32 [cols]
- * vectors dweight and dbias are optional; add and dx have dy's type, and dx may be dy or add.  Without rows, dweight and dbias are 0. */
+ * vectors dweight and dbias are optional; add and dx have dy's type, and dx may be dy or add.  Without rows, dweight and dbias are 0.
+ * Sums are fp32: of a row whose squares add up past its numbers rstd is 0. */
 excp_status excp_layer_norm(excp_handle h, const excp_matrix* x, const void* weight, const void* bias, int vector_dtype, float eps, int rms,
                             const excp_matrix* y_out, float* row_stats_out, void* kept_out, void* cuda_stream);
 size_t excp_layer_norm_grad_scratch(excp_handle h, size_t rows, size_t cols);
@@ -531,6 +535,11 @@ excp_status excp_layer_norm_grad(excp_handle h, const excp_matrix* dy, const exc
  *   excp_linear_grad_input   dx = dy w + add
  *   excp_linear_grad_weight  dw = dy^T x + add
  * residual, add and kept are optional; y may be the residual, and dx or dw may be add (gradients that are summed over several calls).
+ * Sums: the tensor cores cut off what no longer fits a sum, so columns are added up in runs, and the runs' sums in fp32.  A result in 32 bits, or beside one
+ * kept in 32 bits, has runs of at most 768 columns: it is off by 7e-7 of its norm (of terms of one sign 4e-6), whatever the number of columns.  So has any
+ * product of few rows.  Of many rows, runs are as long as 2048 beside values kept in 8 bits with an activation, and otherwise 8192 for fp16 and 65536 for
+ * bfloat16 results, which costs them a fifth of half a unit in their last place at most; there y may round to the other neighbour when
+ * something is kept in 8 or 32 bits.
  * excp_linear_scratch: for the two operands of any of the three; 0 where both start on 16 bytes and their strides are multiples of 8 (or they
  * have one row): others are laid out in the scratch first.  A wait that ran out is reported by excp_score_status. */
 size_t excp_linear_scratch(const excp_matrix* a, const excp_matrix* b);

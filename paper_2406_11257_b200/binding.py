@@ -564,39 +564,41 @@ class Handle:
         return _score.token_logprobs_grad(self._h.value, self.device, logits, tokens, r.row_stats, r.scale, g_logprob, g_entropy, out)
 
     # ---- the layers before the logits, and the way back ----------------------
-    # As the scoring calls: only enqueued, marshalled natively, and torch's autograd sees none of them.
+    # As the scoring calls: only enqueued, and marshalled natively.  Autograd records none of them: results carry no graph, also of inputs that
+    # require a gradient (what is written into an `out` moves its version).  The gradients are calls of their own.
     def act8_quantize(self, x: torch.Tensor, out: torch.Tensor | None = None) -> Act8Matrix:
-        """excp_act8_quantize: x [rows, cols] in 8 bits (into `out`, uint8, if given)."""
+        """excp_act8_quantize: x [rows, cols] in 8 bits (into `out`, uint8, if given).  Not recorded by autograd."""
         data = _score.act8_quantize(self._h.value, self.device, x, out)
         rows, cols = x.shape
         return Act8Matrix(data, rows, cols)
 
     def act8_restore(self, m: Act8Matrix, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
-        """excp_act8_restore: the values that the codes stand for."""
+        """excp_act8_restore: the values that the codes stand for.  Not recorded by autograd."""
         return _score.act8_restore(self._h.value, self.device, m.data, m.rows, m.cols, dtype, out)
 
     def act_grad(self, dy: torch.Tensor, pre: torch.Tensor | Act8Matrix, act: str, again: bool = False, bias: bool = True,
                  out: torch.Tensor | None = None) -> ActGrad:
         """excp_act_grad: the gradient through an activation ("gelu", "gelu_tanh", "silu") from what went into it (`pre`, plain or in 8 bits),
-        the bias's gradient, and with `again` the activation's value.  `out` (for dpre) may be dy."""
+        the bias's gradient, and with `again` the activation's value.  `out` (for dpre) may be dy.  Not recorded by autograd."""
         _same_shape(pre, dy, "pre")
         data, is_packed = _kept(pre)
         return ActGrad(*_score.act_grad(self._h.value, self.device, dy, data, is_packed, ACTIVATIONS[act], True, again, bias, out))
 
     def bias_grad(self, dy: torch.Tensor) -> torch.Tensor:
-        """excp_act_grad without an activation: the sum of dy's rows, float32."""
+        """excp_act_grad without an activation: the sum of dy's rows, float32.  Not recorded by autograd."""
         return _score.act_grad(self._h.value, self.device, dy, None, False, 0, False, False, True, None)[2]
 
     def layer_norm(self, x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5, rms: bool = False,
                    keep: bool = False, out: torch.Tensor | None = None) -> Norm:
-        """excp_layer_norm: the norm of every row of x (rms: without mean and bias); with `keep` also x in 8 bits.  `out` may be x."""
+        """excp_layer_norm: the norm of every row of x (rms: without mean and bias); with `keep` also x in 8 bits.  `out` may be x.
+        Not recorded by autograd: the gradient is layer_norm_grad."""
         y, stats, data = _score.layer_norm(self._h.value, self.device, x, weight, bias, eps, rms, keep, out)
         return Norm(y, stats, None if data is None else Act8Matrix(data, *x.shape), rms)
 
     def layer_norm_grad(self, dy: torch.Tensor, x: torch.Tensor | Act8Matrix, weight: torch.Tensor | None, r: Norm, add: torch.Tensor | None = None,
                         out: torch.Tensor | None = None, vectors: bool = True) -> NormGrad:
         """excp_layer_norm_grad: the gradients of x (plus `add`), weight and bias, from what layer_norm returned for them; x may be r.kept.
-        `out` (for dx) may be dy or add."""
+        `out` (for dx) may be dy or add.  Not recorded by autograd."""
         _same_shape(x, dy, "x")
         data, is_packed = _kept(x)
         return NormGrad(*_score.layer_norm_grad(self._h.value, self.device, dy, data, is_packed, weight, r.rms, r.row_stats, add, out, vectors))
@@ -604,12 +606,13 @@ class Handle:
     def linear(self, x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, act: str = "none", residual: torch.Tensor | None = None,
                out: torch.Tensor | None = None, dtype: torch.dtype | None = None) -> torch.Tensor:
         """excp_linear: act(x w^T + bias) + residual of 16-bit matrices; the result has x's type unless `dtype` or `out` says otherwise.
-        `out` may be the residual."""
+        `out` may be the residual.  Not recorded by autograd: the gradients are linear_grad_input, linear_grad_weight, act_grad and bias_grad."""
         return _score.linear(self._h.value, self.device, x, w, bias, ACTIVATIONS[act], residual, dtype, out, None)[0]
 
     def linear_kept(self, x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, act: str = "none", residual: torch.Tensor | None = None,
                     keep: str | torch.dtype = "act8", out: torch.Tensor | None = None, dtype: torch.dtype | None = None):
-        """The same, and what goes into the activation: an Act8Matrix for keep="act8", else a tensor of that type."""
+        """The same, and what goes into the activation: an Act8Matrix for keep="act8", else a tensor of that type.  With many rows the result may
+        round to the other neighbour than linear's (excp.h: sums)."""
         if isinstance(keep, str) and keep != "act8":
             raise ValueError('keep: "act8" or a torch.dtype')
         y, data = _score.linear(self._h.value, self.device, x, w, bias, ACTIVATIONS[act], residual, dtype, out, True if keep == "act8" else keep)
@@ -617,12 +620,13 @@ class Handle:
 
     def linear_grad_input(self, dy: torch.Tensor, w: torch.Tensor, add: torch.Tensor | None = None, out: torch.Tensor | None = None,
                           dtype: torch.dtype | None = None) -> torch.Tensor:
-        """excp_linear_grad_input: dy w (+ add), in dy's type unless `dtype` or `out` says otherwise.  `out` may be add."""
+        """excp_linear_grad_input: dy w (+ add), in dy's type unless `dtype` or `out` says otherwise.  `out` may be add.  Not
+        recorded by autograd."""
         return _score.linear_grad_input(self._h.value, self.device, dy, w, add, dtype, out)
 
     def linear_grad_weight(self, dy: torch.Tensor, x: torch.Tensor, add: torch.Tensor | None = None, out: torch.Tensor | None = None,
                            dtype: torch.dtype = torch.float32) -> torch.Tensor:
-        """excp_linear_grad_weight: dy^T x (+ add).  `out` may be add (gradients summed over several calls)."""
+        """excp_linear_grad_weight: dy^T x (+ add).  `out` may be add (gradients summed over several calls).  Not recorded by autograd."""
         return _score.linear_grad_weight(self._h.value, self.device, dy, x, add, dtype, out)
 
     def score_status(self) -> None:

@@ -7,8 +7,9 @@
 // Phi from its upper tail: with a = |x| and t = 1 / (1 + 0.3 a), 1 - Phi(a) = exp(-a^2 / 2) t P(t); P is a polynomial of degree 7
 // fitted to erfc(a / sqrt 2) exp(a^2 / 2) / (2 t) over 0 <= a <= 13.5 so that its largest relative error is least (1.3e-7).  The
 // exponential serves the density too: two values and slopes take two reciprocals, two exponentials and 23 other instructions.
-// In fp32 the tail is within 1e-6 of its value (most of it the exponential's argument).  What the formula makes of an infinity is
-// left as it is (0 times infinity is NaN).
+// In fp32 the tail is within about (4 + a^2) 2^-23 of its value (the rounding of the exponential's argument, a^2 / 2, and the approximate
+// instructions): 5e-7 at 0, 2e-6 at 4, 2e-5 at 13, where it is 1e-38.  Of x Phi(x), and of the slope, it is a share that falls faster than that grows.
+// What the formula makes of an infinity is left as it is (0 times infinity is NaN).
 #pragma once
 #include <cuda_runtime.h>
 
