@@ -271,7 +271,7 @@ void launch_column_sums(cudaStream_t s, const float* rows, u32 parts, u64 n, u64
     launch_chained(column_sums_kernel, (u32)((n + 31) / 32), THREADS, 0, 0, s, rows, parts, n, split, out0, out1);
 }
 
-void launch_act8_quantize(int, cudaStream_t s, const Matrix& x, unsigned char* packed) {
+void launch_act8_quantize(cudaStream_t s, const Matrix& x, unsigned char* packed) {
     const Kept k(packed, x.rows, x.cols);
 #define EXCP_Q(T) (in_words(x) ? quantize_as<T, true>(s, x, k) : quantize_as<T, false>(s, x, k))
     if (x.dtype == DT_F32) EXCP_Q(float);
@@ -280,7 +280,7 @@ void launch_act8_quantize(int, cudaStream_t s, const Matrix& x, unsigned char* p
 #undef EXCP_Q
 }
 
-void launch_act8_restore(int, cudaStream_t s, const unsigned char* packed, const Matrix& y) {
+void launch_act8_restore(cudaStream_t s, const unsigned char* packed, const Matrix& y) {
     const Kept k(const_cast<unsigned char*>(packed), y.rows, y.cols);
 #define EXCP_R(T) (in_words(y) ? restore_as<T, true>(s, k, y) : restore_as<T, false>(s, k, y))
     if (y.dtype == DT_F32) EXCP_R(float);

@@ -7,10 +7,10 @@
 // Lanes past the last column have xh 0: (0 - mean) rstd can be infinite, and would spoil the sum of g xh although g is 0 there.
 //
 // A row is held in registers, as it lies in memory, by a group of 32 .. 512 threads, eight columns to a thread and piece: the squares are
-// summed after the mean is known, which costs no second read.  Where there are rows enough a warp takes a row of up to 4096 16-bit
-// values: no barrier, one set of shuffles for 128 values a lane, and a dozen rows on their way to every SM.  (8192 x 4096 bf16: 512
-// threads to a row 85 us, 256 threads with the rows in a ring in shared memory 45.)  Rows past what registers hold are read again.
-// Sums are fp32.
+// summed after the mean is known, which costs no second read.  With few rows a thread has one piece; where there are rows enough, as few threads as hold a
+// row in four: a warp up to 1024 columns (no barrier), 128 threads at 4096.  A warp has 256 columns of one row at a time, so of rows shorter than that
+// some of its lanes have none.  (8192 x 4096 bf16: 512 threads to a row 85 us, 256 threads with the rows in a ring in shared memory 45, 128 threads
+// 36.)  Rows past what registers hold are read again.  Sums are fp32.
 //
 // The gradient of few rows is one kernel: blocks walk over the rows and sum the gradients of weight and bias in registers.  With
 // many rows that costs two barriers a row and half the registers (8192 x 4096 bf16 from 8 bits 103 us); there, dx is one kernel as above,
@@ -304,83 +304,66 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) norm_grad_kernel(const __grid_co
     __shared__ float2 room[2 * GROUP_MAX / 32];
     wait_for_previous();
     let_next_start();
-    constexpr int PIECES = 1;
     const u32 groups = 1u << g.rows_log, group = threadIdx.x >> g.threads_log, t = threadIdx.x & (g.threads - 1), lane = t & 31;
     GroupSums sums = group_sums(room, g.threads, g.threads_log);
-    const u32 first = t / 32 * 256, step = g.threads * PIECE;
+    const u32 base = t / 32 * 256;                 // a thread has one piece
     const float inv_n = 1.f / (float)g.cols;
-    Eight dw[PIECES] = {}, db[PIECES] = {};
-    Raw<T, VEC> dy[PIECES];
-    RawX<T, KEPT, VEC> x[PIECES];
+    Eight dw = {}, db = {};
+    Raw<T, VEC> dy;
+    RawX<T, KEPT, VEC> x;
     float2 st = make_float2(0.f, 0.f);
     const u64 stride = (u64)gridDim.x * groups;
     auto fetch = [&](u64 row) {
         if (row >= g.rows) return;
         st = __ldg(g.stats + row);
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            dy[p].load(g.dy + row * g.dy_stride, first + p * step, lane, g.cols);
-            x[p].load(g, row, first + p * step, lane);
-        }
+        dy.load(g.dy + row * g.dy_stride, base, lane, g.cols);
+        x.load(g, row, base, lane);
     };
     u64 row = (u64)blockIdx.x * groups + group;
     fetch(row);
     for (; row < g.rows; row += stride) {
-        Eight d[PIECES], xh[PIECES];
+        Eight d, xh, w;
         f32x2 s1 = 0, s2 = 0;
         const f32x2 minus_mean = both_2(-st.x), rstd = both_2(st.y);
+        dy.values(d);
+        x.values(xh);
+        load_vector<T, VEC>(g.weight, base, lane, g.cols, 1.f, w);
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            Eight w;
-            dy[p].values(d[p]);
-            x[p].values(xh[p]);
-            load_vector<T, VEC>(g.weight, first + p * step, lane, g.cols, 1.f, w);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                xh[p][i] = mul_2(add_2(xh[p][i], minus_mean), where_column<VEC>(first + p * step, lane, g.cols, i, st.y));
-                db[p][i] = add_2(db[p][i], d[p][i]);       // 0 past the last column
-                dw[p][i] = fma_2(d[p][i], xh[p][i], dw[p][i]);
-                d[p][i] = mul_2(d[p][i], w[i]);
-                s1 = add_2(s1, d[p][i]);
-                s2 = fma_2(d[p][i], xh[p][i], s2);
-            }
+        for (int i = 0; i < 4; ++i) {
+            xh[i] = mul_2(add_2(xh[i], minus_mean), where_column<VEC>(base, lane, g.cols, i, st.y));
+            db[i] = add_2(db[i], d[i]);            // 0 past the last column
+            dw[i] = fma_2(d[i], xh[i], dw[i]);
+            d[i] = mul_2(d[i], w[i]);
+            s1 = add_2(s1, d[i]);
+            s2 = fma_2(d[i], xh[i], s2);
         }
         fetch(row + stride);                       // on its way while the sums are found
         float m1 = low_2(s1) + high_2(s1), m2 = low_2(s2) + high_2(s2);
         sums(m1, m2);
-        if (g.dx) {
+        if (base < g.cols) {                       // a whole warp
             const f32x2 minus_m1 = both_2(g.rms ? 0.f : -m1 * inv_n), minus_m2 = both_2(-m2 * inv_n);
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-                const u32 base = first + p * step;
-                if (base >= g.cols) continue;      // a whole warp
+            for (int i = 0; i < 4; ++i) d[i] = mul_2(rstd, add_2(d[i], fma_2(xh[i], minus_m2, minus_m1)));
+            if (g.add) {
+                Eight a;
+                load_cols<T, VEC>(g.add + row * g.add_stride, base, lane, g.cols, a);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) d[p][i] = mul_2(rstd, add_2(d[p][i], fma_2(xh[p][i], minus_m2, minus_m1)));
-                if (g.add) {
-                    Eight a;
-                    load_cols<T, VEC>(g.add + row * g.add_stride, base, lane, g.cols, a);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) d[p][i] = add_2(d[p][i], a[i]);
-                }
-                store_cols<T, VEC>(g.dx + row * g.dx_stride, base, lane, g.cols, d[p]);
+                for (int i = 0; i < 4; ++i) d[i] = add_2(d[i], a[i]);
             }
+            store_cols<T, VEC>(g.dx + row * g.dx_stride, base, lane, g.cols, d);
         }
     }
-    if (!g.dweight && !g.dbias) return;
     // the groups of the block, one after the other
     for (u32 i = 0; i < groups; ++i) {
         __syncthreads();
         if (i != group) continue;
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-#pragma unroll
-            for (u32 e = 0; e < 8; ++e) {
-                const u32 c = lane_col<VEC>(first + p * step, lane, e);
-                if (c >= g.cols) continue;
-                const float a = e % 2 ? high_2(dw[p][e / 2]) : low_2(dw[p][e / 2]), b = e % 2 ? high_2(db[p][e / 2]) : low_2(db[p][e / 2]);
-                own[c] = i ? own[c] + a : a;
-                own[g.cols + c] = i ? own[g.cols + c] + b : b;
-            }
+        for (u32 e = 0; e < 8; ++e) {
+            const u32 c = lane_col<VEC>(base, lane, e);
+            if (c >= g.cols) continue;
+            const float a = e % 2 ? high_2(dw[e / 2]) : low_2(dw[e / 2]), b = e % 2 ? high_2(db[e / 2]) : low_2(db[e / 2]);
+            own[c] = i ? own[c] + a : a;
+            own[g.cols + c] = i ? own[g.cols + c] + b : b;
         }
     }
     const u32 cluster = blockIdx.x / cg::this_cluster().num_blocks();

@@ -33,8 +33,8 @@ inline bool in_words(const Matrix& m) { return !m.p || (m.cols % 8 == 0 && (m.dt
 inline bool in_words(const ColumnVector& v) { return on_words(v.p, 0, 1); }
 
 // ---- launch wrappers ---------------------------------------------------------------------------------------------------
-void launch_act8_quantize(int sms, cudaStream_t s, const Matrix& x, unsigned char* packed);
-void launch_act8_restore(int sms, cudaStream_t s, const unsigned char* packed, const Matrix& out);
+void launch_act8_quantize(cudaStream_t s, const Matrix& x, unsigned char* packed);
+void launch_act8_restore(cudaStream_t s, const unsigned char* packed, const Matrix& out);
 
 u64 act_grad_scratch(int sms, u64 rows, u64 cols);
 void launch_act_grad(int sms, cudaStream_t s, int act, const Matrix& dy, const Matrix& pre, const Matrix& dpre, const Matrix& again, float* dbias,

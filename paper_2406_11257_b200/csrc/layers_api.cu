@@ -93,7 +93,7 @@ excp_status excp_act8_quantize(excp_handle h, const excp_matrix* x, void* packed
     if (!packed_out || !aligned16(packed_out)) return EXCP_ERR_INVALID_ARG;
     DeviceGuard guard(h->device);
     if (!guard.ok) return EXCP_ERR_CUDA;
-    launch_act8_quantize(h->sms, static_cast<cudaStream_t>(cuda_stream), matrix(x), static_cast<unsigned char*>(packed_out));
+    launch_act8_quantize(static_cast<cudaStream_t>(cuda_stream), matrix(x), static_cast<unsigned char*>(packed_out));
     return finish(h);
 }
 
@@ -103,7 +103,7 @@ excp_status excp_act8_restore(excp_handle h, const void* packed, const excp_matr
     if (!packed || !aligned16(packed)) return EXCP_ERR_INVALID_ARG;
     DeviceGuard guard(h->device);
     if (!guard.ok) return EXCP_ERR_CUDA;
-    launch_act8_restore(h->sms, static_cast<cudaStream_t>(cuda_stream), static_cast<const unsigned char*>(packed), matrix(out));
+    launch_act8_restore(static_cast<cudaStream_t>(cuda_stream), static_cast<const unsigned char*>(packed), matrix(out));
     return finish(h);
 }
 
