@@ -612,7 +612,7 @@ class Handle:
     def linear_kept(self, x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, act: str = "none", residual: torch.Tensor | None = None,
                     keep: str | torch.dtype = "act8", out: torch.Tensor | None = None, dtype: torch.dtype | None = None):
         """The same, and what goes into the activation: an Act8Matrix for keep="act8", else a tensor of that type.  With many rows the result may
-        round to the other neighbour than linear's (excp.h: sums)."""
+        round to the other neighbour than linear's where float32 is kept, or "act8" without an activation (excp.h: sums)."""
         if isinstance(keep, str) and keep != "act8":
             raise ValueError('keep: "act8" or a torch.dtype')
         y, data = _score.linear(self._h.value, self.device, x, w, bias, ACTIVATIONS[act], residual, dtype, out, True if keep == "act8" else keep)

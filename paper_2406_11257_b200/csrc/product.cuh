@@ -13,16 +13,16 @@ constexpr u32 PR_K = 64;                           // columns of a box: 128 byte
 // The tensor core cuts its sums off instead of rounding them: 1024 columns added one after the other lose 1e-6 of a sum (measured), 4096
 // 4e-6, which shows in a result of 32 bits.  There, and in the kernel for few rows always, the columns are added up in runs of at most so many,
 // and the runs' sums in fp32: 7e-7 whatever the length, of terms of both signs.  (Runs of 512: 5e-7, and a twelfth slower.)  Where all terms have
-// one sign every addition cuts off the same way: 4e-6, or 6e-9 a column of one run.
+// one sign every addition cuts off the same way: of fp16 4e-6, or 6e-9 a column of one run.
 constexpr u32 PR_RUN = 768;
-// It shows less in fewer bits, and the kernel for many rows takes longer runs where that is quicker.
+// It shows less in fewer bits, and the kernel for many rows takes longer runs for them.
 // Codes of 8 bits: after 4096 columns in one run seven times as many as of a plain fp32 sum land on the other side of a border, and the kept values of
 // fp16 activations are 1.7 times as far off; runs of 2048 columns leave 1.2 times.  Not shorter with an activation: while such a tile is written out the products
 // can go on for two runs only (4096 x 4096 -> 11008, gelu: runs of 768 columns 369 us, of 2048 317).
 // (Without one they are as short as for 32 bits, 249 -> 331 us: the result beside 8 bits is then the same as beside 32.)
-// Results of 16 bits: a run of terms of one sign loses up to a fifth of half a unit (5e-5 in 8192 columns, and bfloat16 has three bits less; fp16 results
-// of one run of 50304 columns lost 3e-4).
-constexpr u32 PR_RUN_ACT8 = 2048, PR_RUN_F16 = 8192, PR_RUN_BF16 = 65536;
+// Results of 16 bits: the same, so that they do not depend on 8 bits kept beside them.  (One run for all columns is 1.8 us a launch quicker, and fp16
+// results of 50304 columns of one sign lost 3e-4 by it, more than half a unit.)
+constexpr u32 PR_RUN_16 = 2048;
 constexpr u32 PR_CHUNK = 64;                       // rows of a box of an operand that lies the other way round
 constexpr u32 PR_CHUNK_BYTES = PR_CHUNK * PR_K * 2;
 
@@ -46,9 +46,7 @@ struct ProductEnd {
 // Columns of a run of the kernel for many rows.
 inline u32 product_run(const ProductEnd& e) {
     const bool kept32 = e.kept.p && e.kept.dtype == DT_F32, kept8 = e.kept.p && e.kept.dtype == DT_ACT8;
-    if (e.y.dtype == DT_F32 || kept32 || (kept8 && e.act == ACT_NONE)) return PR_RUN;
-    if (kept8) return PR_RUN_ACT8;
-    return e.y.dtype == DT_F16 ? PR_RUN_F16 : PR_RUN_BF16;
+    return e.y.dtype == DT_F32 || kept32 || (kept8 && e.act == ACT_NONE) ? PR_RUN : PR_RUN_16;
 }
 
 struct ProductCall {
