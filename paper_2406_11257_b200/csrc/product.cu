@@ -228,21 +228,40 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
         u32 turn = 0;
         auto take = [&](auto width, u32 c, float (&f)[decltype(width)::value]) {
             constexpr u32 W = decltype(width)::value;
-            u32 v[W];
-            __syncwarp();
-            if (runs) {
-                if constexpr (W == 32) {
-                    tm_load32(lanes + c, v);
+            auto load = [&](u32 at, u32* v, auto columns) {
+                if constexpr (decltype(columns)::value == 32) {
+                    tm_load32(at, v);
                 } else {
 #pragma unroll
-                    for (u32 i = 0; i < W; i += 8) tm_load8(lanes + c + i, v + i);
+                    for (u32 i = 0; i < decltype(columns)::value; i += 8) tm_load8(at + i, v + i);
                 }
+            };
+            constexpr u32 STEP = W < 16 ? W : 16;                          // more does not fit the registers
+            const std::integral_constant<u32, STEP> step;
+            __syncwarp();
+            if (RUNS && runs == 2) {               // both on the same way
+                u32 v[W], t[STEP];
+                load(lanes + c, v, width);
+                load(lanes + g.nt + c, t, step);
+                tm_wait_load();
+#pragma unroll
+                for (u32 e = 0; e < STEP; ++e) f[e] = __uint_as_float(v[e]) + __uint_as_float(t[e]);
+                if constexpr (W > STEP) {
+                    load(lanes + g.nt + c + STEP, t, step);
+                    tm_wait_load();
+#pragma unroll
+                    for (u32 e = STEP; e < W; ++e) f[e] = __uint_as_float(v[e]) + __uint_as_float(t[e - STEP]);
+                }
+                return;
+            }
+            u32 v[W];
+            if (runs) {
+                load(lanes + c, v, width);
                 tm_wait_load();
             }
 #pragma unroll
             for (u32 e = 0; e < W; ++e) f[e] = runs ? __uint_as_float(v[e]) : 0.f;
             if constexpr (RUNS) {
-                constexpr u32 STEP = W < 16 ? W : 16;                      // more does not fit the registers
                 u32 slot = emptied % (ACCS - 1);                           // 0 where there are fewer accumulators
                 for (u32 r = emptied + 1; r < runs; ++r) {
                     const u32 from = lanes + (1 + slot) * g.nt + c;
@@ -251,8 +270,7 @@ __global__ void __launch_bounds__(BOUND_THREADS, 2) product_kernel(const __grid_
                     for (u32 h = 0; h < W; h += STEP) {
                         u32 t[STEP];
                         __syncwarp();
-#pragma unroll
-                        for (u32 i = 0; i < STEP; i += 8) tm_load8(from + h + i, t + i);
+                        load(from + h, t, step);
                         tm_wait_load();
 #pragma unroll
                         for (u32 e = 0; e < STEP; ++e) f[h + e] += __uint_as_float(t[e]);
