@@ -4,8 +4,9 @@
 //   dpre = dy act'(pre), again = act(pre), dbias = sum over rows of dpre
 //
 // A warp takes 256 columns of a row, eight to a lane: a block is four lanes' (two shuffles find A).
-// Bound: of values in 8 bits and back the bytes (4096 x 11008 bf16 28 us, 5.0 TB/s; back 30 us, 4.6 TB/s).  Of the gradient instructions: a
-// gelu and its slope are 13 of the 28 a value takes (4096 x 11008 bf16 from 8 bits, value again: 75 us, 4.2 TB/s; silu 63).
+// Bound: of values in 8 bits and back the bytes (4096 x 11008 bf16 28 us, 5.0 TB/s; back 30 us, 4.6 TB/s).  Of the gradient latency: a value takes 28
+// instructions, 13 of them a gelu and its slope, which fill 57 % of the issue slots with 28 % of the warps that an SM could hold; and the blocks of a strip are a
+// multiple of its cluster, so that some SMs get three where others get two (4096 x 11008 bf16 from 8 bits, value again: 75 us, 4.2 TB/s; silu 63).
 #include <cooperative_groups.h>
 
 #include "layers.cuh"

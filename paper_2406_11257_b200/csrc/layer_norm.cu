@@ -16,7 +16,7 @@
 // many rows that costs two barriers a row and half the registers (8192 x 4096 bf16 from 8 bits 103 us); there, dx is one kernel as above,
 // and the sums are another, which reads dy and x again: strips of 256 columns, a warp to a row (59 us together).  Either way the sums of
 // a cluster's blocks join through distributed shared memory in a fixed order, the clusters' through a further launch.
-// Bound: the bytes; of the forward pass the instructions and the latency of a row's two sums.
+// Bound: the bytes; of the forward pass the latency of a row's two sums, behind which nothing of the next row is on its way (issue slots 46 % busy).
 #include <cooperative_groups.h>
 
 #include "layers.cuh"
@@ -181,8 +181,8 @@ __global__ void __launch_bounds__(block_of<PIECES>(), PIECES < 2 ? 2 : 5) norm_k
 }
 
 // The same for many rows in 16-byte words, with all that can be known when it is compiled: THREADS of a row (so that a piece's place
-// is a constant), and what vectors there are (VECTORS: 1 the weight, 2 the bias too, both of T).  Half the instructions of the kernel above,
-// which is what bounds it (8192 x 4096 bf16: 43 us there, 36 here, 46 with x in 8 bits; 16384 x 1024 25 and 16).
+// is a constant), and what vectors there are (VECTORS: 1 the weight, 2 the bias too, both of T).  Half the instructions of the kernel above
+// (8192 x 4096 bf16: 43 us there, 36 here, 46 with x in 8 bits; 16384 x 1024 25 and 16).
 __host__ __device__ constexpr int rows_block(int threads) { return threads > 128 ? threads : 128; }
 __host__ __device__ constexpr u32 const_log(u32 v) { return v <= 1 ? 0 : 1 + const_log(v / 2); }
 template <typename T, int PIECES, int THREADS, int VECTORS>

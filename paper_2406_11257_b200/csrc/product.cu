@@ -6,13 +6,13 @@
 // tiles for the SMs the columns of a tile are split over a cluster: each CTA sends its part of the accumulator to the CTAs that own its
 // columns (bulk copies between their shared memories), which add the parts in a fixed order.
 //
-// 1 x 4096 -> 11008 bf16 18 us from memory, 16 x 2048 -> 50304 37 us (5.6 TB/s), 333 x 1000 -> 4097 9.3 us, 512 x 1024 -> 1024 5.6 us, one tile
+// 1 x 4096 -> 11008 bf16 18 us from memory, 16 x 2048 -> 50304 38 us (5.5 TB/s), 333 x 1000 -> 4097 9.9 us, 512 x 1024 -> 1024 6.1 us, one tile
 // alone 2.6 us.
 //
 // Sums are taken in runs of at most PR_RUN columns, whatever the results' types, so that they do not depend on what is done with them.  Up to
 // four runs have an accumulator each; of more, all but the last three are added to the first by warps that have nothing else to do, while
 // the products go on in the others.  (One run, which loses more the longer it is: 1 x 4096 -> 4096 8.3 us against 8.8, 512 x 4096 -> 4096
-// 18.7 against 20.4.)
+// 18.7 against 20.3.)
 //
 // Roles: warps 0..3 fetch the operands (tensor maps; what lies past an edge comes as 0), warps 4..7 add up runs, warp 8 issues the products, and at
 // the end warps 0..7 write the result.

@@ -1,7 +1,7 @@
 // The product with plain 16-bit operands, many rows on both sides (product.cu: few).
 //
-// Bound: the tensor cores, and soon the power cap.  4096 x 4096 x 11008 bf16: 230 us in a burst (1.6 PFLOP/s; a library product on the
-// same card 238), dx 256 (236), dw to 32 bits 269; back to back the clock falls to 1.4 GHz, and with it all of them to some 300.
+// Bound: the tensor cores, and soon the power cap.  4096 x 4096 x 11008 bf16: 232 us in a burst (1.6 PFLOP/s; a library product on the
+// same card 238), dx 255 (236), dw to 32 bits 256; back to back the clock falls to 1.4 GHz, and with it all of them to some 300.
 // A pair of CTAs works on a tile of 256 x 256 (tcgen05 cta_group::2): each holds 128 rows of the M side and
 // half of the N side's 256, so that a step of 64 columns costs a CTA 32 KB of shared memory for 512 cycles of products.  The
 // accumulators of two tiles fit tensor memory: one is written out while the next is summed.
