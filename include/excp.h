@@ -537,7 +537,7 @@ excp_status excp_layer_norm_grad(excp_handle h, const excp_matrix* dy, const exc
  * residual, add and kept are optional; y may be the residual, and dx or dw may be add (gradients that are summed over several calls).
  * Sums: the tensor cores cut off what no longer fits a sum, so columns are added up in runs, and the runs' sums in fp32.  Runs are of at most 768 columns
  * where the result is EXCP_F32 or is kept in EXCP_F32, or in EXCP_ACT8 without an activation, and in products of few rows always: a sum is off by 7e-7 of the
- * result's norm, whatever the number of columns (fp16 terms of one sign: 4e-6).  Otherwise they are of at most 2048, which costs some 2e-6 (1.3e-5) before
+ * result's norm (of fp16 1e-6, of terms of one sign 4e-6), whatever the number of columns.  Otherwise they are of at most 2048, which costs some 2e-6 (1.3e-5) before
  * the rounding to 16 or 8 bits.  So y of many rows may round to the other neighbour when p is kept in EXCP_F32, or in EXCP_ACT8 without an activation.
  * excp_linear_scratch: for the two operands of any of the three; 0 where both start on 16 bytes and their strides are multiples of 8 (or they
  * have one row): others are laid out in the scratch first.  A wait that ran out is reported by excp_score_status. */

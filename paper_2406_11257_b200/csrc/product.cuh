@@ -12,7 +12,7 @@ constexpr u32 PR_TILE = 128;                       // rows of an operand tile = 
 constexpr u32 PR_K = 64;                           // columns of a box: 128 bytes, one swizzle span
 // The tensor core cuts its sums off instead of rounding them: 1024 columns added one after the other lose 1e-6 of a sum (measured), 4096
 // 4e-6, which shows in a result of 32 bits.  There, and in the kernel for few rows always, the columns are added up in runs of at most so many,
-// and the runs' sums in fp32: 7e-7 whatever the length, of terms of both signs.  (Runs of 512: 5e-7, and a twelfth slower.)  Where all terms have
+// and the runs' sums in fp32: 7e-7 (of fp16 1e-6) whatever the length, of terms of both signs.  (Runs of 512: 5e-7, and a twelfth slower.)  Where all terms have
 // one sign every addition cuts off the same way: of fp16 4e-6, or 6e-9 a column of one run.
 constexpr u32 PR_RUN = 768;
 // It shows less in fewer bits, and the kernel for many rows takes longer runs for them.

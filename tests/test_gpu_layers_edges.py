@@ -185,3 +185,36 @@ def test_results_move_their_version(h):
         out = new(dy)
         h.linear(x, w, out=out)                    # has no version
         assert torch.equal(out, h.linear(x, w))
+
+
+def test_long_products_on_several_streams_at_once(h):
+    """Products whose runs are added up in tensor memory (all of an SM's, or a part), ones of many rows and 4-bit ones on four streams that nothing orders,
+    and captured in two graphs that are replayed at once: each gives what it gives alone."""
+    calls = []
+    for i, (rows, k, n) in enumerate(((2, 50304, 1000), (64, 11008, 4096), (500, 9000, 500), (16, 30000, 3000), (2304, 3000, 2304))):
+        x, w = big(rows, k, i), big(n, k, i + 10, size=0.1)
+        q = h.mx4_quantize(w, "e8m0_32")
+        calls += [lambda x=x, w=w: h.linear(x, w, dtype=torch.float32), lambda x=x, w=w: h.linear(x, w, act="gelu"), lambda x=x, q=q: h.mx4_linear(x, q)]
+    alone = [f() for f in calls]
+    torch.cuda.synchronize()
+    streams, results = [torch.cuda.Stream() for _ in range(4)], []
+    for turn in range(4):
+        for j, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                results.append([calls[(i * 7 + 5 * j + turn) % len(calls)]() for i in range(len(calls))])
+    torch.cuda.synchronize()
+    for t, r in enumerate(results):
+        for i, y in enumerate(r):
+            assert torch.equal(y, alone[(i * 7 + 5 * (t % 4) + t // 4) % len(calls)])
+    graphs, replayed = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            replayed.append([f() for f in calls])
+    for _ in range(3):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for r in replayed:
+        assert all(torch.equal(y, a) for y, a in zip(r, alone))
+    h.score_status()
